@@ -284,6 +284,114 @@ int vlac_selftest_wait_expiry(vlac_ctx* ctx, unsigned int limit_us, void* stream
 int vlac_greedy_tokens_static(const float* logits, int rows, int vocab, long long row_stride,
                               int* tokens, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Paged K/V pool and attention over a shared prefix
+ *
+ * The cache above holds one dense sequence per control loop.  Several sequences that begin with the same
+ * rows -- action candidates sampled from one prompt, several loops under one instruction -- can share those
+ * rows in a pool of pages.  The pool is caller-owned device memory described by this struct (no handle, no
+ * allocation in the library); its tables are device data, so that every call below can be captured into a
+ * CUDA graph and none waits for the device.
+ *
+ *   k, v    16-bit elements (dtype) [n_layers][n_pages][page_size][n_kv_heads][head_dim], 16-byte aligned,
+ *           keys stored after rotation as in the cache
+ *   table   int32 [n_slots][max_pages]: the pages of each slot's sequence in order, -1 behind the last
+ *   len     int32 [n_slots]: rows held by the slot (0: empty)
+ *   refs    int32 [n_pages], 16-byte aligned: slots that hold the page; 0 = free
+ *   work    scratch of vlac_pages_work_bytes(p) bytes, 16-byte aligned, contents without meaning between calls
+ * A fresh pool has table = -1, len = 0, refs = 0.
+ * page_size: a power of two, 8..256.  head_dim: 64 or 128.  n_pages*page_size and max_pages*page_size < 2^31.
+ *
+ * Rules of all calls below
+ *   - Lists (slots, lengths, status) are device int32 arrays of n entries, n <= VLAC_PAGES_MAX_LIST (TOO_LARGE
+ *     beyond; n = 0 does nothing).  The call returns INVALID_ARG for what the host can see; what only the
+ *     device can see is reported per entry in status[n] (0 or a VLAC_ERR_* code), and an entry that is refused
+ *     changes nothing unless stated otherwise.
+ *   - status INVALID_ARG: a slot outside [0, n_slots), a target slot that an earlier entry of the list names
+ *     (the first stands), a target that another entry reads, a length or position outside its range.
+ *     status BAD_STATE: a length or a page number in the slot's own tables outside its range.
+ *   - Pages are taken lowest number first, entries in list order; when they do not suffice, an entry and every later
+ *     one that needs a page get OOM.  Results depend on the tables alone, never on timing.
+ *   - A sequence's last page is never shared while it is partly filled, so rows are appended in place.
+ *   - Calls that change a pool, and calls that read it, must be stream-ordered with one another (they share work too). */
+#define VLAC_BF16 0
+#define VLAC_FP16 1
+#define VLAC_PAGES_MAX_LIST 1024
+typedef struct {
+  void *k, *v;
+  int dtype, n_layers, n_pages, page_size, n_kv_heads, head_dim;
+  int n_slots, max_pages;
+  int *table, *len, *refs;
+  void* work;
+  unsigned long long work_bytes;
+} vlac_pages;
+
+/* Scratch bytes for a pool of this shape (only n_pages, n_slots and max_pages are read); 0 for a NULL or
+ * impossible shape. */
+unsigned long long vlac_pages_work_bytes(const vlac_pages* p);
+
+/* Give slot seqs[i] the length lens[i] (0..max_pages*page_size): pages are taken behind the last row, or given back from the
+ * end (before any are taken); rows that stay keep their pages and contents, new rows are undefined until written.
+ * BAD_STATE also for a cut inside a page that another slot holds (vlac_pages_compact with the rows to keep does that). */
+int vlac_pages_resize(const vlac_pages* p, const int* seqs, const int* lens, int n, int* status, void* stream);
+/* Give all pages of these slots back: resize to 0. */
+int vlac_pages_free(const vlac_pages* p, const int* seqs, int n, int* status, void* stream);
+
+/* Make slot dst[i] hold the rows of slot src[i].  deep = 0: the full pages are shared and the rows of a partly filled last
+ * page are copied, all layers; deep = 1: every row is copied into pages of its own (rows that a later step overwrites).  A
+ * target that holds a sequence gives it back first; after OOM it is left empty.  A source may appear several times; a target
+ * must not be the source of any entry. */
+int vlac_pages_fork(const vlac_pages* p, const int* src, const int* dst, int n, int deep, int* status, void* stream);
+
+/* Make slot dst[i] hold the rows keep[keep_ptr[i] .. keep_ptr[i+1]) of slot src[i] (positions, strictly ascending,
+ * INVALID_ARG otherwise), in that order and without gaps, all layers: pruned tokens leave the cache.  Leading pages that stay
+ * whole are shared, the other rows gathered into fresh pages.  dst[i] == src[i] prunes in place (its old pages are given
+ * back after the new ones are taken; OOM leaves it as it was); otherwise targets are treated as in vlac_pages_fork.
+ *   keep_ptr  device int32 [n + 1], 0 <= keep_ptr[i] <= keep_ptr[i+1] <= n_keep;  keep  device int32 [n_keep] */
+int vlac_pages_compact(const vlac_pages* p, const int* src, const int* dst, int n, const int* keep_ptr, const int* keep, int n_keep,
+                       int* status, void* stream);
+
+/* Write rows row_ptr[i] .. row_ptr[i+1] of k_rows / v_rows into one layer of slot seqs[i], from position start[i] on
+ * (start = NULL: the last rows of the slot).  The positions must lie inside the slot's length (vlac_pages_resize first) and in
+ * pages that no other slot holds (BAD_STATE otherwise: vlac_pages_fork with deep = 1).
+ *   row_ptr         device int32 [n + 1], 0 <= row_ptr[i] <= row_ptr[i+1] <= rows
+ *   k_rows, v_rows  device, the pool's type, row r at r*k_stride / r*v_stride elements (multiples of 8, at least
+ *                   n_kv_heads*head_dim), 16-byte aligned */
+int vlac_pages_write(const vlac_pages* p, int layer, const int* seqs, const int* start, const int* row_ptr, int n, int rows,
+                     const void* k_rows, long long k_stride, const void* v_rows, long long v_stride, int* status, void* stream);
+
+/* Copy positions 0 .. n_rows-1 of sequence seq of a control-step cache into slot `slot`, all layers: the prompt that a step left
+ * becomes a prefix that candidates share.  Shapes must agree (bf16 pool of the cache's layers, heads and head_dim, n_rows <= the
+ * cache's L + n_action), the slot must already have n_rows rows in pages of its own.  status: device int32 [1]. */
+int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int slot, int n_rows, int* status, void* stream);
+
+/* Attention of new rows over paged sequences, the common prefix read once for all that share it.
+ *
+ * Row q_ptr[i] + j of q is the j-th of the nq_i = q_ptr[i+1] - q_ptr[i] newest rows of slot seqs[i], at position
+ * len - nq_i + j, and sees the positions 0 .. len - nq_i + j of that slot (its own K/V rows are already written).  Query head h
+ * reads K/V head h / (n_heads / n_kv_heads).  out = softmax(scale * q K^T) V, lse = log sum exp of the scaled scores (natural
+ * logarithm); a row that sees nothing (position < 0) gets zeros and -inf.  Values at positions a row does not see never reach it,
+ * infinities and NaN included.
+ *
+ * vlac_prefix_plan finds, from the tables, which neighbours of the list hold the same leading pages and divides the work; it is
+ * called once whenever tables, lengths or q_ptr changed (once per token) and serves the attention of every layer.  List
+ * sequences that share most next to one another.  A slot may be listed twice.  Status per entry as above; the rows of a refused
+ * entry, and rows behind q_ptr[n], are left as they are.
+ *   plan     n (<= VLAC_PAGES_MAX_LIST), rows of q, n_heads (a multiple of n_kv_heads, n_heads*rows < 2^29), and mem: device
+ *            memory of vlac_prefix_bytes(p, n, rows, n_heads) bytes, 16-byte aligned, that holds the plan and the partial sums; a plan
+ *            serves one attention call at a time (two captured graphs that may overlap need two)
+ *   q, out   device, the pool's type, row r at r*q_stride / r*out_stride elements (multiples of 8, at least n_heads*head_dim), 16-byte
+ *            aligned;  lse  device fp32 [rows][n_heads] or NULL */
+typedef struct {
+  int n, rows, n_heads;
+  void* mem;
+  unsigned long long bytes;
+} vlac_prefix;
+unsigned long long vlac_prefix_bytes(const vlac_pages* p, int n, int rows, int n_heads);
+int vlac_prefix_plan(const vlac_pages* p, const vlac_prefix* plan, const int* seqs, const int* q_ptr, int* status, void* stream);
+int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
+                          void* out, long long out_stride, float* lse, void* stream);
+
 const char* vlac_status_string(int status);
 
 #ifdef __cplusplus

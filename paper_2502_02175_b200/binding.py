@@ -52,11 +52,23 @@ class vlac_selection(C.Structure):
                 ("final_mask", C.c_void_p), ("sim", C.c_void_p), ("S", C.c_void_p), ("alpha", C.c_void_p)]
 
 
+class vlac_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + \
+               [(n, C.c_int) for n in ("dtype", "n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim", "n_slots", "max_pages")] + \
+               [("table", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p), ("work", C.c_void_p), ("work_bytes", C.c_ulonglong)]
+
+
+class vlac_prefix(C.Structure):
+    _fields_ = [("n", C.c_int), ("rows", C.c_int), ("n_heads", C.c_int), ("mem", C.c_void_p), ("bytes", C.c_ulonglong)]
+
+
 EXPORTS = ("vlac_create", "vlac_destroy", "vlac_cache_alloc", "vlac_cache_reset", "vlac_cache_free",
            "vlac_cache_read", "vlac_cache_write", "vlac_select", "vlac_select_bf16", "vlac_select_import", "vlac_layer_forward",
            "vlac_step", "vlac_step_chunk", "vlac_step_pruned", "vlac_selection_view", "vlac_launch_count", "vlac_device_error", "vlac_status_string",
            "vlac_profile", "vlac_profile_read", "vlac_profile_segments", "vlac_greedy_tokens_static",
-           "vlac_selftest_wait_expiry")
+           "vlac_selftest_wait_expiry",
+           "vlac_pages_work_bytes", "vlac_pages_resize", "vlac_pages_free", "vlac_pages_fork", "vlac_pages_compact", "vlac_pages_write",
+           "vlac_pages_from_cache", "vlac_prefix_bytes", "vlac_prefix_plan", "vlac_prefix_attention")
 
 lib.vlac_status_string.restype = C.c_char_p
 lib.vlac_status_string.argtypes = [C.c_int]
@@ -86,6 +98,20 @@ lib.vlac_profile.argtypes = [C.c_void_p, C.c_int]
 lib.vlac_profile_segments.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.c_int, C.POINTER(C.c_int)]
 lib.vlac_greedy_tokens_static.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_longlong, C.c_void_p, C.c_void_p]
 lib.vlac_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_ulonglong), C.POINTER(C.c_int)]
+
+_P, _I, _LL = C.c_void_p, C.c_int, C.c_longlong
+lib.vlac_pages_work_bytes.restype = C.c_ulonglong
+lib.vlac_pages_work_bytes.argtypes = [_P]
+lib.vlac_pages_resize.argtypes = [_P, _P, _P, _I, _P, _P]
+lib.vlac_pages_free.argtypes = [_P, _P, _I, _P, _P]
+lib.vlac_pages_fork.argtypes = [_P, _P, _P, _I, _I, _P, _P]
+lib.vlac_pages_compact.argtypes = [_P, _P, _P, _I, _P, _P, _I, _P, _P]
+lib.vlac_pages_write.argtypes = [_P, _I, _P, _P, _P, _I, _I, _P, _LL, _P, _LL, _P, _P]
+lib.vlac_pages_from_cache.argtypes = [_P, _P, _I, _I, _I, _P, _P]
+lib.vlac_prefix_bytes.restype = C.c_ulonglong
+lib.vlac_prefix_bytes.argtypes = [_P, _I, _I, _I]
+lib.vlac_prefix_plan.argtypes = [_P, _P, _P, _P, _P, _P]
+lib.vlac_prefix_attention.argtypes = [_P, _I, _P, _P, _LL, C.c_float, _P, _LL, _P, _P]
 
 
 class VlacError(RuntimeError):
@@ -356,6 +382,151 @@ def vlac_greedy_tokens_static(logits: torch.Tensor, tokens: torch.Tensor) -> Non
     assert tokens.is_cuda and tokens.dtype == torch.int32 and tokens.is_contiguous()
     _check(lib.vlac_greedy_tokens_static(logits.data_ptr(), logits.shape[0], logits.shape[1], logits.stride(0),
                                          tokens.data_ptr(), _stream()), "vlac_greedy_tokens_static")
+
+
+# --------------------------------------------------------------------------- paged K/V pool, attention over a shared prefix
+class Pages:
+    """A pool of K/V pages: the tensors and the ``vlac_pages`` struct that describes them.
+
+    ``k``, ``v``: bf16 or fp16 ``[n_layers, n_pages, page_size, n_kv_heads, head_dim]``; ``table`` int32 ``[n_slots, max_pages]``,
+    ``len`` int32 ``[n_slots]``, ``refs`` int32 ``[n_pages]``, all contiguous on one device.  ``Pages.empty`` makes a fresh pool.
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, len: torch.Tensor, refs: torch.Tensor):
+        assert k.is_cuda and k.dtype in (torch.bfloat16, torch.float16) and k.dim() == 5 and k.is_contiguous()
+        assert v.is_cuda and v.dtype == k.dtype and v.shape == k.shape and v.is_contiguous() and v.device == k.device
+        for t, dims in ((table, 2), (len, 1), (refs, 1)):
+            assert t.device == k.device and t.dtype == torch.int32 and t.dim() == dims and t.is_contiguous()
+        assert len.shape[0] == table.shape[0] and refs.shape[0] == k.shape[1]
+        self.k, self.v, self.table, self.len, self.refs = k, v, table, len, refs
+        self.device, self.dtype = k.device, k.dtype
+        self.struct = vlac_pages(k.data_ptr(), v.data_ptr(), 0 if k.dtype == torch.bfloat16 else 1, *k.shape, *table.shape,
+                                 table.data_ptr(), len.data_ptr(), refs.data_ptr(), None, 0)
+        self.ref = C.byref(self.struct)
+        n = lib.vlac_pages_work_bytes(self.ref)
+        self.work = torch.empty((n,), dtype=torch.uint8, device=k.device)
+        self.struct.work, self.struct.work_bytes = self.work.data_ptr(), n
+
+    @classmethod
+    def empty(cls, n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, n_slots: int, max_pages: int,
+              dtype=torch.bfloat16, device="cuda") -> "Pages":
+        shape = (n_layers, n_pages, page_size, n_kv_heads, head_dim)
+        ints = dict(dtype=torch.int32, device=device)
+        return cls(torch.zeros(shape, dtype=dtype, device=device), torch.zeros(shape, dtype=dtype, device=device),
+                   torch.full((n_slots, max_pages), -1, **ints), torch.zeros((n_slots,), **ints), torch.zeros((n_pages,), **ints))
+
+
+class PrefixPlan:
+    """Device memory of one attention plan: up to ``n`` sequences with together ``rows`` query rows of ``n_heads`` heads."""
+
+    def __init__(self, pages: Pages, n: int, rows: int, n_heads: int):
+        size = lib.vlac_prefix_bytes(pages.ref, n, rows, n_heads)
+        if size == 0 and n > 0 and rows > 0:
+            raise VlacError(-1, "vlac_prefix_bytes")
+        self.n, self.rows, self.n_heads, self.device = n, rows, n_heads, pages.device
+        self.mem = torch.empty((max(size, 16),), dtype=torch.uint8, device=pages.device)
+        self.struct = vlac_prefix(n, rows, n_heads, self.mem.data_ptr(), size)
+        self.ref = C.byref(self.struct)
+
+
+def _here(device: torch.device) -> None:
+    """The library launches on the current device: tensors of another one would be read through the wrong context."""
+    assert device.index == torch.cuda.current_device(), f"tensors on {device}, current device {torch.cuda.current_device()}"
+
+
+def _ints(t: torch.Tensor, n: int, device: torch.device) -> int:
+    assert t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and t.device == device and t.is_contiguous()
+    return t.data_ptr()
+
+
+def vlac_pages_work_bytes(struct: vlac_pages) -> int:
+    return int(lib.vlac_pages_work_bytes(C.byref(struct)))
+
+
+def vlac_pages_resize(pages: Pages, seqs: torch.Tensor, lens: torch.Tensor, status: torch.Tensor) -> None:
+    """Slot ``seqs[i]`` gets length ``lens[i]``; ``status`` (int32, as long as the list) receives a code per entry."""
+    n, dev = seqs.shape[0], pages.device
+    _here(dev)
+    _check(lib.vlac_pages_resize(pages.ref, _ints(seqs, n, dev), _ints(lens, n, dev), n, _ints(status, n, dev), _stream()), "vlac_pages_resize")
+
+
+def vlac_pages_free(pages: Pages, seqs: torch.Tensor, status: torch.Tensor) -> None:
+    n, dev = seqs.shape[0], pages.device
+    _here(dev)
+    _check(lib.vlac_pages_free(pages.ref, _ints(seqs, n, dev), n, _ints(status, n, dev), _stream()), "vlac_pages_free")
+
+
+def vlac_pages_fork(pages: Pages, src: torch.Tensor, dst: torch.Tensor, deep: bool, status: torch.Tensor) -> None:
+    """Slot ``dst[i]`` becomes a copy of slot ``src[i]``: full pages shared, or (``deep``) every row copied."""
+    n, dev = src.shape[0], pages.device
+    _here(dev)
+    _check(lib.vlac_pages_fork(pages.ref, _ints(src, n, dev), _ints(dst, n, dev), n, int(bool(deep)), _ints(status, n, dev), _stream()),
+           "vlac_pages_fork")
+
+
+def vlac_pages_compact(pages: Pages, src: torch.Tensor, dst: torch.Tensor, keep_ptr: torch.Tensor, keep: torch.Tensor,
+                       status: torch.Tensor) -> None:
+    """Slot ``dst[i]`` becomes the rows ``keep[keep_ptr[i]:keep_ptr[i + 1]]`` (ascending positions) of slot ``src[i]``."""
+    n, dev = src.shape[0], pages.device
+    _here(dev)
+    _check(lib.vlac_pages_compact(pages.ref, _ints(src, n, dev), _ints(dst, n, dev), n, _ints(keep_ptr, n + 1, dev),
+                                  _ints(keep, keep.shape[0], dev), keep.shape[0], _ints(status, n, dev), _stream()), "vlac_pages_compact")
+
+
+def _rows(t: torch.Tensor, heads: int, pages: Pages, rows: int) -> None:
+    """[rows, heads, head_dim] of the pool's type, heads side by side, any row stride."""
+    d = pages.struct.head_dim
+    assert t.device == pages.device and t.dtype == pages.dtype and t.dim() == 3 and t.shape[0] == rows and t.shape[1] == heads and t.shape[2] == d
+    assert rows == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d))
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements between rows (a tensor of one row or none may carry any stride)."""
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] * t.shape[2] // 8) * 8
+
+
+def vlac_pages_write(pages: Pages, layer: int, seqs: torch.Tensor, start: Optional[torch.Tensor], row_ptr: torch.Tensor,
+                     k_rows: torch.Tensor, v_rows: torch.Tensor, status: torch.Tensor) -> None:
+    """Rows ``row_ptr[i]:row_ptr[i + 1]`` of ``k_rows`` / ``v_rows`` to slot ``seqs[i]`` from position ``start[i]`` on (``None``: its last rows)."""
+    n, dev, rows = seqs.shape[0], pages.device, k_rows.shape[0]
+    _here(dev)
+    _rows(k_rows, pages.struct.n_kv_heads, pages, rows)
+    _rows(v_rows, pages.struct.n_kv_heads, pages, rows)
+    _check(lib.vlac_pages_write(pages.ref, layer, _ints(seqs, n, dev), None if start is None else _ints(start, n, dev),
+                                _ints(row_ptr, n + 1, dev), n, rows, k_rows.data_ptr(), _row_stride(k_rows), v_rows.data_ptr(),
+                                _row_stride(v_rows), _ints(status, n, dev), _stream()), "vlac_pages_write")
+
+
+def vlac_pages_from_cache(pages: Pages, cache: int, seq: int, slot: int, n_rows: int, status: torch.Tensor) -> None:
+    """Positions ``0 .. n_rows - 1`` of sequence ``seq`` of a control-step cache into ``slot``, all layers."""
+    _here(pages.device)
+    _check(lib.vlac_pages_from_cache(pages.ref, cache, seq, slot, n_rows, _ints(status, 1, pages.device), _stream()), "vlac_pages_from_cache")
+
+
+def vlac_prefix_bytes(pages: Pages, n: int, rows: int, n_heads: int) -> int:
+    return int(lib.vlac_prefix_bytes(pages.ref, n, rows, n_heads))
+
+
+def vlac_prefix_plan(pages: Pages, plan: PrefixPlan, seqs: torch.Tensor, q_ptr: torch.Tensor, status: torch.Tensor) -> None:
+    """Find what neighbours of the list share and divide the work; serves every layer until tables, lengths or ``q_ptr`` change."""
+    dev = pages.device
+    assert plan.device == dev
+    _here(dev)
+    _check(lib.vlac_prefix_plan(pages.ref, plan.ref, _ints(seqs, plan.n, dev), _ints(q_ptr, plan.n + 1, dev), _ints(status, plan.n, dev),
+                                _stream()), "vlac_prefix_plan")
+
+
+def vlac_prefix_attention(pages: Pages, layer: int, plan: PrefixPlan, q: torch.Tensor, scale: float, out: torch.Tensor,
+                          lse: Optional[torch.Tensor] = None) -> None:
+    """Attention of the plan's rows: ``q``, ``out`` ``[rows, n_heads, head_dim]`` of the pool's type, ``lse`` fp32 ``[rows, n_heads]``."""
+    dev = pages.device
+    assert plan.device == dev
+    _here(dev)
+    _rows(q, plan.n_heads, pages, plan.rows)
+    _rows(out, plan.n_heads, pages, plan.rows)
+    assert lse is None or (lse.device == dev and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (plan.rows, plan.n_heads))
+    _check(lib.vlac_prefix_attention(pages.ref, layer, plan.ref, q.data_ptr(), _row_stride(q), scale, out.data_ptr(), _row_stride(out), _ptr(lse),
+                                     _stream()), "vlac_prefix_attention")
 
 
 # --------------------------------------------------------------------------- reading views back

@@ -1,0 +1,372 @@
+"""Attention over paged sequences with a shared prefix against its definition in 64 bits.  Bounds: pages_reference.attention."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import pages_reference as ref
+from paper_2502_02175_b200 import synth
+
+pytestmark = pytest.mark.gpu
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+@pytest.fixture(scope="module")
+def vb():
+    from paper_2502_02175_b200 import binding
+    return binding
+
+
+def dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to("cuda")
+
+
+class Case:
+    """Groups of sequences made with the pool calls: (common rows, [(own rows, query rows), ...]) per group."""
+
+    def __init__(self, vb, groups, heads=4, kv_heads=4, d=64, page=16, dtype=torch.bfloat16, seed=0, layers=1, spare=3, q_scale=2.0, fill=float("nan")):
+        self.vb, self.heads, self.kv_heads, self.d, self.page, self.dtype = vb, heads, kv_heads, d, page, dtype
+        self.gen = torch.Generator(device="cuda")
+        self.gen.manual_seed(seed)
+        total = sum(c + sum(o + page for o, _ in m) for c, m in groups) + spare * page
+        longest = max([c + o for c, m in groups for o, _ in m] + [1])
+        n_slots = sum(len(m) + 1 for _, m in groups) + 1
+        self.pages = p = vb.Pages.empty(layers, -(-total // page) + len(groups) + spare, page, kv_heads, d, n_slots, -(-longest // page) + 1, dtype)
+        p.k.fill_(fill)                                                  # rows nobody wrote must never matter
+        p.v.fill_(fill)
+        self.seqs, self.nq, slot = [], [], 0
+        for c, members in groups:
+            base = slot
+            slot += 1
+            self.resize([base], [c])
+            self.fill(base, 0, c)
+            for o, nq in members:
+                st = self.st(1)
+                vb.vlac_pages_fork(p, dev([base]), dev([slot]), False, st)
+                assert st.item() == 0
+                self.resize([slot], [c + o])
+                self.fill(slot, c, o)
+                self.seqs.append(slot)
+                self.nq.append(nq)
+                slot += 1
+        self.rows = sum(self.nq)
+        self.q = (torch.empty((self.rows, heads, d), device="cuda").normal_(generator=self.gen) * q_scale).to(dtype)
+        self.scale = 1.0 / math.sqrt(d)
+
+    def st(self, n):
+        return torch.full((n,), 9, dtype=torch.int32, device="cuda")
+
+    def resize(self, slots, lens):
+        st = self.st(len(slots))
+        self.vb.vlac_pages_resize(self.pages, dev(slots), dev(lens), st)
+        assert st.tolist() == [0] * len(slots)
+
+    def fill(self, slot, start, n):
+        for l in range(self.pages.k.shape[0]):
+            x, y = (torch.empty((n, self.kv_heads, self.d), device="cuda").normal_(generator=self.gen).to(self.dtype) for _ in range(2))
+            st = self.st(1)
+            self.vb.vlac_pages_write(self.pages, l, dev([slot]), dev([start]), dev([0, n]), x, y, st)
+            assert st.item() == 0
+
+    def run(self, q=None, layer=0, out=None, lse=True, plan=None):
+        n = len(self.seqs)
+        q = self.q if q is None else q
+        plan = plan or self.vb.PrefixPlan(self.pages, n, self.rows, self.heads)
+        out = torch.full((self.rows, self.heads, self.d), 5.0, dtype=self.dtype, device="cuda") if out is None else out
+        l = torch.full((self.rows, self.heads), 5.0, device="cuda") if lse else None
+        st = self.st(n)
+        self.vb.vlac_prefix_plan(self.pages, plan, dev(self.seqs), dev(np.concatenate([[0], np.cumsum(self.nq)])), st)
+        self.vb.vlac_prefix_attention(self.pages, layer, plan, q, self.scale, out, l)
+        assert st.tolist() == [0] * n
+        return out, l
+
+    def want(self, i, layer=0, q=None):
+        """(out, lse, bounds) of sequence i in 64 bits, through its own table."""
+        slot, nq = self.seqs[i], self.nq[i]
+        n = int(self.pages.len[slot])
+        t = self.pages.table[slot, :-(-n // self.page)].long()
+        k, v = (x[layer, t].reshape(-1, self.kv_heads, self.d)[:n].double().cpu().numpy() for x in (self.pages.k, self.pages.v))
+        r0 = sum(self.nq[:i])
+        q = (self.q if q is None else q)[r0:r0 + nq].double().cpu().numpy()
+        return ref.attention(k, v, q, n, nq, self.heads // self.kv_heads, self.scale, HALF[self.dtype])
+
+    def check(self, out, lse, layer=0, q=None, only=None):
+        for i in range(len(self.seqs)) if only is None else only:
+            o, l, eo, el = self.want(i, layer, q)
+            r0 = sum(self.nq[:i])
+            got = out[r0:r0 + self.nq[i]].double().cpu().numpy()
+            bad = np.abs(got - o) > eo
+            assert not np.any(bad | ~np.isfinite(got)), (i, np.argwhere(bad)[:3], np.max(np.abs(got - o) / eo))
+            if lse is not None:
+                gl = lse[r0:r0 + self.nq[i]].double().cpu().numpy()
+                inf = np.isneginf(l)
+                assert np.array_equal(np.isneginf(gl), inf)
+                assert np.all(np.abs(gl[~inf] - l[~inf]) <= el[~inf]), i
+
+
+# (common rows, [(own rows, query rows)])
+GROUPS = {
+    "one_row_one_key": [(0, [(1, 1)])],
+    "two_candidates": [(32, [(3, 1), (5, 1)])],
+    "unshared_tail": [(37, [(1, 1), (20, 1), (64, 1)])],                        # the partly filled page is each one's own
+    "page_ends": [(16, [(15, 1), (16, 1), (17, 1)]), (64, [(64, 1), (1, 1)])],
+    "chunks_of_7": [(100, [(7, 7), (9, 7), (30, 7)])],
+    "prefill": [(0, [(33, 33)]), (48, [(130, 70)]), (0, [(65, 2)])],
+    "more_queries_than_rows": [(0, [(3, 5), (1, 4), (0, 2)])],
+    "nothing_to_do": [(48, [(2, 0), (2, 1), (2, 0), (3, 1)])],
+    "many_single": [(0, [(n, 1)]) for n in (1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 300)],
+    "ragged_groups": [(160, [(n % 23 + 1, 1) for n in range(19)]), (0, [(700, 3)]), (320, [(n + 2, 2) for n in range(9)])],
+    "long": [(4100, [(n + 1, 1) for n in range(5)])],
+    "crowd": [(200, [(n % 7 + 1, 1) for n in range(70)])],
+}
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("heads,kv_heads,d", [(4, 4, 64), (4, 1, 128), (6, 2, 64), (2, 2, 128), (15, 3, 64), (17, 1, 64)])
+@pytest.mark.parametrize("groups", GROUPS, ids=str)
+def test_against_the_definition(vb, groups, heads, kv_heads, d, dtype):
+    c = Case(vb, GROUPS[groups], heads, kv_heads, d, dtype=dtype, seed=len(groups))
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("page", [8, 32, 64, 128, 256])
+def test_page_sizes(vb, page):
+    c = Case(vb, [(page * 3 + 5, [(1, 1), (page, 1), (page + 3, 2)]), (page, [(2, 2)] * 18)], 8, 2, 128, page=page, seed=page)
+    c.check(*c.run())
+
+
+def test_layers_strides_and_no_lse(vb):
+    """A layer of several; q and out as slices of wider buffers (a fused projection's rows); lse left out."""
+    c = Case(vb, [(50, [(3, 1), (4, 2)])], 4, 2, 64, layers=3, seed=2)
+    wide = torch.full((c.rows, 3, c.heads, c.d), 3.0, dtype=c.dtype, device="cuda")
+    wide[:, 1] = c.q
+    for layer in (2, 0):
+        out = torch.full((c.rows + 2, 2 * c.heads, c.d), 7.0, dtype=c.dtype, device="cuda")
+        c.run(q=wide[:, 1], layer=layer, out=out[1:-1, :c.heads], lse=False)
+        c.check(out[1:-1, :c.heads], None, layer)
+        assert torch.all(out[0] == 7) and torch.all(out[-1] == 7) and torch.all(out[:, c.heads:] == 7)
+
+
+def test_refused_entries_leave_their_rows(vb):
+    """Slots and pages out of range: a code each, their rows untouched, the others right; rows behind the last untouched."""
+    c = Case(vb, [(48, [(3, 1), (5, 2), (2, 1), (4, 1)])], seed=4)
+    n, rows = 4, c.rows + 3
+    q = torch.cat([c.q, c.q[:3]])
+    plan = vb.PrefixPlan(c.pages, n, rows, c.heads)
+    ptr = dev([0, 1, 3, 4, 5])
+    keep_table = c.pages.table.clone()
+    for kind, code in (("slot", -1), ("slot_low", -1), ("page", -2), ("page_low", -2), ("len", -2)):
+        seqs = list(c.seqs)
+        keep_len = c.pages.len.clone()
+        if kind == "slot":
+            seqs[1] = 10 ** 6
+        elif kind == "slot_low":
+            seqs[1] = -1
+        elif kind == "page":
+            c.pages.table[seqs[1], 1] = 10 ** 6
+        elif kind == "page_low":
+            c.pages.table[seqs[1], 3] = -7
+        else:
+            c.pages.len[seqs[1]] = 10 ** 7
+        out, lse, st = torch.full((rows, c.heads, c.d), 5.0, dtype=c.dtype, device="cuda"), torch.full((rows, c.heads), 5.0, device="cuda"), c.st(n)
+        vb.vlac_prefix_plan(c.pages, plan, dev(seqs), ptr, st)
+        vb.vlac_prefix_attention(c.pages, 0, plan, q, c.scale, out, lse)
+        assert st.tolist() == [0, code, 0, 0]
+        assert torch.all(out[1:3] == 5) and torch.all(lse[1:3] == 5) and torch.all(out[5:] == 5) and torch.all(lse[5:] == 5)
+        c.pages.table.copy_(keep_table)
+        c.pages.len.copy_(keep_len)
+        c.check(out, lse, only=(0, 2, 3))
+    # pointers: one too large refuses its entry, one that falls refuses all (rows would overlap)
+    for bad, want in (([0, 1, 3, 4, 99], [0, 0, 0, -1]), ([0, 3, 1, 4, 5], [-1] * 4), ([-1, 1, 3, 4, 5], [-1, 0, 0, 0])):
+        out = torch.full((rows, c.heads, c.d), 5.0, dtype=c.dtype, device="cuda")
+        vb.vlac_prefix_plan(c.pages, plan, dev(c.seqs), dev(bad), st)
+        vb.vlac_prefix_attention(c.pages, 0, plan, q, c.scale, out)
+        assert st.tolist() == want
+        r0 = 0 if want[0] else 1
+        assert (torch.all(out == 5) if min(want) == max(want) else torch.all(out[(4 if want[3] else 0):(99 if want[3] else 1)] == 5))
+
+
+def test_values_a_row_does_not_see_never_reach_it(vb):
+    """NaN and infinities in the K and V rows of later queries of the same chunk: earlier rows stay exact, the rows that see them do not."""
+    for d, heads in ((64, 1), (128, 3)):
+        c = Case(vb, [(40, [(12, 7), (9, 9)])], heads, 1, d, seed=d)
+        clean, clean_lse = c.run()
+        slot = c.seqs[0]
+        n = int(c.pages.len[slot])
+        at = lambda pos: (int(c.pages.table[slot, pos // 16]), pos % 16)
+        for pos, what in ((n - 1, float("nan")), (n - 2, float("inf"))):
+            pg, r = at(pos)
+            c.pages.v[0, pg, r, 0, 5] = what
+        pg, r = at(n - 1)
+        c.pages.k[0, pg, r, 0, 3] = float("nan")
+        out, lse = c.run()
+        assert torch.equal(out[:5], clean[:5]) and torch.equal(lse[:6], clean_lse[:6])
+        assert torch.equal(out[7:], clean[7:]) and torch.equal(lse[7:], clean_lse[7:])
+        assert torch.all(torch.isposinf(out[5, :, 5])) and torch.equal(out[5, :, 6:], clean[5, :, 6:]) and torch.equal(out[5, :, :5], clean[5, :, :5])
+        assert torch.all(torch.isnan(out[6])) and torch.all(torch.isnan(lse[6]))
+
+
+def test_extreme_scores(vb):
+    """Scores of some hundreds (one key takes all), and equal ones of zero."""
+    for q_scale in (200.0, 0.0):
+        c = Case(vb, [(70, [(5, 1), (3, 2), (66, 1)]), (0, [(90, 40)])], 4, 2, 64, seed=11, q_scale=q_scale)
+        c.check(*c.run())
+
+
+def test_same_slot_twice_and_any_order(vb):
+    """A slot may be listed twice, and the order of the list decides nothing but the division of the work."""
+    c = Case(vb, [(96, [(3, 1), (20, 1), (1, 1)]), (64, [(2, 1), (9, 1)])], 8, 2, 64, seed=5)
+    c.check(*c.run())
+    order = [4, 0, 2, 1, 3, 0, 4]
+    c.seqs, c.nq, c.q, c.rows = [c.seqs[i] for i in order], [1] * 7, c.q[order].contiguous(), 7
+    c.check(*c.run())
+
+
+def test_repeatable_bits_and_plan_for_all_layers(vb):
+    """The same bits every time; one plan serves several layers and several calls."""
+    c = Case(vb, [(500, [(n + 1, 1) for n in range(12)])], 8, 8, 128, layers=2, seed=6)
+    plan = vb.PrefixPlan(c.pages, len(c.seqs), c.rows, c.heads)
+    first = c.run(plan=plan)
+    for layer in (1, 0, 1):
+        out, lse = torch.zeros_like(first[0]), torch.zeros_like(first[1])
+        vb.vlac_prefix_attention(c.pages, layer, plan, c.q, c.scale, out, lse)
+        c.check(out, lse, layer)
+        if layer == 0:
+            assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+
+
+def test_two_graphs_on_two_streams(vb):
+    """Two captured token passes with plans of their own, replayed at the same time, and again after the sequences grew."""
+    c = Case(vb, [(128, [(3, 1), (4, 1), (9, 1)])], 4, 4, 64, seed=7, spare=12)
+    ptr, streams, work = dev([0, 1, 2, 3]), [torch.cuda.Stream() for _ in range(2)], []
+    seqs = dev(c.seqs)
+    torch.cuda.synchronize()
+    for s in streams:
+        plan, out, st = vb.PrefixPlan(c.pages, 3, 3, 4), torch.zeros((3, 4, 64), dtype=c.dtype, device="cuda"), c.st(3)
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=s):
+            vb.vlac_prefix_plan(c.pages, plan, seqs, ptr, st)
+            vb.vlac_prefix_attention(c.pages, 0, plan, c.q, c.scale, out)
+        work.append((g, plan, out, st))
+    for grow in range(3):
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for s, (g, *_rest) in zip(streams, work):
+                with torch.cuda.stream(s):
+                    g.replay()
+        torch.cuda.synchronize()
+        for _, _, out, st in work:
+            assert st.tolist() == [0, 0, 0]
+            c.check(out, None)
+        lens = [int(c.pages.len[s]) + 7 for s in c.seqs]
+        c.resize(c.seqs, lens)
+        for s, n in zip(c.seqs, lens):
+            c.fill(s, n - 7, 7)
+
+
+def test_far_pages(vb):
+    """Element offsets beyond 2^31 in K and V: the last pages of a pool of 5 GB a side."""
+    n_pages, page, kv, d = 10000, 256, 16, 64
+    k = torch.zeros((1, n_pages, page, kv, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    assert k.numel() > 2 ** 31
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    ids = [n_pages - 1, 3, n_pages - 2, n_pages // 2]
+    for i in ids:
+        k[0, i].normal_(generator=g)
+        v[0, i].normal_(generator=g)
+    pages = vb.Pages(k, v, dev([ids, [ids[0], ids[2], -1, -1]]), dev([4 * 256 - 3, 300]), torch.zeros(n_pages, dtype=torch.int32, device="cuda"))
+    q = (torch.empty((2, 32, d), device="cuda").normal_(generator=g) * 2).to(torch.bfloat16)
+    plan, out, st = vb.PrefixPlan(pages, 2, 2, 32), torch.zeros_like(q), torch.zeros(2, dtype=torch.int32, device="cuda")
+    vb.vlac_prefix_plan(pages, plan, dev([0, 1]), dev([0, 1, 2]), st)
+    vb.vlac_prefix_attention(pages, 0, plan, q, 0.125, out)
+    assert st.tolist() == [0, 0]
+    for i, n in ((0, 4 * 256 - 3), (1, 300)):
+        t = pages.table[i, :-(-n // page)].long()
+        kh, vh = (x[0, t].reshape(-1, kv, d)[:n].double().cpu().numpy() for x in (k, v))
+        o, _, eo, _ = ref.attention(kh, vh, q[i:i + 1].double().cpu().numpy(), n, 1, 2, 0.125, HALF[torch.bfloat16])
+        assert np.all(np.abs(out[i:i + 1].double().cpu().numpy() - o) <= eo)
+
+
+def test_candidates_of_a_control_step(vb):
+    """The whole use: a control step's prompt becomes a prefix, candidates are forked from it, grow token by token, attend in
+    every layer, are pruned and given back."""
+    cfg = synth.tiny_config()
+    model = synth.make_model(cfg, 1)
+    devm = vb.DeviceModel(model)
+    ctx = vb.vlac_create(vb.make_config(cfg, 1), devm.weights)
+    cache = vb.vlac_cache_alloc(ctx, 1)
+    try:
+        rng = np.random.default_rng(1)
+        feats = vb.upload_bf16(synth.f32_to_bf16(rng.standard_normal((1, cfg.n_vision, cfg.hidden), dtype=np.float32)))
+        frames = torch.from_numpy(synth.rerandomised_pair(cfg, 1, 13)[0][None]).to("cuda").contiguous()
+        ids = torch.from_numpy(synth.make_prompt_ids(cfg, 1)).to("cuda")
+        tokens = torch.zeros((1, cfg.n_action), dtype=torch.int32, device="cuda")
+        vb.vlac_step(ctx, cache, frames, feats, ids, vb.make_params()[0], False, tokens)
+        n, L, H, d = 6, cfg.seq_len, cfg.n_heads, cfg.head_dim
+        pages = vb.Pages.empty(cfg.n_layers, 40, 16, H, d, n + 1, 8)
+        st1, st = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+        root, kids = dev([0]), dev(np.arange(1, n + 1))
+        vb.vlac_pages_resize(pages, root, dev([L]), st1)
+        vb.vlac_pages_from_cache(pages, cache, 0, 0, L, st1)
+        vb.vlac_pages_fork(pages, dev([0] * n), kids, False, st)
+        assert int(pages.refs.max()) == n + 1
+        plan, ptr = vb.PrefixPlan(pages, n, n, H), dev(np.arange(n + 1))
+        rows = {}
+        for t in range(4):
+            vb.vlac_pages_resize(pages, kids, dev([L + t + 1] * n), st)
+            vb.vlac_prefix_plan(pages, plan, kids, ptr, st)
+            assert st.tolist() == [0] * n
+            for l in range(cfg.n_layers):
+                q, k, v = (torch.randn((n, H, d), device="cuda").to(torch.bfloat16) for _ in range(3))
+                rows[t, l] = (k, v)
+                out = torch.zeros_like(q)
+                vb.vlac_pages_write(pages, l, kids, None, ptr, k, v, st)
+                vb.vlac_prefix_attention(pages, l, plan, q, d ** -0.5, out)
+                kc, vc = (torch.empty((cfg.max_seq, H, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+                vb.vlac_cache_read(cache, vb.PART_K, 0, l, kc)
+                vb.vlac_cache_read(cache, vb.PART_V, 0, l, vc)
+                for i in range(n):
+                    kk = torch.cat([kc[:L]] + [rows[x, l][0][i:i + 1] for x in range(t + 1)]).double().cpu().numpy()
+                    vv = torch.cat([vc[:L]] + [rows[x, l][1][i:i + 1] for x in range(t + 1)]).double().cpu().numpy()
+                    o, _, eo, _ = ref.attention(kk, vv, q[i:i + 1].double().cpu().numpy(), L + t + 1, 1, 1, d ** -0.5, HALF[torch.bfloat16])
+                    assert np.all(np.abs(out[i:i + 1].double().cpu().numpy() - o) <= eo), (t, l, i)
+        # prune vision tokens of one candidate, attend again, then give everything back
+        keep = np.concatenate([[0], np.arange(1, 65, 2), np.arange(65, L + 4)])
+        vb.vlac_pages_compact(pages, dev([2]), dev([2]), dev([0, len(keep)]), dev(keep), st1)
+        assert st1.item() == 0 and int(pages.len[2]) == len(keep)
+        plan1, q, out = vb.PrefixPlan(pages, 1, 1, H), torch.randn((1, H, d), device="cuda").to(torch.bfloat16), torch.zeros((1, H, d), dtype=torch.bfloat16, device="cuda")
+        vb.vlac_prefix_plan(pages, plan1, dev([2]), dev([0, 1]), st1)
+        vb.vlac_prefix_attention(pages, 1, plan1, q, d ** -0.5, out)
+        kk = torch.cat([kc[:L]] + [rows[x, 1][0][1:2] for x in range(4)])[keep].double().cpu().numpy()
+        vv = torch.cat([vc[:L]] + [rows[x, 1][1][1:2] for x in range(4)])[keep].double().cpu().numpy()
+        o, _, eo, _ = ref.attention(kk, vv, q.double().cpu().numpy(), len(keep), 1, 1, d ** -0.5, HALF[torch.bfloat16])
+        assert np.all(np.abs(out.double().cpu().numpy() - o) <= eo)
+        vb.vlac_pages_free(pages, dev(np.arange(n + 1)), torch.zeros(n + 1, dtype=torch.int32, device="cuda"))
+        assert int(pages.refs.abs().max()) == 0 and int(pages.len.max()) == 0 and int(pages.table.max()) == -1
+    finally:
+        vb.vlac_cache_free(cache)
+        vb.vlac_destroy(ctx)
+
+
+def test_wrong_tensors_are_refused(vb):
+    c = Case(vb, [(16, [(2, 1), (3, 1)])])
+    plan, st, ptr, out = vb.PrefixPlan(c.pages, 2, 2, 4), c.st(2), dev([0, 1, 2]), torch.zeros_like(c.q)
+    seqs = dev(c.seqs)
+    with pytest.raises(AssertionError):
+        vb.vlac_prefix_plan(c.pages, plan, seqs.long(), ptr, st)
+    with pytest.raises(AssertionError):
+        vb.vlac_prefix_plan(c.pages, plan, seqs[:1], ptr, st)
+    vb.vlac_prefix_plan(c.pages, plan, seqs, ptr, st)
+    for q in (c.q.float(), c.q[:1], c.q[:, :2], c.q.half(), c.q.cpu(), c.q.transpose(1, 2)):
+        with pytest.raises(AssertionError):
+            vb.vlac_prefix_attention(c.pages, 0, plan, q, 1.0, out)
+    with pytest.raises(AssertionError):
+        vb.vlac_prefix_attention(c.pages, 0, plan, c.q, 1.0, out, torch.zeros((2, 3), device="cuda"))
+    with pytest.raises(vb.VlacError):
+        vb.vlac_prefix_attention(c.pages, 1, plan, c.q, 1.0, out)
+    with pytest.raises(vb.VlacError):
+        vb.PrefixPlan(vb.Pages.empty(1, 4, 16, 3, 64, 2, 2), 2, 2, 4)
