@@ -391,6 +391,9 @@ unsigned long long vlac_prefix_bytes(const vlac_pages* p, int n, int rows, int n
 int vlac_prefix_plan(const vlac_pages* p, const vlac_prefix* plan, const int* seqs, const int* q_ptr, int* status, void* stream);
 int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
                           void* out, long long out_stride, float* lse, void* stream);
+/* VLAC_ERR_TIMEOUT if a device-side bounded wait of an attention call gave up since the plan was made (its output is then not
+ * valid), as vlac_device_error does for a context; reads one int back and synchronises the stream. */
+int vlac_prefix_error(const vlac_prefix* plan, void* stream);
 
 const char* vlac_status_string(int status);
 

@@ -68,7 +68,8 @@ EXPORTS = ("vlac_create", "vlac_destroy", "vlac_cache_alloc", "vlac_cache_reset"
            "vlac_profile", "vlac_profile_read", "vlac_profile_segments", "vlac_greedy_tokens_static",
            "vlac_selftest_wait_expiry",
            "vlac_pages_work_bytes", "vlac_pages_resize", "vlac_pages_free", "vlac_pages_fork", "vlac_pages_compact", "vlac_pages_write",
-           "vlac_pages_from_cache", "vlac_prefix_bytes", "vlac_prefix_plan", "vlac_prefix_attention")
+           "vlac_pages_from_cache", "vlac_prefix_bytes", "vlac_prefix_plan", "vlac_prefix_attention",
+           "vlac_prefix_error")
 
 lib.vlac_status_string.restype = C.c_char_p
 lib.vlac_status_string.argtypes = [C.c_int]
@@ -111,6 +112,7 @@ lib.vlac_pages_from_cache.argtypes = [_P, _P, _I, _I, _I, _P, _P]
 lib.vlac_prefix_bytes.restype = C.c_ulonglong
 lib.vlac_prefix_bytes.argtypes = [_P, _I, _I, _I]
 lib.vlac_prefix_plan.argtypes = [_P, _P, _P, _P, _P, _P]
+lib.vlac_prefix_error.argtypes = [_P, _P]
 lib.vlac_prefix_attention.argtypes = [_P, _I, _P, _P, _LL, C.c_float, _P, _LL, _P, _P]
 
 
@@ -527,6 +529,10 @@ def vlac_prefix_attention(pages: Pages, layer: int, plan: PrefixPlan, q: torch.T
     assert lse is None or (lse.device == dev and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (plan.rows, plan.n_heads))
     _check(lib.vlac_prefix_attention(pages.ref, layer, plan.ref, q.data_ptr(), _row_stride(q), scale, out.data_ptr(), _row_stride(out), _ptr(lse),
                                      _stream()), "vlac_prefix_attention")
+
+
+def vlac_prefix_error(plan: PrefixPlan) -> int:
+    return int(lib.vlac_prefix_error(plan.ref, _stream()))
 
 
 # --------------------------------------------------------------------------- reading views back

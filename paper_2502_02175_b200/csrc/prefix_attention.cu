@@ -4,21 +4,27 @@
 //     o = sum_i 2^(m_i - M) l_i o_i / sum_i 2^(m_i - M) l_i      (m_i, l_i: maximum and sum of 2^(s - m_i) of set i)
 // so the pages that several sequences have in common are one problem with the query rows of all of them (and of all query
 // heads of a K/V head) stacked, and each sequence's own rows are another with its rows alone.  These problems are "segments";
-// a segment is cut into (K/V head, tile of stacked rows, block of 64 keys) units, and the units of the whole call are dealt to a
-// fixed number of CTAs in equal contiguous runs, whatever the lengths: a run may begin and end inside a tile, every piece of a
+// a segment is cut into (K/V head, tile of stacked rows, block of keys) units, and the units of the whole call are dealt to a
+// fixed number of warps or CTAs in equal contiguous runs, whatever the lengths: a run may begin and end inside a tile, every piece of a
 // tile leaves (unnormalised o, m, l) in a slot of its own, and a second kernel adds a row's pieces in a fixed order.
 #include "pages_internal.h"
 #include "launch_util.h"
+#include <cuda.h>
 #include <cuda_fp16.h>
 #include <math.h>
+#include <stddef.h>
 
 namespace {
 
-constexpr int PF_GRID_A = 2 * 148;              // CTAs of the warp-MMA kernel: two per SM
-constexpr int PF_KB = 64;                       // keys per unit
-constexpr int PF_BM = 64;                       // stacked rows of a tile (16 in segments that have no more)
-constexpr int PF_STAGES = 3;
-constexpr int PF_THREADS = 128;
+// Two kernels share the segments.  Wide: common pages with more than 16 stacked rows, which every row sees whole (tcgen05).  Narrow:
+// the rest -- prefixes of few rows and every sequence's own rows, where the causal mask lies (warp-level tensor cores).
+constexpr int NARROW = 0, WIDE = 1;
+constexpr int PN_WARPS = 4, PN_CTAS = 2 * 148;  // narrow: two CTAs of four warps per SM, every warp works alone
+constexpr int PF_MAX_RUNS = PN_WARPS * PN_CTAS; // runs of the narrow kernel
+constexpr int PW_CTAS = 148;                    // runs of the wide kernel: one CTA per SM
+__host__ __device__ constexpr int pf_bm(int c) { return c == NARROW ? 16 : 128; }        // stacked rows of a tile
+__host__ __device__ constexpr int pf_kb(int c) { return c == NARROW ? 64 : 128; }        // keys of a unit
+__host__ __device__ constexpr int pf_runs(int c) { return c == NARROW ? PF_MAX_RUNS : PW_CTAS; }
 
 struct SeqRec { int slot, row0, nq, len, pre_seg, suf_seg, pad0, pad1; };          // segments: -1 none
 struct SegRec {
@@ -27,17 +33,17 @@ struct SegRec {
   int row0, R;                                  // first q row; stacked rows per K/V head: (q rows) * (query heads per K/V head)
   int key0, key1;                               // positions [key0, key1)
   int pos0;                                     // position of q row row0; INT_MIN in a prefix: every row sees every key
-  int bm, T, KB;                                // rows per tile, tiles, key blocks
+  int cls, T, KB;                               // NARROW or WIDE, tiles, key blocks
   int rowbase;                                  // first slot row of this segment
 };
-struct PlanHead { long long units; int n_seg; int n_act; };
+struct PlanHead { long long units[2]; int n_act, error; };   // error: a wait of the wide kernel gave up
 
 struct PlanMem {
   PlanHead* head;
   int *lcp, *bad;                               // [n] common pages with the previous active sequence; findings
   SeqRec* seq;                                  // [n] active sequences
   SegRec* seg;                                  // [2n]
-  int* first;                                   // [PF_GRID_A] segment of each CTA's first unit
+  int* first[2];                                // segment of each run's first unit
   int* row_k;                                   // [rows] active sequence of each row, -1: none
   float2* ml;                                   // [slot rows] (m, l), m in units of log2
   float* po;                                    // [slot rows][head_dim]
@@ -53,18 +59,23 @@ __host__ __device__ inline PlanMem plan_mem(void* mem, int n, int rows, int n_he
   p.bad = (int*)take(sizeof(int) * n);
   p.seq = (SeqRec*)take(sizeof(SeqRec) * n);
   p.seg = (SegRec*)take(sizeof(SegRec) * 2 * (size_t)n);
-  p.first = (int*)take(sizeof(int) * PF_GRID_A);
+  for (int c = 0; c < 2; ++c) p.first[c] = (int*)take(sizeof(int) * pf_runs(c));
   p.row_k = (int*)take(sizeof(int) * (size_t)(rows > 0 ? rows : 1));
-  const size_t slots = 2 * (size_t)rows * n_heads + (size_t)PF_GRID_A * PF_BM;
+  const size_t slots = 2 * (size_t)rows * n_heads + (size_t)pf_runs(NARROW) * pf_bm(NARROW) + (size_t)pf_runs(WIDE) * pf_bm(WIDE);
   p.ml = (float2*)take(sizeof(float2) * slots);
   p.po = (float*)take(sizeof(float) * slots * head_dim);
   p.bytes = o;
   return p;
 }
 
-// U units are dealt to G = min(U, PF_GRID_A) CTAs, so that no run is empty: run c is [c*U/G, (c+1)*U/G).  The CTA whose run holds u:
-__device__ __forceinline__ long long runs(long long U) { return U < PF_GRID_A ? U : PF_GRID_A; }
-__device__ __forceinline__ int run_of(long long u, long long U) { return (int)(((u + 1) * runs(U) - 1) / U); }
+// The U units of a class are dealt to G = min(U, pf_runs) runs, so that none is empty: run c is [c*U/G, (c+1)*U/G).  The run of unit u:
+__device__ __forceinline__ long long runs(int cls, long long U) { return U < pf_runs(cls) ? U : pf_runs(cls); }
+__device__ __forceinline__ int run_of(int cls, long long u, long long U) { return (int)(((u + 1) * runs(cls, U) - 1) / U); }
+
+// Whether a tile of a segment is one piece and holds everything its rows see: then the piece writes the result itself.
+__device__ __forceinline__ bool tile_direct(const SegRec& s, long long u_tile, long long U) {
+  return s.pos0 != INT_MIN && s.key0 == 0 && run_of(s.cls, u_tile, U) == run_of(s.cls, u_tile + s.KB - 1, U);
+}
 
 // ------------------------------------------------------------------------------------------------ plan
 struct PlanArgs {
@@ -176,45 +187,52 @@ __global__ void __cluster_dims__(PL_CTAS, 1, 1) __launch_bounds__(PL_THREADS, 1)
   __syncthreads();
   // ---- segments: thread k makes the prefix of a group that k leads, and k's own rows
   long long u_pre = 0, u_suf = 0;
-  int r_pre = 0, r_suf = 0, pre = 0, lead = 0, t_pre = 0, t_suf = 0, kb_pre = 0, kb_suf = 0;
+  int r_pre = 0, r_suf = 0, pre = 0, lead = 0, c_pre = NARROW, t_pre = 0, t_suf = 0, kb_pre = 0, kb_suf = 0;
   if (mine && !bad) {
     lead = s_lead[tid];
-    if (s_m[lead] >= 2) pre = s_c[lead] << a.shift;
+    const int r_all = (s_end[lead] - s_row0[lead]) * a.ratio;
+    // a sequence alone: its pages in front of many query rows are worth a segment of their own (no mask, wide tiles)
+    if (s_m[lead] >= 2 || r_all > pf_bm(NARROW)) pre = s_c[lead] << a.shift;
     if (lead == tid && pre > 0) {
-      r_pre = (s_end[tid] - s_row0[tid]) * a.ratio;
-      const int bm = r_pre <= 16 ? 16 : PF_BM;
-      t_pre = (r_pre + bm - 1) / bm; kb_pre = (pre + PF_KB - 1) / PF_KB;
+      r_pre = r_all;
+      c_pre = r_pre > pf_bm(NARROW) ? WIDE : NARROW;
+      t_pre = (r_pre + pf_bm(c_pre) - 1) / pf_bm(c_pre); kb_pre = (pre + pf_kb(c_pre) - 1) / pf_kb(c_pre);
       u_pre = (long long)a.kv_heads * t_pre * kb_pre;
     }
     if (s_len[tid] > pre) {
       r_suf = s_nq[tid] * a.ratio;
-      const int bm = r_suf <= 16 ? 16 : PF_BM;
-      t_suf = (r_suf + bm - 1) / bm; kb_suf = (s_len[tid] - pre + PF_KB - 1) / PF_KB;
+      t_suf = (r_suf + pf_bm(NARROW) - 1) / pf_bm(NARROW); kb_suf = (s_len[tid] - pre + pf_kb(NARROW) - 1) / pf_kb(NARROW);
       u_suf = (long long)a.kv_heads * t_suf * kb_suf;
     }
   }
-  long long units, slots, segs;
-  const long long u0 = plan_scan(u_pre + u_suf, &units);
-  const long long b0 = plan_scan((long long)(r_pre + r_suf) * a.kv_heads, &slots);
+  const bool wide = c_pre == WIDE && u_pre > 0;
+  const long long u_n = (wide ? 0 : u_pre) + u_suf, b_n = (long long)((wide ? 0 : r_pre) + r_suf) * a.kv_heads;
+  long long units[2], slots_n, slots_w, segs;
+  const long long u0_n = plan_scan(u_n, &units[NARROW]), u0_w = plan_scan(wide ? u_pre : 0, &units[WIDE]);
+  const long long b0_n = plan_scan(b_n, &slots_n), b0_w = plan_scan(wide ? (long long)r_pre * a.kv_heads : 0, &slots_w);
   const int g0 = (int)plan_scan((u_pre > 0) + (u_suf > 0), &segs);
   s_c[tid] = g0;                                                        // (s_c was read above, before the scans' barriers)
   __syncthreads();
   if (mine) {
     SeqRec q = {s_slot[tid], s_row0[tid], s_nq[tid], s_len[tid], pre > 0 ? s_c[lead] : -1, u_suf > 0 ? g0 + (u_pre > 0) : -1, 0, 0};
     p.seq[tid] = q;
-    const long long G = runs(units);
-    auto put = [&](int g, long long us, long long n, int R, int k0, int k1, int pos0, int T, int KB, long long base) {
-      SegRec s = {us, us + n, s_slot[tid], s_row0[tid], R, k0, k1, pos0, R <= 16 ? 16 : PF_BM, T, KB, (int)base};
+    auto put = [&](int g, int cls, long long us, long long n, int R, int k0, int k1, int pos0, int T, int KB, long long base) {
+      SegRec s = {us, us + n, s_slot[tid], s_row0[tid], R, k0, k1, pos0, cls, T, KB, (int)base};
       p.seg[g] = s;
-      for (long long c = (us * G + units - 1) / units, e = ((us + n) * G + units - 1) / units; c < e; ++c) p.first[c] = g;
+      const long long U = units[cls], G = runs(cls, U);
+      for (long long c = (us * G + U - 1) / U, e = ((us + n) * G + U - 1) / U; c < e; ++c) p.first[cls][c] = g;
     };
-    if (u_pre > 0) put(g0, u0, u_pre, r_pre, 0, pre, INT_MIN, t_pre, kb_pre, b0);
-    if (u_suf > 0) put(g0 + (u_pre > 0), u0 + u_pre, u_suf, r_suf, pre, s_len[tid], s_len[tid] - s_nq[tid], t_suf, kb_suf, b0 + (long long)r_pre * a.kv_heads);
+    // slots: the narrow pieces' rows, then the wide ones' (each run sets itself off by a tile, see slot_row)
+    const long long at_w = slots_n + (long long)pf_runs(NARROW) * pf_bm(NARROW);
+    if (u_pre > 0) put(g0, c_pre, wide ? u0_w : u0_n, u_pre, r_pre, 0, pre, INT_MIN, t_pre, kb_pre, wide ? at_w + b0_w : b0_n);
+    if (u_suf > 0)
+      put(g0 + (u_pre > 0), NARROW, u0_n + (wide ? 0 : u_pre), u_suf, r_suf, pre, s_len[tid], s_len[tid] - s_nq[tid], t_suf, kb_suf,
+          b0_n + (wide ? 0 : (long long)r_pre * a.kv_heads));
   }
-  if (tid == 0) { PlanHead h = {units, (int)segs, n_act}; *p.head = h; }
+  if (tid == 0) { PlanHead h = {{units[0], units[1]}, n_act, 0}; *p.head = h; }
 }
 
-// ------------------------------------------------------------------------------------------------ attention, warp-level tensor cores
+// ------------------------------------------------------------------------------------------------ both kernels
 struct AttnArgs {
   const void *k, *v;                            // this layer of the pool
   const int* table;
@@ -248,6 +266,46 @@ template <> struct Half2<__half> {
 
 __device__ __forceinline__ unsigned pf_smem(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ float pf_ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+constexpr float PF_LN2 = 0.693147180559945f;
+
+// Piece of a tile that one run computes.
+struct Piece {
+  int slot, head, rt, nr;                       // table; K/V head; tile; valid stacked rows
+  int row0, key0, key1, lim0;                   // q row of stacked row 0 of the segment; keys [key0, key1); see lim0 below
+  int n;                                        // key blocks (steps) of the piece
+  int direct;
+  size_t slot0;                                 // slot row of the tile's first row
+};
+// Run c's piece at unit u (g: its segment, moved on as u passes): fills p and returns its units.
+__device__ __forceinline__ int next_piece(const PlanMem& pm, int cls, long long U, int run, long long u, long long u_end, int* g, Piece* p) {
+  const SegRec* s = pm.seg + *g;
+  while (u >= s->uend || s->cls != cls) s = pm.seg + ++*g;
+  const long long local = u - s->ustart;
+  const int KB = s->KB, T = s->T, per_head = T * KB, head = (int)(local / per_head), rem = (int)(local - (long long)head * per_head);
+  const int rt = rem / KB, kb = rem - rt * KB, R = s->R, bm = pf_bm(cls);
+  const int n = (int)min((long long)(KB - kb), u_end - u);
+  p->slot = s->slot; p->head = head; p->rt = rt; p->nr = min(bm, R - rt * bm); p->row0 = s->row0;
+  p->key0 = s->key0 + kb * pf_kb(cls); p->key1 = min(s->key1, p->key0 + n * pf_kb(cls));
+  // stacked row x of the tile sees the positions below lim0 + x / ratio (x counted from the segment's start)
+  p->lim0 = s->pos0 == INT_MIN ? INT_MIN : s->pos0 + 1;
+  p->n = n;
+  p->direct = tile_direct(*s, u - kb, U);
+  p->slot0 = (size_t)s->rowbase + (size_t)head * R + (size_t)rt * bm + (size_t)run * bm;
+  return n;
+}
+
+// ------------------------------------------------------------------------------------------------ narrow: warp-level tensor cores
+// Every warp walks its own run of units in steps of 16 keys with 16 stacked rows, with a ring of three steps of K and V in shared
+// memory filled by cp.async ahead of the products, across piece boundaries; nothing is synchronised beyond the warp.  Bound: HBM
+// (K/V rows are read once; a lone query row fills one of the 16 rows of the products, which cost nothing next to the loads).
+constexpr int PN_STAGES = 3;
+constexpr int PN_STEP = 16;
+template <int D> struct Narrow {
+  static constexpr int HALF = PN_STEP * 128;                            // 64 elements of 16 rows
+  static constexpr int TILE = PN_STEP * D * 2;
+  static constexpr int WARP = TILE * (1 + 2 * PN_STAGES);               // Q, then the ring
+  static constexpr int SMEM = WARP * PN_WARPS;
+};
 __device__ __forceinline__ void pf_ldsm4(unsigned addr, unsigned* r) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
@@ -257,58 +315,142 @@ __device__ __forceinline__ void pf_ldsm4t(unsigned addr, unsigned* r) {
 __device__ __forceinline__ void pf_cp16(unsigned dst, const void* src, bool valid) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
 }
-// byte offset of 16-byte piece `col16` of row `row` in a [64 rows][64 elements] block whose pieces are XOR-swizzled by the row
-__device__ __forceinline__ unsigned pf_swz(int row, int col16) { return (unsigned)(row * 128 + (((col16 ^ row) & 7) << 4)); }
+// byte offset of 16-byte piece c16 of a row in a [rows][64 elements] block whose pieces are XOR-swizzled by the row
+__device__ __forceinline__ unsigned pf_swz(int row, int c16) { return (unsigned)(row * 128 + (((c16 ^ row) & 7) << 4)); }
 
-// A tile is [halves of 64 elements][64 rows][128 bytes].  Shared memory of a CTA: Q tile, then PF_STAGES x (K tile, V tile).
-template <int D> __host__ __device__ constexpr int pf_tile() { return 64 * D * 2; }
-template <int D> constexpr int pf_smem_bytes() { return pf_tile<D>() * (1 + 2 * PF_STAGES); }
-
-// One 64-key block.  WIDE: 64 rows, warp w holds rows 16w..16w+15 and all keys.  Otherwise 16 rows and warp w holds keys 16w..16w+15.
-template <typename T, int D, bool WIDE>
-struct Block {
-  static constexpr int NK = WIDE ? 8 : 2;       // 8-key column groups of S per warp
-  float o[D / 8][4];
-  float m[2], l[2];                             // of the thread's two rows (lane/4 and lane/4 + 8)
-  unsigned qf[D / 16][4];
-
-  __device__ __forceinline__ void begin(unsigned q_s, int warp, int lane) {
+template <typename T>
+__device__ __forceinline__ bool any_nonfinite(uint4 x) {
+  const unsigned w[4] = {x.x, x.y, x.z, x.w};
+  bool r = false;
 #pragma unroll
-    for (int j = 0; j < D / 8; ++j) { o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f; }
-    m[0] = m[1] = -INFINITY; l[0] = l[1] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      const int row = (WIDE ? warp * 16 : 0) + (lane & 7) + ((lane >> 3) & 1) * 8, c16 = ks * 2 + (lane >> 4);
-      pf_ldsm4(q_s + (unsigned)(c16 >> 3) * 8192u + pf_swz(row, c16 & 7), qf[ks]);
-    }
+  for (int i = 0; i < 4; ++i) {
+    r |= (w[i] & Half2<T>::exp_mask) == Half2<T>::exp_mask;
+    r |= ((w[i] >> 16) & Half2<T>::exp_mask) == Half2<T>::exp_mask;
   }
-  // key_lo: position of the block's first key; lim[r]: first position row r does not see (masked blocks only)
-  __device__ __forceinline__ void step(unsigned k_s, unsigned v_s, const unsigned char* v_p, int warp, int lane, float scale2, bool masked,
-                                       int key_lo, const int* lim, bool dirty) {
-    const int kw = WIDE ? 0 : warp * 16;
-    float s[NK][4];
+  return r;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArgs a) {
+  using N = Narrow<D>;
+  extern __shared__ __align__(1024) unsigned char pn_raw[];
+  __shared__ Piece s_piece[PN_WARPS][2];
+  const PlanMem pm = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_trigger();
+  pdl_wait();
+  const long long U = pm.head->units[NARROW], G = runs(NARROW, U);
+  const int run = warp * PN_CTAS + blockIdx.x;                          // few runs: one per SM before two
+  if (run >= G) return;
+  long long lu = run * U / G;                                           // load cursor: next unit whose piece is not begun
+  const long long u_end = (run + 1) * U / G;
+  int g = pm.first[NARROW][run];
+
+  unsigned char* const base_p = pn_raw + warp * N::WARP;
+  const unsigned q_s = pf_smem(base_p), ring = q_s + N::TILE;
+  constexpr int C16 = D / 8, RSTEP = 32 / C16, NROW = PN_STEP / RSTEP;  // 16-byte pieces of a row; rows a warp copies at once
+  const int c16 = lane % C16, r_first = lane / C16;
+  const unsigned col_off = (unsigned)(c16 >> 3) * N::HALF;
+  const size_t row_el = (size_t)a.kv_heads * D;
+
+  // ---- load cursor
+  int l_begun = 0, l_step = 0, l_steps = 0, l_cnt = 0, pg_lo = 0, pg_hi = 0;
+  int c_begun = 0, c_cnt = 0;
+  const T *kg = nullptr, *vg = nullptr;
+  Piece lp;
+  auto issue = [&]() -> bool {                                          // one more step in flight
+    if (l_step == l_steps) {
+      // the next piece: its Q may be fetched once the previous piece's Q is in registers
+      if (lu >= u_end || l_begun != c_begun) return false;
+      lu += next_piece(pm, NARROW, U, run, lu, u_end, &g, &lp);
+      if (lane == 0) s_piece[warp][l_begun & 1] = lp;
+      ++l_begun;
+      l_step = 0; l_steps = (lp.key1 - lp.key0 + PN_STEP - 1) / PN_STEP;
+      kg = (const T*)a.k + (size_t)lp.head * D + c16 * 8; vg = (const T*)a.v + (size_t)lp.head * D + c16 * 8;
 #pragma unroll
-    for (int j = 0; j < NK; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      const int c16 = ks * 2 + ((lane >> 3) & 1);
-#pragma unroll
-      for (int jp = 0; jp < NK / 2; ++jp) {
-        const int key = kw + jp * 16 + (lane & 7) + ((lane >> 4) & 1) * 8;
-        unsigned b[4];
-        pf_ldsm4(k_s + (unsigned)(c16 >> 3) * 8192u + pf_swz(key, c16 & 7), b);
-        Half2<T>::mma(s[2 * jp], qf[ks], b[0], b[1]);
-        Half2<T>::mma(s[2 * jp + 1], qf[ks], b[2], b[3]);
+      for (int i = 0; i < NROW; ++i) {
+        // stacked row x is q row row0 + x / ratio, query head head * ratio + x % ratio
+        const int r = r_first + i * RSTEP, x = lp.rt * 16 + min(r, lp.nr - 1), xq = x / a.ratio;
+        const T* src = (const T*)a.q + (size_t)(lp.row0 + xq) * a.q_stride + (size_t)(lp.head * a.ratio + x - xq * a.ratio) * D + c16 * 8;
+        pf_cp16(q_s + col_off + pf_swz(r, c16 & 7), src, r < lp.nr);
       }
     }
+    const int k0 = lp.key0 + l_step * PN_STEP;
+    if ((l_step & 31) == 0) {                                           // page numbers of the next 32 steps, one a lane
+      const int* tab = a.table + (size_t)lp.slot * a.max_pages;
+      const int k = k0 + lane * PN_STEP;
+      pg_lo = k < lp.key1 ? tab[k >> a.shift] : -1;
+      pg_hi = a.shift > 3 ? pg_lo : k + 8 < lp.key1 ? tab[(k + 8) >> a.shift] : -1;      // a step is two pages of 8 rows
+    }
+    const int lo = __shfl_sync(0xffffffffu, pg_lo, l_step & 31), hi = __shfl_sync(0xffffffffu, pg_hi, l_step & 31);
+    const unsigned ks = ring + (unsigned)(l_cnt % PN_STAGES) * 2u * N::TILE;
+#pragma unroll
+    for (int i = 0; i < NROW; ++i) {
+      const int r = r_first + i * RSTEP, key = k0 + r, pg = r < 8 ? lo : hi;
+      const bool ok = key < lp.key1 && (unsigned)pg < (unsigned)a.n_pages;               // zeros behind the segment
+      const size_t at = (((size_t)(ok ? pg : 0) << a.shift) + (key & (a.page - 1))) * row_el;
+      const unsigned off = ks + col_off + pf_swz(r, c16 & 7);
+      pf_cp16(off, kg + at, ok);
+      pf_cp16(off + N::TILE, vg + at, ok);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    ++l_step; ++l_cnt;
+    return true;
+  };
+
+  float o[D / 8][4], m[2], l[2];                                        // the lane's two rows: lane / 4 and lane / 4 + 8
+  unsigned qf[D / 16][4];
+  int c_left = 0, key_lo = 0, key1 = 0, lim[2] = {0, 0}, lim_min = 0;
+  while (true) {
+    while (l_cnt - c_cnt < PN_STAGES && issue()) {}
+    if (l_cnt == c_cnt) break;
+    const int younger = l_cnt - 1 - c_cnt;                              // steps in flight behind the one that is needed
+    if (younger == 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    else if (younger == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 2;" ::: "memory");
+    __syncwarp();
+    if (c_left == 0) {                                                  // a piece begins
+      const Piece& p = s_piece[warp][c_begun & 1];
+      key_lo = p.key0; key1 = p.key1;
+      c_left = (key1 - key_lo + PN_STEP - 1) / PN_STEP;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int x = (lane >> 2) + 8 * r;
+        lim[r] = p.lim0 == INT_MIN || x >= p.nr ? key1 : min(key1, p.lim0 + (p.rt * 16 + x) / a.ratio);
+        m[r] = -INFINITY; l[r] = 0.f;
+      }
+      lim_min = p.lim0 == INT_MIN ? key1 : min(key1, p.lim0 + p.rt * 16 / a.ratio);
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) { o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f; }
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const int row = (lane & 7) + ((lane >> 3) & 1) * 8, c = ks * 2 + (lane >> 4);
+        pf_ldsm4(q_s + (unsigned)(c >> 3) * N::HALF + pf_swz(row, c & 7), qf[ks]);
+      }
+      ++c_begun;
+      __syncwarp();
+    }
+    unsigned char* const k_p = base_p + N::TILE + (c_cnt % PN_STAGES) * 2 * N::TILE;
+    const unsigned k_s = pf_smem(k_p), v_s = k_s + N::TILE;
+    float s[2][4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      const int c = ks * 2 + ((lane >> 3) & 1), key = (lane & 7) + ((lane >> 4) & 1) * 8;
+      unsigned b[4];
+      pf_ldsm4(k_s + (unsigned)(c >> 3) * N::HALF + pf_swz(key, c & 7), b);
+      Half2<T>::mma(s[0], qf[ks], b[0], b[1]);
+      Half2<T>::mma(s[1], qf[ks], b[2], b[3]);
+    }
+    const bool masked = key_lo + PN_STEP > lim_min;                     // some row does not see the whole step
     float bm[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int j = 0; j < NK; ++j)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int key = key_lo + kw + j * 8 + 2 * (lane & 3) + (e & 1);
-        float x = s[j][e] * scale2;
-        if (masked && key >= lim[e >> 1]) x = -INFINITY;
+        float x = s[j][e] * a.scale2;
+        if (masked && key_lo + j * 8 + 2 * (lane & 3) + (e & 1) >= lim[e >> 1]) x = -INFINITY;
         s[j][e] = x;
         bm[e >> 1] = fmaxf(bm[e >> 1], x);
       }
@@ -323,246 +465,468 @@ struct Block {
       m[r] = mn;
       l[r] *= al[r];
     }
+    if (__any_sync(0xffffffffu, al[0] != 1.f || al[1] != 1.f)) {
 #pragma unroll
-    for (int j = 0; j < D / 8; ++j) { o[j][0] *= al[0]; o[j][1] *= al[0]; o[j][2] *= al[1]; o[j][3] *= al[1]; }
-    unsigned pf[NK / 2][4];
-    // P is rounded to the 16-bit type for the product with V (half a step: 2^-9 bf16, 2^-12 fp16 of each weight); the sum l takes the
-    // unrounded weights
+      for (int j = 0; j < D / 8; ++j) { o[j][0] *= al[0]; o[j][1] *= al[0]; o[j][2] *= al[1]; o[j][3] *= al[1]; }
+    }
+    // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16); the sum l takes
+    // the unrounded weights
+    unsigned pf[4];
 #pragma unroll
-    for (int j = 0; j < NK; ++j) {
+    for (int j = 0; j < 2; ++j) {
       const float p0 = pf_ex2(s[j][0] - ref[0]), p1 = pf_ex2(s[j][1] - ref[0]), p2 = pf_ex2(s[j][2] - ref[1]), p3 = pf_ex2(s[j][3] - ref[1]);
       l[0] += p0 + p1; l[1] += p2 + p3;
-      pf[j >> 1][(j & 1) * 2] = Half2<T>::pack(p0, p1);
-      pf[j >> 1][(j & 1) * 2 + 1] = Half2<T>::pack(p2, p3);
+      pf[j * 2] = Half2<T>::pack(p0, p1);
+      pf[j * 2 + 1] = Half2<T>::pack(p2, p3);
     }
-    if (dirty) {
-      // a masked block with infinities or NaN in V: they reach the rows that see them, and no other (0 * inf would)
-      for (int key = kw; key < kw + NK * 8; ++key)
+    if (masked && lim_min < key1) {
+      // a row does not see some key of this step: infinities and NaN of such a V row must not reach it as 0 * inf
+      bool bad = false;
+      for (int i = lane; i < N::TILE / 16; i += 32) bad |= any_nonfinite<T>(*reinterpret_cast<const uint4*>(k_p + N::TILE + i * 16));
+      if (__any_sync(0xffffffffu, bad)) {
+        for (int key = 0; key < PN_STEP; ++key)
 #pragma unroll
-        for (int j = 0; j < D / 8; ++j)
+          for (int j = 0; j < D / 8; ++j)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int col = j * 8 + 2 * (lane & 3) + e;
-            const unsigned short x = *reinterpret_cast<const unsigned short*>(v_p + (col >> 6) * 8192 + pf_swz(key, (col & 63) >> 3) + (col & 7) * 2);
-            if ((x & Half2<T>::exp_mask) == Half2<T>::exp_mask) {
-              if (key_lo + key < lim[0]) o[j][e] += Half2<T>::value(x);
-              if (key_lo + key < lim[1]) o[j][2 + e] += Half2<T>::value(x);
+            for (int e = 0; e < 2; ++e) {
+              const int col = j * 8 + 2 * (lane & 3) + e;
+              const unsigned short x =
+                  *reinterpret_cast<const unsigned short*>(k_p + N::TILE + (col >> 6) * N::HALF + pf_swz(key, (col & 63) >> 3) + (col & 7) * 2);
+              if ((x & Half2<T>::exp_mask) == Half2<T>::exp_mask) {
+                if (key_lo + key < lim[0]) o[j][e] += Half2<T>::value(x);
+                if (key_lo + key < lim[1]) o[j][2 + e] += Half2<T>::value(x);
+              }
             }
-          }
-    }
-    if (!dirty) pv(v_s, pf, kw, lane);
-    else {
-      clean(v_p);
-      pv(v_s, pf, kw, lane);
-    }
-  }
-  __device__ __forceinline__ void pv(unsigned v_s, const unsigned (*pf)[4], int kw, int lane) {
-#pragma unroll
-    for (int ks = 0; ks < NK / 2; ++ks) {
-      const int key = kw + ks * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
-#pragma unroll
-      for (int np = 0; np < D / 16; ++np) {
-        const int c16 = np * 2 + (lane >> 4);
-        unsigned b[4];
-        pf_ldsm4t(v_s + (unsigned)(c16 >> 3) * 8192u + pf_swz(key, c16 & 7), b);
-        Half2<T>::mma(o[2 * np], pf[ks], b[0], b[1]);
-        Half2<T>::mma(o[2 * np + 1], pf[ks], b[2], b[3]);
+        __syncwarp();
+        unsigned short* x = reinterpret_cast<unsigned short*>(k_p + N::TILE);
+        for (int i = lane; i < PN_STEP * D; i += 32)
+          if ((x[i] & Half2<T>::exp_mask) == Half2<T>::exp_mask) x[i] = 0;
+        __syncwarp();
       }
     }
+#pragma unroll
+    for (int np = 0; np < D / 16; ++np) {
+      const int c = np * 2 + (lane >> 4), key = (lane & 7) + ((lane >> 3) & 1) * 8;
+      unsigned b[4];
+      pf_ldsm4t(v_s + (unsigned)(c >> 3) * N::HALF + pf_swz(key, c & 7), b);
+      Half2<T>::mma(o[2 * np], pf, b[0], b[1]);
+      Half2<T>::mma(o[2 * np + 1], pf, b[2], b[3]);
+    }
+    key_lo += PN_STEP;
+    ++c_cnt;
+    if (--c_left == 0) {                                                // the piece ends
+      const Piece& p = s_piece[warp][(c_begun - 1) & 1];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+        const int x = (lane >> 2) + 8 * r;
+        if (x >= p.nr) continue;
+        if (p.direct) {
+          const int xs = p.rt * 16 + x, xq = xs / a.ratio, row = p.row0 + xq, h = p.head * a.ratio + xs - xq * a.ratio;
+          T* dst = (T*)a.out + (size_t)row * a.out_stride + (size_t)h * D;
+          const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+#pragma unroll
+          for (int j = 0; j < D / 8; ++j)
+            *reinterpret_cast<unsigned*>(dst + j * 8 + 2 * (lane & 3)) = Half2<T>::pack(o[j][2 * r] * inv, o[j][2 * r + 1] * inv);
+          if (a.lse && (lane & 3) == 0) a.lse[(size_t)row * a.n_heads + h] = (m[r] + log2f(l[r])) * PF_LN2;
+        } else {
+          float* dst = pm.po + (p.slot0 + x) * D;
+#pragma unroll
+          for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(dst + j * 8 + 2 * (lane & 3)) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
+          if ((lane & 3) == 0) pm.ml[p.slot0 + x] = make_float2(m[r], l[r]);
+        }
+      }
+    }
+    __syncwarp();                                                       // the step's tiles (and the piece record) may be refilled
   }
-  // all threads: zeros in the place of infinities and NaN of the V tile
-  static __device__ __noinline__ void clean(const unsigned char* v_p) {
-    __syncthreads();
-    unsigned short* x = reinterpret_cast<unsigned short*>(const_cast<unsigned char*>(v_p));
-    for (int i = threadIdx.x; i < 64 * D; i += PF_THREADS)
-      if ((x[i] & Half2<T>::exp_mask) == Half2<T>::exp_mask) x[i] = 0;
-    __syncthreads();
-  }
+}
+
+// ------------------------------------------------------------------------------------------------ wide: tcgen05
+// One persistent CTA per SM walks its run of (K/V head, tile of 128 stacked rows, block of 128 keys) units:
+//   warp 0        TMA: K and V blocks, one box per (page, 64 elements) into one ring of tiles in the order the products take them
+//   warp 1        one thread issues S_i = Q K_i^T (M 128, N 128) and O_b += P_i V_i (b = i mod 2), A = P from tensor memory
+//   warps 4-7 and 8-11   softmax of the even and of the odd key blocks, a thread per row: each side keeps its own m, l and O, as if
+//                 the keys were split in two, so that neither waits for the other; the sides are added when the piece ends.
+// S_i is followed by S_{i+1} before O += P_i V_i, so the tensor cores work on one block while the other is in the softmax.
+// Every row sees every key of a common prefix: no mask but behind its last key, where zeros are loaded.
+// Bound: the 16384 exponentials of a block (16 a cycle and SM: 1024 cycles, as long as its products at the dense peak) where the rows fill
+// the tile, HBM (64 KB of K and V a block) where they do not.
+constexpr int PW_THREADS = 384;
+constexpr int PW_SOFT = 256;                    // threads of the two softmax sides
+constexpr unsigned long long PW_WAIT_LIMIT_NS = 400000000ull;
+template <int D> struct Wide {
+  static constexpr int HALVES = D / 64;
+  static constexpr int HALF = 128 * 128;        // 64 elements of 128 rows
+  static constexpr int TILE = HALVES * HALF;
+  static constexpr int SLOTS = D == 128 ? 6 : 10;
+  static constexpr int SMEM = 1024 + TILE * (1 + SLOTS);
 };
 
-template <typename T>
-__device__ __forceinline__ bool any_nonfinite(uint4 x) {
-  const unsigned w[4] = {x.x, x.y, x.z, x.w};
-  bool r = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r |= (w[i] & Half2<T>::exp_mask) == Half2<T>::exp_mask;
-    r |= ((w[i] >> 16) & Half2<T>::exp_mask) == Half2<T>::exp_mask;
+__device__ __forceinline__ void pw_bar_init(unsigned long long* bar, unsigned count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(pf_smem(bar)), "r"(count));
+}
+__device__ __forceinline__ void pw_expect(unsigned long long* bar, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(pf_smem(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void pw_arrive(unsigned long long* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(pf_smem(bar)) : "memory");
+}
+__device__ __forceinline__ bool pw_try(unsigned long long* bar, unsigned parity) {
+  unsigned ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(ok) : "r"(pf_smem(bar)), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ unsigned long long pw_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// Wait for a phase, at most PW_WAIT_LIMIT_NS; a wait that gives up (or finds that another has) returns false and marks the plan.
+__device__ __noinline__ bool pw_wait_slow(unsigned long long* bar, unsigned parity, volatile int* abort_flag, int* error) {
+  const unsigned long long t0 = pw_ns();
+  while (true) {
+    for (int i = 0; i < 256; ++i)
+      if (pw_try(bar, parity)) return true;
+    if (*abort_flag) return false;
+    if (pw_ns() - t0 > PW_WAIT_LIMIT_NS) break;
   }
-  return r;
+  *abort_flag = 1;
+  atomicExch(error, VLAC_ERR_TIMEOUT);
+  return false;
+}
+__device__ __forceinline__ bool pw_wait(unsigned long long* bar, unsigned parity, volatile int* abort_flag, int* error) {
+  return pw_try(bar, parity) || pw_wait_slow(bar, parity, abort_flag, error);
+}
+__device__ __forceinline__ void pw_tma(unsigned dst, const CUtensorMap* tm, int x, int y, unsigned long long* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(tm), "r"(x), "r"(y), "r"(pf_smem(bar)) : "memory");
+}
+__device__ __forceinline__ unsigned long long pw_desc(unsigned addr, unsigned lbo, unsigned sbo) {
+  unsigned long long d = 0;
+  d |= (unsigned long long)((addr & 0x3FFFFu) >> 4);
+  d |= (unsigned long long)((lbo >> 4) & 0x3FFFu) << 16;
+  d |= (unsigned long long)((sbo >> 4) & 0x3FFFu) << 32;
+  d |= (unsigned long long)1 << 46;             // descriptor version of this architecture
+  d |= (unsigned long long)2 << 61;             // 128-byte swizzle
+  return d;
+}
+// fp32 accumulate, A and B both bf16 or both fp16, M = 128; B K-major or (b_mn) MN-major
+template <typename T> __device__ __forceinline__ unsigned pw_idesc(int n, bool b_mn) {
+  const unsigned f = sizeof(T) == 2 && Half2<T>::exp_mask == 0x7f80u ? 1u : 0u;
+  return (1u << 4) | (f << 7) | (f << 10) | (b_mn ? 1u << 16 : 0u) | ((unsigned)(n >> 3) << 17) | (8u << 24);
+}
+__device__ __forceinline__ void pw_mma_ss(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, bool acc) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)acc) : "memory");
+}
+__device__ __forceinline__ void pw_mma_ts(unsigned d, unsigned a, unsigned long long b, unsigned idesc, bool acc) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((unsigned)acc) : "memory");
+}
+__device__ __forceinline__ void pw_commit(unsigned long long* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(pf_smem(bar)) : "memory");
+}
+#define PW_R32(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
+#define PW_I32(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
+// 32 columns of the thread's row (no wait)
+__device__ __forceinline__ void pw_ld32(unsigned addr, unsigned* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+               "%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : PW_R32(r, 0), PW_R32(r, 8), PW_R32(r, 16), PW_R32(r, 24) : "r"(addr));
+}
+__device__ __forceinline__ void pw_st32(unsigned addr, const unsigned* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+               "%25,%26,%27,%28,%29,%30,%31};"
+               ::PW_I32(r, 0), PW_I32(r, 8), PW_I32(r, 16), PW_I32(r, 24), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void pw_st16(unsigned addr, const unsigned* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+               ::PW_I32(r, 0), PW_I32(r, 8), "r"(addr) : "memory");
+}
+#define PW_T32(r, o) "+r"(r[o]), "+r"(r[o + 1]), "+r"(r[o + 2]), "+r"(r[o + 3]), "+r"(r[o + 4]), "+r"(r[o + 5]), "+r"(r[o + 6]), "+r"(r[o + 7])
+// the loads so far are done; the registers are named so that no use of them moves in front of the wait
+__device__ __forceinline__ void pw_ld_wait(unsigned* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : PW_T32(r, 0), PW_T32(r, 8), PW_T32(r, 16), PW_T32(r, 24) :: "memory");
+}
+__device__ __forceinline__ void pw_ld_wait(unsigned* r, unsigned* r2) {
+  pw_ld_wait(r);
+  asm volatile("" : PW_T32(r2, 0), PW_T32(r2, 8), PW_T32(r2, 16), PW_T32(r2, 24) :: "memory");
+}
+__device__ __forceinline__ void pw_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void pw_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void pw_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// barrier of the softmax threads that also makes `ok` the same in all of them
+__device__ __forceinline__ bool pw_all_ok(bool ok) {
+  unsigned r;
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbarrier.cta.red.and.pred p, 1, 256, q;\nselp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(r) : "r"((unsigned)ok) : "memory");
+  return r != 0;
 }
 
-template <typename T, int D, bool WIDE>
-__device__ __forceinline__ void piece(const AttnArgs& a, const PlanMem& p, const SegRec& sg, int head, int rt, int kb0, int nkb, int cta, bool direct,
-                                      unsigned char* sm) {
-  constexpr int BM = WIDE ? 64 : 16, C16 = D / 8, RSTEP = PF_THREADS / C16, TILE = pf_tile<D>();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const unsigned q_s = pf_smem(sm), ring = q_s + TILE;
-  const int nr = min(BM, sg.R - rt * BM);
-  const int c16 = tid % C16, r_first = tid / C16;
-  const size_t row_el = (size_t)a.kv_heads * D;
-  const T *kg = (const T*)a.k + head * D + c16 * 8, *vg = (const T*)a.v + head * D + c16 * 8;
-  const int* tab = a.table + (size_t)sg.slot * a.max_pages;
-  const unsigned col_off = (unsigned)(c16 >> 3) * 8192u;
-  auto load = [&](int i) {                                              // key block kb0 + i into stage i % PF_STAGES
-    const unsigned ks = ring + (unsigned)(i % PF_STAGES) * 2u * TILE, vs = ks + TILE;
-    const int k0 = sg.key0 + (kb0 + i) * PF_KB;
-    int pg[64 / RSTEP];
-#pragma unroll
-    for (int x = 0; x < 64 / RSTEP; ++x) {
-      const int key = k0 + r_first + x * RSTEP;
-      pg[x] = key < sg.key1 ? tab[key >> a.shift] : -1;
-    }
-#pragma unroll
-    for (int x = 0; x < 64 / RSTEP; ++x) {
-      const int r = r_first + x * RSTEP, key = k0 + r;
-      const bool ok = (unsigned)pg[x] < (unsigned)a.n_pages;            // beyond the segment: zeros
-      const size_t at = (((size_t)(ok ? pg[x] : 0) << a.shift) + (key & (a.page - 1))) * row_el;
-      const unsigned off = col_off + pf_swz(r, c16 & 7);
-      pf_cp16(ks + off, kg + at, ok);
-      pf_cp16(vs + off, vg + at, ok);
-    }
-  };
-  // Q tile: stacked row x is q row row0 + x / ratio, query head head * ratio + x % ratio
-  for (int r = r_first; r < BM; r += RSTEP) {
-    const int x = rt * BM + min(r, nr - 1);
-    const T* src = (const T*)a.q + (size_t)(sg.row0 + x / a.ratio) * a.q_stride + (size_t)(head * a.ratio + x % a.ratio) * D + c16 * 8;
-    pf_cp16(q_s + col_off + pf_swz(r, c16 & 7), src, r < nr);
-  }
-#pragma unroll
-  for (int i = 0; i < PF_STAGES - 1; ++i) {
-    if (i < nkb) load(i);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  }
-  // the thread's two rows
-  const int rl[2] = {(WIDE ? warp * 16 : 0) + (lane >> 2), (WIDE ? warp * 16 : 0) + (lane >> 2) + 8};
-  int lim[2] = {sg.key1, sg.key1};
-#pragma unroll
-  for (int r = 0; r < 2; ++r)
-    if (rl[r] < nr && sg.pos0 != INT_MIN) lim[r] = min(sg.key1, sg.pos0 + (rt * BM + rl[r]) / a.ratio + 1);
-  const int lim_min = sg.pos0 == INT_MIN ? sg.key1 : min(sg.key1, sg.pos0 + (rt * BM) / a.ratio + 1);
-  Block<T, D, WIDE> blk;
-  for (int i = 0; i < nkb; ++i) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(PF_STAGES - 2) : "memory");
-    __syncthreads();
-    if (i == 0) blk.begin(q_s, warp, lane);
-    if (i + PF_STAGES - 1 < nkb) load(i + PF_STAGES - 1);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    const unsigned st = (unsigned)(i % PF_STAGES) * 2u * TILE;
-    const int key_lo = sg.key0 + (kb0 + i) * PF_KB;
-    const bool masked = key_lo + PF_KB > lim_min;                       // some row does not see the whole block
-    bool dirty = false;
-    if (masked && lim_min < sg.key1) {
-      bool bad = false;
-      const uint4* vt = reinterpret_cast<const uint4*>(sm + TILE + st + TILE);
-      for (int x = tid; x < TILE / 16; x += PF_THREADS) bad |= any_nonfinite<T>(vt[x]);
-      dirty = __syncthreads_or(bad);
-    }
-    blk.step(ring + st, ring + st + TILE, sm + TILE + st + TILE, warp, lane, a.scale2, masked, key_lo, lim, dirty);
-  }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    blk.l[r] += __shfl_xor_sync(0xffffffffu, blk.l[r], 1);
-    blk.l[r] += __shfl_xor_sync(0xffffffffu, blk.l[r], 2);
-  }
-  const size_t slot0 = (size_t)sg.rowbase + (size_t)head * sg.R + (size_t)rt * BM + (size_t)cta * PF_BM;
-  auto where = [&](int r, T** dst, float** lse) {                       // final place of stacked row r
-    const int x = rt * BM + r, row = sg.row0 + x / a.ratio, h = head * a.ratio + x % a.ratio;
-    *dst = (T*)a.out + (size_t)row * a.out_stride + (size_t)h * D;
-    *lse = a.lse ? a.lse + (size_t)row * a.n_heads + h : nullptr;
-  };
-  if (WIDE) {
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      if (rl[r] >= nr) continue;
-      if (direct) {
-        T* dst; float* ls;
-        where(rl[r], &dst, &ls);
-        const float inv = blk.l[r] == 0.f ? 0.f : 1.f / blk.l[r];
-#pragma unroll
-        for (int j = 0; j < D / 8; ++j)
-          *reinterpret_cast<unsigned*>(dst + j * 8 + 2 * (lane & 3)) = Half2<T>::pack(blk.o[j][2 * r] * inv, blk.o[j][2 * r + 1] * inv);
-        if (ls && (lane & 3) == 0) *ls = (blk.m[r] + log2f(blk.l[r])) * 0.693147180559945f;
-      } else {
-        float* dst = p.po + (slot0 + rl[r]) * D;
-#pragma unroll
-        for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(dst + j * 8 + 2 * (lane & 3)) = make_float2(blk.o[j][2 * r], blk.o[j][2 * r + 1]);
-        if ((lane & 3) == 0) p.ml[slot0 + rl[r]] = make_float2(blk.m[r], blk.l[r]);
-      }
-    }
-    __syncthreads();                                                    // the next piece refills the tiles
-  } else {
-    // the four warps hold the same rows over different keys: add them up in warp order through the ring
-    float* ox = reinterpret_cast<float*>(sm + TILE);                    // [4][16][D + 4]
-    float2* mx = reinterpret_cast<float2*>(ox + 4 * 16 * (D + 4));      // [4][16]
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-#pragma unroll
-      for (int j = 0; j < D / 8; ++j)
-        *reinterpret_cast<float2*>(ox + (warp * 16 + rl[r]) * (D + 4) + j * 8 + 2 * (lane & 3)) = make_float2(blk.o[j][2 * r], blk.o[j][2 * r + 1]);
-      if ((lane & 3) == 0) mx[warp * 16 + rl[r]] = make_float2(blk.m[r], blk.l[r]);
-    }
-    __syncthreads();
-    for (int x = tid; x < nr * (D / 4); x += PF_THREADS) {
-      const int r = x / (D / 4), c = (x % (D / 4)) * 4;
-      float M = -INFINITY, l = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) M = fmaxf(M, mx[w * 16 + r].x);
-      const float ref = M == -INFINITY ? 0.f : M;
-      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float2 ml = mx[w * 16 + r];
-        const float f = pf_ex2(ml.x - ref);
-        const float4 o4 = *reinterpret_cast<const float4*>(ox + (w * 16 + r) * (D + 4) + c);
-        l += f * ml.y;
-        s.x += f * o4.x; s.y += f * o4.y; s.z += f * o4.z; s.w += f * o4.w;
-      }
-      if (direct) {
-        T* dst; float* ls;
-        where(r, &dst, &ls);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        *reinterpret_cast<uint2*>(dst + c) = make_uint2(Half2<T>::pack(s.x * inv, s.y * inv), Half2<T>::pack(s.z * inv, s.w * inv));
-        if (ls && c == 0) *ls = (M + log2f(l)) * 0.693147180559945f;
-      } else {
-        *reinterpret_cast<float4*>(p.po + (slot0 + r) * D + c) = s;
-        if (c == 0) p.ml[slot0 + r] = make_float2(M, l);
-      }
-    }
-    __syncthreads();
-  }
-}
-
-// Whether a tile of a segment is one piece and holds everything its rows see: then the piece writes the result itself.
-__device__ __forceinline__ bool tile_direct(const SegRec& s, long long u_tile, long long U) {
-  return s.pos0 != INT_MIN && s.key0 == 0 && run_of(u_tile, U) == run_of(u_tile + s.KB - 1, U);
-}
+struct WideArgs {
+  AttnArgs a;
+  int flip;                                     // 1: the scale is negative (scale2 holds its magnitude; Q's signs are flipped)
+  int box;                                      // rows of a TMA box: min(page, 128)
+};
 
 template <typename T, int D>
-__global__ void __launch_bounds__(PF_THREADS, 2) prefix_mma_kernel(AttnArgs a) {
-  extern __shared__ __align__(1024) unsigned char pf_raw[];
-  const PlanMem p = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
-  pdl_trigger();
+__global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, WideArgs w) {
+  using W = Wide<D>;
+  extern __shared__ unsigned char pw_raw[];
+  __shared__ __align__(8) unsigned long long full[W::SLOTS], empty[W::SLOTS], s_full[2], p_full[2], q_full, o_full, drain;
+  __shared__ unsigned tmem_slot;
+  __shared__ int abort_flag;
+  const AttnArgs& a = w.a;
+  const PlanMem pm = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
+  int* const error = &pm.head->error;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, run = blockIdx.x;
+  unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pw_raw) + 1023) & ~(uintptr_t)1023);
+  const unsigned q_s = pf_smem(smem), ring = q_s + W::TILE;
+  float* const red_m = reinterpret_cast<float*>(smem);                  // [2][128] each, over Q when its products are done
+  float* const red_l = red_m + 256;
+  if (tid == 0) {
+    for (int i = 0; i < W::SLOTS; ++i) { pw_bar_init(&full[i], 1); pw_bar_init(&empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { pw_bar_init(&s_full[i], 1); pw_bar_init(&p_full[i], 128); }
+    pw_bar_init(&q_full, PW_SOFT); pw_bar_init(&o_full, 1); pw_bar_init(&drain, 1);
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
   pdl_wait();
-  const long long U = p.head->units;
-  const int cta = blockIdx.x;
-  const long long G = runs(U);
-  if (cta >= G) return;
-  long long u = cta * U / G;
-  const long long u_end = (cta + 1) * U / G;
-  int g = p.first[cta];
-  SegRec s = p.seg[g];
-  while (u < u_end) {
-    while (u >= s.uend) s = p.seg[++g];
-    const long long local = u - s.ustart;
-    const int per_head = s.T * s.KB, head = (int)(local / per_head), rem = (int)(local % per_head), rt = rem / s.KB, kb = rem % s.KB;
-    const int n = (int)min((long long)(s.KB - kb), u_end - u);
-    const bool direct = tile_direct(s, u - kb, U);
-    if (s.bm == 16) piece<T, D, false>(a, p, s, head, rt, kb, n, cta, direct, pf_raw);
-    else piece<T, D, true>(a, p, s, head, rt, kb, n, cta, direct, pf_raw);
-    u += n;
+  pdl_trigger();
+  const long long U = pm.head->units[WIDE], G = runs(WIDE, U);
+  if (run >= G) return;                                                 // uniform over the CTA
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(pf_smem(&tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pw_before();
+  __syncthreads();
+  pw_after();
+  const unsigned tmem = tmem_slot;                                      // columns: S/P even 0, S/P odd 128, O even 256, O odd 384
+  long long u = run * U / G;
+  const long long u_end = (run + 1) * U / G;
+  int g = pm.first[WIDE][run];
+  Piece p;
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- loads
+    const int per = 128 / w.box, chunk = lane / W::HALVES, half = lane % W::HALVES;
+    const bool mine = chunk < per;
+    const int none = a.n_pages << a.shift;                              // a row behind the pool: zeros
+    int cnt = 0;
+    bool ok = true;
+    auto put = [&](const CUtensorMap* tm, int y, int x0) {
+      const int s = cnt % W::SLOTS;
+      if (cnt >= W::SLOTS) ok = __all_sync(0xffffffffu, pw_wait(&empty[s], ((cnt / W::SLOTS) & 1) ^ 1, &abort_flag, error));
+      if (!ok) return;
+      if (lane == 0) pw_expect(&full[s], W::TILE);
+      __syncwarp();
+      if (mine) pw_tma(ring + (unsigned)s * W::TILE + (unsigned)half * W::HALF + (unsigned)chunk * w.box * 128u, tm, x0 + half * 64, y, &full[s]);
+      ++cnt;
+    };
+    while (u < u_end && ok) {
+      u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
+      const int* tab = a.table + (size_t)p.slot * a.max_pages;
+      auto row = [&](int i) -> int {                                    // pool row of this lane's box of key block i
+        const int key = p.key0 + i * 128 + chunk * w.box;
+        if (!mine || key >= p.key1) return none;
+        const int pg = tab[key >> a.shift];
+        return (unsigned)pg < (unsigned)a.n_pages ? (pg << a.shift) + (key & (a.page - 1)) : none;
+      };
+      int y = row(0), yp = 0;
+      for (int i = 0; i < p.n && ok; ++i) {
+        const int yn = i + 1 < p.n ? row(i + 1) : none;                 // fetched a block ahead of its use
+        put(&tm_k, y, p.head * D);
+        if (i > 0 && ok) put(&tm_v, yp, p.head * D);
+        yp = y; y = yn;
+      }
+      if (ok) put(&tm_v, yp, p.head * D);
+    }
+    if (!ok)                                                            // given up: let what is in flight land
+      for (int c = max(0, cnt - W::SLOTS); c < cnt; ++c) pw_wait(&full[c % W::SLOTS], (c / W::SLOTS) & 1, &abort_flag, error);
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- products
+    if (lane == 0) {
+      const unsigned id_s = pw_idesc<T>(128, false), id_o = pw_idesc<T>(D, true);
+      int cnt = 0, pieces = 0, n_p[2] = {0, 0};
+      bool ok = true;
+      auto tile = [&]() -> unsigned {                                   // the next tile of the ring, when it is there
+        const int s = cnt % W::SLOTS;
+        ok = ok && pw_wait(&full[s], (cnt / W::SLOTS) & 1, &abort_flag, error);
+        return ring + (unsigned)s * W::TILE;
+      };
+      auto pv = [&](int i) {
+        const int b = i & 1;
+        ok = ok && pw_wait(&p_full[b], n_p[b]++ & 1, &abort_flag, error);
+        const unsigned v_s = tile();
+        if (!ok) return;
+        pw_after();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)                                     // 16 keys: 8 columns of packed P; 16 rows of V (MN-major)
+          pw_mma_ts(tmem + 256u + 128u * b, tmem + 128u * b + 8u * j, pw_desc(v_s + (unsigned)j * 2048u, W::HALF, 1024), id_o, i > 1 || j > 0);
+        pw_commit(&empty[cnt % W::SLOTS]);
+        ++cnt;
+      };
+      while (u < u_end && ok) {
+        u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
+        ok = pw_wait(&q_full, pieces & 1, &abort_flag, error);
+        for (int i = 0; i < p.n && ok; ++i) {
+          const unsigned k_s = tile();
+          if (!ok) break;
+          pw_after();
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const unsigned off = (unsigned)(ks >> 2) * W::HALF + (unsigned)(ks & 3) * 32u;
+            pw_mma_ss(tmem + 128u * (i & 1), pw_desc(q_s + off, 16, 1024), pw_desc(k_s + off, 16, 1024), id_s, ks > 0);
+          }
+          pw_commit(&s_full[i & 1]);
+          pw_commit(&empty[cnt % W::SLOTS]);
+          ++cnt;
+          if (i > 0) pv(i - 1);
+        }
+        if (ok) pv(p.n - 1);
+        if (ok) pw_commit(&o_full);
+        ++pieces;
+      }
+      if (!ok) { pw_commit(&drain); pw_wait(&drain, 0, &abort_flag, error); }
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    // ---------------------------------------------------------------- softmax
+    const int st = tid - 128, side = st >> 7, q4 = warp & 3, r = 32 * q4 + lane;
+    const unsigned trow = tmem + ((unsigned)(32 * q4) << 16), s_col = trow + 128u * side, o_col = trow + 256u + 128u * side;
+    int n_s = 0, pieces = 0;
+    bool ok = true;
+    while (u < u_end && ok) {
+      u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
+      // Q: stacked row x is q row row0 + x / ratio, query head head * ratio + x % ratio; rows behind the last are zeros
+      constexpr int C16 = D / 8;
+#pragma unroll
+      for (int i = 0; i < 128 * C16 / PW_SOFT; ++i) {
+        const int c = st + i * PW_SOFT, qr = c / C16, c16 = c % C16, x = p.rt * 128 + min(qr, p.nr - 1), xq = x / a.ratio;
+        uint4 v = *reinterpret_cast<const uint4*>((const T*)a.q + (size_t)(p.row0 + xq) * a.q_stride + (size_t)(p.head * a.ratio + x - xq * a.ratio) * D + c16 * 8);
+        if (w.flip) { v.x ^= 0x80008000u; v.y ^= 0x80008000u; v.z ^= 0x80008000u; v.w ^= 0x80008000u; }
+        if (qr >= p.nr) v = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(smem + (c16 >> 3) * W::HALF + pf_swz(qr, c16 & 7)) = v;
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      pw_before();
+      pw_arrive(&q_full);
+      float m = -INFINITY, l = 0.f;
+      const bool idle = 32 * q4 >= p.nr;                                // a warp without rows: only its arrivals are needed
+      for (int i = side; i < p.n; i += 2) {
+        ok = __all_sync(0xffffffffu, pw_wait(&s_full[side], n_s++ & 1, &abort_flag, error));
+        if (!ok) break;
+        if (!idle) {
+          pw_after();
+          const int valid = p.key1 - p.key0 - i * 128;                  // keys of this block (fewer than 128 in the last)
+          // two sweeps over the scores (the row's 128 do not fit the registers beside the rest): maximum, then weights
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            unsigned v[64];
+            pw_ld32(s_col + 64u * hf, v);
+            pw_ld32(s_col + 64u * hf + 32u, v + 32);
+            pw_ld_wait(v, v + 32);
+            if (valid < 128) {
+#pragma unroll
+              for (int c = 0; c < 64; ++c) if (hf * 64 + c >= valid) v[c] = 0xff800000u;
+            }
+#pragma unroll
+            for (int c = 0; c < 64; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(v[c]));
+          }
+          const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2;
+          // the reference moves only when the maximum has grown by a factor of 2^8: weights up to 256 cost no precision (they are rounded
+          // relative to themselves, l is fp32), and O is seldom rescaled
+          const bool grow = bm > m + 8.f || m == -INFINITY;
+          if (__any_sync(0xffffffffu, grow)) {
+            const float mn = grow ? fmaxf(m, bm) : m;
+            const float al = mn == -INFINITY ? 1.f : pf_ex2(m - mn);    // (m = -inf: nothing summed yet, 0 * 0)
+            m = mn;
+            l *= al;
+            if (i >= 2) {
+#pragma unroll
+              for (int c = 0; c < D / 32; ++c) {
+                unsigned x[32];
+                pw_ld32(o_col + 32u * c, x);
+                pw_ld_wait(x);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * al);
+                pw_st32(o_col + 32u * c, x);
+              }
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+          // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16); the sum takes
+          // the unrounded weights.  P lies over the scores already read: 16 columns a sweep of 32.
+          float ls[4] = {0.f, 0.f, 0.f, 0.f};
+          unsigned v[2][32];
+          pw_ld32(s_col, v[0]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            pw_ld_wait(v[q & 1]);
+            if (q < 3) pw_ld32(s_col + 32u * (q + 1), v[(q + 1) & 1]);
+            unsigned pk[16];
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              float p0 = pf_ex2(fmaf(__uint_as_float(v[q & 1][2 * c]), a.scale2, -ref));
+              float p1 = pf_ex2(fmaf(__uint_as_float(v[q & 1][2 * c + 1]), a.scale2, -ref));
+              if (valid < 128) { if (q * 32 + 2 * c >= valid) p0 = 0.f; if (q * 32 + 2 * c + 1 >= valid) p1 = 0.f; }
+              ls[c & 3] += p0 + p1;
+              pk[c] = Half2<T>::pack(p0, p1);
+            }
+            pw_st16(s_col + 16u * q, pk);
+          }
+          l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+          pw_st_wait();
+        }
+        pw_before();
+        pw_arrive(&p_full[side]);
+      }
+      if (ok) ok = pw_wait(&o_full, pieces & 1, &abort_flag, error);
+      ++pieces;
+      ok = pw_all_ok(ok);                                               // every product of the piece is done: Q's memory is free
+      if (!ok) break;
+      red_m[side * 128 + r] = m; red_l[side * 128 + r] = l;
+      pw_all_ok(true);
+      pw_after();
+      if (!idle) {
+        // the two sides of a row, each thread half of its columns
+        const float m0 = red_m[r], m1 = red_m[128 + r], M = fmaxf(m0, m1), ref = M == -INFINITY ? 0.f : M;
+        const float f0 = pf_ex2(m0 - ref), f1 = pf_ex2(m1 - ref);
+        const bool two = p.n > 1;                                       // one block: the odd side holds nothing
+        float* dst = pm.po + (p.slot0 + r) * D + side * (D / 2);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          unsigned x[32], y[32] = {};
+          pw_ld32(trow + 256u + side * (D / 2) + 32u * c, x);
+          if (two) pw_ld32(trow + 384u + side * (D / 2) + 32u * c, y);
+          pw_ld_wait(x, y);
+          if (r < p.nr) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              float4 o;
+              o.x = f0 * __uint_as_float(x[e]); o.y = f0 * __uint_as_float(x[e + 1]); o.z = f0 * __uint_as_float(x[e + 2]); o.w = f0 * __uint_as_float(x[e + 3]);
+              if (two) {
+                o.x += f1 * __uint_as_float(y[e]); o.y += f1 * __uint_as_float(y[e + 1]); o.z += f1 * __uint_as_float(y[e + 2]); o.w += f1 * __uint_as_float(y[e + 3]);
+              }
+              *reinterpret_cast<float4*>(dst + 32 * c + e) = o;
+            }
+          }
+        }
+        if (side == 0 && r < p.nr) pm.ml[p.slot0 + r] = make_float2(M, f0 * red_l[r] + (two ? f1 * red_l[128 + r] : 0.f));
+      }
+      pw_all_ok(true);                                                  // red_m, red_l may be written again
+    }
+    pw_before();
+  }
+  __syncthreads();
+  if (warp == 1) {
+    pw_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   }
 }
 
@@ -579,24 +943,25 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
   const int row = (int)(w / a.n_heads), h = (int)(w % a.n_heads), kvh = h / a.ratio;
   const int k = p.row_k[row];
   if (k < 0) return;
-  const long long U = p.head->units;
   const SeqRec q = p.seq[k];
-  int np[2] = {0, 0};
+  int np[2] = {0, 0}, pad[2] = {0, 0};
   size_t base[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int g = i ? q.suf_seg : q.pre_seg;
     if (g < 0) continue;
     const SegRec s = p.seg[g];
-    const int x = (row - s.row0) * a.ratio + h % a.ratio, rt = x / s.bm;
+    const int bm = pf_bm(s.cls), x = (row - s.row0) * a.ratio + h % a.ratio, rt = x / bm;
+    const long long U = p.head->units[s.cls];
     const long long u0 = s.ustart + ((long long)kvh * s.T + rt) * s.KB;
     if (tile_direct(s, u0, U)) return;                                  // written by its only piece
-    const int c0 = run_of(u0, U);
-    np[i] = run_of(u0 + s.KB - 1, U) - c0 + 1;
-    base[i] = (size_t)s.rowbase + (size_t)kvh * s.R + x + (size_t)c0 * PF_BM;
+    const int c0 = run_of(s.cls, u0, U);
+    np[i] = run_of(s.cls, u0 + s.KB - 1, U) - c0 + 1;
+    pad[i] = bm;
+    base[i] = (size_t)s.rowbase + (size_t)kvh * s.R + x + (size_t)c0 * bm;
   }
   const int n = np[0] + np[1];
-  auto slot = [&](int i) { return i < np[0] ? base[0] + (size_t)i * PF_BM : base[1] + (size_t)(i - np[0]) * PF_BM; };
+  auto slot = [&](int i) { return i < np[0] ? base[0] + (size_t)i * pad[0] : base[1] + (size_t)(i - np[0]) * pad[1]; };
   float M = -INFINITY;
   for (int i = lane; i < n; i += 32) M = fmaxf(M, p.ml[slot(i)].x);
 #pragma unroll
@@ -622,13 +987,25 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
   T* dst = (T*)a.out + (size_t)row * a.out_stride + (size_t)h * D + lane * E;
 #pragma unroll
   for (int e = 0; e < E; e += 2) *reinterpret_cast<unsigned*>(dst + e) = Half2<T>::pack(o[e] * inv, o[e + 1] * inv);
-  if (a.lse && lane == 0) a.lse[(size_t)row * a.n_heads + h] = (M + log2f(l)) * 0.693147180559945f;
+  if (a.lse && lane == 0) a.lse[(size_t)row * a.n_heads + h] = (M + log2f(l)) * PF_LN2;
 }
 
 template <typename T, int D>
-int launch_attention(const AttnArgs& a, cudaStream_t s) {
-  VLAC_CUDA_CHECK(cudaFuncSetAttribute(prefix_mma_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem_bytes<D>()));
-  VLAC_CUDA_CHECK(launch_pdl(prefix_mma_kernel<T, D>, dim3(PF_GRID_A), dim3(PF_THREADS), pf_smem_bytes<D>(), s, a));
+int launch_attention(const vlac_pages* p, const AttnArgs& a, cudaStream_t s) {
+  // more than 16 stacked rows, or the call cannot have a wide segment
+  if ((long long)a.rows * a.ratio > pf_bm(NARROW)) {
+    WideArgs w = {a, a.scale2 < 0.f, a.page < 128 ? a.page : 128};
+    w.a.scale2 = fabsf(a.scale2);
+    CUtensorMap tk, tv;
+    const int rows = a.n_pages << a.shift, cols = a.kv_heads * D;
+    int rc = vlac_encode_map_2d(&tk, a.k, rows, cols, w.box);
+    if (rc == VLAC_OK) rc = vlac_encode_map_2d(&tv, a.v, rows, cols, w.box);
+    if (rc != VLAC_OK) return rc;
+    VLAC_CUDA_CHECK(cudaFuncSetAttribute(prefix_wide_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Wide<D>::SMEM));
+    VLAC_CUDA_CHECK(launch_pdl(prefix_wide_kernel<T, D>, dim3(PW_CTAS), dim3(PW_THREADS), Wide<D>::SMEM, s, tk, tv, w));
+  }
+  VLAC_CUDA_CHECK(cudaFuncSetAttribute(prefix_narrow_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Narrow<D>::SMEM));
+  VLAC_CUDA_CHECK(launch_pdl(prefix_narrow_kernel<T, D>, dim3(PN_CTAS), dim3(PN_WARPS * 32), Narrow<D>::SMEM, s, a));
   const long long warps = (long long)a.rows * a.n_heads;
   VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, s, a));
   return VLAC_OK;
@@ -671,6 +1048,16 @@ int vlac_prefix_plan(const vlac_pages* p, const vlac_prefix* plan, const int* se
   return VLAC_OK;
 }
 
+int vlac_prefix_error(const vlac_prefix* plan, void* stream) {
+  if (!plan || plan->n < 0 || plan->rows < 0) return VLAC_ERR_INVALID_ARG;
+  if (plan->n == 0 || plan->rows == 0) return VLAC_OK;
+  if (!plan->mem || plan->bytes < sizeof(PlanHead)) return VLAC_ERR_INVALID_ARG;
+  int v = 0;
+  VLAC_CUDA_CHECK(cudaMemcpyAsync(&v, (const char*)plan->mem + offsetof(PlanHead, error), sizeof(int), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
+  VLAC_CUDA_CHECK(cudaStreamSynchronize((cudaStream_t)stream));
+  return v ? VLAC_ERR_TIMEOUT : VLAC_OK;
+}
+
 int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
                           void* out, long long out_stride, float* lse, void* stream) {
   const int rc = plan_check(p, plan);
@@ -687,8 +1074,8 @@ int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* pla
   a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
   a.scale2 = scale * 1.44269504088896f; a.mem = plan->mem;
   cudaStream_t s = (cudaStream_t)stream;
-  if (p->dtype == VLAC_BF16) return p->head_dim == 128 ? launch_attention<__nv_bfloat16, 128>(a, s) : launch_attention<__nv_bfloat16, 64>(a, s);
-  return p->head_dim == 128 ? launch_attention<__half, 128>(a, s) : launch_attention<__half, 64>(a, s);
+  if (p->dtype == VLAC_BF16) return p->head_dim == 128 ? launch_attention<__nv_bfloat16, 128>(p, a, s) : launch_attention<__nv_bfloat16, 64>(p, a, s);
+  return p->head_dim == 128 ? launch_attention<__half, 128>(p, a, s) : launch_attention<__half, 64>(p, a, s);
 }
 
 }  // extern "C"

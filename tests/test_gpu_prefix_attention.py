@@ -79,6 +79,7 @@ class Case:
         self.vb.vlac_prefix_plan(self.pages, plan, dev(self.seqs), dev(np.concatenate([[0], np.cumsum(self.nq)])), st)
         self.vb.vlac_prefix_attention(self.pages, layer, plan, q, self.scale, out, l)
         assert st.tolist() == [0] * n
+        assert self.vb.vlac_prefix_error(plan) == 0
         return out, l
 
     def want(self, i, layer=0, q=None):
@@ -118,6 +119,7 @@ GROUPS = {
     "many_single": [(0, [(n, 1)]) for n in (1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 300)],
     "ragged_groups": [(160, [(n % 23 + 1, 1) for n in range(19)]), (0, [(700, 3)]), (320, [(n + 2, 2) for n in range(9)])],
     "long": [(4100, [(n + 1, 1) for n in range(5)])],
+    "tiles": [(257, [(3, 3)] * 50), (130, [(2, 1)] * 33), (640, [(200, 150)])],
     "crowd": [(200, [(n % 7 + 1, 1) for n in range(70)])],
 }
 
@@ -212,6 +214,34 @@ def test_extreme_scores(vb):
     for q_scale in (200.0, 0.0):
         c = Case(vb, [(70, [(5, 1), (3, 2), (66, 1)]), (0, [(90, 40)])], 4, 2, 64, seed=11, q_scale=q_scale)
         c.check(*c.run())
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
+def test_scales(vb, scale):
+    """Any finite scale, negative ones and zero included, on narrow and wide segments."""
+    c = Case(vb, [(300, [(5, 1), (3, 2), (66, 1)]), (400, [(9, 8)] * 12)], 4, 2, 128, seed=12, q_scale=0.5)
+    c.scale = scale
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("prefix", [128, 129 * 8, 8 * 1000 + 8])
+def test_wide_prefixes_in_small_and_large_pages(vb, prefix):
+    """Common pages that end inside a block of keys, in pages smaller and larger than it; scattered pages."""
+    for page in (8, 256):
+        c = Case(vb, [(prefix, [(n + 1, 1) for n in range(20)])], 2, 1, 64 if page == 8 else 128, page=page, seed=prefix)
+        c.check(*c.run(), only=(0, 7, 19))
+
+
+def test_infinities_in_a_common_page(vb):
+    """What every row sees reaches every row: an infinite V in the prefix gives infinite outputs in that column and no other."""
+    c = Case(vb, [(200, [(n + 1, 1) for n in range(24)])], 4, 4, 64, seed=13)
+    clean, clean_lse = c.run()
+    pg = int(c.pages.table[c.seqs[0], 2])
+    c.pages.v[0, pg, 3, 1, 7] = float("-inf")
+    out, lse = c.run()
+    assert torch.all(torch.isneginf(out[:, 1, 7])) and torch.equal(lse, clean_lse)
+    out[:, 1, 7] = clean[:, 1, 7]
+    assert torch.equal(out, clean)
 
 
 def test_same_slot_twice_and_any_order(vb):
