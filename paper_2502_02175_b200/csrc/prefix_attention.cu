@@ -46,7 +46,7 @@ struct PlanMem {
   int* first[2];                                // segment of each run's first unit
   int* row_k;                                   // [rows] active sequence of each row, -1: none
   float2* ml;                                   // [slot rows] (m, l), m in units of log2
-  float* po;                                    // [slot rows][head_dim]
+  float* po;                                    // [slot rows][head_dim]; of wide segments [slot rows / 8][head_dim / 4][8][4] (see wide_at)
   size_t bytes;
 };
 __host__ __device__ inline PlanMem plan_mem(void* mem, int n, int rows, int n_heads, int head_dim) {
@@ -61,7 +61,8 @@ __host__ __device__ inline PlanMem plan_mem(void* mem, int n, int rows, int n_he
   p.seg = (SegRec*)take(sizeof(SegRec) * 2 * (size_t)n);
   for (int c = 0; c < 2; ++c) p.first[c] = (int*)take(sizeof(int) * pf_runs(c));
   p.row_k = (int*)take(sizeof(int) * (size_t)(rows > 0 ? rows : 1));
-  const size_t slots = 2 * (size_t)rows * n_heads + (size_t)pf_runs(NARROW) * pf_bm(NARROW) + (size_t)pf_runs(WIDE) * pf_bm(WIDE);
+  // a row and head has at most one narrow and one more segment; wide segments have 17 rows at least and are padded to 8 (24 / 17 < 1.5)
+  const size_t slots = (5 * (size_t)rows * n_heads + 1) / 2 + 8 + (size_t)pf_runs(NARROW) * pf_bm(NARROW) + (size_t)pf_runs(WIDE) * pf_bm(WIDE);
   p.ml = (float2*)take(sizeof(float2) * slots);
   p.po = (float*)take(sizeof(float) * slots * head_dim);
   p.bytes = o;
@@ -71,6 +72,12 @@ __host__ __device__ inline PlanMem plan_mem(void* mem, int n, int rows, int n_he
 // The U units of a class are dealt to G = min(U, pf_runs) runs, so that none is empty: run c is [c*U/G, (c+1)*U/G).  The run of unit u:
 __device__ __forceinline__ long long runs(int cls, long long U) { return U < pf_runs(cls) ? U : pf_runs(cls); }
 __device__ __forceinline__ int run_of(int cls, long long u, long long U) { return (int)(((u + 1) * runs(cls, U) - 1) / U); }
+
+// rows of a segment per K/V head in the slots
+__host__ __device__ inline int pf_rows(int cls, int R) { return cls == NARROW ? R : (R + 7) & ~7; }
+// A wide tile's rows lie one per lane, so its partial sums are laid out for lanes to store side by side: 4 floats c4 of 8 rows after one
+// another (a row-major store of 16 bytes a lane touched 32 rows at once: 3.7 us a tile instead of 1).
+__device__ __forceinline__ size_t wide_at(size_t slot_row, int c4, int head_dim) { return ((slot_row >> 3) * (head_dim / 4) + c4) * 32 + (slot_row & 7) * 4; }
 
 // Whether a tile of a segment is one piece and holds everything its rows see: then the piece writes the result itself.
 __device__ __forceinline__ bool tile_direct(const SegRec& s, long long u_tile, long long U) {
@@ -209,7 +216,7 @@ __global__ void __cluster_dims__(PL_CTAS, 1, 1) __launch_bounds__(PL_THREADS, 1)
   const long long u_n = (wide ? 0 : u_pre) + u_suf, b_n = (long long)((wide ? 0 : r_pre) + r_suf) * a.kv_heads;
   long long units[2], slots_n, slots_w, segs;
   const long long u0_n = plan_scan(u_n, &units[NARROW]), u0_w = plan_scan(wide ? u_pre : 0, &units[WIDE]);
-  const long long b0_n = plan_scan(b_n, &slots_n), b0_w = plan_scan(wide ? (long long)r_pre * a.kv_heads : 0, &slots_w);
+  const long long b0_n = plan_scan(b_n, &slots_n), b0_w = plan_scan(wide ? (long long)pf_rows(WIDE, r_pre) * a.kv_heads : 0, &slots_w);
   const int g0 = (int)plan_scan((u_pre > 0) + (u_suf > 0), &segs);
   s_c[tid] = g0;                                                        // (s_c was read above, before the scans' barriers)
   __syncthreads();
@@ -223,7 +230,7 @@ __global__ void __cluster_dims__(PL_CTAS, 1, 1) __launch_bounds__(PL_THREADS, 1)
       for (long long c = (us * G + U - 1) / U, e = ((us + n) * G + U - 1) / U; c < e; ++c) p.first[cls][c] = g;
     };
     // slots: the narrow pieces' rows, then the wide ones' (each run sets itself off by a tile, see slot_row)
-    const long long at_w = slots_n + (long long)pf_runs(NARROW) * pf_bm(NARROW);
+    const long long at_w = (slots_n + 7) / 8 * 8 + (long long)pf_runs(NARROW) * pf_bm(NARROW);
     if (u_pre > 0) put(g0, c_pre, wide ? u0_w : u0_n, u_pre, r_pre, 0, pre, INT_MIN, t_pre, kb_pre, wide ? at_w + b0_w : b0_n);
     if (u_suf > 0)
       put(g0 + (u_pre > 0), NARROW, u0_n + (wide ? 0 : u_pre), u_suf, r_suf, pre, s_len[tid], s_len[tid] - s_nq[tid], t_suf, kb_suf,
@@ -290,7 +297,7 @@ __device__ __forceinline__ int next_piece(const PlanMem& pm, int cls, long long 
   p->lim0 = s->pos0 == INT_MIN ? INT_MIN : s->pos0 + 1;
   p->n = n;
   p->direct = tile_direct(*s, u - kb, U);
-  p->slot0 = (size_t)s->rowbase + (size_t)head * R + (size_t)rt * bm + (size_t)run * bm;
+  p->slot0 = (size_t)s->rowbase + (size_t)head * pf_rows(cls, R) + (size_t)rt * bm + (size_t)run * bm;
   return n;
 }
 
@@ -572,23 +579,24 @@ __device__ __forceinline__ void pw_expect(unsigned long long* bar, unsigned byte
 __device__ __forceinline__ void pw_arrive(unsigned long long* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(pf_smem(bar)) : "memory");
 }
-__device__ __forceinline__ bool pw_try(unsigned long long* bar, unsigned parity) {
-  unsigned ok;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
-               : "=r"(ok) : "r"(pf_smem(bar)), "r"(parity) : "memory");
-  return ok != 0;
-}
 __device__ __forceinline__ unsigned long long pw_ns() {
   unsigned long long t;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
+// (the hint: sleep in the barrier for up to 20 us a try)
+__device__ __forceinline__ bool pw_try_at(unsigned bar, unsigned parity) {
+  unsigned ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\nselp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 // Wait for a phase, at most PW_WAIT_LIMIT_NS; a wait that gives up (or finds that another has) returns false and marks the plan.
-__device__ __noinline__ bool pw_wait_slow(unsigned long long* bar, unsigned parity, volatile int* abort_flag, int* error) {
+__device__ __noinline__ bool pw_wait_slow(unsigned bar, unsigned parity, volatile int* abort_flag, int* error) {
   const unsigned long long t0 = pw_ns();
   while (true) {
-    for (int i = 0; i < 256; ++i)
-      if (pw_try(bar, parity)) return true;
+    for (int i = 0; i < 16; ++i)
+      if (pw_try_at(bar, parity)) return true;
     if (*abort_flag) return false;
     if (pw_ns() - t0 > PW_WAIT_LIMIT_NS) break;
   }
@@ -597,7 +605,7 @@ __device__ __noinline__ bool pw_wait_slow(unsigned long long* bar, unsigned pari
   return false;
 }
 __device__ __forceinline__ bool pw_wait(unsigned long long* bar, unsigned parity, volatile int* abort_flag, int* error) {
-  return pw_try(bar, parity) || pw_wait_slow(bar, parity, abort_flag, error);
+  return pw_try_at(pf_smem(bar), parity) || pw_wait_slow(pf_smem(bar), parity, abort_flag, error);
 }
 __device__ __forceinline__ void pw_tma(unsigned dst, const CUtensorMap* tm, int x, int y, unsigned long long* bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -617,16 +625,20 @@ template <typename T> __device__ __forceinline__ unsigned pw_idesc(int n, bool b
   const unsigned f = sizeof(T) == 2 && Half2<T>::exp_mask == 0x7f80u ? 1u : 0u;
   return (1u << 4) | (f << 7) | (f << 10) | (b_mn ? 1u << 16 : 0u) | ((unsigned)(n >> 3) << 17) | (8u << 24);
 }
-__device__ __forceinline__ void pw_mma_ss(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, bool acc) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)acc) : "memory");
+// The warp that issues products runs converged and one lane's predicate (`one`) lets the instruction through: operands then stay in
+// uniform registers.  Issued from a branch that a single lane takes, every product paid the moves into them (about 70 cycles a product, as
+// long as it executes, and twice that beside the softmax warps).
+__device__ __forceinline__ void pw_mma_ss(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, bool acc, unsigned one) {
+  asm volatile("{\n.reg .pred p, e;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 e, %5, 0;\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)acc), "r"(one) : "memory");
 }
-__device__ __forceinline__ void pw_mma_ts(unsigned d, unsigned a, unsigned long long b, unsigned idesc, bool acc) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((unsigned)acc) : "memory");
+__device__ __forceinline__ void pw_mma_ts(unsigned d, unsigned a, unsigned long long b, unsigned idesc, bool acc, unsigned one) {
+  asm volatile("{\n.reg .pred p, e;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 e, %5, 0;\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((unsigned)acc), "r"(one) : "memory");
 }
-__device__ __forceinline__ void pw_commit(unsigned long long* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(pf_smem(bar)) : "memory");
+__device__ __forceinline__ void pw_commit(unsigned long long* bar, unsigned one) {
+  asm volatile("{\n.reg .pred e;\nsetp.ne.b32 e, %1, 0;\n@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n"
+               ::"r"(pf_smem(bar)), "r"(one) : "memory");
 }
 #define PW_R32(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
 #define PW_I32(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
@@ -654,6 +666,31 @@ __device__ __forceinline__ void pw_ld_wait(unsigned* r, unsigned* r2) {
   pw_ld_wait(r);
   asm volatile("" : PW_T32(r2, 0), PW_T32(r2, 8), PW_T32(r2, 16), PW_T32(r2, 24) :: "memory");
 }
+__device__ __forceinline__ void pw_st1(unsigned addr, unsigned r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%1], {%0};" ::"r"(r), "r"(addr) : "memory");
+}
+// packed pairs of fp32: one instruction for two scores
+__device__ __forceinline__ unsigned long long pw_pair(float lo, float hi) {
+  unsigned long long d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void pw_unpair(unsigned long long d, float* lo, float* hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(d)); }
+__device__ __forceinline__ unsigned long long pw_fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ unsigned long long pw_add2(unsigned long long a, unsigned long long b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float pw_max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ void pw_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void pw_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void pw_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -675,7 +712,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, WideArgs w) {
   using W = Wide<D>;
   extern __shared__ unsigned char pw_raw[];
-  __shared__ __align__(8) unsigned long long full[W::SLOTS], empty[W::SLOTS], s_full[2], p_full[2], q_full, o_full, drain;
+  __shared__ __align__(8) unsigned long long full[W::SLOTS], empty[W::SLOTS], s_full[2], p_full[2][2], q_full, o_full, drain;
   __shared__ unsigned tmem_slot;
   __shared__ int abort_flag;
   const AttnArgs& a = w.a;
@@ -688,7 +725,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   float* const red_l = red_m + 256;
   if (tid == 0) {
     for (int i = 0; i < W::SLOTS; ++i) { pw_bar_init(&full[i], 1); pw_bar_init(&empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { pw_bar_init(&s_full[i], 1); pw_bar_init(&p_full[i], 128); }
+    for (int i = 0; i < 2; ++i) { pw_bar_init(&s_full[i], 1); pw_bar_init(&p_full[i][0], 128); pw_bar_init(&p_full[i][1], 128); }
     pw_bar_init(&q_full, PW_SOFT); pw_bar_init(&o_full, 1); pw_bar_init(&drain, 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -711,10 +748,14 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   int g = pm.first[WIDE][run];
   Piece p;
 
-  if (warp == 0) {
+  if (warp < 4 && warp != 1) {
     // ---------------------------------------------------------------- loads
-    const int per = 128 / w.box, chunk = lane / W::HALVES, half = lane % W::HALVES;
-    const bool mine = chunk < per;
+    // Issuing a box takes a warp about 110 cycles whichever lane does it, and a tile of small pages has up to 32 of them (8 rows): the
+    // boxes of a tile are shared out over three warps.  Each waits for the slot itself; one adds the byte count (a barrier's count of
+    // bytes may run ahead of it: the phase ends only with the arrival).
+    const int first = warp == 0 ? 0 : warp - 1;                         // 0, 1, 2
+    const int n_box = 128 / w.box * W::HALVES, b = first + 3 * lane, chunk = b / W::HALVES, half = b % W::HALVES;
+    const bool mine = b < n_box;
     const int none = a.n_pages << a.shift;                              // a row behind the pool: zeros
     int cnt = 0;
     bool ok = true;
@@ -722,9 +763,9 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       const int s = cnt % W::SLOTS;
       if (cnt >= W::SLOTS) ok = __all_sync(0xffffffffu, pw_wait(&empty[s], ((cnt / W::SLOTS) & 1) ^ 1, &abort_flag, error));
       if (!ok) return;
-      if (lane == 0) pw_expect(&full[s], W::TILE);
-      __syncwarp();
+      if (first == 0 && lane == 0) pw_expect(&full[s], W::TILE);
       if (mine) pw_tma(ring + (unsigned)s * W::TILE + (unsigned)half * W::HALF + (unsigned)chunk * w.box * 128u, tm, x0 + half * 64, y, &full[s]);
+      __syncwarp();
       ++cnt;
     };
     while (u < u_end && ok) {
@@ -749,50 +790,75 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       for (int c = max(0, cnt - W::SLOTS); c < cnt; ++c) pw_wait(&full[c % W::SLOTS], (c / W::SLOTS) & 1, &abort_flag, error);
   } else if (warp == 1) {
     // ---------------------------------------------------------------- products
-    if (lane == 0) {
-      const unsigned id_s = pw_idesc<T>(128, false), id_o = pw_idesc<T>(D, true);
-      int cnt = 0, pieces = 0, n_p[2] = {0, 0};
-      bool ok = true;
-      auto tile = [&]() -> unsigned {                                   // the next tile of the ring, when it is there
-        const int s = cnt % W::SLOTS;
-        ok = ok && pw_wait(&full[s], (cnt / W::SLOTS) & 1, &abort_flag, error);
-        return ring + (unsigned)s * W::TILE;
-      };
-      auto pv = [&](int i) {
-        const int b = i & 1;
-        ok = ok && pw_wait(&p_full[b], n_p[b]++ & 1, &abort_flag, error);
-        const unsigned v_s = tile();
-        if (!ok) return;
-        pw_after();
+    unsigned one;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(one));
+    const unsigned tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const unsigned id_s = pw_idesc<T>(128, false), id_o = pw_idesc<T>(D, true);
+    const unsigned long long q_d = pw_desc(q_s, 16, 1024), k_d = pw_desc(ring, 16, 1024), v_d = pw_desc(ring, W::HALF, 1024);
+    // A wait on the way of every product has to be short (its dependent instructions are issued between those of the softmax warps): an
+    // address and a parity at hand, and failures looked at once a block.
+    const unsigned full_a = pf_smem(full), p_a = pf_smem(p_full);
+    int slot = 0, pieces = 0, n_p[2] = {0, 0};
+    unsigned phase = 0, failed = 0;
+    bool ok = true;
+    auto wait_at = [&](unsigned bar, unsigned parity) {
+      if (!pw_try_at(bar, parity)) failed |= !pw_wait_slow(bar, parity, &abort_flag, error);
+    };
+    auto still_ok = [&]() { return __all_sync(0xffffffffu, !failed); };
+    auto next = [&]() { pw_commit(&empty[slot], one); if (++slot == W::SLOTS) { slot = 0; phase ^= 1; } };
+    auto same = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };    // tells the compiler that a value is the same in all lanes
+    auto there = [&](int ahead) {                                       // the ring's tile `ahead` places on
+      const int sl = slot + ahead, wrap = sl >= W::SLOTS;
+      wait_at(full_a + 8u * (sl - (wrap ? W::SLOTS : 0)), phase ^ wrap);
+    };
+    auto s_mma = [&](int i) {                                           // S_i from the next tile
+      const int b = same(i & 1);
+      const unsigned long long d = k_d + (unsigned long long)(same(slot) * (W::TILE >> 4));
 #pragma unroll
-        for (int j = 0; j < 8; ++j)                                     // 16 keys: 8 columns of packed P; 16 rows of V (MN-major)
-          pw_mma_ts(tmem + 256u + 128u * b, tmem + 128u * b + 8u * j, pw_desc(v_s + (unsigned)j * 2048u, W::HALF, 1024), id_o, i > 1 || j > 0);
-        pw_commit(&empty[cnt % W::SLOTS]);
-        ++cnt;
-      };
-      while (u < u_end && ok) {
-        u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
-        ok = pw_wait(&q_full, pieces & 1, &abort_flag, error);
-        for (int i = 0; i < p.n && ok; ++i) {
-          const unsigned k_s = tile();
-          if (!ok) break;
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const unsigned off = ((unsigned)(ks >> 2) * W::HALF + (unsigned)(ks & 3) * 32u) >> 4;
+        pw_mma_ss(tm + 128u * b, q_d + off, d + off, id_s, ks > 0, one);
+      }
+      pw_commit(&s_full[b], one);
+      next();
+    };
+    // Tiles come in the order K_0, K_1, V_0, K_2, V_1, ..., V_{n-1}.  The weights come last, so everything else is waited for before them:
+    // O += P_i V_i and S_{i+2}, which takes the columns that P_i leaves, then go out in one burst.
+    while (u < u_end && ok) {
+      u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
+      const int n = same(p.n);
+      there(0);
+      if (n > 1) there(1);
+      wait_at(pf_smem(&q_full), pieces & 1);
+      ok = still_ok();
+      if (!ok) break;
+      pw_after();
+      s_mma(0);
+      if (n > 1) s_mma(1);
+      for (int i = 0; i < n; ++i) {
+        const int b = same(i & 1);
+        const unsigned acc = same(i > 1), par = same(n_p[b] & 1);
+        there(0);
+        if (i + 2 < n) there(1);
+        const unsigned long long d = v_d + (unsigned long long)(same(slot) * (W::TILE >> 4));
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {                                // the weights' halves arrive one after the other
+          wait_at(p_a + 16u * b + 8u * hf, par);
           pw_after();
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const unsigned off = (unsigned)(ks >> 2) * W::HALF + (unsigned)(ks & 3) * 32u;
-            pw_mma_ss(tmem + 128u * (i & 1), pw_desc(q_s + off, 16, 1024), pw_desc(k_s + off, 16, 1024), id_s, ks > 0);
-          }
-          pw_commit(&s_full[i & 1]);
-          pw_commit(&empty[cnt % W::SLOTS]);
-          ++cnt;
-          if (i > 0) pv(i - 1);
+          for (int j = 4 * hf; j < 4 * hf + 4; ++j)                     // 16 keys: 8 columns of packed P; 16 rows of V (MN-major)
+            pw_mma_ts(tm + 256u + 128u * b, tm + 128u * b + 8u * j, d + 128u * j, id_o, acc || j > 0, one);
         }
-        if (ok) pv(p.n - 1);
-        if (ok) pw_commit(&o_full);
-        ++pieces;
+        ++n_p[b];
+        next();
+        if (i + 2 < n) s_mma(i + 2);
+        ok = still_ok();
+        if (!ok) break;
       }
-      if (!ok) { pw_commit(&drain); pw_wait(&drain, 0, &abort_flag, error); }
+      if (ok) pw_commit(&o_full, one);
+      ++pieces;
     }
+    if (!ok) { pw_commit(&drain, one); pw_wait(&drain, 0, &abort_flag, error); }
     __syncwarp();
   } else if (warp >= 4) {
     // ---------------------------------------------------------------- softmax
@@ -800,17 +866,29 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     const unsigned trow = tmem + ((unsigned)(32 * q4) << 16), s_col = trow + 128u * side, o_col = trow + 256u + 128u * side;
     int n_s = 0, pieces = 0;
     bool ok = true;
-    while (u < u_end && ok) {
-      u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
-      // Q: stacked row x is q row row0 + x / ratio, query head head * ratio + x % ratio; rows behind the last are zeros
-      constexpr int C16 = D / 8;
+    // Q of a piece: all loads first (a store between them would make each wait for the one before), and for the next piece before the
+    // present one is written out
+    constexpr int C16 = D / 8, NQ = 128 * C16 / PW_SOFT;
+    uint4 qv[NQ];
+    auto load_q = [&](const Piece& p) {
+      // stacked row x is q row row0 + x / ratio, query head head * ratio + x % ratio; rows behind the last are zeros
+      const int x0 = p.rt * 128, q0 = x0 / a.ratio, h0 = x0 - q0 * a.ratio;
+      const T* src = (const T*)a.q + (size_t)(p.row0 + q0) * a.q_stride + (size_t)p.head * a.ratio * D;
 #pragma unroll
-      for (int i = 0; i < 128 * C16 / PW_SOFT; ++i) {
-        const int c = st + i * PW_SOFT, qr = c / C16, c16 = c % C16, x = p.rt * 128 + min(qr, p.nr - 1), xq = x / a.ratio;
-        uint4 v = *reinterpret_cast<const uint4*>((const T*)a.q + (size_t)(p.row0 + xq) * a.q_stride + (size_t)(p.head * a.ratio + x - xq * a.ratio) * D + c16 * 8);
-        if (w.flip) { v.x ^= 0x80008000u; v.y ^= 0x80008000u; v.z ^= 0x80008000u; v.w ^= 0x80008000u; }
-        if (qr >= p.nr) v = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4*>(smem + (c16 >> 3) * W::HALF + pf_swz(qr, c16 & 7)) = v;
+      for (int i = 0; i < NQ; ++i) {
+        const int c = st + i * PW_SOFT, qr = c / C16, c16 = c % C16, x = h0 + qr, xq = x / a.ratio;
+        qv[i] = make_uint4(0, 0, 0, 0);
+        if (qr < p.nr) qv[i] = *reinterpret_cast<const uint4*>(src + (size_t)xq * a.q_stride + (x - xq * a.ratio) * D + c16 * 8);
+      }
+    };
+    u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
+    load_q(p);
+    while (true) {
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        const int c = st + i * PW_SOFT, qr = c / C16, c16 = c % C16;
+        if (w.flip) { qv[i].x ^= 0x80008000u; qv[i].y ^= 0x80008000u; qv[i].z ^= 0x80008000u; qv[i].w ^= 0x80008000u; }
+        *reinterpret_cast<uint4*>(smem + (c16 >> 3) * W::HALF + pf_swz(qr, c16 & 7)) = qv[i];
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       pw_before();
@@ -823,6 +901,10 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
         if (!idle) {
           pw_after();
           const int valid = p.key1 - p.key0 - i * 128;                  // keys of this block (fewer than 128 in the last)
+          if (valid < 128) {
+            for (int c = valid; c < 128; ++c) pw_st1(s_col + c, 0xff800000u);             // -inf behind them
+            pw_st_wait();
+          }
           // two sweeps over the scores (the row's 128 do not fit the registers beside the rest): maximum, then weights
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -831,12 +913,8 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
             pw_ld32(s_col + 64u * hf, v);
             pw_ld32(s_col + 64u * hf + 32u, v + 32);
             pw_ld_wait(v, v + 32);
-            if (valid < 128) {
 #pragma unroll
-              for (int c = 0; c < 64; ++c) if (hf * 64 + c >= valid) v[c] = 0xff800000u;
-            }
-#pragma unroll
-            for (int c = 0; c < 64; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(v[c]));
+            for (int c = 0; c < 32; ++c) mx[c & 3] = pw_max3(mx[c & 3], __uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
           }
           const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2;
           // the reference moves only when the maximum has grown by a factor of 2^8: weights up to 256 cost no precision (they are rounded
@@ -848,7 +926,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
             m = mn;
             l *= al;
             if (i >= 2) {
-#pragma unroll
+#pragma unroll 1
               for (int c = 0; c < D / 32; ++c) {
                 unsigned x[32];
                 pw_ld32(o_col + 32u * c, x);
@@ -862,7 +940,8 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
           const float ref = m == -INFINITY ? 0.f : m;
           // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16); the sum takes
           // the unrounded weights.  P lies over the scores already read: 16 columns a sweep of 32.
-          float ls[4] = {0.f, 0.f, 0.f, 0.f};
+          unsigned long long ls[2] = {0ull, 0ull};                      // two fp32 sums each
+          const unsigned long long sc = pw_pair(a.scale2, a.scale2), nr = pw_pair(-ref, -ref);
           unsigned v[2][32];
           pw_ld32(s_col, v[0]);
 #pragma unroll
@@ -872,20 +951,30 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
             unsigned pk[16];
 #pragma unroll
             for (int c = 0; c < 16; ++c) {
-              float p0 = pf_ex2(fmaf(__uint_as_float(v[q & 1][2 * c]), a.scale2, -ref));
-              float p1 = pf_ex2(fmaf(__uint_as_float(v[q & 1][2 * c + 1]), a.scale2, -ref));
-              if (valid < 128) { if (q * 32 + 2 * c >= valid) p0 = 0.f; if (q * 32 + 2 * c + 1 >= valid) p1 = 0.f; }
-              ls[c & 3] += p0 + p1;
-              pk[c] = Half2<T>::pack(p0, p1);
+              float x0, x1;
+              pw_unpair(pw_fma2(pw_pair(__uint_as_float(v[q & 1][2 * c]), __uint_as_float(v[q & 1][2 * c + 1])), sc, nr), &x0, &x1);
+              x0 = pf_ex2(x0); x1 = pf_ex2(x1);
+              ls[c & 1] = pw_add2(ls[c & 1], pw_pair(x0, x1));
+              pk[c] = Half2<T>::pack(x0, x1);
             }
             pw_st16(s_col + 16u * q, pk);
+            if (q == 1) {
+              pw_st_wait();
+              pw_before();
+              pw_arrive(&p_full[side][0]);
+            }
           }
-          l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+          float l0, l1, l2, l3;
+          pw_unpair(ls[0], &l0, &l1); pw_unpair(ls[1], &l2, &l3);
+          l += (l0 + l1) + (l2 + l3);
           pw_st_wait();
-        }
+        } else pw_arrive(&p_full[side][0]);
         pw_before();
-        pw_arrive(&p_full[side]);
+        pw_arrive(&p_full[side][1]);
       }
+      Piece pn;
+      const bool more = u < u_end;
+      if (more) { u += next_piece(pm, WIDE, U, run, u, u_end, &g, &pn); load_q(pn); }
       if (ok) ok = pw_wait(&o_full, pieces & 1, &abort_flag, error);
       ++pieces;
       ok = pw_all_ok(ok);                                               // every product of the piece is done: Q's memory is free
@@ -898,7 +987,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
         const float m0 = red_m[r], m1 = red_m[128 + r], M = fmaxf(m0, m1), ref = M == -INFINITY ? 0.f : M;
         const float f0 = pf_ex2(m0 - ref), f1 = pf_ex2(m1 - ref);
         const bool two = p.n > 1;                                       // one block: the odd side holds nothing
-        float* dst = pm.po + (p.slot0 + r) * D + side * (D / 2);
+        float* dst = pm.po + wide_at(p.slot0 + r, side * (D / 8), D);
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
           unsigned x[32], y[32] = {};
@@ -913,13 +1002,15 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
               if (two) {
                 o.x += f1 * __uint_as_float(y[e]); o.y += f1 * __uint_as_float(y[e + 1]); o.z += f1 * __uint_as_float(y[e + 2]); o.w += f1 * __uint_as_float(y[e + 3]);
               }
-              *reinterpret_cast<float4*>(dst + 32 * c + e) = o;
+              *reinterpret_cast<float4*>(dst + (8 * c + (e >> 2)) * 32) = o;
             }
           }
         }
         if (side == 0 && r < p.nr) pm.ml[p.slot0 + r] = make_float2(M, f0 * red_l[r] + (two ? f1 * red_l[128 + r] : 0.f));
       }
+      if (!more) break;
       pw_all_ok(true);                                                  // red_m, red_l may be written again
+      p = pn;
     }
     pw_before();
   }
@@ -930,35 +1021,39 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   }
 }
 
-// One warp per (row, query head): the pieces of its prefix and of its own segment, added in order.
+// One warp per (row, query head): the pieces of its prefix and of its own segment, added in order.  The eight warps of a CTA take
+// stacked rows of one K/V head that follow one another (they share the sectors of wide partial sums).
 template <typename T, int D>
 __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
-  constexpr int E = D / 32;                                             // outputs per lane
   const PlanMem p = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
   const int lane = threadIdx.x & 31;
-  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), per = (long long)a.rows * a.ratio;
   pdl_trigger();
   pdl_wait();
-  if (w >= (long long)a.rows * a.n_heads) return;
-  const int row = (int)(w / a.n_heads), h = (int)(w % a.n_heads), kvh = h / a.ratio;
+  if (w >= per * a.kv_heads) return;
+  const int kvh = (int)(w / per), xr = (int)(w - kvh * per), row = xr / a.ratio, h = kvh * a.ratio + xr - row * a.ratio;
   const int k = p.row_k[row];
   if (k < 0) return;
   const SeqRec q = p.seq[k];
-  int np[2] = {0, 0}, pad[2] = {0, 0};
+  int np[2] = {0, 0}, pad[2] = {0, 0}, wide = 0;
   size_t base[2] = {0, 0};
+  const PlanHead hd = *p.head;
+  SegRec sg[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) sg[i] = p.seg[max(0, i ? q.suf_seg : q.pre_seg)];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int g = i ? q.suf_seg : q.pre_seg;
-    if (g < 0) continue;
-    const SegRec s = p.seg[g];
-    const int bm = pf_bm(s.cls), x = (row - s.row0) * a.ratio + h % a.ratio, rt = x / bm;
-    const long long U = p.head->units[s.cls];
+    if ((i ? q.suf_seg : q.pre_seg) < 0) continue;
+    const SegRec& s = sg[i];
+    const int bm = pf_bm(s.cls), x = (row - s.row0) * a.ratio + h - kvh * a.ratio, rt = x / bm;
+    const long long U = hd.units[s.cls];
     const long long u0 = s.ustart + ((long long)kvh * s.T + rt) * s.KB;
-    if (tile_direct(s, u0, U)) return;                                  // written by its only piece
-    const int c0 = run_of(s.cls, u0, U);
-    np[i] = run_of(s.cls, u0 + s.KB - 1, U) - c0 + 1;
+    const int c0 = run_of(s.cls, u0, U), c1 = run_of(s.cls, u0 + s.KB - 1, U);
+    if (s.pos0 != INT_MIN && s.key0 == 0 && c0 == c1) return;           // written by its only piece (tile_direct)
+    np[i] = c1 - c0 + 1;
     pad[i] = bm;
-    base[i] = (size_t)s.rowbase + (size_t)kvh * s.R + x + (size_t)c0 * bm;
+    if (s.cls == WIDE) wide = 1;                                        // (only a prefix is wide)
+    base[i] = (size_t)s.rowbase + (size_t)kvh * pf_rows(s.cls, s.R) + x + (size_t)c0 * bm;
   }
   const int n = np[0] + np[1];
   auto slot = [&](int i) { return i < np[0] ? base[0] + (size_t)i * pad[0] : base[1] + (size_t)(i - np[0]) * pad[1]; };
@@ -967,26 +1062,22 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   const float ref = M == -INFINITY ? 0.f : M;
-  float l = 0.f, o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int c4 = lane < D / 4 ? lane : 0;
 #pragma unroll 4
   for (int i = 0; i < n; ++i) {
     const size_t sl = slot(i);
     const float2 ml = p.ml[sl];
+    const float4 v = *reinterpret_cast<const float4*>(p.po + (wide && i < np[0] ? wide_at(sl, c4, D) : sl * D + c4 * 4));
     const float f = pf_ex2(ml.x - ref);
     l += f * ml.y;
-    const float* src = p.po + sl * D + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      const float2 v = *reinterpret_cast<const float2*>(src + e);
-      o[e] += f * v.x; o[e + 1] += f * v.y;
-    }
+    o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* dst = (T*)a.out + (size_t)row * a.out_stride + (size_t)h * D + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; e += 2) *reinterpret_cast<unsigned*>(dst + e) = Half2<T>::pack(o[e] * inv, o[e + 1] * inv);
+  if (lane < D / 4)
+    *reinterpret_cast<uint2*>((T*)a.out + (size_t)row * a.out_stride + (size_t)h * D + lane * 4) =
+        make_uint2(Half2<T>::pack(o.x * inv, o.y * inv), Half2<T>::pack(o.z * inv, o.w * inv));
   if (a.lse && lane == 0) a.lse[(size_t)row * a.n_heads + h] = (M + log2f(l)) * PF_LN2;
 }
 
@@ -995,7 +1086,7 @@ int launch_attention(const vlac_pages* p, const AttnArgs& a, cudaStream_t s) {
   // more than 16 stacked rows, or the call cannot have a wide segment
   if ((long long)a.rows * a.ratio > pf_bm(NARROW)) {
     WideArgs w = {a, a.scale2 < 0.f, a.page < 128 ? a.page : 128};
-    w.a.scale2 = fabsf(a.scale2);
+    w.a.scale2 = fmaxf(fabsf(a.scale2), 1e-30f);                        // not zero: -inf marks what is not there
     CUtensorMap tk, tv;
     const int rows = a.n_pages << a.shift, cols = a.kv_heads * D;
     int rc = vlac_encode_map_2d(&tk, a.k, rows, cols, w.box);
