@@ -22,11 +22,11 @@ constexpr int NARROW = 0, WIDE = 1;
 constexpr int PN_WARPS = 4, PN_CTAS = 2 * 148;  // narrow: two CTAs of four warps per SM, every warp works alone
 constexpr int PF_MAX_RUNS = PN_WARPS * PN_CTAS; // runs of the narrow kernel
 constexpr int PW_CTAS = 148;                    // runs of the wide kernel: one CTA per SM
-__host__ __device__ constexpr int pf_bm(int c) { return c == NARROW ? 16 : 128; }        // stacked rows of a tile
+__host__ __device__ constexpr int pf_bm(int c) { return c == NARROW ? 16 : 256; }        // stacked rows of a tile
 __host__ __device__ constexpr int pf_kb(int c) { return c == NARROW ? 64 : 128; }        // keys of a unit
 __host__ __device__ constexpr int pf_runs(int c) { return c == NARROW ? PF_MAX_RUNS : PW_CTAS; }
 
-struct SeqRec { int slot, row0, nq, len, pre_seg, suf_seg, pad0, pad1; };          // segments: -1 none
+struct SeqRec { int slot /* -1: refused */, row0, nq, len, pre_seg, suf_seg, pad0, pad1; };          // segments: -1 none
 struct SegRec {
   long long ustart, uend;                       // units of this segment in the call's order
   int slot;                                     // whose table holds the keys
@@ -40,7 +40,6 @@ struct PlanHead { long long units[2]; int n_act, error; };   // error: a wait of
 
 struct PlanMem {
   PlanHead* head;
-  int *lcp, *bad;                               // [n] common pages with the previous active sequence; findings
   SeqRec* seq;                                  // [n] active sequences
   SegRec* seg;                                  // [2n]
   int* first[2];                                // segment of each run's first unit
@@ -55,8 +54,6 @@ __host__ __device__ inline PlanMem plan_mem(void* mem, int n, int rows, int n_he
   size_t o = 0;
   auto take = [&](size_t bytes) { unsigned char* r = b + o; o = (o + bytes + 255) & ~(size_t)255; return r; };
   p.head = (PlanHead*)take(sizeof(PlanHead));
-  p.lcp = (int*)take(sizeof(int) * n);
-  p.bad = (int*)take(sizeof(int) * n);
   p.seq = (SeqRec*)take(sizeof(SeqRec) * n);
   p.seg = (SegRec*)take(sizeof(SegRec) * 2 * (size_t)n);
   for (int c = 0; c < 2; ++c) p.first[c] = (int*)take(sizeof(int) * pf_runs(c));
@@ -93,150 +90,218 @@ struct PlanArgs {
   int* status;
   void* mem;
 };
+// One launch, bound by the chain of dependent reads and barriers, not by bytes: one CTA of 8 warps for few sequences with short tables, a cluster
+// of eight CTAs that reads the tables together otherwise.
 constexpr int PL_CTAS = 8;
-constexpr int PL_THREADS = 1024;
-constexpr int PL_WARPS = PL_CTAS * PL_THREADS / 32;
+constexpr int PL_MAX = VLAC_PAGES_MAX_LIST;
+constexpr int PL_ONE = 4096;                    // table entries up to which one CTA is faster
+struct Sums { long long u[2]; int r[2], g; };                           // units and slot rows of both classes, segments
+__device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) { return {{x.u[0] + y.u[0], x.u[1] + y.u[1]}, {x.r[0] + y.r[0], x.r[1] + y.r[1]}, x.g + y.g}; }
+struct PlanShared {
+  int i[PL_MAX], slot[PL_MAX], row0[PL_MAX], nq[PL_MAX], len[PL_MAX], lcp[PL_MAX], bad[PL_MAX];
+  int c[PL_MAX], m[PL_MAX], last[PL_MAX], g[PL_MAX];                    // of a group, at its leader: common pages, members, last member; segment
+  long long u0[2][PL_MAX];                                              // first unit of the sequence's segments, per class
+  unsigned leads[PL_MAX / 32];
+  int warps[32];
+  Sums part[32];
+};
 
-// exclusive sum over the block of 1024 threads
-__device__ long long plan_scan(long long v, long long* total) {
-  __shared__ long long part[32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long x = v;
+// exclusive sums over the block's first n threads of five values (the barrier's cost is shared)
+__device__ Sums plan_scan(Sums* part, const Sums& v, int n, Sums* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = (n + 31) >> 5;
+  Sums before = {};
+  if (warp < nw) {
+    Sums x = v;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += t; }
-  __syncthreads();
-  if (lane == 31) part[warp] = x;
-  __syncthreads();
-  if (warp == 0) {
-    long long y = part[lane];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, y, o); if (lane >= o) y += t; }
-    part[lane] = y;
+    for (int o = 1; o < 32; o <<= 1) {
+      const Sums t = {{__shfl_up_sync(0xffffffffu, x.u[0], o), __shfl_up_sync(0xffffffffu, x.u[1], o)},
+                      {__shfl_up_sync(0xffffffffu, x.r[0], o), __shfl_up_sync(0xffffffffu, x.r[1], o)}, __shfl_up_sync(0xffffffffu, x.g, o)};
+      if (lane >= o) x = x + t;
+    }
+    if (lane == 31) part[warp] = x;
+    before = {{x.u[0] - v.u[0], x.u[1] - v.u[1]}, {x.r[0] - v.r[0], x.r[1] - v.r[1]}, x.g - v.g};
   }
   __syncthreads();
-  *total = part[31];
-  return x - v + (warp ? part[warp - 1] : 0);
+  Sums all = {};
+  for (int w = 0; w < nw; ++w) {
+    if (w == warp) before = before + all;
+    all = all + part[w];
+  }
+  *total = all;
+  return before;
 }
 
-__global__ void __cluster_dims__(PL_CTAS, 1, 1) __launch_bounds__(PL_THREADS, 1) prefix_plan_kernel(PlanArgs a) {
-  __shared__ int s_i[1024], s_slot[1024], s_row0[1024], s_nq[1024], s_len[1024], s_lcp[1024], s_lead[1024], s_c[1024], s_m[1024], s_end[1024];
-  const int tid = threadIdx.x, lane = tid & 31, rank = (int)cluster_rank();
-  const int gwarp = (tid >> 5) * PL_CTAS + rank;
+template <int CTAS>
+__global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_plan_kernel(PlanArgs a) {
+  extern __shared__ __align__(16) unsigned char pl_raw[];
+  PlanShared& s = *reinterpret_cast<PlanShared*>(pl_raw);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = blockDim.x >> 5, rank = CTAS > 1 ? (int)cluster_rank() : 0;
   const PlanMem p = plan_mem(a.mem, a.n, a.rows, a.n_heads, a.head_dim);
+  if (CTAS > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // (all CTAs run before one writes into another)
   pdl_trigger();
   pdl_wait();
   // ---- the active sequences (rows to compute), in list order: every CTA for itself
   int status = VLAC_OK, slot = 0, q0 = 0, q1 = 0, len = 0;
-  if (tid < a.n) { q0 = a.q_ptr[tid]; q1 = a.q_ptr[tid + 1]; }
-  const int broken = __syncthreads_or(tid < a.n && q1 < q0);            // rows would overlap: nothing is computed
   if (tid < a.n) {
-    slot = a.seqs[tid];
-    if (broken || q0 < 0 || q1 > a.rows || (unsigned)slot >= (unsigned)a.n_slots) status = VLAC_ERR_INVALID_ARG;
+    q0 = a.q_ptr[tid]; q1 = a.q_ptr[tid + 1]; slot = a.seqs[tid];
+    if (q0 < 0 || q1 > a.rows || (unsigned)slot >= (unsigned)a.n_slots) status = VLAC_ERR_INVALID_ARG;
     else {
       len = a.len[slot];
       if (len < 0 || len > a.max_pages << a.shift) status = VLAC_ERR_BAD_STATE;
     }
   }
-  const bool act = tid < a.n && status == VLAC_OK && q1 > q0;
-  long long tot;
-  const int k_of = (int)plan_scan(act ? 1 : 0, &tot);
-  const int n_act = (int)tot;
-  if (act) { s_i[k_of] = tid; s_slot[k_of] = slot; s_row0[k_of] = q0; s_nq[k_of] = q1 - q0; s_len[k_of] = len; }
-  if (rank == 0 && tid < a.n) { p.lcp[tid] = INT_MAX; p.bad[tid] = 0; a.status[tid] = status; }
-  cluster_sync_all();
-
-  // ---- tables: page numbers in range; leading pages in common with the previous active sequence
-  int team = 1;
-  while (team < 32 && team * 2 * n_act <= PL_WARPS) team *= 2;
-  const int n_teams = PL_WARPS / team;
-  for (int k = gwarp / team; k < n_act; k += n_teams) {
-    const int *t = a.table + (size_t)s_slot[k] * a.max_pages, *tp = k ? a.table + (size_t)s_slot[k - 1] * a.max_pages : t;
-    const int np = (s_len[k] + a.page - 1) >> a.shift;
-    // only whole pages in front of every member's queries are shared: all rows of the group see all of them
-    const int m = k ? min(max(0, s_len[k] - s_nq[k]), max(0, s_len[k - 1] - s_nq[k - 1])) >> a.shift : 0;
-    int bad = 0, lcp = m;
-#pragma unroll 4
-    for (int j = (gwarp % team) * 32 + lane; j < np; j += team * 32) {
-      const int x = t[j];
-      bad |= (unsigned)x >= (unsigned)a.n_pages;
-      if (j < m && x != tp[j]) lcp = min(lcp, j);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) { bad |= __shfl_xor_sync(0xffffffffu, bad, o); lcp = min(lcp, __shfl_xor_sync(0xffffffffu, lcp, o)); }
-    if (lane == 0) { atomicMin(&p.lcp[k], lcp); if (bad) atomicOr(&p.bad[k], 1); }
-  }
-  cluster_sync_all();
-  const bool mine = tid < n_act, bad = mine && __ldcg(&p.bad[tid]);
-  // which sequence each row belongs to
-  for (int r = rank * PL_THREADS + tid; r < a.rows; r += PL_CTAS * PL_THREADS) {
-    int lo = 0, hi = n_act - 1;
-    while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (s_row0[m] <= r) lo = m; else hi = m - 1; }
-    const bool in = n_act > 0 && r >= s_row0[lo] && r < s_row0[lo] + s_nq[lo] && !__ldcg(&p.bad[lo]);
-    p.row_k[r] = in ? lo : -1;
-  }
-  if (rank != 0) return;
-
-  // ---- neighbours into groups
-  if (mine) s_lcp[tid] = bad ? -1 : __ldcg(&p.lcp[tid]);
-  if (bad) a.status[s_i[tid]] = VLAC_ERR_BAD_STATE;
+  const bool want = tid < a.n && status == VLAC_OK && q1 > q0;
+  const unsigned ball = __ballot_sync(0xffffffffu, want);
+  if (lane == 0) s.warps[warp] = __popc(ball);
+  const int broken = __syncthreads_or(tid < a.n && q1 < q0);            // rows would overlap: nothing is computed
+  if (broken && tid < a.n) status = VLAC_ERR_INVALID_ARG;
+  int n_act = 0, k_of = __popc(ball & ((1u << lane) - 1));
+  for (int w = 0; w < (a.n + 31) >> 5; ++w) { const int c = s.warps[w]; n_act += c; if (w < warp) k_of += c; }
+  if (broken) n_act = 0;
+  if (want && !broken) { s.i[k_of] = tid; s.slot[k_of] = slot; s.row0[k_of] = q0; s.nq[k_of] = q1 - q0; s.len[k_of] = len; }
+  if (tid < PL_MAX / 32) s.leads[tid] = 0;
+  for (int k = tid; k < n_act; k += blockDim.x) { s.lcp[k] = INT_MAX; s.bad[k] = 0; }
+  if (rank == 0 && tid < a.n) a.status[tid] = status;
   __syncthreads();
-  if (tid == 0) {
-    int lead = 0, c = 0, m = 0;
-    for (int k = 0; k < n_act; ++k) {
-      // joining spares the newcomer the reading of c2 common pages and costs the others the reading of c - c2 pages each
-      const int c2 = min(c, s_lcp[k]);
-      const bool join = m > 0 && s_lcp[k] >= 0 && s_lcp[lead] >= 0 && s_row0[k] == s_end[lead] && (long long)c2 > (long long)(c - c2) * (m - 1);
-      if (join) { c = c2; ++m; }
-      else { lead = k; m = 1; c = max(0, s_len[k] - s_nq[k]) >> a.shift; }
-      s_lead[k] = lead; s_c[lead] = c; s_m[lead] = m; s_end[lead] = s_row0[k] + s_nq[k];
+
+  // ---- tables: page numbers in range; leading pages in common with the previous active sequence.  CTA r has the sequences r, r + CTAS, ..
+  const int n_mine = (n_act - rank + CTAS - 1) / CTAS;
+  int team = 1;
+  while (team < nw && team * 2 * n_mine <= nw) team *= 2;
+  for (int x = warp / team; x < n_mine; x += nw / team) {
+    const int k = x * CTAS + rank;
+    const int *t = a.table + (size_t)s.slot[k] * a.max_pages, *tp = k ? a.table + (size_t)s.slot[k - 1] * a.max_pages : t;
+    const int np = (s.len[k] + a.page - 1) >> a.shift;
+    // only whole pages in front of every member's queries are shared: all rows of the group see all of them
+    const int m = k ? min(max(0, s.len[k] - s.nq[k]), max(0, s.len[k - 1] - s.nq[k - 1])) >> a.shift : 0;
+    int bad = 0, lcp = m;
+#pragma unroll 8
+    for (int j = (warp % team) * 32 + lane; j < np; j += team * 32) {
+      const int y = t[j], z = j < m ? tp[j] : y;
+      bad |= (unsigned)y >= (unsigned)a.n_pages;
+      if (y != z) lcp = min(lcp, j);
     }
+    lcp = __reduce_min_sync(0xffffffffu, lcp);
+    bad = __any_sync(0xffffffffu, bad);
+    if (lane == 0) { atomicMin(&s.lcp[k], lcp); if (bad) atomicOr(&s.bad[k], 1); }
+  }
+  // which sequence each row belongs to
+  for (int r = rank * blockDim.x + tid; r < a.rows; r += CTAS * blockDim.x) {
+    int lo = 0, hi = n_act - 1;
+    while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (s.row0[m] <= r) lo = m; else hi = m - 1; }
+    p.row_k[r] = n_act > 0 && r >= s.row0[lo] && r < s.row0[lo] + s.nq[lo] ? lo : -1;
+  }
+  __syncthreads();
+  if (CTAS > 1) {
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    for (int x = tid; x < n_mine && rank; x += blockDim.x) {
+      const int k = x * CTAS + rank;
+      unsigned to;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to) : "r"((unsigned)__cvta_generic_to_shared(&s.lcp[k])));
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(s.lcp[k]) : "memory");
+      asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to) : "r"((unsigned)__cvta_generic_to_shared(&s.bad[k])));
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(s.bad[k]) : "memory");
+    }
+    cluster_sync_all();
+    if (rank != 0) return;
+  }
+
+  // ---- neighbours into groups (one warp, 32 sequences at a time, from one change of the common length to the next)
+  if (warp == 0) {
+    int lead = 0, c = 0, m = 0;
+    for (int k0 = 0; k0 < n_act; k0 += 32) {
+      const int k = k0 + lane;
+      int l = INT_MAX, vis = 0;                                         // lanes behind the last sequence never end a run
+      if (k < n_act) {
+        vis = max(0, s.len[k] - s.nq[k]) >> a.shift;
+        const bool next = k > 0 && !s.bad[k] && !s.bad[k - 1] && s.row0[k] == s.row0[k - 1] + s.nq[k - 1];
+        l = next ? s.lcp[k] : -1;                                       // -1: cannot follow its neighbour
+      }
+      unsigned flags = 0;
+      const int count = min(32, n_act - k0);
+      for (int pos = 0; pos < count;) {
+        const unsigned stop = __ballot_sync(0xffffffffu, k < n_act && (l < c || c == 0 || m == 0)) & (0xffffffffu << pos);
+        const int at = stop ? __ffs(stop) - 1 : count;                  // up to here all share at least the c pages
+        m += at - pos;
+        if (at == count) break;
+        // joining spares the newcomer the reading of c2 common pages and costs the others the reading of c - c2 pages each
+        const int c2 = min(c, __shfl_sync(0xffffffffu, l, at)), v = __shfl_sync(0xffffffffu, vis, at);
+        if (m > 0 && c2 > 0 && (long long)c2 > (long long)(c - c2) * (m - 1)) { c = c2; ++m; }
+        else {
+          if (lane == 0 && m > 0) { s.c[lead] = c; s.m[lead] = m; s.last[lead] = k0 + at - 1; }
+          lead = k0 + at; m = 1; c = v;
+          flags |= 1u << at;
+        }
+        pos = at + 1;
+      }
+      if (lane == 0) s.leads[k0 >> 5] = flags;
+    }
+    if (lane == 0 && m > 0) { s.c[lead] = c; s.m[lead] = m; s.last[lead] = n_act - 1; }
   }
   __syncthreads();
   // ---- segments: thread k makes the prefix of a group that k leads, and k's own rows
+  const bool mine = tid < n_act, bad = mine && s.bad[tid];
   long long u_pre = 0, u_suf = 0;
-  int r_pre = 0, r_suf = 0, pre = 0, lead = 0, c_pre = NARROW, t_pre = 0, t_suf = 0, kb_pre = 0, kb_suf = 0;
+  int r_pre = 0, r_suf = 0, pre = 0, lead = tid, c_pre = NARROW, t_pre = 0, t_suf = 0, kb_pre = 0, kb_suf = 0;
+  if (bad) a.status[s.i[tid]] = VLAC_ERR_BAD_STATE;
   if (mine && !bad) {
-    lead = s_lead[tid];
-    const int r_all = (s_end[lead] - s_row0[lead]) * a.ratio;
+    int w = tid >> 5;
+    unsigned f = s.leads[w] & (0xffffffffu >> (31 - lane));
+    while (!f) f = s.leads[--w];                                        // (sequence 0 leads)
+    lead = w * 32 + 31 - __clz(f);
+    const int last = s.last[lead], r_all = (s.row0[last] + s.nq[last] - s.row0[lead]) * a.ratio;
     // a sequence alone: its pages in front of many query rows are worth a segment of their own (no mask, wide tiles)
-    if (s_m[lead] >= 2 || r_all > pf_bm(NARROW)) pre = s_c[lead] << a.shift;
+    if (s.m[lead] >= 2 || r_all > pf_bm(NARROW)) pre = s.c[lead] << a.shift;
     if (lead == tid && pre > 0) {
       r_pre = r_all;
       c_pre = r_pre > pf_bm(NARROW) ? WIDE : NARROW;
       t_pre = (r_pre + pf_bm(c_pre) - 1) / pf_bm(c_pre); kb_pre = (pre + pf_kb(c_pre) - 1) / pf_kb(c_pre);
       u_pre = (long long)a.kv_heads * t_pre * kb_pre;
     }
-    if (s_len[tid] > pre) {
-      r_suf = s_nq[tid] * a.ratio;
-      t_suf = (r_suf + pf_bm(NARROW) - 1) / pf_bm(NARROW); kb_suf = (s_len[tid] - pre + pf_kb(NARROW) - 1) / pf_kb(NARROW);
+    if (s.len[tid] > pre) {
+      r_suf = s.nq[tid] * a.ratio;
+      t_suf = (r_suf + pf_bm(NARROW) - 1) / pf_bm(NARROW); kb_suf = (s.len[tid] - pre + pf_kb(NARROW) - 1) / pf_kb(NARROW);
       u_suf = (long long)a.kv_heads * t_suf * kb_suf;
     }
   }
   const bool wide = c_pre == WIDE && u_pre > 0;
-  const long long u_n = (wide ? 0 : u_pre) + u_suf, b_n = (long long)((wide ? 0 : r_pre) + r_suf) * a.kv_heads;
-  long long units[2], slots_n, slots_w, segs;
-  const long long u0_n = plan_scan(u_n, &units[NARROW]), u0_w = plan_scan(wide ? u_pre : 0, &units[WIDE]);
-  const long long b0_n = plan_scan(b_n, &slots_n), b0_w = plan_scan(wide ? (long long)pf_rows(WIDE, r_pre) * a.kv_heads : 0, &slots_w);
-  const int g0 = (int)plan_scan((u_pre > 0) + (u_suf > 0), &segs);
-  s_c[tid] = g0;                                                        // (s_c was read above, before the scans' barriers)
+  const Sums own = {{(wide ? 0 : u_pre) + u_suf, wide ? u_pre : 0},
+                    {((wide ? 0 : r_pre) + r_suf) * a.kv_heads, wide ? pf_rows(WIDE, r_pre) * a.kv_heads : 0}, (u_pre > 0) + (u_suf > 0)};
+  Sums all;
+  const Sums at = plan_scan(s.part, own, n_act, &all);
+  const int g0 = at.g;
+  if (mine) { s.g[tid] = g0; s.u0[NARROW][tid] = at.u[0]; s.u0[WIDE][tid] = at.u[1]; }
+  if (tid == 0) { PlanHead h = {{all.u[0], all.u[1]}, n_act, 0}; *p.head = h; }
   __syncthreads();
   if (mine) {
-    SeqRec q = {s_slot[tid], s_row0[tid], s_nq[tid], s_len[tid], pre > 0 ? s_c[lead] : -1, u_suf > 0 ? g0 + (u_pre > 0) : -1, 0, 0};
+    SeqRec q = {bad ? -1 : s.slot[tid], s.row0[tid], s.nq[tid], s.len[tid], pre > 0 ? s.g[lead] : -1, u_suf > 0 ? g0 + (u_pre > 0) : -1, 0, 0};
     p.seq[tid] = q;
-    auto put = [&](int g, int cls, long long us, long long n, int R, int k0, int k1, int pos0, int T, int KB, long long base) {
-      SegRec s = {us, us + n, s_slot[tid], s_row0[tid], R, k0, k1, pos0, cls, T, KB, (int)base};
-      p.seg[g] = s;
-      const long long U = units[cls], G = runs(cls, U);
-      for (long long c = (us * G + U - 1) / U, e = ((us + n) * G + U - 1) / U; c < e; ++c) p.first[cls][c] = g;
-    };
-    // slots: the narrow pieces' rows, then the wide ones' (each run sets itself off by a tile, see slot_row)
-    const long long at_w = (slots_n + 7) / 8 * 8 + (long long)pf_runs(NARROW) * pf_bm(NARROW);
-    if (u_pre > 0) put(g0, c_pre, wide ? u0_w : u0_n, u_pre, r_pre, 0, pre, INT_MIN, t_pre, kb_pre, wide ? at_w + b0_w : b0_n);
-    if (u_suf > 0)
-      put(g0 + (u_pre > 0), NARROW, u0_n + (wide ? 0 : u_pre), u_suf, r_suf, pre, s_len[tid], s_len[tid] - s_nq[tid], t_suf, kb_suf,
-          b0_n + (wide ? 0 : (long long)r_pre * a.kv_heads));
+    // slots: the narrow pieces' rows, then the wide ones' (each run sets itself off by a tile, see next_piece)
+    const long long at_w = (all.r[0] + 7) / 8 * 8 + (long long)pf_runs(NARROW) * pf_bm(NARROW);
+    if (u_pre > 0) {
+      const long long us = wide ? at.u[1] : at.u[0];
+      SegRec r = {us, us + u_pre, s.slot[tid], s.row0[tid], r_pre, 0, pre, INT_MIN, c_pre, t_pre, kb_pre, (int)(wide ? at_w + at.r[1] : at.r[0])};
+      p.seg[g0] = r;
+    }
+    if (u_suf > 0) {
+      const long long us = at.u[0] + (wide ? 0 : u_pre);
+      SegRec r = {us, us + u_suf, s.slot[tid], s.row0[tid], r_suf, pre, s.len[tid], s.len[tid] - s.nq[tid], NARROW, t_suf, kb_suf,
+                  (int)(at.r[0] + (wide ? 0 : (long long)r_pre * a.kv_heads))};
+      p.seg[g0 + (u_pre > 0)] = r;
+    }
   }
-  if (tid == 0) { PlanHead h = {{units[0], units[1]}, n_act, 0}; *p.head = h; }
+  // ---- the segment of each run's first unit: the last sequence whose units begin at or before it (its kernel walks on from there)
+#pragma unroll
+  for (int cls = 0; cls < 2; ++cls) {
+    const long long U = all.u[cls];
+    const int G = (int)runs(cls, U);
+    for (int c = tid; c < G; c += blockDim.x) {
+      const long long u = U < 1 << 20 ? (long long)((unsigned)c * (unsigned)U / (unsigned)G) : c * U / G;     // (a 64-bit division is five times as long)
+      int lo = 0, hi = n_act - 1;
+      while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (s.u0[cls][m] <= u) lo = m; else hi = m - 1; }
+      p.first[cls][c] = s.g[lo];
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ both kernels
@@ -550,15 +615,17 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
 }
 
 // ------------------------------------------------------------------------------------------------ wide: tcgen05
-// One persistent CTA per SM walks its run of (K/V head, tile of 128 stacked rows, block of 128 keys) units:
-//   warp 0        TMA: K and V blocks, one box per (page, 64 elements) into one ring of tiles in the order the products take them
-//   warp 1        one thread issues S_i = Q K_i^T (M 128, N 128) and O_b += P_i V_i (b = i mod 2), A = P from tensor memory
-//   warps 4-7 and 8-11   softmax of the even and of the odd key blocks, a thread per row: each side keeps its own m, l and O, as if
-//                 the keys were split in two, so that neither waits for the other; the sides are added when the piece ends.
-// S_i is followed by S_{i+1} before O += P_i V_i, so the tensor cores work on one block while the other is in the softmax.
-// Every row sees every key of a common prefix: no mask but behind its last key, where zeros are loaded.
-// Bound: the 16384 exponentials of a block (16 a cycle and SM: 1024 cycles, as long as its products at the dense peak) where the rows fill
-// the tile, HBM (64 KB of K and V a block) where they do not.
+// One persistent CTA per SM walks its run of (K/V head, tile of 256 stacked rows, block of 128 keys) units:
+//   warps 0, 2, 3  TMA: K and V blocks, one box per (page, 64 elements) into one ring of tiles in the order the products take them
+//   warp 1         issues S = Q K^T (M 128, N 128) and O += P V, A = P from tensor memory
+//   warps 4-7 and 8-11   softmax, a thread per row, in two sides with an S/P buffer and an O of their own:
+//                  more than 128 rows (two): side b has rows 128 b .. and every key block; a K/V tile in shared memory serves both
+//                  up to 128 rows: side b has all rows and every second key block, as if the keys were split in two; the sides' sums are
+//                  added when the piece ends
+// Either way the tensor cores work for one side while the other is in the softmax.  Every row sees every key of a common prefix: no mask
+// but behind its last key, where zeros are loaded.
+// Bound: the 16384 exponentials of 128 rows and keys (16 a cycle and SM: 1024 cycles, as long as their products at the dense peak) where the
+// rows fill the tile, HBM (64 KB of K and V a block) where they do not.
 constexpr int PW_THREADS = 384;
 constexpr int PW_SOFT = 256;                    // threads of the two softmax sides
 constexpr unsigned long long PW_WAIT_LIMIT_NS = 400000000ull;
@@ -566,8 +633,8 @@ template <int D> struct Wide {
   static constexpr int HALVES = D / 64;
   static constexpr int HALF = 128 * 128;        // 64 elements of 128 rows
   static constexpr int TILE = HALVES * HALF;
-  static constexpr int SLOTS = D == 128 ? 6 : 10;
-  static constexpr int SMEM = 1024 + TILE * (1 + SLOTS);
+  static constexpr int SLOTS = D == 128 ? 5 : 10;
+  static constexpr int SMEM = 1024 + TILE * (2 + SLOTS);                // two tiles of Q, then the ring of K and V tiles
 };
 
 __device__ __forceinline__ void pw_bar_init(unsigned long long* bar, unsigned count) {
@@ -720,7 +787,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   int* const error = &pm.head->error;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, run = blockIdx.x;
   unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pw_raw) + 1023) & ~(uintptr_t)1023);
-  const unsigned q_s = pf_smem(smem), ring = q_s + W::TILE;
+  const unsigned q_s = pf_smem(smem), ring = q_s + 2 * W::TILE;
   float* const red_m = reinterpret_cast<float*>(smem);                  // [2][128] each, over Q when its products are done
   float* const red_l = red_m + 256;
   if (tid == 0) {
@@ -777,14 +844,16 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
         const int pg = tab[key >> a.shift];
         return (unsigned)pg < (unsigned)a.n_pages ? (pg << a.shift) + (key & (a.page - 1)) : none;
       };
+      const bool two = p.nr > 128;
       int y = row(0), yp = 0;
       for (int i = 0; i < p.n && ok; ++i) {
         const int yn = i + 1 < p.n ? row(i + 1) : none;                 // fetched a block ahead of its use
         put(&tm_k, y, p.head * D);
-        if (i > 0 && ok) put(&tm_v, yp, p.head * D);
+        if (two) { if (ok) put(&tm_v, y, p.head * D); }
+        else if (i > 0 && ok) put(&tm_v, yp, p.head * D);
         yp = y; y = yn;
       }
-      if (ok) put(&tm_v, yp, p.head * D);
+      if (ok && !two) put(&tm_v, yp, p.head * D);
     }
     if (!ok)                                                            // given up: let what is in flight land
       for (int c = max(0, cnt - W::SLOTS); c < cnt; ++c) pw_wait(&full[c % W::SLOTS], (c / W::SLOTS) & 1, &abort_flag, error);
@@ -805,55 +874,73 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       if (!pw_try_at(bar, parity)) failed |= !pw_wait_slow(bar, parity, &abort_flag, error);
     };
     auto still_ok = [&]() { return __all_sync(0xffffffffu, !failed); };
-    auto next = [&]() { pw_commit(&empty[slot], one); if (++slot == W::SLOTS) { slot = 0; phase ^= 1; } };
     auto same = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };    // tells the compiler that a value is the same in all lanes
-    auto there = [&](int ahead) {                                       // the ring's tile `ahead` places on
-      const int sl = slot + ahead, wrap = sl >= W::SLOTS;
-      wait_at(full_a + 8u * (sl - (wrap ? W::SLOTS : 0)), phase ^ wrap);
-    };
-    auto s_mma = [&](int i) {                                           // S_i from the next tile
-      const int b = same(i & 1);
-      const unsigned long long d = k_d + (unsigned long long)(same(slot) * (W::TILE >> 4));
+    auto place = [&](int ahead) { const int sl = slot + ahead; return sl >= W::SLOTS ? sl - W::SLOTS : sl; };
+    auto there = [&](int ahead) { wait_at(full_a + 8u * place(ahead), phase ^ (slot + ahead >= W::SLOTS)); };   // the ring's tile `ahead` places on
+    auto next = [&]() { pw_commit(&empty[slot], one); if (++slot == W::SLOTS) { slot = 0; phase ^= 1; } };       // its first tile is done with
+    auto s_mma = [&](int b, int q_tile, int sl) {                       // S of side b from the tile of Q and the K tile in slot sl
+      const int bu = same(b);
+      const unsigned long long d = k_d + (unsigned long long)(same(sl) * (W::TILE >> 4)), qd = q_d + (unsigned long long)(same(q_tile) * (W::TILE >> 4));
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         const unsigned off = ((unsigned)(ks >> 2) * W::HALF + (unsigned)(ks & 3) * 32u) >> 4;
-        pw_mma_ss(tm + 128u * b, q_d + off, d + off, id_s, ks > 0, one);
+        pw_mma_ss(tm + 128u * bu, qd + off, d + off, id_s, ks > 0, one);
       }
       pw_commit(&s_full[b], one);
-      next();
     };
-    // Tiles come in the order K_0, K_1, V_0, K_2, V_1, ..., V_{n-1}.  The weights come last, so everything else is waited for before them:
-    // O += P_i V_i and S_{i+2}, which takes the columns that P_i leaves, then go out in one burst.
+    auto pv_mma = [&](int b, int sl, bool add) {                        // O of side b; the weights' halves arrive one after the other
+      const int bu = same(b);
+      const unsigned acc = same(add), par = n_p[b]++ & 1;
+      const unsigned long long d = v_d + (unsigned long long)(same(sl) * (W::TILE >> 4));
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        wait_at(p_a + 16u * b + 8u * hf, par);
+        pw_after();
+#pragma unroll
+        for (int j = 4 * hf; j < 4 * hf + 4; ++j)                       // 16 keys: 8 columns of packed P; 16 rows of V (MN-major)
+          pw_mma_ts(tm + 256u + 128u * bu, tm + 128u * bu + 8u * j, d + 128u * j, id_o, acc || j > 0, one);
+      }
+    };
+    // The weights come last, so everything else is waited for before them: O += P V and the side's next S, which takes the columns that P
+    // leaves, then go out in one burst.
     while (u < u_end && ok) {
       u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
-      const int n = same(p.n);
+      const int n = same(p.n), two = same(p.nr > 128);
       there(0);
-      if (n > 1) there(1);
       wait_at(pf_smem(&q_full), pieces & 1);
       ok = still_ok();
       if (!ok) break;
       pw_after();
-      s_mma(0);
-      if (n > 1) s_mma(1);
-      for (int i = 0; i < n; ++i) {
-        const int b = same(i & 1);
-        const unsigned acc = same(i > 1), par = same(n_p[b] & 1);
-        there(0);
-        if (i + 2 < n) there(1);
-        const unsigned long long d = v_d + (unsigned long long)(same(slot) * (W::TILE >> 4));
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {                                // the weights' halves arrive one after the other
-          wait_at(p_a + 16u * b + 8u * hf, par);
-          pw_after();
-#pragma unroll
-          for (int j = 4 * hf; j < 4 * hf + 4; ++j)                     // 16 keys: 8 columns of packed P; 16 rows of V (MN-major)
-            pw_mma_ts(tm + 256u + 128u * b, tm + 128u * b + 8u * j, d + 128u * j, id_o, acc || j > 0, one);
-        }
-        ++n_p[b];
+      s_mma(0, 0, slot);
+      if (two) {                                                        // tiles K_0, V_0, K_1, V_1, ...
+        s_mma(1, 1, slot);
         next();
-        if (i + 2 < n) s_mma(i + 2);
-        ok = still_ok();
-        if (!ok) break;
+        for (int i = 0; i < n; ++i) {
+          const bool more = i + 1 < n;
+          there(0);
+          if (more) there(1);
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            pv_mma(b, slot, i > 0);
+            if (more) s_mma(b, b, place(1));
+          }
+          next();
+          if (more) next();
+          ok = still_ok();
+          if (!ok) break;
+        }
+      } else {                                                          // tiles K_0, K_1, V_0, K_2, V_1, ..., V_{n-1}
+        next();
+        if (n > 1) { there(0); s_mma(1, 0, slot); next(); }
+        for (int i = 0; i < n; ++i) {
+          there(0);
+          if (i + 2 < n) there(1);
+          pv_mma(i & 1, slot, i > 1);
+          next();
+          if (i + 2 < n) { s_mma(i & 1, 0, slot); next(); }
+          ok = still_ok();
+          if (!ok) break;
+        }
       }
       if (ok) pw_commit(&o_full, one);
       ++pieces;
@@ -868,15 +955,18 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     bool ok = true;
     // Q of a piece: all loads first (a store between them would make each wait for the one before), and for the next piece before the
     // present one is written out
-    constexpr int C16 = D / 8, NQ = 128 * C16 / PW_SOFT;
+    constexpr int C16 = D / 8, NQ = 128 * C16 / 128;
     uint4 qv[NQ];
+    // 16-byte pieces of Q: with two tiles each side copies its own (NQ a thread), otherwise both share one (NQ / 2)
     auto load_q = [&](const Piece& p) {
       // stacked row x is q row row0 + x / ratio, query head head * ratio + x % ratio; rows behind the last are zeros
-      const int x0 = p.rt * 128, q0 = x0 / a.ratio, h0 = x0 - q0 * a.ratio;
+      const bool two = p.nr > 128;
+      const int x0 = p.rt * 256, q0 = x0 / a.ratio, h0 = x0 - q0 * a.ratio, c0 = two ? side * 128 * C16 + (st & 127) : st, dc = two ? 128 : 256;
       const T* src = (const T*)a.q + (size_t)(p.row0 + q0) * a.q_stride + (size_t)p.head * a.ratio * D;
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
-        const int c = st + i * PW_SOFT, qr = c / C16, c16 = c % C16, x = h0 + qr, xq = x / a.ratio;
+        if (i >= NQ / 2 && !two) break;
+        const int c = c0 + i * dc, qr = c / C16, c16 = c % C16, x = h0 + qr, xq = x / a.ratio;
         qv[i] = make_uint4(0, 0, 0, 0);
         if (qr < p.nr) qv[i] = *reinterpret_cast<const uint4*>(src + (size_t)xq * a.q_stride + (x - xq * a.ratio) * D + c16 * 8);
       }
@@ -884,18 +974,23 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
     load_q(p);
     while (true) {
+      const bool two = p.nr > 128;
+      const int c0 = two ? side * 128 * C16 + (st & 127) : st, dc = two ? 128 : 256;
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
-        const int c = st + i * PW_SOFT, qr = c / C16, c16 = c % C16;
+        if (i >= NQ / 2 && !two) break;
+        const int c = c0 + i * dc, qr = c / C16, c16 = c % C16;
         if (w.flip) { qv[i].x ^= 0x80008000u; qv[i].y ^= 0x80008000u; qv[i].z ^= 0x80008000u; qv[i].w ^= 0x80008000u; }
-        *reinterpret_cast<uint4*>(smem + (c16 >> 3) * W::HALF + pf_swz(qr, c16 & 7)) = qv[i];
+        *reinterpret_cast<uint4*>(smem + (qr >> 7) * W::TILE + (c16 >> 3) * W::HALF + pf_swz(qr & 127, c16 & 7)) = qv[i];
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       pw_before();
       pw_arrive(&q_full);
       float m = -INFINITY, l = 0.f;
-      const bool idle = 32 * q4 >= p.nr;                                // a warp without rows: only its arrivals are needed
-      for (int i = side; i < p.n; i += 2) {
+      const int row_t = (two ? 128 * side : 0) + r;                     // the thread's row in the tile
+      const bool idle = row_t - lane >= p.nr;                           // a warp without rows: only its arrivals are needed
+      const int step = two ? 1 : 2, first = two ? 0 : side;
+      for (int i = first; i < p.n; i += step) {
         ok = __all_sync(0xffffffffu, pw_wait(&s_full[side], n_s++ & 1, &abort_flag, error));
         if (!ok) break;
         if (!idle) {
@@ -925,7 +1020,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
             const float al = mn == -INFINITY ? 1.f : pf_ex2(m - mn);    // (m = -inf: nothing summed yet, 0 * 0)
             m = mn;
             l *= al;
-            if (i >= 2) {
+            if (i >= step) {
 #pragma unroll 1
               for (int c = 0; c < D / 32; ++c) {
                 unsigned x[32];
@@ -979,34 +1074,52 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       ++pieces;
       ok = pw_all_ok(ok);                                               // every product of the piece is done: Q's memory is free
       if (!ok) break;
-      red_m[side * 128 + r] = m; red_l[side * 128 + r] = l;
-      pw_all_ok(true);
+      if (!two) {
+        red_m[side * 128 + r] = m; red_l[side * 128 + r] = l;
+        pw_all_ok(true);
+      }
       pw_after();
       if (!idle) {
-        // the two sides of a row, each thread half of its columns
-        const float m0 = red_m[r], m1 = red_m[128 + r], M = fmaxf(m0, m1), ref = M == -INFINITY ? 0.f : M;
-        const float f0 = pf_ex2(m0 - ref), f1 = pf_ex2(m1 - ref);
-        const bool two = p.n > 1;                                       // one block: the odd side holds nothing
-        float* dst = pm.po + wide_at(p.slot0 + r, side * (D / 8), D);
+        if (two) {
+          // every side its own rows
+          float* dst = pm.po + wide_at(p.slot0 + row_t, 0, D);
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            unsigned x[32];
+            pw_ld32(o_col + 32u * c, x);
+            pw_ld_wait(x);
+            if (row_t < p.nr) {
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          unsigned x[32], y[32] = {};
-          pw_ld32(trow + 256u + side * (D / 2) + 32u * c, x);
-          if (two) pw_ld32(trow + 384u + side * (D / 2) + 32u * c, y);
-          pw_ld_wait(x, y);
-          if (r < p.nr) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              float4 o;
-              o.x = f0 * __uint_as_float(x[e]); o.y = f0 * __uint_as_float(x[e + 1]); o.z = f0 * __uint_as_float(x[e + 2]); o.w = f0 * __uint_as_float(x[e + 3]);
-              if (two) {
-                o.x += f1 * __uint_as_float(y[e]); o.y += f1 * __uint_as_float(y[e + 1]); o.z += f1 * __uint_as_float(y[e + 2]); o.w += f1 * __uint_as_float(y[e + 3]);
-              }
-              *reinterpret_cast<float4*>(dst + (8 * c + (e >> 2)) * 32) = o;
+              for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(dst + (8 * c + (e >> 2)) * 32) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
             }
           }
+          if (row_t < p.nr) pm.ml[p.slot0 + row_t] = make_float2(m, l);
+        } else {
+          // the two sides of a row, each thread half of its columns
+          const float m0 = red_m[r], m1 = red_m[128 + r], M = fmaxf(m0, m1), ref = M == -INFINITY ? 0.f : M;
+          const float f0 = pf_ex2(m0 - ref), f1 = pf_ex2(m1 - ref);
+          const bool odd = p.n > 1;                                     // one block: the odd side holds nothing
+          float* dst = pm.po + wide_at(p.slot0 + r, side * (D / 8), D);
+#pragma unroll 1
+          for (int c = 0; c < D / 64; ++c) {
+            unsigned x[32], y[32] = {};
+            pw_ld32(trow + 256u + side * (D / 2) + 32u * c, x);
+            if (odd) pw_ld32(trow + 384u + side * (D / 2) + 32u * c, y);
+            pw_ld_wait(x, y);
+            if (r < p.nr) {
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                float4 o;
+                o.x = f0 * __uint_as_float(x[e]); o.y = f0 * __uint_as_float(x[e + 1]); o.z = f0 * __uint_as_float(x[e + 2]); o.w = f0 * __uint_as_float(x[e + 3]);
+                if (odd) {
+                  o.x += f1 * __uint_as_float(y[e]); o.y += f1 * __uint_as_float(y[e + 1]); o.z += f1 * __uint_as_float(y[e + 2]); o.w += f1 * __uint_as_float(y[e + 3]);
+                }
+                *reinterpret_cast<float4*>(dst + (8 * c + (e >> 2)) * 32) = o;
+              }
+            }
+          }
+          if (side == 0 && r < p.nr) pm.ml[p.slot0 + r] = make_float2(M, f0 * red_l[r] + (odd ? f1 * red_l[128 + r] : 0.f));
         }
-        if (side == 0 && r < p.nr) pm.ml[p.slot0 + r] = make_float2(M, f0 * red_l[r] + (two ? f1 * red_l[128 + r] : 0.f));
       }
       if (!more) break;
       pw_all_ok(true);                                                  // red_m, red_l may be written again
@@ -1035,6 +1148,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
   const int k = p.row_k[row];
   if (k < 0) return;
   const SeqRec q = p.seq[k];
+  if (q.slot < 0) return;                                               // refused
   int np[2] = {0, 0}, pad[2] = {0, 0}, wide = 0;
   size_t base[2] = {0, 0};
   const PlanHead hd = *p.head;
@@ -1135,7 +1249,14 @@ int vlac_prefix_plan(const vlac_pages* p, const vlac_prefix* plan, const int* se
   a.table = p->table; a.len = p->len; a.n_slots = p->n_slots; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size;
   a.shift = pages_shift(p->page_size); a.kv_heads = p->n_kv_heads; a.ratio = plan->n_heads / p->n_kv_heads; a.head_dim = p->head_dim;
   a.n = plan->n; a.rows = plan->rows; a.n_heads = plan->n_heads; a.seqs = seqs; a.q_ptr = q_ptr; a.status = status; a.mem = plan->mem;
-  VLAC_CUDA_CHECK(launch_pdl(prefix_plan_kernel, dim3(PL_CTAS), dim3(PL_THREADS), 0, (cudaStream_t)stream, a));
+  const size_t smem = sizeof(PlanShared);
+  if (plan->n <= 16 && (long long)plan->n * p->max_pages <= PL_ONE) {
+    VLAC_CUDA_CHECK(cudaFuncSetAttribute(prefix_plan_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    VLAC_CUDA_CHECK(launch_pdl(prefix_plan_kernel<1>, dim3(1), dim3(256), smem, (cudaStream_t)stream, a));
+  } else {
+    VLAC_CUDA_CHECK(cudaFuncSetAttribute(prefix_plan_kernel<PL_CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    VLAC_CUDA_CHECK(launch_pdl(prefix_plan_kernel<PL_CTAS>, dim3(PL_CTAS), dim3(1024), smem, (cudaStream_t)stream, a));
+  }
   return VLAC_OK;
 }
 
