@@ -401,7 +401,7 @@ class Pages:
             assert t.device == k.device and t.dtype == torch.int32 and t.dim() == dims and t.is_contiguous()
         assert len.shape[0] == table.shape[0] and refs.shape[0] == k.shape[1]
         self.k, self.v, self.table, self.len, self.refs = k, v, table, len, refs
-        self.device, self.dtype = k.device, k.dtype
+        self.index, self.dtype = k.get_device(), k.dtype
         self.struct = vlac_pages(k.data_ptr(), v.data_ptr(), 0 if k.dtype == torch.bfloat16 else 1, *k.shape, *table.shape,
                                  table.data_ptr(), len.data_ptr(), refs.data_ptr(), None, 0)
         self.ref = C.byref(self.struct)
@@ -425,19 +425,20 @@ class PrefixPlan:
         size = lib.vlac_prefix_bytes(pages.ref, n, rows, n_heads)
         if size == 0 and n > 0 and rows > 0:
             raise VlacError(-1, "vlac_prefix_bytes")
-        self.n, self.rows, self.n_heads, self.device = n, rows, n_heads, pages.device
-        self.mem = torch.empty((max(size, 16),), dtype=torch.uint8, device=pages.device)
+        self.n, self.rows, self.n_heads, self.index = n, rows, n_heads, pages.index
+        self.mem = torch.empty((max(size, 16),), dtype=torch.uint8, device=pages.k.device)
         self.struct = vlac_prefix(n, rows, n_heads, self.mem.data_ptr(), size)
         self.ref = C.byref(self.struct)
 
 
-def _here(device: torch.device) -> None:
-    """The library launches on the current device: tensors of another one would be read through the wrong context."""
-    assert device.index == torch.cuda.current_device(), f"tensors on {device}, current device {torch.cuda.current_device()}"
+def _here(index: int) -> int:
+    """The current stream; the library launches on the current device, so tensors of another one are refused."""
+    assert index == torch.cuda.current_device(), f"tensors on cuda:{index}, current device {torch.cuda.current_device()}"
+    return torch._C._cuda_getCurrentRawStream(index)            # (a call a token and layer: current_stream() costs 1.5 us)
 
 
-def _ints(t: torch.Tensor, n: int, device: torch.device) -> int:
-    assert t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and t.device == device and t.is_contiguous()
+def _ints(t: torch.Tensor, n: int, index: int) -> int:
+    assert t.dtype is torch.int32 and t.get_device() == index and t.dim() == 1 and t.size(0) == n and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -447,62 +448,60 @@ def vlac_pages_work_bytes(struct: vlac_pages) -> int:
 
 def vlac_pages_resize(pages: Pages, seqs: torch.Tensor, lens: torch.Tensor, status: torch.Tensor) -> None:
     """Slot ``seqs[i]`` gets length ``lens[i]``; ``status`` (int32, as long as the list) receives a code per entry."""
-    n, dev = seqs.shape[0], pages.device
-    _here(dev)
-    _check(lib.vlac_pages_resize(pages.ref, _ints(seqs, n, dev), _ints(lens, n, dev), n, _ints(status, n, dev), _stream()), "vlac_pages_resize")
+    n, dev = seqs.size(0), pages.index
+    stream = _here(dev)
+    _check(lib.vlac_pages_resize(pages.ref, _ints(seqs, n, dev), _ints(lens, n, dev), n, _ints(status, n, dev), stream), "vlac_pages_resize")
 
 
 def vlac_pages_free(pages: Pages, seqs: torch.Tensor, status: torch.Tensor) -> None:
-    n, dev = seqs.shape[0], pages.device
-    _here(dev)
-    _check(lib.vlac_pages_free(pages.ref, _ints(seqs, n, dev), n, _ints(status, n, dev), _stream()), "vlac_pages_free")
+    n, dev = seqs.size(0), pages.index
+    stream = _here(dev)
+    _check(lib.vlac_pages_free(pages.ref, _ints(seqs, n, dev), n, _ints(status, n, dev), stream), "vlac_pages_free")
 
 
 def vlac_pages_fork(pages: Pages, src: torch.Tensor, dst: torch.Tensor, deep: bool, status: torch.Tensor) -> None:
     """Slot ``dst[i]`` becomes a copy of slot ``src[i]``: full pages shared, or (``deep``) every row copied."""
-    n, dev = src.shape[0], pages.device
-    _here(dev)
-    _check(lib.vlac_pages_fork(pages.ref, _ints(src, n, dev), _ints(dst, n, dev), n, int(bool(deep)), _ints(status, n, dev), _stream()),
-           "vlac_pages_fork")
+    n, dev = src.size(0), pages.index
+    stream = _here(dev)
+    _check(lib.vlac_pages_fork(pages.ref, _ints(src, n, dev), _ints(dst, n, dev), n, 1 if deep else 0, _ints(status, n, dev), stream), "vlac_pages_fork")
 
 
 def vlac_pages_compact(pages: Pages, src: torch.Tensor, dst: torch.Tensor, keep_ptr: torch.Tensor, keep: torch.Tensor,
                        status: torch.Tensor) -> None:
     """Slot ``dst[i]`` becomes the rows ``keep[keep_ptr[i]:keep_ptr[i + 1]]`` (ascending positions) of slot ``src[i]``."""
-    n, dev = src.shape[0], pages.device
-    _here(dev)
-    _check(lib.vlac_pages_compact(pages.ref, _ints(src, n, dev), _ints(dst, n, dev), n, _ints(keep_ptr, n + 1, dev),
-                                  _ints(keep, keep.shape[0], dev), keep.shape[0], _ints(status, n, dev), _stream()), "vlac_pages_compact")
+    n, dev, n_keep = src.size(0), pages.index, keep.size(0)
+    stream = _here(dev)
+    _check(lib.vlac_pages_compact(pages.ref, _ints(src, n, dev), _ints(dst, n, dev), n, _ints(keep_ptr, n + 1, dev), _ints(keep, n_keep, dev), n_keep,
+                                  _ints(status, n, dev), stream), "vlac_pages_compact")
 
 
-def _rows(t: torch.Tensor, heads: int, pages: Pages, rows: int) -> None:
-    """[rows, heads, head_dim] of the pool's type, heads side by side, any row stride."""
+def _rows(t: torch.Tensor, heads: int, pages: Pages, rows: int) -> int:
+    """Pointer of [rows, heads, head_dim] of the pool's type, heads side by side, any row stride."""
     d = pages.struct.head_dim
-    assert t.device == pages.device and t.dtype == pages.dtype and t.dim() == 3 and t.shape[0] == rows and t.shape[1] == heads and t.shape[2] == d
-    assert rows == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d))
+    assert t.dtype is pages.dtype and t.get_device() == pages.index and t.dim() == 3 and t.size(0) == rows and t.size(1) == heads and t.size(2) == d
+    assert t.is_contiguous() or rows == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d))
+    return t.data_ptr()
 
 
 def _row_stride(t: torch.Tensor) -> int:
     """Elements between rows (a tensor of one row or none may carry any stride)."""
-    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] * t.shape[2] // 8) * 8
+    return t.stride(0) if t.size(0) > 1 else -(-t.size(1) * t.size(2) // 8) * 8
 
 
 def vlac_pages_write(pages: Pages, layer: int, seqs: torch.Tensor, start: Optional[torch.Tensor], row_ptr: torch.Tensor,
                      k_rows: torch.Tensor, v_rows: torch.Tensor, status: torch.Tensor) -> None:
     """Rows ``row_ptr[i]:row_ptr[i + 1]`` of ``k_rows`` / ``v_rows`` to slot ``seqs[i]`` from position ``start[i]`` on (``None``: its last rows)."""
-    n, dev, rows = seqs.shape[0], pages.device, k_rows.shape[0]
-    _here(dev)
-    _rows(k_rows, pages.struct.n_kv_heads, pages, rows)
-    _rows(v_rows, pages.struct.n_kv_heads, pages, rows)
-    _check(lib.vlac_pages_write(pages.ref, layer, _ints(seqs, n, dev), None if start is None else _ints(start, n, dev),
-                                _ints(row_ptr, n + 1, dev), n, rows, k_rows.data_ptr(), _row_stride(k_rows), v_rows.data_ptr(),
-                                _row_stride(v_rows), _ints(status, n, dev), _stream()), "vlac_pages_write")
+    n, dev, rows, heads = seqs.size(0), pages.index, k_rows.size(0), pages.struct.n_kv_heads
+    stream = _here(dev)
+    _check(lib.vlac_pages_write(pages.ref, layer, _ints(seqs, n, dev), None if start is None else _ints(start, n, dev), _ints(row_ptr, n + 1, dev), n, rows,
+                                _rows(k_rows, heads, pages, rows), _row_stride(k_rows), _rows(v_rows, heads, pages, rows), _row_stride(v_rows),
+                                _ints(status, n, dev), stream), "vlac_pages_write")
 
 
 def vlac_pages_from_cache(pages: Pages, cache: int, seq: int, slot: int, n_rows: int, status: torch.Tensor) -> None:
     """Positions ``0 .. n_rows - 1`` of sequence ``seq`` of a control-step cache into ``slot``, all layers."""
-    _here(pages.device)
-    _check(lib.vlac_pages_from_cache(pages.ref, cache, seq, slot, n_rows, _ints(status, 1, pages.device), _stream()), "vlac_pages_from_cache")
+    stream = _here(pages.index)
+    _check(lib.vlac_pages_from_cache(pages.ref, cache, seq, slot, n_rows, _ints(status, 1, pages.index), stream), "vlac_pages_from_cache")
 
 
 def vlac_prefix_bytes(pages: Pages, n: int, rows: int, n_heads: int) -> int:
@@ -511,28 +510,25 @@ def vlac_prefix_bytes(pages: Pages, n: int, rows: int, n_heads: int) -> int:
 
 def vlac_prefix_plan(pages: Pages, plan: PrefixPlan, seqs: torch.Tensor, q_ptr: torch.Tensor, status: torch.Tensor) -> None:
     """Find what neighbours of the list share and divide the work; serves every layer until tables, lengths or ``q_ptr`` change."""
-    dev = pages.device
-    assert plan.device == dev
-    _here(dev)
-    _check(lib.vlac_prefix_plan(pages.ref, plan.ref, _ints(seqs, plan.n, dev), _ints(q_ptr, plan.n + 1, dev), _ints(status, plan.n, dev),
-                                _stream()), "vlac_prefix_plan")
+    dev, n = pages.index, plan.n
+    stream = _here(dev)
+    assert plan.index == dev
+    _check(lib.vlac_prefix_plan(pages.ref, plan.ref, _ints(seqs, n, dev), _ints(q_ptr, n + 1, dev), _ints(status, n, dev), stream), "vlac_prefix_plan")
 
 
 def vlac_prefix_attention(pages: Pages, layer: int, plan: PrefixPlan, q: torch.Tensor, scale: float, out: torch.Tensor,
                           lse: Optional[torch.Tensor] = None) -> None:
     """Attention of the plan's rows: ``q``, ``out`` ``[rows, n_heads, head_dim]`` of the pool's type, ``lse`` fp32 ``[rows, n_heads]``."""
-    dev = pages.device
-    assert plan.device == dev
-    _here(dev)
-    _rows(q, plan.n_heads, pages, plan.rows)
-    _rows(out, plan.n_heads, pages, plan.rows)
-    assert lse is None or (lse.device == dev and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (plan.rows, plan.n_heads))
-    _check(lib.vlac_prefix_attention(pages.ref, layer, plan.ref, q.data_ptr(), _row_stride(q), scale, out.data_ptr(), _row_stride(out), _ptr(lse),
-                                     _stream()), "vlac_prefix_attention")
+    dev, rows, heads = pages.index, plan.rows, plan.n_heads
+    stream = _here(dev)
+    assert plan.index == dev
+    assert lse is None or (lse.dtype is torch.float32 and lse.get_device() == dev and lse.is_contiguous() and tuple(lse.shape) == (rows, heads))
+    _check(lib.vlac_prefix_attention(pages.ref, layer, plan.ref, _rows(q, heads, pages, rows), _row_stride(q), scale, _rows(out, heads, pages, rows),
+                                     _row_stride(out), _ptr(lse), stream), "vlac_prefix_attention")
 
 
 def vlac_prefix_error(plan: PrefixPlan) -> int:
-    return int(lib.vlac_prefix_error(plan.ref, _stream()))
+    return int(lib.vlac_prefix_error(plan.ref, _here(plan.index)))
 
 
 # --------------------------------------------------------------------------- reading views back

@@ -278,6 +278,192 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
   }
 }
 
+// The same for few entries with short tables, which a chain of cluster barriers and reads through L2 would only hold up: one CTA, everything
+// between its phases in shared memory, entries compared pair by pair, free pages searched from the lowest on until there are enough.
+constexpr int PO_THREADS = 512;
+constexpr int PO_LIST = 64;                     // entries
+constexpr int PO_ENTRIES = 8192;                // table or keep-list entries of all together
+constexpr int PO_POOL = 32768;                  // pages of the pool (2048 a look)
+constexpr int PO_PAGES = 2048;                  // new pages remembered in shared memory
+
+__global__ void __launch_bounds__(PO_THREADS, 1) pages_book_one_kernel(BookArgs a) {
+  __shared__ int s_dst[PO_LIST], s_src[PO_LIST], s_ls[PO_LIST], s_ld[PO_LIST], s_bad[PO_LIST], s_lead[PO_LIST], s_shared[PO_LIST], s_total[PO_LIST], s_start[PO_LIST];
+  __shared__ int s_new[PO_PAGES], s_warp[PO_THREADS / 32], s_need, s_taken;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const PagesWork w = pages_work(a.work, a.n_slots, a.n_pages);
+  pdl_trigger();
+  pdl_wait();
+  // ---- the lists
+  int d = -1, s = -1, k0 = 0, k1 = 0, rows = 0;
+  if (tid < a.n) {
+    d = slot_of(a.dst, tid, a.n_slots);
+    s = a.op == OP_RESIZE ? d : slot_of(a.src, tid, a.n_slots);
+    if (a.op == OP_COMPACT) { k0 = a.keep_ptr[tid]; k1 = a.keep_ptr[tid + 1]; }
+    if (a.op == OP_RESIZE) rows = a.lens ? a.lens[tid] : 0;
+    s_dst[tid] = d; s_src[tid] = s; s_bad[tid] = 0; s_lead[tid] = INT_MAX;
+  }
+  __syncthreads();
+  // ---- lengths; targets named before or read by another entry
+  int status = VLAC_OK, ls = 0, ld = 0;
+  if (tid < a.n) {
+    if (d < 0 || s < 0 || (a.op == OP_FORK && s == d)) status = VLAC_ERR_INVALID_ARG;
+    if (d >= 0 && s >= 0) {
+      ls = a.len[s]; ld = a.len[d];
+      for (int j = 0; j < a.n; ++j) {
+        if (j < tid && s_dst[j] == d) status = VLAC_ERR_INVALID_ARG;
+        if (a.op != OP_RESIZE && s_src[j] == d && !(a.op == OP_COMPACT && s_dst[j] == d)) status = VLAC_ERR_INVALID_ARG;
+      }
+      const int most = a.max_pages << a.shift;
+      if (status == VLAC_OK && (ls < 0 || ls > most || ld < 0 || ld > most)) status = VLAC_ERR_BAD_STATE;
+      if (status == VLAC_OK && (a.op == OP_COMPACT ? k0 < 0 || k1 < k0 || k1 > a.n_keep : rows < 0 || rows > most)) s_bad[tid] = 2;
+    }
+    s_ls[tid] = status == VLAC_OK ? ls : 0; s_ld[tid] = status == VLAC_OK ? ld : 0;          // (nothing is read for a refused entry)
+  }
+  __syncthreads();
+  // ---- tables in range, keep lists ascending: teams of warps, an entry each
+  int team = 1;
+  while (team < PO_THREADS / 32 && team * 2 * a.n <= PO_THREADS / 32) team *= 2;
+  const int n_teams = PO_THREADS / 32 / team, my_team = warp / team, step = team * 32, at0 = (warp % team) * 32 + lane;
+  for (int i = my_team; i < a.n; i += n_teams) {
+    const int e_d = s_dst[i], e_s = s_src[i], e_ls = s_ls[i];
+    const int ps = (e_ls + a.page - 1) >> a.shift, pd = e_d == e_s ? 0 : (s_ld[i] + a.page - 1) >> a.shift;
+    int bad = 0;
+    if (ps | pd) {
+      const int *ts = a.table + (size_t)e_s * a.max_pages, *td = a.table + (size_t)e_d * a.max_pages;
+#pragma unroll 4
+      for (int j = at0; j < max(ps, pd); j += step) {
+        if (j < ps) bad |= (unsigned)ts[j] >= (unsigned)a.n_pages;
+        if (j < pd) bad |= (unsigned)td[j] >= (unsigned)a.n_pages;
+      }
+    }
+    if (a.op == OP_COMPACT && !s_bad[i]) {
+      const int e_k0 = a.keep_ptr[i], n = a.keep_ptr[i + 1] - e_k0;
+      int lead = INT_MAX;
+#pragma unroll 4
+      for (int t = at0; t < n; t += step) {
+        const int x = a.keep[e_k0 + t], y = t ? a.keep[e_k0 + t - 1] : -1;
+        if (x < 0 || x >= e_ls || x <= y) bad |= 2;
+        if (x != t) lead = min(lead, t);
+      }
+      lead = __reduce_min_sync(0xffffffffu, lead);
+      if (lane == 0) atomicMin(&s_lead[i], lead);
+    }
+    bad = __reduce_or_sync(0xffffffffu, bad);
+    if (lane == 0 && bad) atomicOr(&s_bad[i], bad);
+  }
+  __syncthreads();
+  // ---- what each entry needs (two warps hold the entries)
+  int total = 0, shared = 0, had = 0;
+  if (tid < a.n && status == VLAC_OK) {
+    if (s_bad[tid] & 1) status = VLAC_ERR_BAD_STATE;
+    else if (s_bad[tid] & 2) status = VLAC_ERR_INVALID_ARG;
+    else {
+      had = (ld + a.page - 1) >> a.shift;
+      if (a.op == OP_RESIZE) {
+        total = (rows + a.page - 1) >> a.shift;
+        shared = min(total, had);
+        if (rows < ls && (rows & (a.page - 1)) && __ldcg(&a.refs[a.table[(size_t)d * a.max_pages + total - 1]]) > 1) status = VLAC_ERR_BAD_STATE;
+      } else {
+        rows = a.op == OP_FORK ? ls : k1 - k0;
+        total = (rows + a.page - 1) >> a.shift;
+        shared = (a.op == OP_FORK ? (a.deep ? 0 : rows) : min(rows, s_lead[tid])) >> a.shift;
+      }
+    }
+  }
+  if (status != VLAC_OK) total = shared = rows = 0;
+  const int need = total - shared;
+  int start = need;                                                     // (at most 64 x 8192)
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, start, o); if (lane >= o) start += t; }
+  if (tid < PO_LIST && lane == 31) s_warp[warp] = start;
+  __syncthreads();                                                      // (also: every reference count has been read before any changes)
+  if (tid < PO_LIST && warp == 1) start += s_warp[0];
+  start -= need;
+  if (tid == PO_LIST - 1) s_need = start + need;
+  if (tid < a.n) {
+    if (status != VLAC_OK) s_dst[tid] = -1;
+    s_shared[tid] = shared; s_total[tid] = total; s_start[tid] = start;
+  }
+  if (tid == 0) s_taken = 0;
+  __syncthreads();
+  // ---- give back
+  for (int i = my_team; i < a.n; i += n_teams) {
+    const int t = s_dst[i];
+    if (t < 0 || (a.op == OP_COMPACT && s_src[i] == t)) continue;
+    int* td = a.table + (size_t)t * a.max_pages;
+    const int pd = (s_ld[i] + a.page - 1) >> a.shift;
+#pragma unroll 4
+    for (int j = (a.op == OP_RESIZE ? s_shared[i] : 0) + at0; j < pd; j += step) {
+      atomicSub(&a.refs[td[j]], 1);
+      td[j] = -1;
+    }
+  }
+  __syncthreads();
+  // ---- the lowest free pages, in order
+  const int want = s_need;
+  int found = 0;
+  for (int p = 0; p < a.n_pages && found < want; p += PO_THREADS * 4) {
+    const int q = p + tid * 4;
+    int m = 0;
+    if (q + 3 < a.n_pages) {
+      const int4 r = __ldcg(reinterpret_cast<const int4*>(a.refs + q));
+      m = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
+    } else
+      for (int b = 0; b < 4; ++b) if (q + b < a.n_pages && __ldcg(a.refs + q + b) == 0) m |= 1 << b;
+    const int c = __popc(m);
+    int x = c;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += t; }
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    int at = found + x - c;
+    for (int v = 0; v < PO_THREADS / 32; ++v) { const int y = s_warp[v]; found += y; if (v < warp) at += y; }
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      if (m >> b & 1) { if (at < want) { w.list[at] = q + b; if (at < PO_PAGES) s_new[at] = q + b; } ++at; }
+    __syncthreads();
+  }
+  // ---- fates: when there are too few, an entry that needs more than is left and every later one that needs any
+  if (need > 0 && start + need > found) status = VLAC_ERR_OOM;
+  if (tid < a.n && status == VLAC_OK && need > 0) atomicMax(&s_taken, start + need);
+  if (tid < a.n) {
+    w.ok[tid] = status == VLAC_OK; w.src[tid] = s; w.dst[tid] = d; w.shared[tid] = shared; w.rows[tid] = rows; w.start[tid] = start;
+    a.status[tid] = status;
+    if (status == VLAC_OK || (status == VLAC_ERR_OOM && a.op != OP_RESIZE && !(a.op == OP_COMPACT && s == d)))
+      a.len[d] = status == VLAC_OK ? rows : 0;
+    if (status != VLAC_OK) s_dst[tid] = -1;
+  }
+  __syncthreads();
+  const int taken = s_taken;
+  if (tid == 0) w.taken[0] = taken;
+  auto page_of = [&](int i) { return i < PO_PAGES ? s_new[i] : __ldcg(&w.list[i]); };
+  for (int i = tid; i < taken; i += PO_THREADS) a.refs[page_of(i)] = 1;
+  // ---- the new tables
+  for (int i = my_team; i < a.n; i += n_teams) {
+    const int t = s_dst[i];
+    if (t < 0) continue;
+    int* td = a.table + (size_t)t * a.max_pages;
+    const int sh = s_shared[i], tot = s_total[i], st = s_start[i];
+    if (a.op == OP_RESIZE) {
+      for (int j = sh + at0; j < tot; j += step) td[j] = page_of(st + j - sh);
+      continue;
+    }
+    const bool in_place = s_src[i] == t;
+    const int* ts = a.table + (size_t)s_src[i] * a.max_pages;
+    int* to = w.old + (size_t)t * a.max_pages;
+    for (int j = at0; j < (in_place ? (s_ld[i] + a.page - 1) >> a.shift : tot); j += step) {
+      const int p = in_place || j < sh ? ts[j] : 0;
+      if (in_place) to[j] = p;
+      if (j < sh) {
+        if (!in_place) { td[j] = p; atomicAdd(&a.refs[p], 1); }
+      } else {
+        if (in_place) atomicSub(&a.refs[p], 1);
+        td[j] = j < tot ? page_of(st + j - sh) : -1;
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------
 // Rows of the new pages of a fork / compaction: unit = (new page, layer); a CTA of 256 threads moves its K and V rows with
 // 16-byte accesses, four of each in flight per thread.  HBM-bound: read once, written once.
@@ -433,7 +619,10 @@ int book(const vlac_pages* p, int op, const int* src, const int* dst, const int*
   b.n_slots = p->n_slots; b.max_pages = p->max_pages; b.n_pages = p->n_pages; b.page = p->page_size; b.shift = pages_shift(p->page_size);
   b.op = op; b.n = n; b.deep = deep; b.n_keep = n_keep; b.src = src; b.dst = dst; b.lens = lens; b.keep_ptr = keep_ptr; b.keep = keep;
   b.status = status;
-  VLAC_CUDA_CHECK(launch_pdl(pages_book_kernel, dim3(PB_CTAS), dim3(PB_THREADS), 0, s, b));
+  if (n <= PO_LIST && (long long)n * p->max_pages <= PO_ENTRIES && n_keep <= PO_ENTRIES && p->n_pages <= PO_POOL)
+    VLAC_CUDA_CHECK(launch_pdl(pages_book_one_kernel, dim3(1), dim3(PO_THREADS), 0, s, b));
+  else
+    VLAC_CUDA_CHECK(launch_pdl(pages_book_kernel, dim3(PB_CTAS), dim3(PB_THREADS), 0, s, b));
   if (op == OP_RESIZE) return VLAC_OK;
   int n_sm = 0;
   const int rc = sm_count(&n_sm);
