@@ -76,11 +76,6 @@ __host__ __device__ inline int pf_rows(int cls, int R) { return cls == NARROW ? 
 // another (a row-major store of 16 bytes a lane touched 32 rows at once: 3.7 us a tile instead of 1).
 __device__ __forceinline__ size_t wide_at(size_t slot_row, int c4, int head_dim) { return ((slot_row >> 3) * (head_dim / 4) + c4) * 32 + (slot_row & 7) * 4; }
 
-// Whether a tile of a segment is one piece and holds everything its rows see: then the piece writes the result itself.
-__device__ __forceinline__ bool tile_direct(const SegRec& s, long long u_tile, long long U) {
-  return s.pos0 != INT_MIN && s.key0 == 0 && run_of(s.cls, u_tile, U) == run_of(s.cls, u_tile + s.KB - 1, U);
-}
-
 // ------------------------------------------------------------------------------------------------ plan
 struct PlanArgs {
   const int *table, *len;
@@ -348,34 +343,59 @@ struct Piece {
   int direct;
   size_t slot0;                                 // slot row of the tile's first row
 };
-// Run c's piece at unit u (g: its segment, moved on as u passes): fills p and returns its units.
-__device__ __forceinline__ int next_piece(const PlanMem& pm, int cls, long long U, int run, long long u, long long u_end, int* g, Piece* p) {
-  const SegRec* s = pm.seg + *g;
-  while (u >= s->uend || s->cls != cls) s = pm.seg + ++*g;
-  const long long local = u - s->ustart;
-  const int KB = s->KB, T = s->T, per_head = T * KB, head = (int)(local / per_head), rem = (int)(local - (long long)head * per_head);
-  const int rt = rem / KB, kb = rem - rt * KB, R = s->R, bm = pf_bm(cls);
-  const int n = (int)min((long long)(KB - kb), u_end - u);
-  p->slot = s->slot; p->head = head; p->rt = rt; p->nr = min(bm, R - rt * bm); p->row0 = s->row0;
-  p->key0 = s->key0 + kb * pf_kb(cls); p->key1 = min(s->key1, p->key0 + n * pf_kb(cls));
-  // stacked row x of the tile sees the positions below lim0 + x / ratio (x counted from the segment's start)
-  p->lim0 = s->pos0 == INT_MIN ? INT_MIN : s->pos0 + 1;
-  p->n = n;
-  p->direct = tile_direct(*s, u - kb, U);
-  p->slot0 = (size_t)s->rowbase + (size_t)head * pf_rows(cls, R) + (size_t)rt * bm + (size_t)run * bm;
-  return n;
-}
+// Walks a run's pieces: one division to find the first, then tile after tile, segment after segment.
+struct Cursor {
+  long long u, u_end;                           // next unit, end of the run
+  int cls, run, g;
+  SegRec s;                                     // segment of the next unit
+  int head, rt, kb;                             // its place in the segment
+  __device__ __forceinline__ void begin(const PlanMem& pm, int c, int r, long long U, long long G, int first) {
+    cls = c; run = r; g = first;
+    if (U < 1 << 20) {                          // (a 64-bit division is five times as long)
+      u = (unsigned)r * (unsigned)U / (unsigned)G; u_end = (unsigned)(r + 1) * (unsigned)U / (unsigned)G;
+    } else { u = r * U / G; u_end = (r + 1) * U / G; }
+    s = pm.seg[g];
+    while (u >= s.uend || s.cls != cls) s = pm.seg[++g];
+    const long long local = u - s.ustart, per_head = (long long)s.T * s.KB;
+    head = (int)(local / per_head);
+    const long long rem = local - head * per_head;
+    rt = (int)(rem / s.KB); kb = (int)(rem - (long long)rt * s.KB);
+  }
+  __device__ __forceinline__ bool more() const { return u < u_end; }
+  __device__ __forceinline__ void next(const PlanMem& pm, Piece* p) {
+    if (kb == s.KB) {                           // the last piece ended its tile
+      kb = 0;
+      if (++rt == s.T) { rt = 0; ++head; }
+      if (u >= s.uend) {
+        do s = pm.seg[++g]; while (u >= s.uend || s.cls != cls);
+        head = 0;
+      }
+    }
+    const int bm = pf_bm(cls), n = (int)min((long long)(s.KB - kb), u_end - u);
+    p->slot = s.slot; p->head = head; p->rt = rt; p->nr = min(bm, s.R - rt * bm); p->row0 = s.row0;
+    p->key0 = s.key0 + kb * pf_kb(cls); p->key1 = min(s.key1, p->key0 + n * pf_kb(cls));
+    // stacked row x of the tile sees the positions below lim0 + x / ratio (x counted from the segment's start)
+    p->lim0 = s.pos0 == INT_MIN ? INT_MIN : s.pos0 + 1;
+    p->n = n;
+    p->direct = n == s.KB && s.pos0 != INT_MIN && s.key0 == 0;          // a whole tile, and all that its rows see: written as the result
+    p->slot0 = (size_t)s.rowbase + (size_t)head * pf_rows(cls, s.R) + (size_t)rt * bm + (size_t)run * bm;
+    kb += n; u += n;
+  }
+};
 
 // ------------------------------------------------------------------------------------------------ narrow: warp-level tensor cores
-// Every warp walks its own run of units in steps of 16 keys with 16 stacked rows, with a ring of three steps of K and V in shared
-// memory filled by cp.async ahead of the products, across piece boundaries; nothing is synchronised beyond the warp.  Bound: HBM
-// (K/V rows are read once; a lone query row fills one of the 16 rows of the products, which cost nothing next to the loads).
+// Every warp walks its own run of units in steps of 16 (head_dim 128) or 32 keys with 16 stacked rows, with a ring of three steps of K and V
+// in shared memory filled by cp.async ahead of the products, across piece boundaries; nothing is synchronised beyond the warp.  Bound: HBM
+// (K/V rows are read once; a lone query row fills one of the 16 rows of the products, which cost nothing next to the loads), and with
+// head_dim 64 the latency of a step's dependent instructions, which is why its steps are twice as long (ncu, 16 keys: 1.95 warps a
+// scheduler, 43 % of the issue slots, 3.8 TB/s).
 constexpr int PN_STAGES = 3;
-constexpr int PN_STEP = 16;
 template <int D> struct Narrow {
-  static constexpr int HALF = PN_STEP * 128;                            // 64 elements of 16 rows
-  static constexpr int TILE = PN_STEP * D * 2;
-  static constexpr int WARP = TILE * (1 + 2 * PN_STAGES);               // Q, then the ring
+  static constexpr int STEP = D == 128 ? 16 : 32;
+  static constexpr int HALF = STEP * 128;                               // 64 elements of a step's rows
+  static constexpr int TILE = STEP * D * 2;
+  static constexpr int Q_HALF = 16 * 128, Q_TILE = 16 * D * 2;
+  static constexpr int WARP = Q_TILE + TILE * 2 * PN_STAGES;            // Q, then the ring
   static constexpr int SMEM = WARP * PN_WARPS;
 };
 __device__ __forceinline__ void pf_ldsm4(unsigned addr, unsigned* r) {
@@ -386,6 +406,9 @@ __device__ __forceinline__ void pf_ldsm4t(unsigned addr, unsigned* r) {
 }
 __device__ __forceinline__ void pf_cp16(unsigned dst, const void* src, bool valid) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void pf_cp16(unsigned dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 // byte offset of 16-byte piece c16 of a row in a [rows][64 elements] block whose pieces are XOR-swizzled by the row
 __device__ __forceinline__ unsigned pf_swz(int row, int c16) { return (unsigned)(row * 128 + (((c16 ^ row) & 7) << 4)); }
@@ -405,65 +428,94 @@ __device__ __forceinline__ bool any_nonfinite(uint4 x) {
 template <typename T, int D>
 __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArgs a) {
   using N = Narrow<D>;
+  constexpr int STEP = N::STEP, NB = STEP / 16;                         // blocks of 16 keys in a step
   extern __shared__ __align__(1024) unsigned char pn_raw[];
-  __shared__ Piece s_piece[PN_WARPS][2];
+  __shared__ Piece s_piece[PN_WARPS][4];
   const PlanMem pm = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_trigger();
   pdl_wait();
-  const long long U = pm.head->units[NARROW], G = runs(NARROW, U);
   const int run = warp * PN_CTAS + blockIdx.x;                          // few runs: one per SM before two
+  const long long U = pm.head->units[NARROW], G = runs(NARROW, U);
+  const int g = pm.first[NARROW][run];
   if (run >= G) return;
-  long long lu = run * U / G;                                           // load cursor: next unit whose piece is not begun
-  const long long u_end = (run + 1) * U / G;
-  int g = pm.first[NARROW][run];
+  Cursor cur;                                                           // pieces not yet begun
+  cur.begin(pm, NARROW, run, U, G, g);
 
   unsigned char* const base_p = pn_raw + warp * N::WARP;
-  const unsigned q_s = pf_smem(base_p), ring = q_s + N::TILE;
-  constexpr int C16 = D / 8, RSTEP = 32 / C16, NROW = PN_STEP / RSTEP;  // 16-byte pieces of a row; rows a warp copies at once
+  const unsigned q_s = pf_smem(base_p), ring = q_s + N::Q_TILE;
+  constexpr int C16 = D / 8, RSTEP = 32 / C16, NROW = 16 / RSTEP;       // 16-byte pieces of a row; rows a warp copies at once; times for 16
   const int c16 = lane % C16, r_first = lane / C16;
-  const unsigned col_off = (unsigned)(c16 >> 3) * N::HALF;
+  const unsigned q_off = (unsigned)(c16 >> 3) * N::Q_HALF, col_off = (unsigned)(c16 >> 3) * N::HALF;
   const size_t row_el = (size_t)a.kv_heads * D;
 
-  // ---- load cursor
-  int l_begun = 0, l_step = 0, l_steps = 0, l_cnt = 0, pg_lo = 0, pg_hi = 0;
+  // ---- load cursor.  Pieces may be a step or two long (a sequence's own rows), so that loads run up to three pieces ahead: three Q tiles
+  // of up to 5 rows lie side by side in the 16 rows of the Q buffer; a larger one has it alone.
+  constexpr int QN = 3, QR = 5;
+  int l_begun = 0, l_step = 0, l_steps = 0, l_cnt = 0, pg = 0, pg_slot = -1, pg_key = -1, pg_end = -1;
   int c_begun = 0, c_cnt = 0;
+  bool have = false, l_big = false;                                     // lp is prepared but not begun; the piece begun last has Q alone
   const T *kg = nullptr, *vg = nullptr;
   Piece lp;
+  const int page_step = a.shift < 4 ? 3 : 4;                            // page numbers are fetched for blocks of 8 or 16 keys, one a lane
   auto issue = [&]() -> bool {                                          // one more step in flight
     if (l_step == l_steps) {
-      // the next piece: its Q may be fetched once the previous piece's Q is in registers
-      if (lu >= u_end || l_begun != c_begun) return false;
-      lu += next_piece(pm, NARROW, U, run, lu, u_end, &g, &lp);
-      if (lane == 0) s_piece[warp][l_begun & 1] = lp;
+      if (!have) {
+        if (!cur.more()) return false;
+        cur.next(pm, &lp);
+        have = true;
+      }
+      const bool big = lp.nr > QR;
+      if (l_begun - c_begun >= (big || l_big ? 1 : QN) || (big && l_begun != c_begun)) return false;
+      have = false; l_big = big;
+      const int qs = big ? 0 : (l_begun % QN) * QR;                     // first row of its Q
+      if (lane == 0) s_piece[warp][l_begun & 3] = lp;
       ++l_begun;
-      l_step = 0; l_steps = (lp.key1 - lp.key0 + PN_STEP - 1) / PN_STEP;
-      kg = (const T*)a.k + (size_t)lp.head * D + c16 * 8; vg = (const T*)a.v + (size_t)lp.head * D + c16 * 8;
-#pragma unroll
-      for (int i = 0; i < NROW; ++i) {
+      l_step = 0; l_steps = (lp.key1 - lp.key0 + STEP - 1) / STEP;
+      const size_t col = (size_t)r_first * row_el + (size_t)lp.head * D + c16 * 8;
+      kg = (const T*)a.k + col; vg = (const T*)a.v + col;
+      for (int r = r_first; r < lp.nr; r += RSTEP) {
         // stacked row x is q row row0 + x / ratio, query head head * ratio + x % ratio
-        const int r = r_first + i * RSTEP, x = lp.rt * 16 + min(r, lp.nr - 1), xq = x / a.ratio;
+        const int x = lp.rt * 16 + r, xq = x / a.ratio;
         const T* src = (const T*)a.q + (size_t)(lp.row0 + xq) * a.q_stride + (size_t)(lp.head * a.ratio + x - xq * a.ratio) * D + c16 * 8;
-        pf_cp16(q_s + col_off + pf_swz(r, c16 & 7), src, r < lp.nr);
+        pf_cp16(q_s + q_off + pf_swz(qs + r, c16 & 7), src);
       }
     }
-    const int k0 = lp.key0 + l_step * PN_STEP;
-    if ((l_step & 31) == 0) {                                           // page numbers of the next 32 steps, one a lane
-      const int* tab = a.table + (size_t)lp.slot * a.max_pages;
-      const int k = k0 + lane * PN_STEP;
-      pg_lo = k < lp.key1 ? tab[k >> a.shift] : -1;
-      pg_hi = a.shift > 3 ? pg_lo : k + 8 < lp.key1 ? tab[(k + 8) >> a.shift] : -1;      // a step is two pages of 8 rows
+    const int k0 = lp.key0 + l_step * STEP;
+    const int per = STEP >> page_step, at = (l_step * per) & 31;        // page numbers of a step, and where the lanes hold them
+    if (at == 0 && !(pg_slot == lp.slot && pg_key == k0 && pg_end == lp.key1)) {             // (the next head's piece begins where the last one did)
+      const int k = k0 + (lane << page_step);
+      pg_slot = lp.slot; pg_key = k0; pg_end = lp.key1;
+      pg = k < lp.key1 ? a.table[(size_t)lp.slot * a.max_pages + (k >> a.shift)] : -1;
+      if ((unsigned)pg >= (unsigned)a.n_pages) pg = -1;
     }
-    const int lo = __shfl_sync(0xffffffffu, pg_lo, l_step & 31), hi = __shfl_sync(0xffffffffu, pg_hi, l_step & 31);
-    const unsigned ks = ring + (unsigned)(l_cnt % PN_STAGES) * 2u * N::TILE;
+    const unsigned ks = ring + (unsigned)(l_cnt % PN_STAGES) * 2u * N::TILE + col_off;
 #pragma unroll
-    for (int i = 0; i < NROW; ++i) {
-      const int r = r_first + i * RSTEP, key = k0 + r, pg = r < 8 ? lo : hi;
-      const bool ok = key < lp.key1 && (unsigned)pg < (unsigned)a.n_pages;               // zeros behind the segment
-      const size_t at = (((size_t)(ok ? pg : 0) << a.shift) + (key & (a.page - 1))) * row_el;
-      const unsigned off = ks + col_off + pf_swz(r, c16 & 7);
-      pf_cp16(off, kg + at, ok);
-      pf_cp16(off + N::TILE, vg + at, ok);
+    for (int b = 0; b < NB; ++b) {
+      const int kb = k0 + 16 * b;
+      const int lo = __shfl_sync(0xffffffffu, pg, at + (b << (4 - page_step)));
+      const int hi = page_step == 4 ? lo : __shfl_sync(0xffffffffu, pg, at + 2 * b + 1);
+      const size_t at_lo = (((size_t)lo << a.shift) + (kb & (a.page - 1))) * row_el;
+      const size_t at_hi = page_step == 4 ? at_lo + 8 * row_el : ((size_t)hi << a.shift) * row_el;
+      if (kb + 16 <= lp.key1 && lo >= 0 && hi >= 0) {
+#pragma unroll
+        for (int i = 0; i < NROW; ++i) {
+          const size_t o = i < NROW / 2 ? at_lo + i * RSTEP * row_el : at_hi + (i - NROW / 2) * RSTEP * row_el;
+          const unsigned off = ks + pf_swz(16 * b + r_first + i * RSTEP, c16 & 7);
+          pf_cp16(off, kg + o);
+          pf_cp16(off + N::TILE, vg + o);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NROW; ++i) {                                // zeros behind the segment
+          const int r = r_first + i * RSTEP;
+          const bool ok = kb + r < lp.key1 && (i < NROW / 2 ? lo : hi) >= 0;
+          const size_t o = !ok ? 0 : i < NROW / 2 ? at_lo + i * RSTEP * row_el : at_hi + (i - NROW / 2) * RSTEP * row_el;
+          const unsigned off = ks + pf_swz(16 * b + r, c16 & 7);
+          pf_cp16(off, kg + o, ok);
+          pf_cp16(off + N::TILE, vg + o, ok);
+        }
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     ++l_step; ++l_cnt;
@@ -482,9 +534,10 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
     else asm volatile("cp.async.wait_group 2;" ::: "memory");
     __syncwarp();
     if (c_left == 0) {                                                  // a piece begins
-      const Piece& p = s_piece[warp][c_begun & 1];
+      const Piece& p = s_piece[warp][c_begun & 3];
+      const int qs = p.nr > QR ? 0 : (c_begun % QN) * QR;
       key_lo = p.key0; key1 = p.key1;
-      c_left = (key1 - key_lo + PN_STEP - 1) / PN_STEP;
+      c_left = (key1 - key_lo + STEP - 1) / STEP;
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int x = (lane >> 2) + 8 * r;
@@ -496,29 +549,34 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
       for (int j = 0; j < D / 8; ++j) { o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f; }
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
-        const int row = (lane & 7) + ((lane >> 3) & 1) * 8, c = ks * 2 + (lane >> 4);
-        pf_ldsm4(q_s + (unsigned)(c >> 3) * N::HALF + pf_swz(row, c & 7), qf[ks]);
+        // (rows behind the last repeat it: nothing of them is kept)
+        const int row = qs + min((lane & 7) + ((lane >> 3) & 1) * 8, p.nr - 1), c = ks * 2 + (lane >> 4);
+        pf_ldsm4(q_s + (unsigned)(c >> 3) * N::Q_HALF + pf_swz(row, c & 7), qf[ks]);
       }
       ++c_begun;
       __syncwarp();
     }
-    unsigned char* const k_p = base_p + N::TILE + (c_cnt % PN_STAGES) * 2 * N::TILE;
+    unsigned char* const k_p = base_p + N::Q_TILE + (c_cnt % PN_STAGES) * 2 * N::TILE;
     const unsigned k_s = pf_smem(k_p), v_s = k_s + N::TILE;
-    float s[2][4];
+    float s[2 * NB][4];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+    for (int j = 0; j < 2 * NB; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
-      const int c = ks * 2 + ((lane >> 3) & 1), key = (lane & 7) + ((lane >> 4) & 1) * 8;
-      unsigned b[4];
-      pf_ldsm4(k_s + (unsigned)(c >> 3) * N::HALF + pf_swz(key, c & 7), b);
-      Half2<T>::mma(s[0], qf[ks], b[0], b[1]);
-      Half2<T>::mma(s[1], qf[ks], b[2], b[3]);
+      const int c = ks * 2 + ((lane >> 3) & 1);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int key = 16 * b + (lane & 7) + ((lane >> 4) & 1) * 8;
+        unsigned f[4];
+        pf_ldsm4(k_s + (unsigned)(c >> 3) * N::HALF + pf_swz(key, c & 7), f);
+        Half2<T>::mma(s[2 * b], qf[ks], f[0], f[1]);
+        Half2<T>::mma(s[2 * b + 1], qf[ks], f[2], f[3]);
+      }
     }
-    const bool masked = key_lo + PN_STEP > lim_min;                     // some row does not see the whole step
+    const bool masked = key_lo + STEP > lim_min;                        // some row does not see the whole step
     float bm[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2 * NB; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float x = s[j][e] * a.scale2;
@@ -543,20 +601,20 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
     }
     // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16); the sum l takes
     // the unrounded weights
-    unsigned pf[4];
+    unsigned pf[NB][4];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < 2 * NB; ++j) {
       const float p0 = pf_ex2(s[j][0] - ref[0]), p1 = pf_ex2(s[j][1] - ref[0]), p2 = pf_ex2(s[j][2] - ref[1]), p3 = pf_ex2(s[j][3] - ref[1]);
       l[0] += p0 + p1; l[1] += p2 + p3;
-      pf[j * 2] = Half2<T>::pack(p0, p1);
-      pf[j * 2 + 1] = Half2<T>::pack(p2, p3);
+      pf[j >> 1][(j & 1) * 2] = Half2<T>::pack(p0, p1);
+      pf[j >> 1][(j & 1) * 2 + 1] = Half2<T>::pack(p2, p3);
     }
     if (masked && lim_min < key1) {
       // a row does not see some key of this step: infinities and NaN of such a V row must not reach it as 0 * inf
       bool bad = false;
       for (int i = lane; i < N::TILE / 16; i += 32) bad |= any_nonfinite<T>(*reinterpret_cast<const uint4*>(k_p + N::TILE + i * 16));
       if (__any_sync(0xffffffffu, bad)) {
-        for (int key = 0; key < PN_STEP; ++key)
+        for (int key = 0; key < STEP; ++key)
 #pragma unroll
           for (int j = 0; j < D / 8; ++j)
 #pragma unroll
@@ -571,23 +629,25 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
             }
         __syncwarp();
         unsigned short* x = reinterpret_cast<unsigned short*>(k_p + N::TILE);
-        for (int i = lane; i < PN_STEP * D; i += 32)
+        for (int i = lane; i < STEP * D; i += 32)
           if ((x[i] & Half2<T>::exp_mask) == Half2<T>::exp_mask) x[i] = 0;
         __syncwarp();
       }
     }
 #pragma unroll
-    for (int np = 0; np < D / 16; ++np) {
-      const int c = np * 2 + (lane >> 4), key = (lane & 7) + ((lane >> 3) & 1) * 8;
-      unsigned b[4];
-      pf_ldsm4t(v_s + (unsigned)(c >> 3) * N::HALF + pf_swz(key, c & 7), b);
-      Half2<T>::mma(o[2 * np], pf, b[0], b[1]);
-      Half2<T>::mma(o[2 * np + 1], pf, b[2], b[3]);
-    }
-    key_lo += PN_STEP;
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int np = 0; np < D / 16; ++np) {
+        const int c = np * 2 + (lane >> 4), key = 16 * b + (lane & 7) + ((lane >> 3) & 1) * 8;
+        unsigned f[4];
+        pf_ldsm4t(v_s + (unsigned)(c >> 3) * N::HALF + pf_swz(key, c & 7), f);
+        Half2<T>::mma(o[2 * np], pf[b], f[0], f[1]);
+        Half2<T>::mma(o[2 * np + 1], pf[b], f[2], f[3]);
+      }
+    key_lo += STEP;
     ++c_cnt;
     if (--c_left == 0) {                                                // the piece ends
-      const Piece& p = s_piece[warp][(c_begun - 1) & 1];
+      const Piece& p = s_piece[warp][(c_begun - 1) & 3];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
@@ -801,6 +861,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   pdl_wait();
   pdl_trigger();
   const long long U = pm.head->units[WIDE], G = runs(WIDE, U);
+  const int g_first = pm.first[WIDE][run];
   if (run >= G) return;                                                 // uniform over the CTA
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(pf_smem(&tmem_slot)), "r"(512u) : "memory");
@@ -810,9 +871,8 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   __syncthreads();
   pw_after();
   const unsigned tmem = tmem_slot;                                      // columns: S/P even 0, S/P odd 128, O even 256, O odd 384
-  long long u = run * U / G;
-  const long long u_end = (run + 1) * U / G;
-  int g = pm.first[WIDE][run];
+  Cursor cur;
+  cur.begin(pm, WIDE, run, U, G, g_first);
   Piece p;
 
   if (warp < 4 && warp != 1) {
@@ -835,8 +895,8 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       __syncwarp();
       ++cnt;
     };
-    while (u < u_end && ok) {
-      u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
+    while (cur.more() && ok) {
+      cur.next(pm, &p);
       const int* tab = a.table + (size_t)p.slot * a.max_pages;
       auto row = [&](int i) -> int {                                    // pool row of this lane's box of key block i
         const int key = p.key0 + i * 128 + chunk * w.box;
@@ -903,8 +963,8 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     };
     // The weights come last, so everything else is waited for before them: O += P V and the side's next S, which takes the columns that P
     // leaves, then go out in one burst.
-    while (u < u_end && ok) {
-      u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
+    while (cur.more() && ok) {
+      cur.next(pm, &p);
       const int n = same(p.n), two = same(p.nr > 128);
       there(0);
       wait_at(pf_smem(&q_full), pieces & 1);
@@ -971,7 +1031,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
         if (qr < p.nr) qv[i] = *reinterpret_cast<const uint4*>(src + (size_t)xq * a.q_stride + (x - xq * a.ratio) * D + c16 * 8);
       }
     };
-    u += next_piece(pm, WIDE, U, run, u, u_end, &g, &p);
+    cur.next(pm, &p);
     load_q(p);
     while (true) {
       const bool two = p.nr > 128;
@@ -1068,8 +1128,8 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
         pw_arrive(&p_full[side][1]);
       }
       Piece pn;
-      const bool more = u < u_end;
-      if (more) { u += next_piece(pm, WIDE, U, run, u, u_end, &g, &pn); load_q(pn); }
+      const bool more = cur.more();
+      if (more) { cur.next(pm, &pn); load_q(pn); }
       if (ok) ok = pw_wait(&o_full, pieces & 1, &abort_flag, error);
       ++pieces;
       ok = pw_all_ok(ok);                                               // every product of the piece is done: Q's memory is free
@@ -1163,7 +1223,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
     const long long U = hd.units[s.cls];
     const long long u0 = s.ustart + ((long long)kvh * s.T + rt) * s.KB;
     const int c0 = run_of(s.cls, u0, U), c1 = run_of(s.cls, u0 + s.KB - 1, U);
-    if (s.pos0 != INT_MIN && s.key0 == 0 && c0 == c1) return;           // written by its only piece (tile_direct)
+    if (s.pos0 != INT_MIN && s.key0 == 0 && c0 == c1) return;           // written by its only piece
     np[i] = c1 - c0 + 1;
     pad[i] = bm;
     if (s.cls == WIDE) wide = 1;                                        // (only a prefix is wide)
