@@ -610,13 +610,17 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeTiledFn g_encode = nullptr;
 
+int find_encode() {
+  if (g_encode) return VLAC_OK;
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult qres;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || !fn) return VLAC_ERR_CUDA;
+  g_encode = (EncodeTiledFn)fn;
+  return VLAC_OK;
+}
+
 int encode_map(CUtensorMap* out, const void* base, int rows, int K, int box_rows) {
-  if (!g_encode) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || !fn) return VLAC_ERR_CUDA;
-    g_encode = (EncodeTiledFn)fn;
-  }
+  if (find_encode() != VLAC_OK) return VLAC_ERR_CUDA;
   cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)K * 2};
   cuuint32_t box[2] = {(cuuint32_t)TG_BK, (cuuint32_t)box_rows};
@@ -637,6 +641,19 @@ int vlac_launch_wait_expiry(vlac_ctx* ctx, unsigned long long limit_ns, cudaStre
 
 int vlac_encode_map_2d(void* out, const void* base, int rows, int cols, int box_rows) {
   return encode_map((CUtensorMap*)out, base, rows, cols, box_rows);
+}
+
+// 16-bit [rows][heads][head_dim] with any row stride (elements): boxes of 64 elements x box_heads x box_rows, 128-byte swizzle.
+int vlac_encode_map_heads(void* out, const void* base, int rows, int heads, int head_dim, long long row_stride, int box_heads, int box_rows) {
+  if (find_encode() != VLAC_OK) return VLAC_ERR_CUDA;
+  cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)rows};
+  cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)row_stride * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = g_encode((CUtensorMap*)out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? VLAC_OK : VLAC_ERR_CUDA;
 }
 
 // Tensor maps of one context: 7 per layer (weights) + 3 activation buffers x 4 box heights.

@@ -13,6 +13,8 @@
 #include <cuda_fp16.h>
 #include <math.h>
 #include <stddef.h>
+#include <algorithm>
+#include <atomic>
 
 namespace {
 
@@ -43,7 +45,6 @@ struct PlanMem {
   SeqRec* seq;                                  // [n] active sequences
   SegRec* seg;                                  // [2n]
   int* first[2];                                // segment of each run's first unit
-  int* row_k;                                   // [rows] active sequence of each row, -1: none
   float2* ml;                                   // [slot rows] (m, l), m in units of log2
   float* po;                                    // [slot rows][head_dim]; of wide segments [slot rows / 8][head_dim / 4][8][4] (see wide_at)
   size_t bytes;
@@ -57,7 +58,6 @@ __host__ __device__ inline PlanMem plan_mem(void* mem, int n, int rows, int n_he
   p.seq = (SeqRec*)take(sizeof(SeqRec) * n);
   p.seg = (SegRec*)take(sizeof(SegRec) * 2 * (size_t)n);
   for (int c = 0; c < 2; ++c) p.first[c] = (int*)take(sizeof(int) * pf_runs(c));
-  p.row_k = (int*)take(sizeof(int) * (size_t)(rows > 0 ? rows : 1));
   // a row and head has at most one narrow and one more segment; wide segments have 17 rows at least and are padded to 8 (24 / 17 < 1.5)
   const size_t slots = (5 * (size_t)rows * n_heads + 1) / 2 + 8 + (size_t)pf_runs(NARROW) * pf_bm(NARROW) + (size_t)pf_runs(WIDE) * pf_bm(WIDE);
   p.ml = (float2*)take(sizeof(float2) * slots);
@@ -68,7 +68,10 @@ __host__ __device__ inline PlanMem plan_mem(void* mem, int n, int rows, int n_he
 
 // The U units of a class are dealt to G = min(U, pf_runs) runs, so that none is empty: run c is [c*U/G, (c+1)*U/G).  The run of unit u:
 __device__ __forceinline__ long long runs(int cls, long long U) { return U < pf_runs(cls) ? U : pf_runs(cls); }
-__device__ __forceinline__ int run_of(int cls, long long u, long long U) { return (int)(((u + 1) * runs(cls, U) - 1) / U); }
+__device__ __forceinline__ int run_of(int cls, long long u, long long U) {
+  if (U < 1 << 20) return (int)(((unsigned)(u + 1) * (unsigned)runs(cls, U) - 1) / (unsigned)U);         // (a 64-bit division is five times as long)
+  return (int)(((u + 1) * runs(cls, U) - 1) / U);
+}
 
 // rows of a segment per K/V head in the slots
 __host__ __device__ inline int pf_rows(int cls, int R) { return cls == NARROW ? R : (R + 7) & ~7; }
@@ -179,12 +182,6 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
     lcp = __reduce_min_sync(0xffffffffu, lcp);
     bad = __any_sync(0xffffffffu, bad);
     if (lane == 0) { atomicMin(&s.lcp[k], lcp); if (bad) atomicOr(&s.bad[k], 1); }
-  }
-  // which sequence each row belongs to
-  for (int r = rank * blockDim.x + tid; r < a.rows; r += CTAS * blockDim.x) {
-    int lo = 0, hi = n_act - 1;
-    while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (s.row0[m] <= r) lo = m; else hi = m - 1; }
-    p.row_k[r] = n_act > 0 && r >= s.row0[lo] && r < s.row0[lo] + s.nq[lo] ? lo : -1;
   }
   __syncthreads();
   if (CTAS > 1) {
@@ -694,7 +691,7 @@ template <int D> struct Wide {
   static constexpr int HALF = 128 * 128;        // 64 elements of 128 rows
   static constexpr int TILE = HALVES * HALF;
   static constexpr int SLOTS = D == 128 ? 5 : 10;
-  static constexpr int SMEM = 1024 + TILE * (2 + SLOTS);                // two tiles of Q, then the ring of K and V tiles
+  static constexpr int SMEM = TILE * (2 + SLOTS) + 2048;                // two tiles of Q, the ring of K and V tiles, the sides' (m, l)
 };
 
 __device__ __forceinline__ void pw_bar_init(unsigned long long* bar, unsigned count) {
@@ -737,6 +734,10 @@ __device__ __forceinline__ bool pw_wait(unsigned long long* bar, unsigned parity
 __device__ __forceinline__ void pw_tma(unsigned dst, const CUtensorMap* tm, int x, int y, unsigned long long* bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(dst), "l"(tm), "r"(x), "r"(y), "r"(pf_smem(bar)) : "memory");
+}
+__device__ __forceinline__ void pw_tma3(unsigned dst, const CUtensorMap* tm, int x, int y, int z, unsigned long long* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(tm), "r"(x), "r"(y), "r"(z), "r"(pf_smem(bar)) : "memory");
 }
 __device__ __forceinline__ unsigned long long pw_desc(unsigned addr, unsigned lbo, unsigned sbo) {
   unsigned long long d = 0;
@@ -835,25 +836,30 @@ struct WideArgs {
   int box;                                      // rows of a TMA box: min(page, 128)
 };
 
-template <typename T, int D>
-__global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, WideArgs w) {
+// QTMA: Q comes by TMA, boxes of (64 elements, the query heads of a K/V head, rows), which lie in shared memory as the stacked rows do.  Needs a
+// number of query heads per K/V head that divides 128 and a positive scale; otherwise the softmax warps copy it (through L2, behind the
+// first K and V tiles: 5-8 us later).
+template <typename T, int D, bool QTMA>
+__global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                                                                    const __grid_constant__ CUtensorMap tm_q, WideArgs w) {
   using W = Wide<D>;
-  extern __shared__ unsigned char pw_raw[];
-  __shared__ __align__(8) unsigned long long full[W::SLOTS], empty[W::SLOTS], s_full[2], p_full[2][2], q_full, o_full, drain;
+  extern __shared__ __align__(1024) unsigned char pw_raw[];
+  __shared__ __align__(8) unsigned long long full[W::SLOTS], empty[W::SLOTS], s_full[2], p_full[2][2], q_full, o_full, o_free, drain;
   __shared__ unsigned tmem_slot;
   __shared__ int abort_flag;
   const AttnArgs& a = w.a;
   const PlanMem pm = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
   int* const error = &pm.head->error;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, run = blockIdx.x;
-  unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pw_raw) + 1023) & ~(uintptr_t)1023);
+  unsigned char* const smem = pw_raw;
+  if (pf_smem(pw_raw) & 1023u) { if (tid == 0) atomicExch(error, VLAC_ERR_TIMEOUT); return; }        // (the swizzled tiles need it; uniform)
   const unsigned q_s = pf_smem(smem), ring = q_s + 2 * W::TILE;
-  float* const red_m = reinterpret_cast<float*>(smem);                  // [2][128] each, over Q when its products are done
+  float* const red_m = reinterpret_cast<float*>(smem + W::TILE * (2 + W::SLOTS));            // [2][128] each
   float* const red_l = red_m + 256;
   if (tid == 0) {
     for (int i = 0; i < W::SLOTS; ++i) { pw_bar_init(&full[i], 1); pw_bar_init(&empty[i], 1); }
     for (int i = 0; i < 2; ++i) { pw_bar_init(&s_full[i], 1); pw_bar_init(&p_full[i][0], 128); pw_bar_init(&p_full[i][1], 128); }
-    pw_bar_init(&q_full, PW_SOFT); pw_bar_init(&o_full, 1); pw_bar_init(&drain, 1);
+    pw_bar_init(&q_full, QTMA ? 1 : PW_SOFT); pw_bar_init(&o_full, 1); pw_bar_init(&o_free, PW_SOFT); pw_bar_init(&drain, 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -966,7 +972,19 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     while (cur.more() && ok) {
       cur.next(pm, &p);
       const int n = same(p.n), two = same(p.nr > 128);
+      if (QTMA) {
+        if (pieces > 0) wait_at(pf_smem(&o_full), (pieces - 1) & 1);    // the last piece's products are done: Q's memory is free
+        if (one) {
+          pw_expect(&q_full, (unsigned)(W::TILE << two));
+          for (int t = 0; t <= two; ++t)
+#pragma unroll
+            for (int hf = 0; hf < W::HALVES; ++hf)
+              pw_tma3(q_s + t * W::TILE + hf * W::HALF, &tm_q, hf * 64, p.head * a.ratio, p.row0 + (p.rt * 256 + t * 128) / a.ratio, &q_full);
+        }
+        __syncwarp();
+      }
       there(0);
+      if (QTMA && pieces > 0) wait_at(pf_smem(&o_free), (pieces - 1) & 1);                     // and its O has been read
       wait_at(pf_smem(&q_full), pieces & 1);
       ok = still_ok();
       if (!ok) break;
@@ -1032,20 +1050,22 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       }
     };
     cur.next(pm, &p);
-    load_q(p);
+    if (!QTMA) load_q(p);
     while (true) {
       const bool two = p.nr > 128;
       const int c0 = two ? side * 128 * C16 + (st & 127) : st, dc = two ? 128 : 256;
 #pragma unroll
-      for (int i = 0; i < NQ; ++i) {
+      for (int i = 0; i < (QTMA ? 0 : NQ); ++i) {
         if (i >= NQ / 2 && !two) break;
         const int c = c0 + i * dc, qr = c / C16, c16 = c % C16;
         if (w.flip) { qv[i].x ^= 0x80008000u; qv[i].y ^= 0x80008000u; qv[i].z ^= 0x80008000u; qv[i].w ^= 0x80008000u; }
         *reinterpret_cast<uint4*>(smem + (qr >> 7) * W::TILE + (c16 >> 3) * W::HALF + pf_swz(qr & 127, c16 & 7)) = qv[i];
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      pw_before();
-      pw_arrive(&q_full);
+      if (!QTMA) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        pw_before();
+        pw_arrive(&q_full);
+      }
       float m = -INFINITY, l = 0.f;
       const int row_t = (two ? 128 * side : 0) + r;                     // the thread's row in the tile
       const bool idle = row_t - lane >= p.nr;                           // a warp without rows: only its arrivals are needed
@@ -1129,7 +1149,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       }
       Piece pn;
       const bool more = cur.more();
-      if (more) { cur.next(pm, &pn); load_q(pn); }
+      if (more) { cur.next(pm, &pn); if (!QTMA) load_q(pn); }
       if (ok) ok = pw_wait(&o_full, pieces & 1, &abort_flag, error);
       ++pieces;
       ok = pw_all_ok(ok);                                               // every product of the piece is done: Q's memory is free
@@ -1182,7 +1202,10 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
         }
       }
       if (!more) break;
-      pw_all_ok(true);                                                  // red_m, red_l may be written again
+      if (QTMA) {
+        pw_before();
+        pw_arrive(&o_free);
+      }
       p = pn;
     }
     pw_before();
@@ -1194,85 +1217,123 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   }
 }
 
-// One warp per (row, query head): the pieces of its prefix and of its own segment, added in order.  The eight warps of a CTA take
-// stacked rows of one K/V head that follow one another (they share the sectors of wide partial sums).
+// Pieces to results: grid (sequences, shares); a warp takes (K/V head, stacked row) items of its sequence and adds the pieces of the row's
+// prefix and of its own segment in order, partial sums and their (m, l) read together.  The warps of a CTA take rows that follow one
+// another (they share the sectors of wide partial sums).
 template <typename T, int D>
 __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
   const PlanMem p = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
   const int lane = threadIdx.x & 31;
-  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), per = (long long)a.rows * a.ratio;
   pdl_trigger();
   pdl_wait();
-  if (w >= per * a.kv_heads) return;
-  const int kvh = (int)(w / per), xr = (int)(w - kvh * per), row = xr / a.ratio, h = kvh * a.ratio + xr - row * a.ratio;
-  const int k = p.row_k[row];
-  if (k < 0) return;
-  const SeqRec q = p.seq[k];
-  if (q.slot < 0) return;                                               // refused
-  int np[2] = {0, 0}, pad[2] = {0, 0}, wide = 0;
-  size_t base[2] = {0, 0};
   const PlanHead hd = *p.head;
+  const SeqRec q = p.seq[blockIdx.x];
+  if ((int)blockIdx.x >= hd.n_act || q.slot < 0) return;                // (slot -1: refused)
   SegRec sg[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) sg[i] = p.seg[max(0, i ? q.suf_seg : q.pre_seg)];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if ((i ? q.suf_seg : q.pre_seg) < 0) continue;
-    const SegRec& s = sg[i];
-    const int bm = pf_bm(s.cls), x = (row - s.row0) * a.ratio + h - kvh * a.ratio, rt = x / bm;
-    const long long U = hd.units[s.cls];
-    const long long u0 = s.ustart + ((long long)kvh * s.T + rt) * s.KB;
-    const int c0 = run_of(s.cls, u0, U), c1 = run_of(s.cls, u0 + s.KB - 1, U);
-    if (s.pos0 != INT_MIN && s.key0 == 0 && c0 == c1) return;           // written by its only piece
-    np[i] = c1 - c0 + 1;
-    pad[i] = bm;
-    if (s.cls == WIDE) wide = 1;                                        // (only a prefix is wide)
-    base[i] = (size_t)s.rowbase + (size_t)kvh * pf_rows(s.cls, s.R) + x + (size_t)c0 * bm;
-  }
-  const int n = np[0] + np[1];
-  auto slot = [&](int i) { return i < np[0] ? base[0] + (size_t)i * pad[0] : base[1] + (size_t)(i - np[0]) * pad[1]; };
-  float M = -INFINITY;
-  for (int i = lane; i < n; i += 32) M = fmaxf(M, p.ml[slot(i)].x);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  const float ref = M == -INFINITY ? 0.f : M;
-  float l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int per = q.nq * a.ratio, items = per * a.kv_heads;
   const int c4 = lane < D / 4 ? lane : 0;
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const size_t sl = slot(i);
-    const float2 ml = p.ml[sl];
-    const float4 v = *reinterpret_cast<const float4*>(p.po + (wide && i < np[0] ? wide_at(sl, c4, D) : sl * D + c4 * 4));
-    const float f = pf_ex2(ml.x - ref);
-    l += f * ml.y;
-    o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
+  for (int it = blockIdx.y * 8 + (threadIdx.x >> 5); it < items; it += gridDim.y * 8) {
+    const int kvh = it / per, xr = it - kvh * per, xq = xr / a.ratio, row = q.row0 + xq, h = kvh * a.ratio + xr - xq * a.ratio;
+    int np[2] = {0, 0}, pad[2] = {0, 0}, wide = 0;
+    size_t base[2] = {0, 0};
+    bool done = false;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if ((i ? q.suf_seg : q.pre_seg) < 0) continue;
+      const SegRec& s = sg[i];
+      const int bm = pf_bm(s.cls), x = (row - s.row0) * a.ratio + xr - xq * a.ratio, rt = x / bm;
+      const long long U = hd.units[s.cls], u0 = s.ustart + ((long long)kvh * s.T + rt) * s.KB;
+      const int c0 = run_of(s.cls, u0, U), c1 = run_of(s.cls, u0 + s.KB - 1, U);
+      if (s.pos0 != INT_MIN && s.key0 == 0 && c0 == c1) done = true;    // written by its only piece
+      np[i] = c1 - c0 + 1;
+      pad[i] = bm;
+      if (s.cls == WIDE) wide = 1;                                      // (only a prefix is wide)
+      base[i] = (size_t)s.rowbase + (size_t)kvh * pf_rows(s.cls, s.R) + x + (size_t)c0 * bm;
+    }
+    if (done) continue;
+    const int n = np[0] + np[1];
+    float M = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int B = 8;                                                // partial sums in flight
+    for (int i0 = 0; i0 < n; i0 += B) {
+      float2 ml[B];
+      float4 v[B];
+#pragma unroll
+      for (int e = 0; e < B; ++e) {
+        const int i = i0 + e, first = i < np[0];
+        ml[e] = make_float2(-INFINITY, 0.f);
+        v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < n) {
+          const size_t sl = first ? base[0] + (size_t)i * pad[0] : base[1] + (size_t)(i - np[0]) * pad[1];
+          ml[e] = p.ml[sl];
+          v[e] = *reinterpret_cast<const float4*>(p.po + (wide && first ? wide_at(sl, c4, D) : sl * D + c4 * 4));
+        }
+      }
+      float m = M;
+#pragma unroll
+      for (int e = 0; e < B; ++e) m = fmaxf(m, ml[e].x);
+      const float ref = m == -INFINITY ? 0.f : m, f = pf_ex2(M - ref);
+      M = m;
+      l *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+#pragma unroll
+      for (int e = 0; e < B; ++e) {
+        const float g = pf_ex2(ml[e].x - ref);
+        l += g * ml[e].y;
+        o.x += g * v[e].x; o.y += g * v[e].y; o.z += g * v[e].z; o.w += g * v[e].w;
+      }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (lane < D / 4)
+      *reinterpret_cast<uint2*>((T*)a.out + (size_t)row * a.out_stride + (size_t)h * D + lane * 4) =
+          make_uint2(Half2<T>::pack(o.x * inv, o.y * inv), Half2<T>::pack(o.z * inv, o.w * inv));
+    if (a.lse && lane == 0) a.lse[(size_t)row * a.n_heads + h] = (M + log2f(l)) * PF_LN2;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (lane < D / 4)
-    *reinterpret_cast<uint2*>((T*)a.out + (size_t)row * a.out_stride + (size_t)h * D + lane * 4) =
-        make_uint2(Half2<T>::pack(o.x * inv, o.y * inv), Half2<T>::pack(o.z * inv, o.w * inv));
-  if (a.lse && lane == 0) a.lse[(size_t)row * a.n_heads + h] = (M + log2f(l)) * PF_LN2;
+}
+
+// Dynamic shared memory beyond 48 KB is asked for once per device and kernel.
+template <auto kernel> int big_smem(int bytes) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  VLAC_CUDA_CHECK(cudaGetDevice(&dev));
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_acquire) & bit) return VLAC_OK;
+  VLAC_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  done.fetch_or(bit, std::memory_order_release);
+  return VLAC_OK;
+}
+#define TRY(x) do { const int rc__ = (x); if (rc__ != VLAC_OK) return rc__; } while (0)
+
+template <typename T, int D, bool QTMA>
+int launch_wide(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq, const WideArgs& w, cudaStream_t s) {
+  TRY((big_smem<prefix_wide_kernel<T, D, QTMA>>(Wide<D>::SMEM)));
+  VLAC_CUDA_CHECK(launch_pdl(prefix_wide_kernel<T, D, QTMA>, dim3(PW_CTAS), dim3(PW_THREADS), Wide<D>::SMEM, s, tk, tv, tq, w));
+  return VLAC_OK;
 }
 
 template <typename T, int D>
-int launch_attention(const vlac_pages* p, const AttnArgs& a, cudaStream_t s) {
+int launch_attention(const AttnArgs& a, cudaStream_t s) {
   // more than 16 stacked rows, or the call cannot have a wide segment
   if ((long long)a.rows * a.ratio > pf_bm(NARROW)) {
     WideArgs w = {a, a.scale2 < 0.f, a.page < 128 ? a.page : 128};
     w.a.scale2 = fmaxf(fabsf(a.scale2), 1e-30f);                        // not zero: -inf marks what is not there
-    CUtensorMap tk, tv;
+    CUtensorMap tk, tv, tq;
     const int rows = a.n_pages << a.shift, cols = a.kv_heads * D;
-    int rc = vlac_encode_map_2d(&tk, a.k, rows, cols, w.box);
-    if (rc == VLAC_OK) rc = vlac_encode_map_2d(&tv, a.v, rows, cols, w.box);
-    if (rc != VLAC_OK) return rc;
-    VLAC_CUDA_CHECK(cudaFuncSetAttribute(prefix_wide_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Wide<D>::SMEM));
-    VLAC_CUDA_CHECK(launch_pdl(prefix_wide_kernel<T, D>, dim3(PW_CTAS), dim3(PW_THREADS), Wide<D>::SMEM, s, tk, tv, w));
+    TRY(vlac_encode_map_2d(&tk, a.k, rows, cols, w.box));
+    TRY(vlac_encode_map_2d(&tv, a.v, rows, cols, w.box));
+    if (!w.flip && 128 % a.ratio == 0) {
+      TRY(vlac_encode_map_heads(&tq, a.q, a.rows, a.n_heads, D, a.q_stride, a.ratio, 128 / a.ratio));
+      TRY((launch_wide<T, D, true>(tk, tv, tq, w, s)));
+    } else
+      TRY((launch_wide<T, D, false>(tk, tv, tk, w, s)));
   }
-  VLAC_CUDA_CHECK(cudaFuncSetAttribute(prefix_narrow_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Narrow<D>::SMEM));
+  TRY((big_smem<prefix_narrow_kernel<T, D>>(Narrow<D>::SMEM)));
   VLAC_CUDA_CHECK(launch_pdl(prefix_narrow_kernel<T, D>, dim3(PN_CTAS), dim3(PN_WARPS * 32), Narrow<D>::SMEM, s, a));
-  const long long warps = (long long)a.rows * a.n_heads;
-  VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, s, a));
+  // shares: an item a warp (what an item costs is the chain of its reads), up to a few waves of CTAs
+  const long long items = (long long)a.rows * a.n_heads;
+  const int shares = (int)std::max(1ll, std::min({(items / a.n + 7) / 8, 4096ll / a.n + 1, 65535ll}));
+  VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D>, dim3(a.n, shares), dim3(256), 0, s, a));
   return VLAC_OK;
 }
 
@@ -1311,10 +1372,10 @@ int vlac_prefix_plan(const vlac_pages* p, const vlac_prefix* plan, const int* se
   a.n = plan->n; a.rows = plan->rows; a.n_heads = plan->n_heads; a.seqs = seqs; a.q_ptr = q_ptr; a.status = status; a.mem = plan->mem;
   const size_t smem = sizeof(PlanShared);
   if (plan->n <= 16 && (long long)plan->n * p->max_pages <= PL_ONE) {
-    VLAC_CUDA_CHECK(cudaFuncSetAttribute(prefix_plan_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    TRY(big_smem<prefix_plan_kernel<1>>((int)smem));
     VLAC_CUDA_CHECK(launch_pdl(prefix_plan_kernel<1>, dim3(1), dim3(256), smem, (cudaStream_t)stream, a));
   } else {
-    VLAC_CUDA_CHECK(cudaFuncSetAttribute(prefix_plan_kernel<PL_CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    TRY(big_smem<prefix_plan_kernel<PL_CTAS>>((int)smem));
     VLAC_CUDA_CHECK(launch_pdl(prefix_plan_kernel<PL_CTAS>, dim3(PL_CTAS), dim3(1024), smem, (cudaStream_t)stream, a));
   }
   return VLAC_OK;
@@ -1346,8 +1407,8 @@ int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* pla
   a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
   a.scale2 = scale * 1.44269504088896f; a.mem = plan->mem;
   cudaStream_t s = (cudaStream_t)stream;
-  if (p->dtype == VLAC_BF16) return p->head_dim == 128 ? launch_attention<__nv_bfloat16, 128>(p, a, s) : launch_attention<__nv_bfloat16, 64>(p, a, s);
-  return p->head_dim == 128 ? launch_attention<__half, 128>(p, a, s) : launch_attention<__half, 64>(p, a, s);
+  if (p->dtype == VLAC_BF16) return p->head_dim == 128 ? launch_attention<__nv_bfloat16, 128>(a, s) : launch_attention<__nv_bfloat16, 64>(a, s);
+  return p->head_dim == 128 ? launch_attention<__half, 128>(a, s) : launch_attention<__half, 64>(a, s);
 }
 
 }  // extern "C"

@@ -137,6 +137,7 @@ int vlac_tc_projector(vlac_ctx* ctx, vlac_cache* c, int* n_splits, cudaStream_t 
 
 // ---- tiled prefill attention (attention_kernels.cu)
 int vlac_encode_map_2d(void* out, const void* base, int rows, int cols, int box_rows);
+int vlac_encode_map_heads(void* out, const void* base, int rows, int heads, int head_dim, long long row_stride, int box_heads, int box_rows);
 int vlac_attention_setup(vlac_ctx* ctx);
 int vlac_attention_cache_setup(vlac_ctx* ctx, vlac_cache* c);
 int vlac_launch_prefill_attention(vlac_ctx* ctx, vlac_cache* c, int layer, cudaStream_t s);
