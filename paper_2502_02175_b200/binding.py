@@ -401,7 +401,7 @@ class Pages:
             assert t.device == k.device and t.dtype == torch.int32 and t.dim() == dims and t.is_contiguous()
         assert len.shape[0] == table.shape[0] and refs.shape[0] == k.shape[1]
         self.k, self.v, self.table, self.len, self.refs = k, v, table, len, refs
-        self.index, self.dtype = k.get_device(), k.dtype
+        self.index, self.dtype, self.n_kv_heads, self.head_dim = k.get_device(), k.dtype, k.shape[3], k.shape[4]
         self.struct = vlac_pages(k.data_ptr(), v.data_ptr(), 0 if k.dtype == torch.bfloat16 else 1, *k.shape, *table.shape,
                                  table.data_ptr(), len.data_ptr(), refs.data_ptr(), None, 0)
         self.ref = C.byref(self.struct)
@@ -438,7 +438,7 @@ def _here(index: int) -> int:
 
 
 def _ints(t: torch.Tensor, n: int, index: int) -> int:
-    assert t.dtype is torch.int32 and t.get_device() == index and t.dim() == 1 and t.size(0) == n and t.is_contiguous()
+    assert t.dtype is torch.int32 and t.get_device() == index and t.numel() == n and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -477,7 +477,7 @@ def vlac_pages_compact(pages: Pages, src: torch.Tensor, dst: torch.Tensor, keep_
 
 def _rows(t: torch.Tensor, heads: int, pages: Pages, rows: int) -> int:
     """Pointer of [rows, heads, head_dim] of the pool's type, heads side by side, any row stride."""
-    d = pages.struct.head_dim
+    d = pages.head_dim
     assert t.dtype is pages.dtype and t.get_device() == pages.index and t.dim() == 3 and t.size(0) == rows and t.size(1) == heads and t.size(2) == d
     assert t.is_contiguous() or rows == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d))
     return t.data_ptr()
@@ -485,13 +485,13 @@ def _rows(t: torch.Tensor, heads: int, pages: Pages, rows: int) -> int:
 
 def _row_stride(t: torch.Tensor) -> int:
     """Elements between rows (a tensor of one row or none may carry any stride)."""
-    return t.stride(0) if t.size(0) > 1 else -(-t.size(1) * t.size(2) // 8) * 8
+    return t.stride(0) if t.size(0) > 1 else t.size(1) * t.size(2)
 
 
 def vlac_pages_write(pages: Pages, layer: int, seqs: torch.Tensor, start: Optional[torch.Tensor], row_ptr: torch.Tensor,
                      k_rows: torch.Tensor, v_rows: torch.Tensor, status: torch.Tensor) -> None:
     """Rows ``row_ptr[i]:row_ptr[i + 1]`` of ``k_rows`` / ``v_rows`` to slot ``seqs[i]`` from position ``start[i]`` on (``None``: its last rows)."""
-    n, dev, rows, heads = seqs.size(0), pages.index, k_rows.size(0), pages.struct.n_kv_heads
+    n, dev, rows, heads = seqs.size(0), pages.index, k_rows.size(0), pages.n_kv_heads
     stream = _here(dev)
     _check(lib.vlac_pages_write(pages.ref, layer, _ints(seqs, n, dev), None if start is None else _ints(start, n, dev), _ints(row_ptr, n + 1, dev), n, rows,
                                 _rows(k_rows, heads, pages, rows), _row_stride(k_rows), _rows(v_rows, heads, pages, rows), _row_stride(v_rows),

@@ -22,11 +22,10 @@ namespace {
 // the rest -- prefixes of few rows and every sequence's own rows, where the causal mask lies (warp-level tensor cores).
 constexpr int NARROW = 0, WIDE = 1;
 constexpr int PN_WARPS = 4, PN_CTAS = 2 * 148;  // narrow: two CTAs of four warps per SM, every warp works alone
-constexpr int PF_MAX_RUNS = PN_WARPS * PN_CTAS; // runs of the narrow kernel
 constexpr int PW_CTAS = 148;                    // runs of the wide kernel: one CTA per SM
 __host__ __device__ constexpr int pf_bm(int c) { return c == NARROW ? 16 : 256; }        // stacked rows of a tile
 __host__ __device__ constexpr int pf_kb(int c) { return c == NARROW ? 64 : 128; }        // keys of a unit
-__host__ __device__ constexpr int pf_runs(int c) { return c == NARROW ? PF_MAX_RUNS : PW_CTAS; }
+__host__ __device__ constexpr int pf_runs(int c) { return c == NARROW ? PN_WARPS * PN_CTAS : PW_CTAS; }     // most runs
 
 struct SeqRec { int slot /* -1: refused */, row0, nq, len, pre_seg, suf_seg, pad0, pad1; };          // segments: -1 none
 struct SegRec {
@@ -46,7 +45,7 @@ struct PlanMem {
   SegRec* seg;                                  // [2n]
   int* first[2];                                // segment of each run's first unit
   float2* ml;                                   // [slot rows] (m, l), m in units of log2
-  float* po;                                    // [slot rows][head_dim]; of wide segments [slot rows / 8][head_dim / 4][8][4] (see wide_at)
+  float* po;                                    // [slot rows][head_dim]
   size_t bytes;
 };
 __host__ __device__ inline PlanMem plan_mem(void* mem, int n, int rows, int n_heads, int head_dim) {
@@ -58,26 +57,22 @@ __host__ __device__ inline PlanMem plan_mem(void* mem, int n, int rows, int n_he
   p.seq = (SeqRec*)take(sizeof(SeqRec) * n);
   p.seg = (SegRec*)take(sizeof(SegRec) * 2 * (size_t)n);
   for (int c = 0; c < 2; ++c) p.first[c] = (int*)take(sizeof(int) * pf_runs(c));
-  // a row and head has at most one narrow and one more segment; wide segments have 17 rows at least and are padded to 8 (24 / 17 < 1.5)
-  const size_t slots = (5 * (size_t)rows * n_heads + 1) / 2 + 8 + (size_t)pf_runs(NARROW) * pf_bm(NARROW) + (size_t)pf_runs(WIDE) * pf_bm(WIDE);
+  const size_t slots = 2 * (size_t)rows * n_heads + (size_t)pf_runs(NARROW) * pf_bm(NARROW) + (size_t)pf_runs(WIDE) * pf_bm(WIDE);
   p.ml = (float2*)take(sizeof(float2) * slots);
   p.po = (float*)take(sizeof(float) * slots * head_dim);
   p.bytes = o;
   return p;
 }
 
-// The U units of a class are dealt to G = min(U, pf_runs) runs, so that none is empty: run c is [c*U/G, (c+1)*U/G).  The run of unit u:
+// The U units of a class are dealt to G = min(U, pf_runs) runs of equal length, so that none is empty: run c is [c*U/G, (c+1)*U/G).
+// (Narrow, measured: three runs a warp, taken up as warps come free, gained nothing -- every run adds a partial sum per row -- although warps
+// of some SMs get their bytes 1.4 times as fast as those of others.)
 __device__ __forceinline__ long long runs(int cls, long long U) { return U < pf_runs(cls) ? U : pf_runs(cls); }
+// The run of unit u:
 __device__ __forceinline__ int run_of(int cls, long long u, long long U) {
   if (U < 1 << 20) return (int)(((unsigned)(u + 1) * (unsigned)runs(cls, U) - 1) / (unsigned)U);         // (a 64-bit division is five times as long)
   return (int)(((u + 1) * runs(cls, U) - 1) / U);
 }
-
-// rows of a segment per K/V head in the slots
-__host__ __device__ inline int pf_rows(int cls, int R) { return cls == NARROW ? R : (R + 7) & ~7; }
-// A wide tile's rows lie one per lane, so its partial sums are laid out for lanes to store side by side: 4 floats c4 of 8 rows after one
-// another (a row-major store of 16 bytes a lane touched 32 rows at once: 3.7 us a tile instead of 1).
-__device__ __forceinline__ size_t wide_at(size_t slot_row, int c4, int head_dim) { return ((slot_row >> 3) * (head_dim / 4) + c4) * 32 + (slot_row & 7) * 4; }
 
 // ------------------------------------------------------------------------------------------------ plan
 struct PlanArgs {
@@ -258,7 +253,7 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
   }
   const bool wide = c_pre == WIDE && u_pre > 0;
   const Sums own = {{(wide ? 0 : u_pre) + u_suf, wide ? u_pre : 0},
-                    {((wide ? 0 : r_pre) + r_suf) * a.kv_heads, wide ? pf_rows(WIDE, r_pre) * a.kv_heads : 0}, (u_pre > 0) + (u_suf > 0)};
+                    {((wide ? 0 : r_pre) + r_suf) * a.kv_heads, wide ? r_pre * a.kv_heads : 0}, (u_pre > 0) + (u_suf > 0)};
   Sums all;
   const Sums at = plan_scan(s.part, own, n_act, &all);
   const int g0 = at.g;
@@ -269,7 +264,7 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
     SeqRec q = {bad ? -1 : s.slot[tid], s.row0[tid], s.nq[tid], s.len[tid], pre > 0 ? s.g[lead] : -1, u_suf > 0 ? g0 + (u_pre > 0) : -1, 0, 0};
     p.seq[tid] = q;
     // slots: the narrow pieces' rows, then the wide ones' (each run sets itself off by a tile, see next_piece)
-    const long long at_w = (all.r[0] + 7) / 8 * 8 + (long long)pf_runs(NARROW) * pf_bm(NARROW);
+    const long long at_w = all.r[0] + (long long)pf_runs(NARROW) * pf_bm(NARROW);
     if (u_pre > 0) {
       const long long us = wide ? at.u[1] : at.u[0];
       SegRec r = {us, us + u_pre, s.slot[tid], s.row0[tid], r_pre, 0, pre, INT_MIN, c_pre, t_pre, kb_pre, (int)(wide ? at_w + at.r[1] : at.r[0])};
@@ -375,7 +370,7 @@ struct Cursor {
     p->lim0 = s.pos0 == INT_MIN ? INT_MIN : s.pos0 + 1;
     p->n = n;
     p->direct = n == s.KB && s.pos0 != INT_MIN && s.key0 == 0;          // a whole tile, and all that its rows see: written as the result
-    p->slot0 = (size_t)s.rowbase + (size_t)head * pf_rows(cls, s.R) + (size_t)rt * bm + (size_t)run * bm;
+    p->slot0 = (size_t)s.rowbase + (size_t)head * s.R + (size_t)rt * bm + (size_t)run * bm;
     kb += n; u += n;
   }
 };
@@ -776,6 +771,13 @@ __device__ __forceinline__ void pw_ld32(unsigned addr, unsigned* r) {
                "%25,%26,%27,%28,%29,%30,%31}, [%32];"
                : PW_R32(r, 0), PW_R32(r, 8), PW_R32(r, 16), PW_R32(r, 24) : "r"(addr));
 }
+// 16 rows (the warp's lanes 0-15 or 16-31 of tensor memory) x 64 columns: registers 4j + {0, 1} are row lane / 4, {2, 3} row lane / 4 + 8, columns
+// 8j + 2 (lane % 4) + {0, 1} (no wait)
+__device__ __forceinline__ void pw_ld_frag(unsigned addr, unsigned* r) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+               "%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : PW_R32(r, 0), PW_R32(r, 8), PW_R32(r, 16), PW_R32(r, 24) : "r"(addr));
+}
 __device__ __forceinline__ void pw_st32(unsigned addr, const unsigned* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
                "%25,%26,%27,%28,%29,%30,%31};"
@@ -1160,45 +1162,51 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       }
       pw_after();
       if (!idle) {
+        // O in the layout of fragments: four lanes hold 32 bytes of a row, which go out together
         if (two) {
           // every side its own rows
-          float* dst = pm.po + wide_at(p.slot0 + row_t, 0, D);
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
+          for (int q = 0; q < 2 * (D / 64); ++q) {
+            const int hf = q & 1, c0 = (q >> 1) * 64, row = row_t - lane + 16 * hf + (lane >> 2);
             unsigned x[32];
-            pw_ld32(o_col + 32u * c, x);
+            pw_ld_frag(o_col + ((unsigned)(16 * hf) << 16) + c0, x);
             pw_ld_wait(x);
-            if (row_t < p.nr) {
+            float* dst = pm.po + (p.slot0 + row) * D + c0 + 2 * (lane & 3);
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(dst + (8 * c + (e >> 2)) * 32) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            for (int j = 0; j < 8; ++j) {
+              if (row < p.nr) *reinterpret_cast<uint2*>(dst + 8 * j) = make_uint2(x[4 * j], x[4 * j + 1]);
+              if (row + 8 < p.nr) *reinterpret_cast<uint2*>(dst + 8 * D + 8 * j) = make_uint2(x[4 * j + 2], x[4 * j + 3]);
             }
           }
           if (row_t < p.nr) pm.ml[p.slot0 + row_t] = make_float2(m, l);
         } else {
-          // the two sides of a row, each thread half of its columns
-          const float m0 = red_m[r], m1 = red_m[128 + r], M = fmaxf(m0, m1), ref = M == -INFINITY ? 0.f : M;
-          const float f0 = pf_ex2(m0 - ref), f1 = pf_ex2(m1 - ref);
+          // the two sides of a row: this side 16 of the warp's 32 rows
           const bool odd = p.n > 1;                                     // one block: the odd side holds nothing
-          float* dst = pm.po + wide_at(p.slot0 + r, side * (D / 8), D);
-#pragma unroll 1
-          for (int c = 0; c < D / 64; ++c) {
-            unsigned x[32], y[32] = {};
-            pw_ld32(trow + 256u + side * (D / 2) + 32u * c, x);
-            if (odd) pw_ld32(trow + 384u + side * (D / 2) + 32u * c, y);
-            pw_ld_wait(x, y);
-            if (r < p.nr) {
+          const int row = 32 * q4 + 16 * side + (lane >> 2);
+          float f0[2], f1[2];
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                float4 o;
-                o.x = f0 * __uint_as_float(x[e]); o.y = f0 * __uint_as_float(x[e + 1]); o.z = f0 * __uint_as_float(x[e + 2]); o.w = f0 * __uint_as_float(x[e + 3]);
-                if (odd) {
-                  o.x += f1 * __uint_as_float(y[e]); o.y += f1 * __uint_as_float(y[e + 1]); o.z += f1 * __uint_as_float(y[e + 2]); o.w += f1 * __uint_as_float(y[e + 3]);
-                }
-                *reinterpret_cast<float4*>(dst + (8 * c + (e >> 2)) * 32) = o;
-              }
-            }
+          for (int e = 0; e < 2; ++e) {
+            const int rr = row + 8 * e;
+            const float m0 = red_m[rr], m1 = red_m[128 + rr], M = fmaxf(m0, m1), ref = M == -INFINITY ? 0.f : M;
+            f0[e] = pf_ex2(m0 - ref); f1[e] = pf_ex2(m1 - ref);
+            if ((lane & 3) == 0 && rr < p.nr) pm.ml[p.slot0 + rr] = make_float2(M, f0[e] * red_l[rr] + (odd ? f1[e] * red_l[128 + rr] : 0.f));
           }
-          if (side == 0 && r < p.nr) pm.ml[p.slot0 + r] = make_float2(M, f0 * red_l[r] + (odd ? f1 * red_l[128 + r] : 0.f));
+#pragma unroll 1
+          for (int c0 = 0; c0 < D; c0 += 64) {
+            unsigned x[32], y[32] = {};
+            pw_ld_frag(trow + ((unsigned)(16 * side) << 16) + 256u + c0, x);
+            if (odd) pw_ld_frag(trow + ((unsigned)(16 * side) << 16) + 384u + c0, y);
+            pw_ld_wait(x, y);
+            float* dst = pm.po + (p.slot0 + row) * D + c0 + 2 * (lane & 3);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                float2 o = make_float2(f0[e] * __uint_as_float(x[4 * j + 2 * e]), f0[e] * __uint_as_float(x[4 * j + 2 * e + 1]));
+                if (odd) { o.x += f1[e] * __uint_as_float(y[4 * j + 2 * e]); o.y += f1[e] * __uint_as_float(y[4 * j + 2 * e + 1]); }
+                if (row + 8 * e < p.nr) *reinterpret_cast<float2*>(dst + e * 8 * D + 8 * j) = o;
+              }
+          }
         }
       }
       if (!more) break;
@@ -1218,8 +1226,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
 }
 
 // Pieces to results: grid (sequences, shares); a warp takes (K/V head, stacked row) items of its sequence and adds the pieces of the row's
-// prefix and of its own segment in order, partial sums and their (m, l) read together.  The warps of a CTA take rows that follow one
-// another (they share the sectors of wide partial sums).
+// prefix and of its own segment in order, eight partial sums and their (m, l) in flight.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
   const PlanMem p = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
@@ -1236,7 +1243,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
   const int c4 = lane < D / 4 ? lane : 0;
   for (int it = blockIdx.y * 8 + (threadIdx.x >> 5); it < items; it += gridDim.y * 8) {
     const int kvh = it / per, xr = it - kvh * per, xq = xr / a.ratio, row = q.row0 + xq, h = kvh * a.ratio + xr - xq * a.ratio;
-    int np[2] = {0, 0}, pad[2] = {0, 0}, wide = 0;
+    int np[2] = {0, 0}, pad[2] = {0, 0};
     size_t base[2] = {0, 0};
     bool done = false;
 #pragma unroll
@@ -1249,8 +1256,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
       if (s.pos0 != INT_MIN && s.key0 == 0 && c0 == c1) done = true;    // written by its only piece
       np[i] = c1 - c0 + 1;
       pad[i] = bm;
-      if (s.cls == WIDE) wide = 1;                                      // (only a prefix is wide)
-      base[i] = (size_t)s.rowbase + (size_t)kvh * pf_rows(s.cls, s.R) + x + (size_t)c0 * bm;
+      base[i] = (size_t)s.rowbase + (size_t)kvh * s.R + x + (size_t)c0 * bm;
     }
     if (done) continue;
     const int n = np[0] + np[1];
@@ -1268,7 +1274,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
         if (i < n) {
           const size_t sl = first ? base[0] + (size_t)i * pad[0] : base[1] + (size_t)(i - np[0]) * pad[1];
           ml[e] = p.ml[sl];
-          v[e] = *reinterpret_cast<const float4*>(p.po + (wide && first ? wide_at(sl, c4, D) : sl * D + c4 * 4));
+          v[e] = *reinterpret_cast<const float4*>(p.po + sl * D + c4 * 4);
         }
       }
       float m = M;

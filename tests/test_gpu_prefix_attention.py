@@ -216,6 +216,19 @@ def test_extreme_scores(vb):
         c.check(*c.run())
 
 
+def test_more_work_than_warps(vb):
+    """Runs of many units that cut tiles and span pieces: the same bits every time, one plan for several layers."""
+    c = Case(vb, [(390, [(n % 5 + 1, 1) for n in range(3)])] + [(0, [(380 + n, 1)]) for n in range(60)], 32, 32, 64, layers=2, seed=14)
+    plan = vb.PrefixPlan(c.pages, len(c.seqs), c.rows, c.heads)
+    first = c.run(plan=plan)
+    c.check(*first, only=(0, 2, 3, 40, 62))
+    for layer in (1, 0, 1):
+        out, lse = torch.zeros_like(first[0]), torch.zeros_like(first[1])
+        vb.vlac_prefix_attention(c.pages, layer, plan, c.q, c.scale, out, lse)
+        c.check(out, lse, layer, only=(1, 20, 62))
+        assert layer == 1 or (torch.equal(out, first[0]) and torch.equal(lse, first[1]))
+
+
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
 def test_scales(vb, scale):
     """Any finite scale, negative ones and zero included, on narrow and wide segments."""
