@@ -28,7 +28,7 @@ __host__ __device__ constexpr int pf_kb(int c) { return c == NARROW ? 64 : 128; 
 __host__ __device__ constexpr int pf_runs(int c) { return c == NARROW ? PN_WARPS * PN_CTAS : PW_CTAS; }     // most runs
 
 struct SeqRec { int slot /* -1: refused */, row0, nq, len, pre_seg, suf_seg, pad0, pad1; };          // segments: -1 none
-struct SegRec {
+struct __align__(16) SegRec {
   long long ustart, uend;                       // units of this segment in the call's order
   int slot;                                     // whose table holds the keys
   int row0, R;                                  // first q row; stacked rows per K/V head: (q rows) * (query heads per K/V head)
@@ -335,6 +335,15 @@ struct Piece {
   int direct;
   size_t slot0;                                 // slot row of the tile's first row
 };
+// (through L2: the narrow kernel may start before the kernel in front of it has ended, and with it the life of what L1 holds)
+__device__ __forceinline__ SegRec load_seg(const SegRec* p) {
+  static_assert(sizeof(SegRec) % 16 == 0, "whole 16-byte pieces");
+  union { SegRec s; int4 v[sizeof(SegRec) / 16]; } u;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(SegRec) / 16); ++i) u.v[i] = __ldcg(reinterpret_cast<const int4*>(p) + i);
+  return u.s;
+}
+
 // Walks a run's pieces: one division to find the first, then tile after tile, segment after segment.
 struct Cursor {
   long long u, u_end;                           // next unit, end of the run
@@ -346,8 +355,8 @@ struct Cursor {
     if (U < 1 << 20) {                          // (a 64-bit division is five times as long)
       u = (unsigned)r * (unsigned)U / (unsigned)G; u_end = (unsigned)(r + 1) * (unsigned)U / (unsigned)G;
     } else { u = r * U / G; u_end = (r + 1) * U / G; }
-    s = pm.seg[g];
-    while (u >= s.uend || s.cls != cls) s = pm.seg[++g];
+    s = load_seg(pm.seg + g);
+    while (u >= s.uend || s.cls != cls) s = load_seg(pm.seg + ++g);
     const long long local = u - s.ustart, per_head = (long long)s.T * s.KB;
     head = (int)(local / per_head);
     const long long rem = local - head * per_head;
@@ -359,7 +368,7 @@ struct Cursor {
       kb = 0;
       if (++rt == s.T) { rt = 0; ++head; }
       if (u >= s.uend) {
-        do s = pm.seg[++g]; while (u >= s.uend || s.cls != cls);
+        do s = load_seg(pm.seg + ++g); while (u >= s.uend || s.cls != cls);
         head = 0;
       }
     }
@@ -417,7 +426,9 @@ __device__ __forceinline__ bool any_nonfinite(uint4 x) {
   return r;
 }
 
-template <typename T, int D>
+// EARLY: behind the wide kernel of the same call, of which it reads nothing.  That kernel lets its successor start only once it has seen the plan
+// complete, so the CTAs here begin as SMs come free and wait for its end before their own (what comes after reads both).
+template <typename T, int D, bool EARLY>
 __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArgs a) {
   using N = Narrow<D>;
   constexpr int STEP = N::STEP, NB = STEP / 16;                         // blocks of 16 keys in a step
@@ -426,11 +437,11 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
   const PlanMem pm = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_trigger();
-  pdl_wait();
+  if (!EARLY) pdl_wait();
   const int run = warp * PN_CTAS + blockIdx.x;                          // few runs: one per SM before two
-  const long long U = pm.head->units[NARROW], G = runs(NARROW, U);
-  const int g = pm.first[NARROW][run];
-  if (run >= G) return;
+  const long long U = __ldcg(&pm.head->units[NARROW]), G = runs(NARROW, U);
+  const int g = __ldcg(&pm.first[NARROW][run]);
+  if (run >= G) { if (EARLY) pdl_wait(); return; }
   Cursor cur;                                                           // pieces not yet begun
   cur.begin(pm, NARROW, run, U, G, g);
 
@@ -478,7 +489,7 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
     if (at == 0 && !(pg_slot == lp.slot && pg_key == k0 && pg_end == lp.key1)) {             // (the next head's piece begins where the last one did)
       const int k = k0 + (lane << page_step);
       pg_slot = lp.slot; pg_key = k0; pg_end = lp.key1;
-      pg = k < lp.key1 ? a.table[(size_t)lp.slot * a.max_pages + (k >> a.shift)] : -1;
+      pg = k < lp.key1 ? __ldcg(&a.table[(size_t)lp.slot * a.max_pages + (k >> a.shift)]) : -1;
       if ((unsigned)pg >= (unsigned)a.n_pages) pg = -1;
     }
     const unsigned ks = ring + (unsigned)(l_cnt % PN_STAGES) * 2u * N::TILE + col_off;
@@ -664,6 +675,7 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
     }
     __syncwarp();                                                       // the step's tiles (and the piece record) may be refilled
   }
+  if (EARLY) pdl_wait();
 }
 
 // ------------------------------------------------------------------------------------------------ wide: tcgen05
@@ -1226,9 +1238,13 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
 }
 
 // Pieces to results: grid (sequences, shares); a warp takes (K/V head, stacked row) items of its sequence and adds the pieces of the row's
-// prefix and of its own segment in order, eight partial sums and their (m, l) in flight.
-template <typename T, int D>
+// prefix and of its own segment in order, eight partial sums and their (m, l) in flight.  SHARE, for calls of few items, which may have hundreds
+// of pieces each: a CTA takes an item, its warps every eighth piece, and their sums are added in order.
+template <typename T, int D, bool SHARE>
 __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
+  __shared__ float4 s_o[SHARE ? 8 : 1][D / 4];
+  __shared__ float2 s_ml[8];
+  const int warp = threadIdx.x >> 5;
   const PlanMem p = plan_mem(a.mem, a.n, a.rows, a.n_heads, D);
   const int lane = threadIdx.x & 31;
   pdl_trigger();
@@ -1241,7 +1257,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
   for (int i = 0; i < 2; ++i) sg[i] = p.seg[max(0, i ? q.suf_seg : q.pre_seg)];
   const int per = q.nq * a.ratio, items = per * a.kv_heads;
   const int c4 = lane < D / 4 ? lane : 0;
-  for (int it = blockIdx.y * 8 + (threadIdx.x >> 5); it < items; it += gridDim.y * 8) {
+  for (int it = SHARE ? blockIdx.y : blockIdx.y * 8 + warp; it < items; it += SHARE ? gridDim.y : gridDim.y * 8) {
     const int kvh = it / per, xr = it - kvh * per, xq = xr / a.ratio, row = q.row0 + xq, h = kvh * a.ratio + xr - xq * a.ratio;
     int np[2] = {0, 0}, pad[2] = {0, 0};
     size_t base[2] = {0, 0};
@@ -1262,13 +1278,14 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
     const int n = np[0] + np[1];
     float M = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int B = 8;                                                // partial sums in flight
-    for (int i0 = 0; i0 < n; i0 += B) {
+    constexpr int B = SHARE ? 4 : 8;                                    // partial sums in flight (of a warp)
+    const int step = SHARE ? 8 : 1;
+    for (int i0 = SHARE ? warp : 0; i0 < n; i0 += B * step) {
       float2 ml[B];
       float4 v[B];
 #pragma unroll
       for (int e = 0; e < B; ++e) {
-        const int i = i0 + e, first = i < np[0];
+        const int i = i0 + e * step, first = i < np[0];
         ml[e] = make_float2(-INFINITY, 0.f);
         v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (i < n) {
@@ -1289,6 +1306,27 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
         l += g * ml[e].y;
         o.x += g * v[e].x; o.y += g * v[e].y; o.z += g * v[e].z; o.w += g * v[e].w;
       }
+    }
+    if (SHARE) {
+      if (lane < D / 4) s_o[warp][lane] = o;
+      if (lane == 0) s_ml[warp] = make_float2(M, l);
+      __syncthreads();
+      if (warp == 0) {
+        M = -INFINITY; l = 0.f;
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) M = fmaxf(M, s_ml[e].x);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float g = pf_ex2(s_ml[e].x - ref);
+          const float4 v = s_o[e][c4];
+          l += g * s_ml[e].y;
+          o.x += g * v.x; o.y += g * v.y; o.z += g * v.z; o.w += g * v.w;
+        }
+      }
+      __syncthreads();
+      if (warp != 0) continue;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (lane < D / 4)
@@ -1318,6 +1356,13 @@ int launch_wide(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap&
   return VLAC_OK;
 }
 
+template <typename T, int D, bool EARLY>
+int launch_narrow(const AttnArgs& a, cudaStream_t s) {
+  TRY((big_smem<prefix_narrow_kernel<T, D, EARLY>>(Narrow<D>::SMEM)));
+  VLAC_CUDA_CHECK(launch_pdl(prefix_narrow_kernel<T, D, EARLY>, dim3(PN_CTAS), dim3(PN_WARPS * 32), Narrow<D>::SMEM, s, a));
+  return VLAC_OK;
+}
+
 template <typename T, int D>
 int launch_attention(const AttnArgs& a, cudaStream_t s) {
   // more than 16 stacked rows, or the call cannot have a wide segment
@@ -1333,13 +1378,18 @@ int launch_attention(const AttnArgs& a, cudaStream_t s) {
       TRY((launch_wide<T, D, true>(tk, tv, tq, w, s)));
     } else
       TRY((launch_wide<T, D, false>(tk, tv, tk, w, s)));
+    TRY((launch_narrow<T, D, true>(a, s)));
+  } else
+    TRY((launch_narrow<T, D, false>(a, s)));
+  // an item a CTA while the GPU holds them in two waves, else an item a warp (what an item costs is the chain of its reads): 32 rows behind
+  // 32,768 positions of 8 heads 33 us against 46, but 1024 items behind 65,600 84 against 79
+  const long long items = (long long)a.rows * a.n_heads, mean = (items + a.n - 1) / a.n;
+  if (items <= 592) {
+    VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D, true>, dim3(a.n, (unsigned)mean), dim3(256), 0, s, a));
+  } else {
+    const int shares = (int)std::max(1ll, std::min({(mean + 7) / 8, 4096ll / a.n + 1, 65535ll}));
+    VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D, false>, dim3(a.n, shares), dim3(256), 0, s, a));
   }
-  TRY((big_smem<prefix_narrow_kernel<T, D>>(Narrow<D>::SMEM)));
-  VLAC_CUDA_CHECK(launch_pdl(prefix_narrow_kernel<T, D>, dim3(PN_CTAS), dim3(PN_WARPS * 32), Narrow<D>::SMEM, s, a));
-  // shares: an item a warp (what an item costs is the chain of its reads), up to a few waves of CTAs
-  const long long items = (long long)a.rows * a.n_heads;
-  const int shares = (int)std::max(1ll, std::min({(items / a.n + 7) / 8, 4096ll / a.n + 1, 65535ll}));
-  VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D>, dim3(a.n, shares), dim3(256), 0, s, a));
   return VLAC_OK;
 }
 
