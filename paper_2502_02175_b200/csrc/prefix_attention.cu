@@ -1238,10 +1238,10 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
 }
 
 // Pieces to results: grid (sequences, shares); a warp takes (K/V head, stacked row) items of its sequence and adds the pieces of the row's
-// prefix and of its own segment in order, eight partial sums and their (m, l) in flight.  SHARE, for calls of few items, which may have hundreds
+// prefix and of its own segment in order, B partial sums and their (m, l) in flight.  SHARE, for calls of few items, which may have hundreds
 // of pieces each: a CTA takes an item, its warps every eighth piece, and their sums are added in order.
-template <typename T, int D, bool SHARE>
-__global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
+template <typename T, int D, bool SHARE, int B, int OCC>
+__global__ void __launch_bounds__(256, OCC) prefix_join_kernel(AttnArgs a) {
   __shared__ float4 s_o[SHARE ? 8 : 1][D / 4];
   __shared__ float2 s_ml[8];
   const int warp = threadIdx.x >> 5;
@@ -1278,7 +1278,6 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnArgs a) {
     const int n = np[0] + np[1];
     float M = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int B = SHARE ? 4 : 8;                                    // partial sums in flight (of a warp)
     const int step = SHARE ? 8 : 1;
     for (int i0 = SHARE ? warp : 0; i0 < n; i0 += B * step) {
       float2 ml[B];
@@ -1384,12 +1383,11 @@ int launch_attention(const AttnArgs& a, cudaStream_t s) {
   // an item a CTA while the GPU holds them in two waves, else an item a warp (what an item costs is the chain of its reads): 32 rows behind
   // 32,768 positions of 8 heads 33 us against 46, but 1024 items behind 65,600 84 against 79
   const long long items = (long long)a.rows * a.n_heads, mean = (items + a.n - 1) / a.n;
-  if (items <= 592) {
-    VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D, true>, dim3(a.n, (unsigned)mean), dim3(256), 0, s, a));
-  } else {
-    const int shares = (int)std::max(1ll, std::min({(mean + 7) / 8, 4096ll / a.n + 1, 65535ll}));
-    VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D, false>, dim3(a.n, shares), dim3(256), 0, s, a));
-  }
+  // (a row's pieces are about as many as runs per tile: more items, fewer pieces, and then more warps in flight count for more than loads)
+  const dim3 grid(a.n, (unsigned)std::max(1ll, std::min({(mean + 7) / 8, 4096ll / a.n + 1, 65535ll})));
+  if (items <= 592) VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D, true, 4, 2>, dim3(a.n, (unsigned)mean), dim3(256), 0, s, a));
+  else if (items < 8192) VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D, false, 8, 2>, grid, dim3(256), 0, s, a));
+  else VLAC_CUDA_CHECK(launch_pdl(prefix_join_kernel<T, D, false, 4, 4>, grid, dim3(256), 0, s, a));
   return VLAC_OK;
 }
 
