@@ -54,25 +54,23 @@ __device__ __forceinline__ int slot_of(const int* list, int i, int n_slots) {
   return (unsigned)s < (unsigned)n_slots ? s : -1;
 }
 
-// exclusive sum of v over the block (blockDim = 1024), total in *total; 64-bit: needs of bad lists may be large
-__device__ long long block_scan(long long v, long long* total) {
-  __shared__ long long part[33];
+// exclusive sum of v over the block (blockDim = 1024), total in *total; the 64-bit form for needs of bad lists, which may be large
+template <typename I>
+__device__ I block_scan(I v, I* total) {
+  __shared__ I part[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long x = v;
+  I x = v;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += t; }
+  for (int o = 1; o < 32; o <<= 1) { const I t = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += t; }
   __syncthreads();                              // part may still be read by the previous scan
   if (lane == 31) part[warp] = x;
   __syncthreads();
-  if (warp == 0) {
-    long long y = part[lane];
+  I y = part[lane];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, y, o); if (lane >= o) y += t; }
-    part[lane] = y;
-  }
-  __syncthreads();
-  *total = part[31];
-  return x - v + (warp ? part[warp - 1] : 0);
+  for (int o = 1; o < 32; o <<= 1) { const I t = __shfl_up_sync(0xffffffffu, y, o); if (lane >= o) y += t; }
+  *total = __shfl_sync(0xffffffffu, y, 31);
+  const I before = __shfl_sync(0xffffffffu, y, warp ? warp - 1 : 0);
+  return x - v + (warp ? before : 0);
 }
 
 __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1) pages_book_kernel(BookArgs a) {
@@ -117,11 +115,17 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
     else {
       const int ps = (ls + a.page - 1) >> a.shift, pd = (ld + a.page - 1) >> a.shift;
       const int *ts = a.table + (size_t)s * a.max_pages, *td = a.table + (size_t)d * a.max_pages;
-#pragma unroll 4
-      for (int j = at0; j < ps; j += step) bad |= (unsigned)ts[j] >= (unsigned)a.n_pages;
-      if (d != s)
-#pragma unroll 4
-        for (int j = at0; j < pd; j += step) bad |= (unsigned)td[j] >= (unsigned)a.n_pages;
+      for (int j0 = at0; j0 < max(ps, d == s ? 0 : pd); j0 += step * 4) {
+        int x[4], y[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int j = j0 + q * step;
+          x[q] = j < ps ? ts[j] : 0;
+          y[q] = d != s && j < pd ? td[j] : 0;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) bad |= (unsigned)x[q] >= (unsigned)a.n_pages || (unsigned)y[q] >= (unsigned)a.n_pages;
+      }
       if (a.op == OP_COMPACT) {
         const int k0 = a.keep_ptr[i], k1 = a.keep_ptr[i + 1];
         if (k0 >= 0 && k1 >= k0 && k1 <= a.n_keep) {
@@ -176,7 +180,7 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
   if (status != VLAC_OK) total = shared = rows = 0;
   const int need = total - shared;
   long long need_all;
-  const long long start = block_scan(need, &need_all);
+  const long long start = block_scan((long long)need, &need_all);
   if (tid < a.n) {
     s_dst[tid] = status == VLAC_OK ? d : -1;
     s_src[tid] = s; s_shared[tid] = shared; s_total[tid] = total; s_had[tid] = had;
@@ -189,34 +193,41 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
     if (t < 0 || (a.op == OP_COMPACT && s_src[i] == t)) continue;
     int* td = a.table + (size_t)t * a.max_pages;
     const int pd = (a.len[t] + a.page - 1) >> a.shift;
-#pragma unroll 4
-    for (int j = (a.op == OP_RESIZE ? s_shared[i] : 0) + at0; j < pd; j += step) {
-      atomicSub(&a.refs[td[j]], 1);
-      td[j] = -1;
+    for (int j0 = (a.op == OP_RESIZE ? s_shared[i] : 0) + at0; j0 < pd; j0 += step * 8) {
+      int page[8];                                                      // (loads first: each would wait for the write before it)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) { const int j = j0 + q * step; page[q] = j < pd ? td[j] : -1; }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) { const int j = j0 + q * step; if (j < pd) { atomicSub(&a.refs[page[q]], 1); td[j] = -1; } }
     }
   }
   cluster_sync_all();
 
-  // ---- 4: free pages in ascending order.  CTA r owns a run of pages; first the counts, then the ranks.
-  const int per = ((a.n_pages + PB_CTAS * 4 - 1) / (PB_CTAS * 4)) * 4;      // multiple of 4: 16-byte loads
-  const int p0 = min(a.n_pages, rank * per), p1 = min(a.n_pages, p0 + per);
-  auto free4 = [&](int p) -> int {                                        // bits of pages p .. p+3 that are free
-    if (p + 3 < p1) {
-      const int4 r = __ldcg(reinterpret_cast<const int4*>(a.refs + p));
-      return (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
-    }
-    int m = 0;
-    for (int q = 0; q < 4; ++q) if (p + q < p1 && __ldcg(a.refs + p + q) == 0) m |= 1 << q;
+  // ---- 4: free pages in ascending order.  CTA r owns a run of pages, looked at 16384 at a time: 512 to a warp, 16 to a lane, 32 side by side
+  // (so that pages and list entries are written side by side too); first the counts, then the ranks.
+  constexpr int LOOK = PB_THREADS * 16;
+  const int per = ((a.n_pages + PB_CTAS * 32 - 1) / (PB_CTAS * 32)) * 32;
+  const int p0 = min(a.n_pages, rank * per), p1 = min(a.n_pages, p0 + per), mine = (tid >> 5) * 512 + lane;
+  auto free16 = [&](int p) -> unsigned {                                 // bit g: page p + 32 g is free
+    int r[16];
+    unsigned m = 0;
+#pragma unroll
+    for (int g = 0; g < 16; ++g) r[g] = p + 32 * g < p1 ? __ldcg(a.refs + p + 32 * g) : 1;
+#pragma unroll
+    for (int g = 0; g < 16; ++g) m |= (r[g] == 0 ? 1u : 0u) << g;
     return m;
   };
   if (tid == 0) s_red = 0;
   __syncthreads();
+  unsigned mask = 0;                                                     // of the first look
   if (need_all > 0) {
     int c = 0;
-#pragma unroll 4
-    for (int p = p0 + tid * 4; p < p1; p += PB_THREADS * 4) c += __popc(free4(p));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+    for (int p = p0; p < p1; p += LOOK) {
+      const unsigned m = free16(p + mine);
+      if (p == p0) mask = m;
+      c += __popc(m);
+    }
+    c = __reduce_add_sync(0xffffffffu, c);
     if (lane == 0) atomicAdd(&s_red, c);
   }
   __syncthreads();
@@ -241,13 +252,22 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
       if (tid == 0) w.taken[0] = taken;
     }
   }
-  for (int p = p0; p < p1 && before < taken; p += PB_THREADS * 4) {       // uniform over the CTA
-    const int q = p + tid * 4, m = q < p1 ? free4(q) : 0;
-    long long all;
-    long long at = before + block_scan(__popc(m), &all);
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-      if (m >> b & 1) { if (at < taken) { w.list[at] = q + b; a.refs[q + b] = 1; } ++at; }
+  for (int p = p0; p < p1 && before < taken; p += LOOK) {                 // uniform over the CTA
+    const unsigned m = p == p0 ? mask : free16(p + mine);
+    const int count = __reduce_add_sync(0xffffffffu, __popc(m));
+    int all;
+    long long at = before + block_scan(lane == 31 ? count : 0, &all);    // (lane 31 holds its warp's count, every lane the sum before it)
+    at = __shfl_sync(0xffffffffu, at, 0);
+    for (int g = 0; g < 16 && at < taken; ++g) {
+      const unsigned b = __ballot_sync(0xffffffffu, m >> g & 1);
+      const long long i = at + __popc(b & ((1u << lane) - 1));
+      if ((m >> g & 1) && i < taken) {
+        const int page = p + mine + 32 * g;
+        w.list[i] = page;
+        a.refs[page] = 1;
+      }
+      at += __popc(b);
+    }
     before += all;
   }
   cluster_sync_all();
