@@ -485,58 +485,67 @@ __global__ void __launch_bounds__(PO_THREADS, 1) pages_book_one_kernel(BookArgs 
 }
 
 // ------------------------------------------------------------------------------------------------
-// Rows of the new pages of a fork / compaction: unit = (new page, layer); a CTA of 256 threads moves its K and V rows with
-// 16-byte accesses, four of each in flight per thread.  HBM-bound: read once, written once.
+// Rows of the new pages of a fork / compaction: unit = (new page, layer, part of the page's rows, at most 32 KB of K and of V); a CTA of 256
+// threads moves it with 16-byte accesses, four of K and four of V in flight per thread.  HBM-bound: read once, written once.
 constexpr int PC_THREADS = 256;
+struct Rows16 {                                 // rows of 16-byte pieces
+  int n;                                        // pieces of a row
+  int shift;                                    // log2(n), or -1
+  __device__ __forceinline__ int row(int c) const { return shift >= 0 ? c >> shift : c / n; }
+  __device__ __forceinline__ int col(int c, int r) const { return c - r * n; }
+};
 struct CopyArgs {
   uint4 *k, *v;
   const int *table;
   int* work;
   int n_slots, max_pages, n_pages, page, shift, n_layers, n;
-  int row16;                                    // 16-byte pieces of a row
+  Rows16 row16;
+  int part_rows, parts;                         // rows of a part, parts of a page
   const int *keep_ptr, *keep;                   // NULL: row at position x is row x of the source
 };
 
 __global__ void __launch_bounds__(PC_THREADS) pages_copy_kernel(CopyArgs a) {
   __shared__ int s_start[VLAC_PAGES_MAX_LIST];  // first new page of each entry (not decreasing)
-  __shared__ long long s_from[256];             // source row of each row of the page
+  __shared__ long long s_from[256];             // source row of each row of the part
   __shared__ int s_rows;
   __shared__ long long s_to;
   const int tid = threadIdx.x;
   const PagesWork w = pages_work(a.work, a.n_slots, a.n_pages);
   pdl_wait();
   const int taken = w.taken[0];
-  const long long units = (long long)taken * a.n_layers;
+  const long long per_layer = (long long)taken * a.parts, units = per_layer * a.n_layers;
   if ((long long)blockIdx.x >= units) return;
   for (int i = tid; i < a.n; i += PC_THREADS) s_start[i] = w.start[i];
-  const size_t layer16 = ((size_t)a.n_pages << a.shift) * a.row16;
+  const size_t layer16 = ((size_t)a.n_pages << a.shift) * a.row16.n;
   for (long long u = blockIdx.x; u < units; u += gridDim.x) {
-    const int np = (int)(u % taken), layer = (int)(u / taken);
+    const int layer = (int)(u / per_layer), in = (int)(u - layer * per_layer), np = in / a.parts, r0 = (in - np * a.parts) * a.part_rows;
     __syncthreads();
     // the entry that owns new page np: the last with start <= np (entries that take none share their successor's start)
     int lo = 0, hi = a.n - 1;
     while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (s_start[m] <= np) lo = m; else hi = m - 1; }
     const int e = lo, shared = w.shared[e], src = w.src[e], dst = w.dst[e];
-    const int j = shared + np - s_start[e], first = j << a.shift;
-    const int rows = w.ok[e] ? min(a.page, w.rows[e] - first) : 0;
+    const int j = shared + np - s_start[e], first = (j << a.shift) + r0;
+    const int rows = w.ok[e] ? min(a.part_rows, w.rows[e] - first) : 0;
     if (tid < rows) {
       const int x = first + tid, y = a.keep_ptr ? a.keep[a.keep_ptr[e] + x] : x;
       const int* from = (src == dst ? w.old : a.table) + (size_t)src * a.max_pages;
       s_from[tid] = ((long long)from[y >> a.shift] << a.shift) + (y & (a.page - 1));
     }
-    if (tid == 0) { s_rows = rows; s_to = (long long)w.list[np] << a.shift; }
+    if (tid == 0) { s_rows = rows; s_to = ((long long)w.list[np] << a.shift) + r0; }
     __syncthreads();
-    const int n16 = s_rows * a.row16;
+    const int n16 = max(0, s_rows) * a.row16.n;
     const size_t base = (size_t)layer * layer16;
-    uint4 *ko = a.k + base + (size_t)s_to * a.row16, *vo = a.v + base + (size_t)s_to * a.row16;
+    const uint4 *kl = a.k + base, *vl = a.v + base;
+    uint4 *ko = a.k + base + (size_t)s_to * a.row16.n, *vo = a.v + base + (size_t)s_to * a.row16.n;
     for (int c0 = tid; c0 < n16; c0 += PC_THREADS * 4) {
       uint4 x[4], y[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int c = c0 + q * PC_THREADS;
         if (c < n16) {
-          const size_t at = base + (size_t)s_from[c / a.row16] * a.row16 + c % a.row16;
-          x[q] = a.k[at]; y[q] = a.v[at];
+          const int r = a.row16.row(c);
+          const size_t at = (size_t)s_from[r] * a.row16.n + a.row16.col(c, r);
+          x[q] = kl[at]; y[q] = vl[at];
         }
       }
 #pragma unroll
@@ -556,7 +565,8 @@ constexpr int PR_ROWS = 8;                      // rows of K and of V per group
 struct WriteArgs {
   uint4 *k, *v;
   const int *table, *len, *refs;
-  int n_slots, max_pages, n_pages, page, shift, row16, layer, n, rows;
+  int n_slots, max_pages, n_pages, page, shift, layer, n, rows;
+  Rows16 row16;
   const int *seqs, *start, *row_ptr;            // NULL seqs: one entry, `slot`, rows 0 .. rows-1 at position 0
   int slot;
   const uint4 *kin, *vin;
@@ -593,26 +603,26 @@ __global__ void __launch_bounds__(PR_THREADS) pages_write_kernel(WriteArgs a) {
   if (__syncthreads_or(bad) && code == 0) code = VLAC_ERR_BAD_STATE;
   if (tid == 0 && blockIdx.x == 0 && blockIdx.z == 0) a.status[i] = code;
   if (code != 0) return;
-  const size_t base = (size_t)(a.layer + blockIdx.z) * ((size_t)a.n_pages << a.shift) * a.row16;
+  const size_t base = (size_t)(a.layer + blockIdx.z) * ((size_t)a.n_pages << a.shift) * a.row16.n;
   const uint4 *kin = a.kin + blockIdx.z * a.layer_stride16, *vin = a.vin + blockIdx.z * a.layer_stride16;
   for (int g = r0 + blockIdx.x * PR_ROWS; g < r1; g += gridDim.x * PR_ROWS) {
-    const int n16 = min(PR_ROWS, r1 - g) * a.row16;
+    const int n16 = min(PR_ROWS, r1 - g) * a.row16.n;
     for (int c0 = tid; c0 < n16; c0 += PR_THREADS * 4) {
       uint4 x[4], y[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int c = c0 + q * PR_THREADS;
         if (c < n16) {
-          const int r = g + c / a.row16, o = c % a.row16;
-          x[q] = kin[(size_t)r * a.kstride16 + o]; y[q] = vin[(size_t)r * a.vstride16 + o];
+          const int r = a.row16.row(c), o = a.row16.col(c, r);
+          x[q] = kin[(size_t)(g + r) * a.kstride16 + o]; y[q] = vin[(size_t)(g + r) * a.vstride16 + o];
         }
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int c = c0 + q * PR_THREADS;
         if (c < n16) {
-          const int at = pos + (g - r0) + c / a.row16;
-          const size_t to = base + (((size_t)t[at >> a.shift] << a.shift) + (at & (a.page - 1))) * a.row16 + c % a.row16;
+          const int r = a.row16.row(c), at = pos + (g - r0) + r;
+          const size_t to = base + (((size_t)t[at >> a.shift] << a.shift) + (at & (a.page - 1))) * a.row16.n + a.row16.col(c, r);
           a.k[to] = x[q]; a.v[to] = y[q];
         }
       }
@@ -625,6 +635,11 @@ int sm_count(int* out) {
   VLAC_CUDA_CHECK(cudaGetDevice(&dev));
   VLAC_CUDA_CHECK(cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev));
   return VLAC_OK;
+}
+
+Rows16 rows16(const vlac_pages* p) {
+  const int n = (int)(pages_row(p) / 8);
+  return {n, n & (n - 1) ? -1 : pages_shift(n)};
 }
 
 int list_check(int n) {
@@ -650,7 +665,11 @@ int book(const vlac_pages* p, int op, const int* src, const int* dst, const int*
   CopyArgs c = {};
   c.k = (uint4*)p->k; c.v = (uint4*)p->v; c.table = p->table; c.work = (int*)p->work;
   c.n_slots = p->n_slots; c.max_pages = p->max_pages; c.n_pages = p->n_pages; c.page = p->page_size; c.shift = b.shift;
-  c.n_layers = p->n_layers; c.n = n; c.row16 = (int)(pages_row(p) / 8); c.keep_ptr = keep_ptr; c.keep = keep;
+  c.n_layers = p->n_layers; c.n = n; c.row16 = rows16(p);
+  c.part_rows = p->page_size;
+  while (c.part_rows > 1 && (long long)c.part_rows * c.row16.n > 2048) c.part_rows /= 2;
+  c.parts = p->page_size / c.part_rows;
+  c.keep_ptr = keep_ptr; c.keep = keep;
   VLAC_CUDA_CHECK(launch_pdl(pages_copy_kernel, dim3(n_sm * 8), dim3(PC_THREADS), 0, s, c));
   return VLAC_OK;
 }
@@ -661,7 +680,7 @@ int write_rows(const vlac_pages* p, WriteArgs a, int n, int layers, cudaStream_t
   if (rc != VLAC_OK) return rc;
   a.k = (uint4*)p->k; a.v = (uint4*)p->v; a.table = p->table; a.len = p->len; a.refs = p->refs;
   a.n_slots = p->n_slots; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size; a.shift = pages_shift(p->page_size);
-  a.row16 = (int)(pages_row(p) / 8); a.n = n;
+  a.row16 = rows16(p); a.n = n;
   // enough CTAs for the whole GPU; no more per entry than one entry could use
   const int groups = (a.rows + PR_ROWS - 1) / PR_ROWS, spread = (n_sm * 8 + n * layers - 1) / (n * layers);
   const int x = groups < 1 ? 1 : groups < spread ? groups : spread;
