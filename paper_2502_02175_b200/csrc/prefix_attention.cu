@@ -24,7 +24,10 @@ constexpr int NARROW = 0, WIDE = 1;
 constexpr int PN_WARPS = 4, PN_CTAS = 2 * 148;  // narrow: two CTAs of four warps per SM, every warp works alone
 constexpr int PW_CTAS = 148;                    // runs of the wide kernel: one CTA per SM
 __host__ __device__ constexpr int pf_bm(int c) { return c == NARROW ? 16 : 256; }        // stacked rows of a tile
-__host__ __device__ constexpr int pf_kb(int c) { return c == NARROW ? 64 : 128; }        // keys of a unit
+constexpr int WIDE_KEYS = 128;                  // keys of a unit
+// Narrow: 64 (with fewer, a sequence's few own rows would count for less than they cost), or 32 while every unit has a warp of its own (8
+// candidates, attention alone: 9.9 -> 8.7 us)
+constexpr int NARROW_KEYS = 64, NARROW_FINE = 32;
 __host__ __device__ constexpr int pf_runs(int c) { return c == NARROW ? PN_WARPS * PN_CTAS : PW_CTAS; }     // most runs
 
 struct SeqRec { int slot /* -1: refused */, row0, nq, len, pre_seg, suf_seg, pad0, pad1; };          // segments: -1 none
@@ -36,6 +39,7 @@ struct __align__(16) SegRec {
   int pos0;                                     // position of q row row0; INT_MIN in a prefix: every row sees every key
   int cls, T, KB;                               // NARROW or WIDE, tiles, key blocks
   int rowbase;                                  // first slot row of this segment
+  int keys;                                     // keys of a unit
 };
 struct PlanHead { long long units[2]; int n_act, error; };   // error: a wait of the wide kernel gave up
 
@@ -88,8 +92,8 @@ struct PlanArgs {
 constexpr int PL_CTAS = 8;
 constexpr int PL_MAX = VLAC_PAGES_MAX_LIST;
 constexpr int PL_ONE = 4096;                    // table entries up to which one CTA is faster
-struct Sums { long long u[2]; int r[2], g; };                           // units and slot rows of both classes, segments
-__device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) { return {{x.u[0] + y.u[0], x.u[1] + y.u[1]}, {x.r[0] + y.r[0], x.r[1] + y.r[1]}, x.g + y.g}; }
+struct Sums { long long u[3]; int r[2], g; };                           // units (narrow, wide, narrow if fine), slot rows of both classes, segments
+__device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) { return {{x.u[0] + y.u[0], x.u[1] + y.u[1], x.u[2] + y.u[2]}, {x.r[0] + y.r[0], x.r[1] + y.r[1]}, x.g + y.g}; }
 struct PlanShared {
   int i[PL_MAX], slot[PL_MAX], row0[PL_MAX], nq[PL_MAX], len[PL_MAX], lcp[PL_MAX], bad[PL_MAX];
   int c[PL_MAX], m[PL_MAX], last[PL_MAX], g[PL_MAX];                    // of a group, at its leader: common pages, members, last member; segment
@@ -107,12 +111,12 @@ __device__ Sums plan_scan(Sums* part, const Sums& v, int n, Sums* total) {
     Sums x = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const Sums t = {{__shfl_up_sync(0xffffffffu, x.u[0], o), __shfl_up_sync(0xffffffffu, x.u[1], o)},
+      const Sums t = {{__shfl_up_sync(0xffffffffu, x.u[0], o), __shfl_up_sync(0xffffffffu, x.u[1], o), __shfl_up_sync(0xffffffffu, x.u[2], o)},
                       {__shfl_up_sync(0xffffffffu, x.r[0], o), __shfl_up_sync(0xffffffffu, x.r[1], o)}, __shfl_up_sync(0xffffffffu, x.g, o)};
       if (lane >= o) x = x + t;
     }
     if (lane == 31) part[warp] = x;
-    before = {{x.u[0] - v.u[0], x.u[1] - v.u[1]}, {x.r[0] - v.r[0], x.r[1] - v.r[1]}, x.g - v.g};
+    before = {{x.u[0] - v.u[0], x.u[1] - v.u[1], x.u[2] - v.u[2]}, {x.r[0] - v.r[0], x.r[1] - v.r[1]}, x.g - v.g};
   }
   __syncthreads();
   Sums all = {};
@@ -228,8 +232,7 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
   __syncthreads();
   // ---- segments: thread k makes the prefix of a group that k leads, and k's own rows
   const bool mine = tid < n_act, bad = mine && s.bad[tid];
-  long long u_pre = 0, u_suf = 0;
-  int r_pre = 0, r_suf = 0, pre = 0, lead = tid, c_pre = NARROW, t_pre = 0, t_suf = 0, kb_pre = 0, kb_suf = 0;
+  int r_pre = 0, r_suf = 0, pre = 0, lead = tid, c_pre = NARROW, t_pre = 0, t_suf = 0, n_pre = 0, n_suf = 0;    // rows, tiles, keys
   if (bad) a.status[s.i[tid]] = VLAC_ERR_BAD_STATE;
   if (mine && !bad) {
     int w = tid >> 5;
@@ -242,20 +245,25 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
     if (lead == tid && pre > 0) {
       r_pre = r_all;
       c_pre = r_pre > pf_bm(NARROW) ? WIDE : NARROW;
-      t_pre = (r_pre + pf_bm(c_pre) - 1) / pf_bm(c_pre); kb_pre = (pre + pf_kb(c_pre) - 1) / pf_kb(c_pre);
-      u_pre = (long long)a.kv_heads * t_pre * kb_pre;
+      t_pre = (r_pre + pf_bm(c_pre) - 1) / pf_bm(c_pre); n_pre = pre;
     }
     if (s.len[tid] > pre) {
       r_suf = s.nq[tid] * a.ratio;
-      t_suf = (r_suf + pf_bm(NARROW) - 1) / pf_bm(NARROW); kb_suf = (s.len[tid] - pre + pf_kb(NARROW) - 1) / pf_kb(NARROW);
-      u_suf = (long long)a.kv_heads * t_suf * kb_suf;
+      t_suf = (r_suf + pf_bm(NARROW) - 1) / pf_bm(NARROW); n_suf = s.len[tid] - pre;
     }
   }
-  const bool wide = c_pre == WIDE && u_pre > 0;
-  const Sums own = {{(wide ? 0 : u_pre) + u_suf, wide ? u_pre : 0},
-                    {((wide ? 0 : r_pre) + r_suf) * a.kv_heads, wide ? r_pre * a.kv_heads : 0}, (u_pre > 0) + (u_suf > 0)};
+  const bool wide = c_pre == WIDE;                                      // (then there is a prefix)
+  auto units = [&](int t, int n, int keys) { return (long long)a.kv_heads * t * ((n + keys - 1) / keys); };
+  const Sums own = {{(wide ? 0 : units(t_pre, n_pre, NARROW_KEYS)) + units(t_suf, n_suf, NARROW_KEYS), wide ? units(t_pre, n_pre, WIDE_KEYS) : 0,
+                     (wide ? 0 : units(t_pre, n_pre, NARROW_FINE)) + units(t_suf, n_suf, NARROW_FINE)},
+                    {((wide ? 0 : r_pre) + r_suf) * a.kv_heads, wide ? r_pre * a.kv_heads : 0}, (n_pre > 0) + (n_suf > 0)};
   Sums all;
-  const Sums at = plan_scan(s.part, own, n_act, &all);
+  Sums at = plan_scan(s.part, own, n_act, &all);
+  const bool fine = all.u[2] <= pf_runs(NARROW);
+  if (fine) { at.u[0] = at.u[2]; all.u[0] = all.u[2]; }
+  const int keys_n = fine ? NARROW_FINE : NARROW_KEYS, keys_pre = wide ? WIDE_KEYS : keys_n;
+  const int kb_pre = (n_pre + keys_pre - 1) / keys_pre, kb_suf = (n_suf + keys_n - 1) / keys_n;
+  const long long u_pre = units(t_pre, n_pre, keys_pre), u_suf = units(t_suf, n_suf, keys_n);
   const int g0 = at.g;
   if (mine) { s.g[tid] = g0; s.u0[NARROW][tid] = at.u[0]; s.u0[WIDE][tid] = at.u[1]; }
   if (tid == 0) { PlanHead h = {{all.u[0], all.u[1]}, n_act, 0}; *p.head = h; }
@@ -267,13 +275,13 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
     const long long at_w = all.r[0] + (long long)pf_runs(NARROW) * pf_bm(NARROW);
     if (u_pre > 0) {
       const long long us = wide ? at.u[1] : at.u[0];
-      SegRec r = {us, us + u_pre, s.slot[tid], s.row0[tid], r_pre, 0, pre, INT_MIN, c_pre, t_pre, kb_pre, (int)(wide ? at_w + at.r[1] : at.r[0])};
+      SegRec r = {us, us + u_pre, s.slot[tid], s.row0[tid], r_pre, 0, pre, INT_MIN, c_pre, t_pre, kb_pre, (int)(wide ? at_w + at.r[1] : at.r[0]), keys_pre};
       p.seg[g0] = r;
     }
     if (u_suf > 0) {
       const long long us = at.u[0] + (wide ? 0 : u_pre);
       SegRec r = {us, us + u_suf, s.slot[tid], s.row0[tid], r_suf, pre, s.len[tid], s.len[tid] - s.nq[tid], NARROW, t_suf, kb_suf,
-                  (int)(at.r[0] + (wide ? 0 : (long long)r_pre * a.kv_heads))};
+                  (int)(at.r[0] + (wide ? 0 : (long long)r_pre * a.kv_heads)), keys_n};
       p.seg[g0 + (u_pre > 0)] = r;
     }
   }
@@ -374,7 +382,7 @@ struct Cursor {
     }
     const int bm = pf_bm(cls), n = (int)min((long long)(s.KB - kb), u_end - u);
     p->slot = s.slot; p->head = head; p->rt = rt; p->nr = min(bm, s.R - rt * bm); p->row0 = s.row0;
-    p->key0 = s.key0 + kb * pf_kb(cls); p->key1 = min(s.key1, p->key0 + n * pf_kb(cls));
+    p->key0 = s.key0 + kb * s.keys; p->key1 = min(s.key1, p->key0 + n * s.keys);
     // stacked row x of the tile sees the positions below lim0 + x / ratio (x counted from the segment's start)
     p->lim0 = s.pos0 == INT_MIN ? INT_MIN : s.pos0 + 1;
     p->n = n;
