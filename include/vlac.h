@@ -379,7 +379,8 @@ int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int s
  * entry, and rows behind q_ptr[n], are left as they are.
  *   plan     n (<= VLAC_PAGES_MAX_LIST), rows of q, n_heads (a multiple of n_kv_heads, n_heads*rows < 2^29), and mem: device
  *            memory of vlac_prefix_bytes(p, n, rows, n_heads) bytes, 16-byte aligned, that holds the plan and the partial sums; a plan
- *            serves one attention call at a time (two captured graphs that may overlap need two)
+ *            is made before its first attention call (or its first 256 bytes are zero: then nothing is computed), with the pool and the
+ *            struct that the attention calls get, and serves one of them at a time (two captured graphs that may overlap need two)
  *   q, out   device, the pool's type, row r at r*q_stride / r*out_stride elements (multiples of 8, at least n_heads*head_dim), 16-byte
  *            aligned;  lse  device fp32 [rows][n_heads] or NULL */
 typedef struct {

@@ -427,6 +427,7 @@ class PrefixPlan:
             raise VlacError(-1, "vlac_prefix_bytes")
         self.n, self.rows, self.n_heads, self.index = n, rows, n_heads, pages.index
         self.mem = torch.empty((max(size, 16),), dtype=torch.uint8, device=pages.k.device)
+        self.mem[:256].zero_()                                   # no plan yet: an attention call before the first one computes nothing
         self.struct = vlac_prefix(n, rows, n_heads, self.mem.data_ptr(), size)
         self.ref = C.byref(self.struct)
 

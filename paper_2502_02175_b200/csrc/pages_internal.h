@@ -31,6 +31,7 @@ static inline size_t pages_row(const vlac_pages* p) { return (size_t)p->n_kv_hea
 static inline size_t pages_layer(const vlac_pages* p) { return (size_t)p->n_pages * p->page_size * pages_row(p); }
 
 __device__ __forceinline__ void cluster_sync_all() {
+  __syncwarp();                                 // (the aligned form wants whole warps, also after loops whose lanes ended apart)
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ unsigned cluster_rank() {

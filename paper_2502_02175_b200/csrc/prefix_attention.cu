@@ -943,8 +943,10 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       }
       if (ok && !two) put(&tm_v, yp, p.head * D);
     }
-    if (!ok)                                                            // given up: let what is in flight land
-      for (int c = max(0, cnt - W::SLOTS); c < cnt; ++c) pw_wait(&full[c % W::SLOTS], (c / W::SLOTS) & 1, &abort_flag, error);
+    if (!ok) {                                                          // given up: let what is in flight land (whoever else gave up)
+      int alone = 0;
+      for (int c = max(0, cnt - W::SLOTS); c < cnt; ++c) pw_wait(&full[c % W::SLOTS], (c / W::SLOTS) & 1, &alone, error);
+    }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- products
     unsigned one;
@@ -1045,7 +1047,11 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       if (ok) pw_commit(&o_full, one);
       ++pieces;
     }
-    if (!ok) { pw_commit(&drain, one); pw_wait(&drain, 0, &abort_flag, error); }
+    if (!ok) {
+      int alone = 0;
+      pw_commit(&drain, one);
+      pw_wait(&drain, 0, &alone, error);
+    }
     __syncwarp();
   } else if (warp >= 4) {
     // ---------------------------------------------------------------- softmax

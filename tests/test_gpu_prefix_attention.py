@@ -395,6 +395,22 @@ def test_candidates_of_a_control_step(vb):
         vb.vlac_destroy(ctx)
 
 
+def test_without_a_plan_nothing_is_computed(vb):
+    c = Case(vb, [(400, [(n + 1, 1) for n in range(20)])], 4, 4, 64, seed=15)
+    plan, out = vb.PrefixPlan(c.pages, 20, 20, 4), torch.full_like(c.q, 5.0)
+    vb.vlac_prefix_attention(c.pages, 0, plan, c.q, c.scale, out)
+    assert torch.all(out == 5.0) and vb.vlac_prefix_error(plan) == 0
+    vb.vlac_prefix_attention(c.pages, 0, vb.PrefixPlan(c.pages, 0, 0, 4), c.q[:0], c.scale, out[:0])
+    vb.vlac_prefix_plan(c.pages, vb.PrefixPlan(c.pages, 2, 0, 4), dev(c.seqs[:2]), dev([0, 0, 0]), c.st(2))
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(64, 1), (24, 1), (128, 1), (192, 1), (66, 33), (64, 64)])
+def test_many_heads_a_group_and_many_groups(vb, heads, kv_heads):
+    """Query heads per K/V head that divide a tile, do not, and are more than one; K/V heads that are no power of two."""
+    c = Case(vb, [(270, [(3, 2), (1, 1), (40, 3)]), (0, [(70, 1)])], heads, kv_heads, 64, seed=heads)
+    c.check(*c.run())
+
+
 def test_wrong_tensors_are_refused(vb):
     c = Case(vb, [(16, [(2, 1), (3, 1)])])
     plan, st, ptr, out = vb.PrefixPlan(c.pages, 2, 2, 4), c.st(2), dev([0, 1, 2]), torch.zeros_like(c.q)
