@@ -434,8 +434,9 @@ class PrefixPlan:
 
 def _here(index: int) -> int:
     """The current stream; the library launches on the current device, so tensors of another one are refused."""
-    assert index == torch.cuda.current_device(), f"tensors on cuda:{index}, current device {torch.cuda.current_device()}"
-    return torch._C._cuda_getCurrentRawStream(index)            # (a call a token and layer: current_stream() costs 1.5 us)
+    # (a call a token and layer: torch.cuda.current_device() and current_stream() cost 1.5 us more)
+    assert index == torch._C._cuda_getDevice(), f"tensors on cuda:{index}, current device {torch.cuda.current_device()}"
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _ints(t: torch.Tensor, n: int, index: int) -> int:
@@ -476,27 +477,24 @@ def vlac_pages_compact(pages: Pages, src: torch.Tensor, dst: torch.Tensor, keep_
                                   _ints(status, n, dev), stream), "vlac_pages_compact")
 
 
-def _rows(t: torch.Tensor, heads: int, pages: Pages, rows: int) -> int:
-    """Pointer of [rows, heads, head_dim] of the pool's type, heads side by side, any row stride."""
-    d = pages.head_dim
-    assert t.dtype is pages.dtype and t.get_device() == pages.index and t.dim() == 3 and t.size(0) == rows and t.size(1) == heads and t.size(2) == d
-    assert t.is_contiguous() or rows == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d))
-    return t.data_ptr()
-
-
-def _row_stride(t: torch.Tensor) -> int:
-    """Elements between rows (a tensor of one row or none may carry any stride)."""
-    return t.stride(0) if t.size(0) > 1 else t.size(1) * t.size(2)
+def _rows(t: torch.Tensor, shape: tuple, pages: Pages):
+    """Pointer and row stride of ``shape`` = (rows, heads, head_dim) of the pool's type, heads side by side, any row stride."""
+    assert t.dtype is pages.dtype and t.get_device() == pages.index and t.shape == shape
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1] * shape[2]
+    assert t.stride(2) == 1 and (shape[1] == 1 or t.stride(1) == shape[2])
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
 
 
 def vlac_pages_write(pages: Pages, layer: int, seqs: torch.Tensor, start: Optional[torch.Tensor], row_ptr: torch.Tensor,
                      k_rows: torch.Tensor, v_rows: torch.Tensor, status: torch.Tensor) -> None:
     """Rows ``row_ptr[i]:row_ptr[i + 1]`` of ``k_rows`` / ``v_rows`` to slot ``seqs[i]`` from position ``start[i]`` on (``None``: its last rows)."""
-    n, dev, rows, heads = seqs.size(0), pages.index, k_rows.size(0), pages.n_kv_heads
-    stream = _here(dev)
+    n, dev, rows = seqs.size(0), pages.index, k_rows.size(0)
+    stream, shape = _here(dev), (rows, pages.n_kv_heads, pages.head_dim)
+    k_ptr, k_stride = _rows(k_rows, shape, pages)
+    v_ptr, v_stride = _rows(v_rows, shape, pages)
     _check(lib.vlac_pages_write(pages.ref, layer, _ints(seqs, n, dev), None if start is None else _ints(start, n, dev), _ints(row_ptr, n + 1, dev), n, rows,
-                                _rows(k_rows, heads, pages, rows), _row_stride(k_rows), _rows(v_rows, heads, pages, rows), _row_stride(v_rows),
-                                _ints(status, n, dev), stream), "vlac_pages_write")
+                                k_ptr, k_stride, v_ptr, v_stride, _ints(status, n, dev), stream), "vlac_pages_write")
 
 
 def vlac_pages_from_cache(pages: Pages, cache: int, seq: int, slot: int, n_rows: int, status: torch.Tensor) -> None:
@@ -520,12 +518,14 @@ def vlac_prefix_plan(pages: Pages, plan: PrefixPlan, seqs: torch.Tensor, q_ptr: 
 def vlac_prefix_attention(pages: Pages, layer: int, plan: PrefixPlan, q: torch.Tensor, scale: float, out: torch.Tensor,
                           lse: Optional[torch.Tensor] = None) -> None:
     """Attention of the plan's rows: ``q``, ``out`` ``[rows, n_heads, head_dim]`` of the pool's type, ``lse`` fp32 ``[rows, n_heads]``."""
-    dev, rows, heads = pages.index, plan.rows, plan.n_heads
+    dev, shape = pages.index, (plan.rows, plan.n_heads, pages.head_dim)
     stream = _here(dev)
     assert plan.index == dev
-    assert lse is None or (lse.dtype is torch.float32 and lse.get_device() == dev and lse.is_contiguous() and tuple(lse.shape) == (rows, heads))
-    _check(lib.vlac_prefix_attention(pages.ref, layer, plan.ref, _rows(q, heads, pages, rows), _row_stride(q), scale, _rows(out, heads, pages, rows),
-                                     _row_stride(out), _ptr(lse), stream), "vlac_prefix_attention")
+    assert lse is None or (lse.dtype is torch.float32 and lse.get_device() == dev and lse.is_contiguous() and lse.shape == shape[:2])
+    q_ptr, q_stride = _rows(q, shape, pages)
+    out_ptr, out_stride = _rows(out, shape, pages)
+    _check(lib.vlac_prefix_attention(pages.ref, layer, plan.ref, q_ptr, q_stride, scale, out_ptr, out_stride, _ptr(lse), stream),
+           "vlac_prefix_attention")
 
 
 def vlac_prefix_error(plan: PrefixPlan) -> int:

@@ -77,6 +77,7 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
   __shared__ int s_dst[VLAC_PAGES_MAX_LIST];    // target slot, -1: refused
   __shared__ int s_src[VLAC_PAGES_MAX_LIST];
   __shared__ int s_shared[VLAC_PAGES_MAX_LIST], s_total[VLAC_PAGES_MAX_LIST], s_start[VLAC_PAGES_MAX_LIST], s_had[VLAC_PAGES_MAX_LIST];
+  __shared__ int s_d[VLAC_PAGES_MAX_LIST], s_s[VLAC_PAGES_MAX_LIST], s_ls[VLAC_PAGES_MAX_LIST], s_ld[VLAC_PAGES_MAX_LIST];  // the lists, slots' lengths
   __shared__ int s_red;
   const int tid = threadIdx.x, lane = tid & 31, rank = (int)cluster_rank();
   const int gthread = rank * PB_THREADS + tid, gwarp = (tid >> 5) * PB_CTAS + rank;
@@ -89,28 +90,31 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
   while (team < 32 && team * 2 * a.n <= PB_WARPS) team *= 2;
   const int n_teams = PB_WARPS / team, my_team = gwarp / team, step = team * 32, at0 = (gwarp % team) * 32 + lane;
 
-  // ---- 0: clear the marks of the slots named as targets
-  for (int i = gthread; i < a.n; i += PB_CTAS * PB_THREADS) {
-    const int d = slot_of(a.dst, i, a.n_slots);
+  // ---- 0: the lists and lengths into every CTA's shared memory; clear the marks of the slots named as targets
+  if (tid < a.n) {
+    const int d = slot_of(a.dst, tid, a.n_slots), s = a.op == OP_RESIZE ? d : slot_of(a.src, tid, a.n_slots);
+    s_d[tid] = d; s_s[tid] = s;
+    s_ls[tid] = s >= 0 ? a.len[s] : 0; s_ld[tid] = d >= 0 ? a.len[d] : 0;
+  }
+  __syncthreads();
+  if (gthread < a.n) {
+    const int d = s_d[gthread];
     if (d >= 0) { w.first[d] = INT_MAX; w.read_by[d] = 0; }
-    w.bad[i] = 0; w.lead[i] = INT_MAX;
+    w.bad[gthread] = 0; w.lead[gthread] = INT_MAX;
   }
   cluster_sync_all();
 
   // ---- 1: who names which slot; scan the tables and keep lists
-  for (int i = gthread; i < a.n; i += PB_CTAS * PB_THREADS) {
-    const int d = slot_of(a.dst, i, a.n_slots);
-    if (d >= 0) atomicMin(&w.first[d], i);
-    if (a.op != OP_RESIZE) {
-      const int s = slot_of(a.src, i, a.n_slots);
-      if (s >= 0 && !(a.op == OP_COMPACT && s == d)) w.read_by[s] = 1;
-    }
+  if (gthread < a.n) {
+    const int d = s_d[gthread], s = s_s[gthread];
+    if (d >= 0) atomicMin(&w.first[d], gthread);
+    if (a.op != OP_RESIZE && s >= 0 && !(a.op == OP_COMPACT && s == d)) w.read_by[s] = 1;
   }
   for (int i = my_team; i < a.n; i += n_teams) {
-    const int d = slot_of(a.dst, i, a.n_slots), s = a.op == OP_RESIZE ? d : slot_of(a.src, i, a.n_slots);
+    const int d = s_d[i], s = s_s[i];
     if (d < 0 || s < 0) continue;
     int bad = 0;
-    const int ls = a.len[s], ld = a.len[d];
+    const int ls = s_ls[i], ld = s_ld[i];
     if (ls < 0 || ls > a.max_pages << a.shift || ld < 0 || ld > a.max_pages << a.shift) bad = 1;
     else {
       const int ps = (ls + a.page - 1) >> a.shift, pd = (ld + a.page - 1) >> a.shift;
@@ -151,16 +155,16 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
   // ---- 2: the entries' fates as far as they do not depend on free pages (every CTA for itself: thread i has entry i)
   int status = VLAC_OK, d = -1, s = -1, total = 0, shared = 0, had = 0, rows = 0;
   if (tid < a.n) {
-    d = slot_of(a.dst, tid, a.n_slots);
-    s = a.op == OP_RESIZE ? d : slot_of(a.src, tid, a.n_slots);
+    d = s_d[tid];
+    s = s_s[tid];
     const int bad = d >= 0 && s >= 0 ? __ldcg(&w.bad[tid]) : 0;
     if (d < 0 || s < 0 || __ldcg(&w.first[d]) != tid || (a.op != OP_RESIZE && __ldcg(&w.read_by[d])) || (a.op == OP_FORK && s == d))
       status = VLAC_ERR_INVALID_ARG;
     else if (bad & 1) status = VLAC_ERR_BAD_STATE;
     else if (bad & 2) status = VLAC_ERR_INVALID_ARG;
     else {
-      const int ls = a.len[s];
-      had = (a.len[d] + a.page - 1) >> a.shift;
+      const int ls = s_ls[tid];
+      had = (s_ld[tid] + a.page - 1) >> a.shift;
       if (a.op == OP_RESIZE) {
         rows = a.lens ? a.lens[tid] : 0;
         if (rows < 0 || rows > a.max_pages << a.shift) status = VLAC_ERR_INVALID_ARG;
@@ -192,7 +196,7 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
     const int t = s_dst[i];
     if (t < 0 || (a.op == OP_COMPACT && s_src[i] == t)) continue;
     int* td = a.table + (size_t)t * a.max_pages;
-    const int pd = (a.len[t] + a.page - 1) >> a.shift;
+    const int pd = (s_ld[i] + a.page - 1) >> a.shift;
     for (int j0 = (a.op == OP_RESIZE ? s_shared[i] : 0) + at0; j0 < pd; j0 += step * 8) {
       int page[8];                                                      // (loads first: each would wait for the write before it)
 #pragma unroll
@@ -201,7 +205,6 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
       for (int q = 0; q < 8; ++q) { const int j = j0 + q * step; if (j < pd) { atomicSub(&a.refs[page[q]], 1); td[j] = -1; } }
     }
   }
-  cluster_sync_all();
 
   // ---- 4: free pages in ascending order.  CTA r owns a run of pages, looked at 16384 at a time: 512 to a warp, 16 to a lane, 32 side by side
   // (so that pages and list entries are written side by side too); first the counts, then the ranks.
@@ -217,10 +220,14 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
     for (int g = 0; g < 16; ++g) m |= (r[g] == 0 ? 1u : 0u) << g;
     return m;
   };
+  // (a call that takes no page goes on to the tables: what it gives back counts for nobody, and its threads write the entries that they gave
+  // back)
+  unsigned mask = 0;                                                     // of the first look
+  long long n_free = 0, before = 0;
   if (tid == 0) s_red = 0;
   __syncthreads();
-  unsigned mask = 0;                                                     // of the first look
   if (need_all > 0) {
+    cluster_sync_all();                                                  // every page is given back
     int c = 0;
     for (int p = p0; p < p1; p += LOOK) {
       const unsigned m = free16(p + mine);
@@ -229,13 +236,12 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
     }
     c = __reduce_add_sync(0xffffffffu, c);
     if (lane == 0) atomicAdd(&s_red, c);
-  }
-  __syncthreads();
-  if (tid == 0) { w.count[rank] = s_red; s_red = 0; }
-  cluster_sync_all();
-  long long n_free = 0, before = 0;
+    __syncthreads();
+    if (tid == 0) { w.count[rank] = s_red; s_red = 0; }
+    cluster_sync_all();
 #pragma unroll
-  for (int r = 0; r < PB_CTAS; ++r) { const int c = __ldcg(&w.count[r]); n_free += c; before += r < rank ? c : 0; }
+    for (int r = 0; r < PB_CTAS; ++r) { const int x = __ldcg(&w.count[r]); n_free += x; before += r < rank ? x : 0; }
+  }
   if (need > 0 && start + need > n_free) status = VLAC_ERR_OOM;           // and every later one that needs a page: start only grows
   if (tid < a.n && status == VLAC_OK && need > 0) atomicMax(&s_red, (int)(start + need));
   __syncthreads();
@@ -270,7 +276,7 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
     }
     before += all;
   }
-  cluster_sync_all();
+  if (need_all > 0) cluster_sync_all();
 
   // ---- 5: the new tables
   for (int i = my_team; i < a.n; i += n_teams) {
