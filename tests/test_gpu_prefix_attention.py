@@ -23,16 +23,21 @@ def dev(x):
 
 
 class Case:
-    """Groups of sequences made with the pool calls: (common rows, [(own rows, query rows), ...]) per group."""
+    """Groups of sequences made with the pool calls: (common rows, [(own rows, query rows), ...]) per group.
 
-    def __init__(self, vb, groups, heads=4, kv_heads=4, d=64, page=16, dtype=torch.bfloat16, seed=0, layers=1, spare=3, q_scale=2.0, fill=float("nan")):
+    ``columns``: further columns of the tables.  Calls on narrow tables with few rows take a form of their own; wide tables keep them to the
+    general one.
+    """
+
+    def __init__(self, vb, groups, heads=4, kv_heads=4, d=64, page=16, dtype=torch.bfloat16, seed=0, layers=1, spare=3, q_scale=2.0, fill=float("nan"),
+                 columns=30000):
         self.vb, self.heads, self.kv_heads, self.d, self.page, self.dtype = vb, heads, kv_heads, d, page, dtype
         self.gen = torch.Generator(device="cuda")
         self.gen.manual_seed(seed)
         total = sum(c + sum(o + page for o, _ in m) for c, m in groups) + spare * page
         longest = max([c + o for c, m in groups for o, _ in m] + [1])
         n_slots = sum(len(m) + 1 for _, m in groups) + 1
-        self.pages = p = vb.Pages.empty(layers, -(-total // page) + len(groups) + spare, page, kv_heads, d, n_slots, -(-longest // page) + 1, dtype)
+        self.pages = p = vb.Pages.empty(layers, -(-total // page) + len(groups) + spare, page, kv_heads, d, n_slots, -(-longest // page) + 1 + columns, dtype)
         p.k.fill_(fill)                                                  # rows nobody wrote must never matter
         p.v.fill_(fill)
         self.seqs, self.nq, slot = [], [], 0
@@ -127,9 +132,13 @@ GROUPS = {
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
 @pytest.mark.parametrize("heads,kv_heads,d", [(4, 4, 64), (4, 1, 128), (6, 2, 64), (2, 2, 128), (15, 3, 64), (17, 1, 64)])
 @pytest.mark.parametrize("groups", GROUPS, ids=str)
-def test_against_the_definition(vb, groups, heads, kv_heads, d, dtype):
-    c = Case(vb, GROUPS[groups], heads, kv_heads, d, dtype=dtype, seed=len(groups))
-    c.check(*c.run())
+@pytest.mark.parametrize("columns", [0, 30000], ids=["narrow_tables", "wide_tables"])
+def test_against_the_definition(vb, columns, groups, heads, kv_heads, d, dtype):
+    c = Case(vb, GROUPS[groups], heads, kv_heads, d, dtype=dtype, seed=len(groups), columns=columns)
+    first = c.run()
+    c.check(*first)
+    again = c.run()                                                          # and once more: nothing is left over
+    assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
 
 
 @pytest.mark.parametrize("page", [8, 32, 64, 128, 256])
@@ -138,9 +147,10 @@ def test_page_sizes(vb, page):
     c.check(*c.run())
 
 
-def test_layers_strides_and_no_lse(vb):
+@pytest.mark.parametrize("columns", [0, 30000], ids=["narrow_tables", "wide_tables"])
+def test_layers_strides_and_no_lse(vb, columns):
     """A layer of several; q and out as slices of wider buffers (a fused projection's rows); lse left out."""
-    c = Case(vb, [(50, [(3, 1), (4, 2)])], 4, 2, 64, layers=3, seed=2)
+    c = Case(vb, [(50, [(3, 1), (4, 2)])], 4, 2, 64, layers=3, seed=2, columns=columns)
     wide = torch.full((c.rows, 3, c.heads, c.d), 3.0, dtype=c.dtype, device="cuda")
     wide[:, 1] = c.q
     for layer in (2, 0):
@@ -150,9 +160,10 @@ def test_layers_strides_and_no_lse(vb):
         assert torch.all(out[0] == 7) and torch.all(out[-1] == 7) and torch.all(out[:, c.heads:] == 7)
 
 
-def test_refused_entries_leave_their_rows(vb):
+@pytest.mark.parametrize("columns", [0, 30000], ids=["narrow_tables", "wide_tables"])
+def test_refused_entries_leave_their_rows(vb, columns):
     """Slots and pages out of range: a code each, their rows untouched, the others right; rows behind the last untouched."""
-    c = Case(vb, [(48, [(3, 1), (5, 2), (2, 1), (4, 1)])], seed=4)
+    c = Case(vb, [(48, [(3, 1), (5, 2), (2, 1), (4, 1)])], seed=4, columns=columns)
     n, rows = 4, c.rows + 3
     q = torch.cat([c.q, c.q[:3]])
     plan = vb.PrefixPlan(c.pages, n, rows, c.heads)
@@ -189,10 +200,11 @@ def test_refused_entries_leave_their_rows(vb):
         assert (torch.all(out == 5) if min(want) == max(want) else torch.all(out[(4 if want[3] else 0):(99 if want[3] else 1)] == 5))
 
 
-def test_values_a_row_does_not_see_never_reach_it(vb):
+@pytest.mark.parametrize("columns", [0, 30000], ids=["narrow_tables", "wide_tables"])
+def test_values_a_row_does_not_see_never_reach_it(vb, columns):
     """NaN and infinities in the K and V rows of later queries of the same chunk: earlier rows stay exact, the rows that see them do not."""
     for d, heads in ((64, 1), (128, 3)):
-        c = Case(vb, [(40, [(12, 7), (9, 9)])], heads, 1, d, seed=d)
+        c = Case(vb, [(40, [(12, 7), (9, 9)])], heads, 1, d, seed=d, columns=columns)
         clean, clean_lse = c.run()
         slot = c.seqs[0]
         n = int(c.pages.len[slot])
@@ -209,10 +221,11 @@ def test_values_a_row_does_not_see_never_reach_it(vb):
         assert torch.all(torch.isnan(out[6])) and torch.all(torch.isnan(lse[6]))
 
 
-def test_extreme_scores(vb):
+@pytest.mark.parametrize("columns", [0, 30000], ids=["narrow_tables", "wide_tables"])
+def test_extreme_scores(vb, columns):
     """Scores of some hundreds (one key takes all), and equal ones of zero."""
     for q_scale in (200.0, 0.0):
-        c = Case(vb, [(70, [(5, 1), (3, 2), (66, 1)]), (0, [(90, 40)])], 4, 2, 64, seed=11, q_scale=q_scale)
+        c = Case(vb, [(70, [(5, 1), (3, 2), (66, 1)]), (0, [(90, 40)])], 4, 2, 64, seed=11, q_scale=q_scale, columns=columns)
         c.check(*c.run())
 
 
@@ -257,18 +270,20 @@ def test_infinities_in_a_common_page(vb):
     assert torch.equal(out, clean)
 
 
-def test_same_slot_twice_and_any_order(vb):
+@pytest.mark.parametrize("columns", [0, 30000], ids=["narrow_tables", "wide_tables"])
+def test_same_slot_twice_and_any_order(vb, columns):
     """A slot may be listed twice, and the order of the list decides nothing but the division of the work."""
-    c = Case(vb, [(96, [(3, 1), (20, 1), (1, 1)]), (64, [(2, 1), (9, 1)])], 8, 2, 64, seed=5)
+    c = Case(vb, [(96, [(3, 1), (20, 1), (1, 1)]), (64, [(2, 1), (9, 1)])], 8, 2, 64, seed=5, columns=columns)
     c.check(*c.run())
     order = [4, 0, 2, 1, 3, 0, 4]
     c.seqs, c.nq, c.q, c.rows = [c.seqs[i] for i in order], [1] * 7, c.q[order].contiguous(), 7
     c.check(*c.run())
 
 
-def test_repeatable_bits_and_plan_for_all_layers(vb):
+@pytest.mark.parametrize("columns", [0, 30000], ids=["narrow_tables", "wide_tables"])
+def test_repeatable_bits_and_plan_for_all_layers(vb, columns):
     """The same bits every time; one plan serves several layers and several calls."""
-    c = Case(vb, [(500, [(n + 1, 1) for n in range(12)])], 8, 8, 128, layers=2, seed=6)
+    c = Case(vb, [(500, [(n + 1, 1) for n in range(12)])], 8, 8, 128, layers=2, seed=6, columns=columns)
     plan = vb.PrefixPlan(c.pages, len(c.seqs), c.rows, c.heads)
     first = c.run(plan=plan)
     for layer in (1, 0, 1):
@@ -279,9 +294,10 @@ def test_repeatable_bits_and_plan_for_all_layers(vb):
             assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
 
 
-def test_two_graphs_on_two_streams(vb):
+@pytest.mark.parametrize("columns", [0, 30000], ids=["narrow_tables", "wide_tables"])
+def test_two_graphs_on_two_streams(vb, columns):
     """Two captured token passes with plans of their own, replayed at the same time, and again after the sequences grew."""
-    c = Case(vb, [(128, [(3, 1), (4, 1), (9, 1)])], 4, 4, 64, seed=7, spare=12)
+    c = Case(vb, [(128, [(3, 1), (4, 1), (9, 1)])], 4, 4, 64, seed=7, spare=12, columns=columns + 4)
     ptr, streams, work = dev([0, 1, 2, 3]), [torch.cuda.Stream() for _ in range(2)], []
     seqs = dev(c.seqs)
     torch.cuda.synchronize()
