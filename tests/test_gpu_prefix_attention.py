@@ -350,6 +350,38 @@ def test_far_pages(vb):
         assert np.all(np.abs(out[i:i + 1].double().cpu().numpy() - o) <= eo)
 
 
+def test_far_pages_of_the_last_layer(vb):
+    """The same offsets through writes, forks, copies and a wide segment: only the last pages of a two-layer pool are free."""
+    n_pages, page, kv, d, L = 5000, 256, 16, 64, 2
+    pages = vb.Pages.empty(L, n_pages, page, kv, d, 24, 6)
+    assert pages.k.numel() > 2 ** 31
+    free = 32
+    pages.refs[:n_pages - free] = 1
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    st1, n = torch.zeros(1, dtype=torch.int32, device="cuda"), 1000
+    vb.vlac_pages_resize(pages, dev([0]), dev([n]), st1)
+    rows = [torch.empty((n, kv, d), device="cuda").normal_(generator=g).to(torch.bfloat16) for _ in range(2)]
+    vb.vlac_pages_write(pages, 1, dev([0]), dev([0]), dev([0, n]), *rows, st1)
+    assert st1.item() == 0 and int(pages.table[0, 0]) == n_pages - free
+    vb.vlac_pages_fork(pages, dev([0]), dev([1]), True, st1)
+    kids = dev(range(2, 22))
+    st = torch.zeros(20, dtype=torch.int32, device="cuda")
+    vb.vlac_pages_fork(pages, dev([1] * 20), kids, False, st)
+    assert st.tolist() == [0] * 20 and int(pages.refs[n_pages - 1]) in (0, 1)
+    t = pages.table[1, :4].long()
+    assert torch.equal(pages.k[1, t].reshape(-1, kv, d)[:n], rows[0]) and torch.equal(pages.v[1, t].reshape(-1, kv, d)[:n], rows[1])
+    q = (torch.empty((20, 32, d), device="cuda").normal_(generator=g) * 2).to(torch.bfloat16)
+    plan, out = vb.PrefixPlan(pages, 20, 20, 32), torch.zeros_like(q)
+    vb.vlac_prefix_plan(pages, plan, kids, dev(range(21)), st)
+    vb.vlac_prefix_attention(pages, 1, plan, q, 0.125, out)
+    assert st.tolist() == [0] * 20 and vb.vlac_prefix_error(plan) == 0
+    kh, vh = (x.double().cpu().numpy() for x in rows)
+    for i in (0, 19):
+        o, _, eo, _ = ref.attention(kh, vh, q[i:i + 1].double().cpu().numpy(), n, 1, 2, 0.125, HALF[torch.bfloat16])
+        assert np.all(np.abs(out[i:i + 1].double().cpu().numpy() - o) <= eo)
+
+
 def test_candidates_of_a_control_step(vb):
     """The whole use: a control step's prompt becomes a prefix, candidates are forked from it, grow token by token, attend in
     every layer, are pruned and given back."""
