@@ -1108,20 +1108,44 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
             for (int c = valid; c < 128; ++c) pw_st1(s_col + c, 0xff800000u);             // -inf behind them
             pw_st_wait();
           }
-          // two sweeps over the scores (the row's 128 do not fit the registers beside the rest): maximum, then weights
+          // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16); the sum takes
+          // the unrounded weights.  P lies over scores already read: 16 columns for 32.
+          const unsigned long long sc = pw_pair(a.scale2, a.scale2);
+          unsigned long long ls[2] = {0ull, 0ull};                      // two fp32 sums each
+          auto weights = [&](const unsigned* v, unsigned long long nr, unsigned* pk) {
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              float x0, x1;
+              pw_unpair(pw_fma2(pw_pair(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), sc, nr), &x0, &x1);
+              x0 = pf_ex2(x0); x1 = pf_ex2(x1);
+              ls[c & 1] = pw_add2(ls[c & 1], pw_pair(x0, x1));
+              pk[c] = Half2<T>::pack(x0, x1);
+            }
+          };
+          // The weights of the first half are formed with the reference of the block before while the maximum of all 128 scores is still being
+          // found, and formed again in the rare block that moves the reference.  It moves when the maximum has grown by a factor of 2^8:
+          // weights up to 256 cost no precision (they are rounded relative to themselves, l is fp32), and O is seldom rescaled.
+          unsigned pk[32], v[32], x[32];
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          {
+            const float ref = m == -INFINITY ? 0.f : m;
+            const unsigned long long nr = pw_pair(-ref, -ref);
+            pw_ld32(s_col, v);
+            pw_ld32(s_col + 64u, x);
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            unsigned v[64];
-            pw_ld32(s_col + 64u * hf, v);
-            pw_ld32(s_col + 64u * hf + 32u, v + 32);
-            pw_ld_wait(v, v + 32);
+            for (int q = 0; q < 2; ++q) {
+              pw_ld_wait(v, x);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) mx[c & 3] = pw_max3(mx[c & 3], __uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
+              for (int c = 0; c < 16; ++c) {
+                mx[c & 3] = pw_max3(mx[c & 3], __uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
+                mx[c & 3] = pw_max3(mx[c & 3], __uint_as_float(x[2 * c]), __uint_as_float(x[2 * c + 1]));
+              }
+              if (q == 0) pw_ld32(s_col + 96u, x);
+              weights(v, nr, pk + 16 * q);
+              if (q == 0) pw_ld32(s_col + 32u, v);
+            }
           }
           const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2;
-          // the reference moves only when the maximum has grown by a factor of 2^8: weights up to 256 cost no precision (they are rounded
-          // relative to themselves, l is fp32), and O is seldom rescaled
           const bool grow = bm > m + 8.f || m == -INFINITY;
           if (__any_sync(0xffffffffu, grow)) {
             const float mn = grow ? fmaxf(m, bm) : m;
@@ -1131,7 +1155,6 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
             if (i >= step) {
 #pragma unroll 1
               for (int c = 0; c < D / 32; ++c) {
-                unsigned x[32];
                 pw_ld32(o_col + 32u * c, x);
                 pw_ld_wait(x);
 #pragma unroll
@@ -1139,33 +1162,28 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
                 pw_st32(o_col + 32u * c, x);
               }
             }
+            ls[0] = ls[1] = 0ull;
+            const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              pw_ld32(s_col + 32u * q, v);
+              pw_ld_wait(v);
+              weights(v, pw_pair(-ref, -ref), pk + 16 * q);
+            }
           }
-          const float ref = m == -INFINITY ? 0.f : m;
-          // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16); the sum takes
-          // the unrounded weights.  P lies over the scores already read: 16 columns a sweep of 32.
-          unsigned long long ls[2] = {0ull, 0ull};                      // two fp32 sums each
-          const unsigned long long sc = pw_pair(a.scale2, a.scale2), nr = pw_pair(-ref, -ref);
-          unsigned v[2][32];
-          pw_ld32(s_col, v[0]);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            pw_ld_wait(v[q & 1]);
-            if (q < 3) pw_ld32(s_col + 32u * (q + 1), v[(q + 1) & 1]);
-            unsigned pk[16];
-#pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              float x0, x1;
-              pw_unpair(pw_fma2(pw_pair(__uint_as_float(v[q & 1][2 * c]), __uint_as_float(v[q & 1][2 * c + 1])), sc, nr), &x0, &x1);
-              x0 = pf_ex2(x0); x1 = pf_ex2(x1);
-              ls[c & 1] = pw_add2(ls[c & 1], pw_pair(x0, x1));
-              pk[c] = Half2<T>::pack(x0, x1);
-            }
-            pw_st16(s_col + 16u * q, pk);
-            if (q == 1) {
-              pw_st_wait();
-              pw_before();
-              pw_arrive(&p_full[side][0]);
-            }
+          pw_ld32(s_col + 64u, v);
+          pw_st32(s_col, pk);
+          pw_st_wait();
+          pw_before();
+          pw_arrive(&p_full[side][0]);
+          {
+            const float ref = m == -INFINITY ? 0.f : m;
+            const unsigned long long nr = pw_pair(-ref, -ref);
+            pw_ld32(s_col + 96u, x);
+            pw_ld_wait(v, x);
+            weights(v, nr, pk);
+            weights(x, nr, pk + 16);
+            pw_st32(s_col + 32u, pk);
           }
           float l0, l1, l2, l3;
           pw_unpair(ls[0], &l0, &l1); pw_unpair(ls[1], &l2, &l3);
