@@ -419,13 +419,13 @@ class Pages:
 
 
 class PrefixPlan:
-    """Device memory of one attention plan: up to ``n`` sequences with together ``rows`` query rows of ``n_heads`` heads."""
+    """Device memory of one attention plan over the pool ``pages``: ``n`` sequences with together ``rows`` query rows of ``n_heads`` heads."""
 
     def __init__(self, pages: Pages, n: int, rows: int, n_heads: int):
         size = lib.vlac_prefix_bytes(pages.ref, n, rows, n_heads)
         if size == 0 and n > 0 and rows > 0:
             raise VlacError(-1, "vlac_prefix_bytes")
-        self.n, self.rows, self.n_heads, self.index = n, rows, n_heads, pages.index
+        self.pages, self.n, self.rows, self.n_heads, self.index = pages, n, rows, n_heads, pages.index
         self.mem = torch.empty((max(size, 16),), dtype=torch.uint8, device=pages.k.device)
         self.mem[:256].zero_()                                   # no plan yet: an attention call before the first one computes nothing
         self.struct = vlac_prefix(n, rows, n_heads, self.mem.data_ptr(), size)
@@ -511,7 +511,7 @@ def vlac_prefix_plan(pages: Pages, plan: PrefixPlan, seqs: torch.Tensor, q_ptr: 
     """Find what neighbours of the list share and divide the work; serves every layer until tables, lengths or ``q_ptr`` change."""
     dev, n = pages.index, plan.n
     stream = _here(dev)
-    assert plan.index == dev
+    assert plan.pages is pages                                   # (the slots and page counts in a plan are those of its pool)
     _check(lib.vlac_prefix_plan(pages.ref, plan.ref, _ints(seqs, n, dev), _ints(q_ptr, n + 1, dev), _ints(status, n, dev), stream), "vlac_prefix_plan")
 
 
@@ -520,7 +520,7 @@ def vlac_prefix_attention(pages: Pages, layer: int, plan: PrefixPlan, q: torch.T
     """Attention of the plan's rows: ``q``, ``out`` ``[rows, n_heads, head_dim]`` of the pool's type, ``lse`` fp32 ``[rows, n_heads]``."""
     dev, shape = pages.index, (plan.rows, plan.n_heads, pages.head_dim)
     stream = _here(dev)
-    assert plan.index == dev
+    assert plan.pages is pages
     assert lse is None or (lse.dtype is torch.float32 and lse.get_device() == dev and lse.is_contiguous() and lse.shape == shape[:2])
     q_ptr, q_stride = _rows(q, shape, pages)
     out_ptr, out_stride = _rows(out, shape, pages)

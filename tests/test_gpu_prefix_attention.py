@@ -477,3 +477,13 @@ def test_wrong_tensors_are_refused(vb):
         vb.vlac_prefix_attention(c.pages, 1, plan, c.q, 1.0, out)
     with pytest.raises(vb.VlacError):
         vb.PrefixPlan(vb.Pages.empty(1, 4, 16, 3, 64, 2, 2), 2, 2, 4)
+
+
+def test_a_plan_of_another_pool_is_refused(vb):
+    """A plan's slots and page counts are those of its pool's tables."""
+    c, other = Case(vb, [(16, [(2, 1), (3, 1)])]), Case(vb, [(16, [(2, 1), (3, 1)])])
+    plan, st, ptr, out = vb.PrefixPlan(other.pages, 2, 2, 4), c.st(2), dev([0, 1, 2]), torch.zeros_like(c.q)
+    with pytest.raises(AssertionError):
+        vb.vlac_prefix_plan(c.pages, plan, dev(c.seqs), ptr, st)
+    with pytest.raises(AssertionError):
+        vb.vlac_prefix_attention(c.pages, 0, plan, c.q, 1.0, out)
