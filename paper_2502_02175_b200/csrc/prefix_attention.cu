@@ -963,7 +963,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     unsigned phase = 0, failed = 0;
     bool ok = true;
     auto wait_at = [&](unsigned bar, unsigned parity) {
-      if (!pw_try_at(bar, parity)) failed |= !pw_wait_slow(bar, parity, &abort_flag, error);
+      if (!__all_sync(0xffffffffu, pw_try_at(bar, parity))) failed |= !pw_wait_slow(bar, parity, &abort_flag, error);       // (all lanes or none)
     };
     auto still_ok = [&]() { return __all_sync(0xffffffffu, !failed); };
     auto same = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };    // tells the compiler that a value is the same in all lanes
