@@ -134,7 +134,6 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
   PlanShared& s = *reinterpret_cast<PlanShared*>(pl_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = blockDim.x >> 5, rank = CTAS > 1 ? (int)cluster_rank() : 0;
   const PlanMem p = plan_mem(a.mem, a.n, a.rows, a.n_heads, a.head_dim);
-  if (CTAS > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // (all CTAs run before one writes into another)
   pdl_trigger();
   pdl_wait();
   // ---- the active sequences (rows to compute), in list order: every CTA for itself
@@ -160,6 +159,8 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
   for (int k = tid; k < n_act; k += blockDim.x) { s.lcp[k] = INT_MAX; s.bad[k] = 0; }
   if (rank == 0 && tid < a.n) a.status[tid] = status;
   __syncthreads();
+  // (findings of the other CTAs go into CTA 0's memory only behind this: it has cleared its own, and every CTA runs)
+  if (CTAS > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 
   // ---- tables: page numbers in range; leading pages in common with the previous active sequence.  CTA r has the sequences r, r + CTAS, ..
   const int n_mine = (n_act - rank + CTAS - 1) / CTAS;
@@ -184,7 +185,7 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
   }
   __syncthreads();
   if (CTAS > 1) {
-    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     for (int x = tid; x < n_mine && rank; x += blockDim.x) {
       const int k = x * CTAS + rank;
       unsigned to;

@@ -487,3 +487,27 @@ def test_a_plan_of_another_pool_is_refused(vb):
         vb.vlac_prefix_plan(c.pages, plan, dev(c.seqs), ptr, st)
     with pytest.raises(AssertionError):
         vb.vlac_prefix_attention(c.pages, 0, plan, c.q, 1.0, out)
+
+
+@pytest.mark.parametrize("n", [17, 200, 1024])
+def test_findings_of_every_cta_reach_the_plan(vb, n):
+    """Many sequences of two pages in wide tables, none with a neighbour's pages, some with a page out of range: hardly anything to read, so
+    the plan's CTAs report to the first as early as they can.  A sequence that joined its neighbour would see the neighbour's first page."""
+    page, d, heads = 8, 64, 2
+    pages = vb.Pages.empty(1, n + 1, page, heads, d, n, 5000)
+    pages.v[0] = (torch.arange(n + 1, device="cuda") % 251).to(torch.bfloat16)[:, None, None, None]        # (whole numbers up to 256 are exact)
+    order = torch.randperm(n, generator=torch.Generator().manual_seed(n)).to(torch.int32)
+    bad = torch.arange(n) % 7 == 3
+    pages.table[:, :2] = torch.where(bad, n + 1, order).cuda()[:, None]                                     # one page, twice
+    pages.len.fill_(2 * page)
+    q = torch.ones((n, heads, d), dtype=torch.bfloat16, device="cuda")
+    plan, seqs, ptr, st = vb.PrefixPlan(pages, n, n, heads), dev(np.arange(n)), dev(np.arange(n + 1)), torch.full((n,), 9, dtype=torch.int32, device="cuda")
+    want = torch.where(bad, 5, order % 251).to(torch.bfloat16).cuda()[:, None, None].expand(n, heads, d)    # (scores of zero: weights of one)
+    codes = torch.where(bad, -2, 0).cuda()
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(200):
+        out = torch.full_like(q, 5.0)
+        vb.vlac_prefix_plan(pages, plan, seqs, ptr, st)
+        vb.vlac_prefix_attention(pages, 0, plan, q, 0.125, out)
+        wrong += (out != want).sum() + (st != codes).sum()
+    assert wrong.item() == 0 and vb.vlac_prefix_error(plan) == 0
