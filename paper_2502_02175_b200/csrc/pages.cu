@@ -343,8 +343,9 @@ __global__ void __launch_bounds__(PO_THREADS, 1) pages_book_one_kernel(BookArgs 
       }
       const int most = a.max_pages << a.shift;
       if (status == VLAC_OK && (ls < 0 || ls > most || ld < 0 || ld > most)) status = VLAC_ERR_BAD_STATE;
-      if (status == VLAC_OK && (a.op == OP_COMPACT ? k0 < 0 || k1 < k0 || k1 > a.n_keep : rows < 0 || rows > most)) s_bad[tid] = 2;
+      if (status == VLAC_OK && a.op == OP_RESIZE && (rows < 0 || rows > most)) s_bad[tid] = 2;
     }
+    if (a.op == OP_COMPACT && (status != VLAC_OK || k0 < 0 || k1 < k0 || k1 > a.n_keep)) s_bad[tid] = 2;   // its keep list is not looked at
     s_ls[tid] = status == VLAC_OK ? ls : 0; s_ld[tid] = status == VLAC_OK ? ld : 0;          // (nothing is read for a refused entry)
   }
   __syncthreads();

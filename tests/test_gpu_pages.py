@@ -295,3 +295,28 @@ def test_from_cache_takes_a_steps_prompt(vb):
     finally:
         vb.vlac_cache_free(cache)
         vb.vlac_destroy(ctx)
+
+
+@pytest.mark.parametrize("shape", [dict(), dict(max_pages=9000, cap=112)], ids=["short_tables", "long_tables"])
+def test_refused_entries_with_keep_pointers_out_of_range(vb, shape):
+    """Both forms of the bookkeeping: a padded, repeated, read or broken entry is refused for what it is, its pointers are never followed, and
+    the others stand.  (The keep list lies inside a larger buffer.)"""
+    p = Pair(vb, 12, slots=12, **shape)
+    p.resize([0, 1, 2, 3, 4], [40, 40, 40, 40, 40])
+    p.host.len[3] = 10 ** 6
+    p.pages.len.copy_(dev(p.host.len))
+    room = torch.full((20000,), 10 ** 9, dtype=torch.int32, device="cuda")
+    keep = room[10000:10004]
+    keep.copy_(dev([0, 1, 5, 30]))
+    far, low = 9000, -9000
+    src = [0, -1, 12, 1, 1, 3, 2, 4, 2, 0]
+    dst = [5, 6, 7, 5, -7, 8, 2, 12, 9, 10]
+    ptr = [0, 4, far, far, low, low + 1, far, 4, far, 2, 4]
+    want = [0, -1, -1, -1, -1, -2, -1, -1, -1, 0]
+    st = p.status(10)
+    vb.vlac_pages_compact(p.pages, dev(src), dev(dst), dev(ptr), keep, st)
+    assert st.tolist() == want
+    kept = {0: [0, 1, 5, 30], 9: [5, 30]}
+    for i, (a, b) in {i: (src[i], dst[i]) for i in kept}.items():
+        assert p.host.compact([a], [b], [kept[i]]) == [0]
+    p.same(st, want)
