@@ -316,6 +316,7 @@ constexpr int PO_PAGES = 2048;                  // new pages remembered in share
 
 __global__ void __launch_bounds__(PO_THREADS, 1) pages_book_one_kernel(BookArgs a) {
   __shared__ int s_dst[PO_LIST], s_src[PO_LIST], s_ls[PO_LIST], s_ld[PO_LIST], s_bad[PO_LIST], s_lead[PO_LIST], s_shared[PO_LIST], s_total[PO_LIST], s_start[PO_LIST];
+  __shared__ int s_keep0[PO_LIST], s_keeps[PO_LIST];                    // the part of the keep list that is looked at: first, number (0 of a refused entry)
   __shared__ int s_new[PO_PAGES], s_warp[PO_THREADS / 32], s_need, s_taken;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const PagesWork w = pages_work(a.work, a.n_slots, a.n_pages);
@@ -345,7 +346,8 @@ __global__ void __launch_bounds__(PO_THREADS, 1) pages_book_one_kernel(BookArgs 
       if (status == VLAC_OK && (ls < 0 || ls > most || ld < 0 || ld > most)) status = VLAC_ERR_BAD_STATE;
       if (status == VLAC_OK && a.op == OP_RESIZE && (rows < 0 || rows > most)) s_bad[tid] = 2;
     }
-    if (a.op == OP_COMPACT && (status != VLAC_OK || k0 < 0 || k1 < k0 || k1 > a.n_keep)) s_bad[tid] = 2;   // its keep list is not looked at
+    if (a.op == OP_COMPACT && (status != VLAC_OK || k0 < 0 || k1 < k0 || k1 > a.n_keep)) { s_bad[tid] = 2; k0 = k1 = 0; }
+    s_keep0[tid] = k0; s_keeps[tid] = k1 - k0;
     s_ls[tid] = status == VLAC_OK ? ls : 0; s_ld[tid] = status == VLAC_OK ? ld : 0;          // (nothing is read for a refused entry)
   }
   __syncthreads();
@@ -365,12 +367,13 @@ __global__ void __launch_bounds__(PO_THREADS, 1) pages_book_one_kernel(BookArgs 
         if (j < pd) bad |= (unsigned)td[j] >= (unsigned)a.n_pages;
       }
     }
-    if (a.op == OP_COMPACT && !s_bad[i]) {
-      const int e_k0 = a.keep_ptr[i], n = a.keep_ptr[i + 1] - e_k0;
+    if (a.op == OP_COMPACT) {                                           // (uniform over the team: what it goes by was written before the barrier)
+      const int* k = a.keep + s_keep0[i];
+      const int n = s_keeps[i];
       int lead = INT_MAX;
 #pragma unroll 4
       for (int t = at0; t < n; t += step) {
-        const int x = a.keep[e_k0 + t], y = t ? a.keep[e_k0 + t - 1] : -1;
+        const int x = k[t], y = t ? k[t - 1] : -1;
         if (x < 0 || x >= e_ls || x <= y) bad |= 2;
         if (x != t) lead = min(lead, t);
       }

@@ -320,3 +320,19 @@ def test_refused_entries_with_keep_pointers_out_of_range(vb, shape):
     for i, (a, b) in {i: (src[i], dst[i]) for i in kept}.items():
         assert p.host.compact([a], [b], [kept[i]]) == [0]
     p.same(st, want)
+
+
+def test_one_wrong_position_anywhere_in_a_long_keep_list(vb):
+    """One entry, all warps of the bookkeeping on its list: whichever of them meets the wrong position, the code is the same, and a list without
+    one stands."""
+    p = Pair(vb, 13, layers=1, n_pages=600, page=8, heads=1, slots=3, max_pages=300)
+    p.resize([0], [2400])
+    rng, st = p.rng, p.status(1)
+    for at in [1, 31, 32, 511, 512, 513, 1999] + rng.integers(1, 2000, 40).tolist():
+        keep = sorted(rng.choice(2400, 2000, replace=False).tolist())
+        keep[at] = keep[at - 1] if at % 2 else 2400 if at == 1999 else -1
+        vb.vlac_pages_compact(p.pages, dev([0]), dev([1]), dev([0, 2000]), dev(keep), st)
+        assert st.item() == -1, at
+    p.same(st, [-1])
+    assert p.compact([0], [1], [sorted(rng.choice(2400, 2000, replace=False).tolist())]) == [0]
+    assert p.compact([0], [0], [list(range(2000))]) == [0]
