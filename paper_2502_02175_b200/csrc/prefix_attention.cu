@@ -312,6 +312,13 @@ struct AttnArgs {
   void* mem;
 };
 
+// Weights are rounded to the 16-bit type for the product with V.  `shift`: the reference of the exponentials lies that many powers of two below the
+// maximum that moved it, so that the weights use the upper part of the type's range; sums and outputs are scaled alike, and the division by the
+// sum takes it out.  `growth`: the wide kernel moves its reference once the maximum has grown by that many.  bf16 has the exponents of fp32 and needs
+// no shift.  fp16 ends at 2^16 and loses a bit with every power below 2^-14: with the maximum at 2^9 .. 2^15 (narrow: at 2^14) a weight keeps its 11
+// bits down to 2^-23 (2^-28) of the maximum and is lost only below 2^-34 (2^-39), so that many keys far behind a single one count for what they are
+// (65,600 keys 2^-25 behind one hold 0.2 % of the sum; with the maximum at 1 all of them were lost to the output).  The border between shift and
+// growth, measured on 64 chunks of 7 in fp16, all kernels: growth 8 (no shift) 111 us, 6 115, 5 120, 4 127 (O is rescaled more often).
 template <typename T> struct Half2;
 template <> struct Half2<__nv_bfloat16> {
   static __device__ __forceinline__ unsigned pack(float lo, float hi) { __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<unsigned*>(&v); }
@@ -320,6 +327,7 @@ template <> struct Half2<__nv_bfloat16> {
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
   static constexpr unsigned exp_mask = 0x7f80u;
+  static constexpr float shift_narrow = 0.f, shift_wide = 0.f, growth = 8.f;
   static __device__ __forceinline__ float value(unsigned short x) { return __uint_as_float((unsigned)x << 16); }
 };
 template <> struct Half2<__half> {
@@ -329,6 +337,7 @@ template <> struct Half2<__half> {
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
   static constexpr unsigned exp_mask = 0x7c00u;
+  static constexpr float shift_narrow = 14.f, shift_wide = 9.f, growth = 6.f;
   static __device__ __forceinline__ float value(unsigned short x) { return __half2float(__ushort_as_half(x)); }
 };
 
@@ -601,7 +610,7 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
     for (int r = 0; r < 2; ++r) {
       bm[r] = fmaxf(bm[r], __shfl_xor_sync(0xffffffffu, bm[r], 1));
       bm[r] = fmaxf(bm[r], __shfl_xor_sync(0xffffffffu, bm[r], 2));
-      const float mn = fmaxf(m[r], bm[r]);
+      const float mn = fmaxf(m[r], bm[r] - Half2<T>::shift_narrow);
       ref[r] = mn == -INFINITY ? 0.f : mn;                              // a row that has seen nothing yet: no inf - inf
       al[r] = pf_ex2(m[r] - ref[r]);
       m[r] = mn;
@@ -611,8 +620,8 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
 #pragma unroll
       for (int j = 0; j < D / 8; ++j) { o[j][0] *= al[0]; o[j][1] *= al[0]; o[j][2] *= al[1]; o[j][3] *= al[1]; }
     }
-    // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16); the sum l takes
-    // the unrounded weights
+    // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16 and at least 2^-39 of the largest
+    // one, see Half2); the sum l takes the unrounded weights
     unsigned pf[NB][4];
 #pragma unroll
     for (int j = 0; j < 2 * NB; ++j) {
@@ -1111,8 +1120,8 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
             for (int c = valid; c < 128; ++c) pw_st1(s_col + c, 0xff800000u);             // -inf behind them
             pw_st_wait();
           }
-          // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16); the sum takes
-          // the unrounded weights.  P lies over scores already read: 16 columns for 32.
+          // P is rounded to the 16-bit type for the product with V (half a step: 2^-8 of each weight for bf16, 2^-11 for fp16 and at least 2^-34 of the
+          // largest one, see Half2); the sum takes the unrounded weights.  P lies over scores already read: 16 columns for 32.
           const unsigned long long sc = pw_pair(a.scale2, a.scale2);
           unsigned long long ls[2] = {0ull, 0ull};                      // two fp32 sums each
           auto weights = [&](const unsigned* v, unsigned long long nr, unsigned* pk) {
@@ -1126,8 +1135,8 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
             }
           };
           // The weights of the first half are formed with the reference of the block before while the maximum of all 128 scores is still being
-          // found, and formed again in the rare block that moves the reference.  It moves when the maximum has grown by a factor of 2^8:
-          // weights up to 256 cost no precision (they are rounded relative to themselves, l is fp32), and O is seldom rescaled.
+          // found, and formed again in the rare block that moves the reference.  It moves when the maximum has grown by a factor of 2^8 (fp16: 2^6):
+          // larger weights cost no precision (they are rounded relative to themselves, l is fp32), and O is seldom rescaled.
           unsigned pk[32], v[32], x[32];
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
           {
@@ -1148,8 +1157,8 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
               if (q == 0) pw_ld32(s_col + 32u, v);
             }
           }
-          const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2;
-          const bool grow = bm > m + 8.f || m == -INFINITY;
+          const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2 - Half2<T>::shift_wide;
+          const bool grow = bm > m + Half2<T>::growth || m == -INFINITY;
           if (__any_sync(0xffffffffu, grow)) {
             const float mn = grow ? fmaxf(m, bm) : m;
             const float al = mn == -INFINITY ? 1.f : pf_ex2(m - mn);    // (m = -inf: nothing summed yet, 0 * 0)

@@ -511,3 +511,33 @@ def test_findings_of_every_cta_reach_the_plan(vb, n):
         vb.vlac_prefix_attention(pages, 0, plan, q, 0.125, out)
         wrong += (out != want).sum() + (st != codes).sum()
     assert wrong.item() == 0 and vb.vlac_prefix_error(plan) == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("gap", [10.0, 14.0, 16.0, 17.4, 19.0])
+@pytest.mark.parametrize("kv_heads,n,members", [(1024, 4096, 12), (160, 16384, 20)], ids=["narrow", "wide"])
+def test_many_keys_far_behind_one(vb, kv_heads, n, members, gap, dtype):
+    """One key takes nearly all of the sum, and thousands of equal ones make the whole output (its V row is zero): weights far below the largest
+    are not lost to the range of fp16.  So many heads that a piece holds most of a head's keys; the one lies early in some, late in others.
+    Bound: that of the definition, and below fp16's normal numbers half a step of them (2^-25): for the output, and for every weight, in units of the
+    largest (2^14 narrow, at least 2^9 wide)."""
+    c = Case(vb, [(n, [(1, 1)] * members)], kv_heads, kv_heads, 64, page=64, dtype=dtype, seed=int(gap), fill=0.0)
+    p, t = c.pages, c.pages.table[c.seqs[0], :-(-n // c.page)].long()
+    p.k.zero_()
+    p.v[0].uniform_(0.5, 1.0, generator=c.gen)
+    heads = torch.arange(kv_heads, device="cuda")
+    at = (heads * 37) % n                                                     # position of the head's one key
+    p.k[0, t[at // c.page], at % c.page, heads, 0] = gap / 2
+    p.v[0, t[at // c.page], at % c.page, heads] = 0
+    c.q.zero_()
+    c.q[:, :, 0] = 16.0                                                       # times the scale of 1/8: the gap
+    out, lse = c.run()
+    some = [0, 1, kv_heads // 3, kv_heads - 1]
+    t = torch.cat([t, c.pages.table[c.seqs[-1], n // c.page:n // c.page + 1].long()])
+    k, v = (x[0, t][:, :, some].reshape(-1, 4, 64)[:n + 1].double().cpu().numpy() for x in (p.k, p.v))
+    o, l, eo, el = ref.attention(k, v, c.q[-1:, some].double().cpu().numpy(), n + 1, 1, 1, c.scale, HALF[dtype])
+    if dtype is torch.float16:
+        eo = eo + 2.0 ** -25 + n * 2.0 ** -25 * 2.0 ** (-14 if members <= 16 else -9)
+    assert np.all(o > 3 * eo)                                                 # (the bound tells a lost sum from a kept one)
+    assert np.all(np.abs(out[-1:, some].double().cpu().numpy() - o) <= eo)
+    assert np.all(np.abs(lse[-1:, some].double().cpu().numpy() - l) <= el)
