@@ -362,7 +362,9 @@ int vlac_pages_write(const vlac_pages* p, int layer, const int* seqs, const int*
 
 /* Copy positions 0 .. n_rows-1 of sequence seq of a control-step cache into slot `slot`, all layers: the prompt that a step left
  * becomes a prefix that candidates share.  Shapes must agree (bf16 pool of the cache's layers, heads and head_dim, n_rows <= the
- * cache's L + n_action), the slot must already have n_rows rows in pages of its own.  status: device int32 [1]. */
+ * cache's L + n_action), the slot must already have n_rows rows in pages of its own.  status: device int32 [1]; BAD_STATE also where
+ * vlac_step_pruned has dropped one of these positions and no step has recomputed every position of the sequence since (the layers behind the
+ * pruning have no row there). */
 int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int slot, int n_rows, int* status, void* stream);
 
 /* Attention of new rows over paged sequences, the common prefix read once for all that share it.

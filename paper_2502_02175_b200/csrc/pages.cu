@@ -583,6 +583,7 @@ struct WriteArgs {
   Rows16 row16;
   const int *seqs, *start, *row_ptr;            // NULL seqs: one entry, `slot`, rows 0 .. rows-1 at position 0
   int slot;
+  const unsigned char* hidden;                  // with `slot`: 1 = the source holds no row at this position, or NULL
   const uint4 *kin, *vin;
   long long kstride16, vstride16, layer_stride16;
   int* status;
@@ -613,6 +614,7 @@ __global__ void __launch_bounds__(PR_THREADS) pages_write_kernel(WriteArgs a) {
       const int p = t[j];
       bad |= (unsigned)p >= (unsigned)a.n_pages || a.refs[p] != 1;
     }
+  if (code == 0 && a.hidden) for (int j = tid; j < r1; j += PR_THREADS) bad |= a.hidden[j] != 0;
   if (__syncthreads_or(dup)) code = VLAC_ERR_INVALID_ARG;
   if (__syncthreads_or(bad) && code == 0) code = VLAC_ERR_BAD_STATE;
   if (tid == 0 && blockIdx.x == 0 && blockIdx.z == 0) a.status[i] = code;
@@ -771,7 +773,7 @@ int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int s
     return VLAC_ERR_INVALID_ARG;
   const size_t kv = kv_layer_elems(ctx), off = (size_t)seq * kv;
   WriteArgs a = {};
-  a.layer = 0; a.rows = n_rows; a.slot = slot;
+  a.layer = 0; a.rows = n_rows; a.slot = slot; a.hidden = cache->hidden_keys + (size_t)seq * ctx->max_seq;
   a.kin = (const uint4*)(cache->k + off); a.vin = (const uint4*)(cache->v + off);
   a.kstride16 = a.vstride16 = (long long)(pages_row(p) / 8); a.layer_stride16 = (long long)(cache->batch * kv / 8);
   a.status = status;

@@ -68,9 +68,14 @@ void free_cache_buffers(vlac_cache* c) {
   cudaFree(c->tot); cudaFree(c->hidden_keys); cudaFree(c->rowmap); cudaFree(c->slot); cudaFree(c->tmaps_kv);
 }
 
-__global__ void set_warm_kernel(int* warm, int n, int value) {
-  const int i = blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < n) warm[i] = value;
+// The end of a step, a warp per sequence: it is warm, and if every layer recomputed every position no earlier pruning has left holes in its rows.
+__global__ void end_step_kernel(int* warm, const int* M, unsigned char* hidden_keys, int nl, int L, int max_seq) {
+  const int b = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  bool whole = true;
+  for (int l = lane; l < nl; l += 32) whole &= M[b * nl + l] == L;
+  if (__all_sync(0xffffffffu, whole))
+    for (int p = lane; p < max_seq; p += 32) hidden_keys[(size_t)b * max_seq + p] = 0;
+  if (lane == 0) warm[b] = 1;
 }
 
 }  // namespace
@@ -412,7 +417,7 @@ static int enqueue_step(vlac_ctx* ctx, vlac_cache* cache, const unsigned char* f
   VLAC_CUDA_CHECK(cudaMemcpyAsync(cache->prev_frames, frames, frame, cudaMemcpyDeviceToDevice, s));
   VLAC_CUDA_CHECK(cudaMemcpyAsync(cache->attn_prev, cache->attn_next, sizeof(float) * (size_t)B * nl * g.n_heads * ctx->Lv,
                                   cudaMemcpyDeviceToDevice, s));
-  set_warm_kernel<<<1, 32, 0, s>>>(cache->warm, B, 1);
+  end_step_kernel<<<1, 32 * B, 0, s>>>(cache->warm, cache->M, cache->hidden_keys, nl, ctx->L, ctx->max_seq);
   ctx->prune_layer = 0;
   VLAC_LAUNCH_CHECK(ctx);
   return VLAC_OK;

@@ -100,7 +100,7 @@ struct vlac_cache {
   unsigned char *static_mask, *task_mask, *final_mask;       // [b][Lv]
   int *rank, *n_reuse;               // [b][Lv], [b][nl]
   int *M, *rows;                     // [b][nl], [b][nl][L]
-  unsigned char* hidden_keys;        // [batch][max_seq]     1 = position dropped by the pruning baseline (vlac_step_pruned)
+  unsigned char* hidden_keys;        // [batch][max_seq]     1 = position dropped by the pruning baseline (vlac_step_pruned); cleared by a step that recomputes all
   int *tot;                          // [nl]                 total rows over the batch
   int *rowmap;                       // [nl][batch*L]        compact index -> b*L + pos
   int *slot;                         // [nl][batch*L]        b*L + pos -> compact index or -1

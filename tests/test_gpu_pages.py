@@ -336,3 +336,60 @@ def test_one_wrong_position_anywhere_in_a_long_keep_list(vb):
     p.same(st, [-1])
     assert p.compact([0], [1], [sorted(rng.choice(2400, 2000, replace=False).tolist())]) == [0]
     assert p.compact([0], [0], [list(range(2000))]) == [0]
+
+
+def test_from_cache_refuses_what_a_pruned_step_left(vb):
+    """A step that drops vision tokens leaves holes in the later layers: refused, also behind a step that reuses rows, until a sequence is
+    recomputed whole; rows in front of the first hole are taken."""
+    cfg = synth.tiny_config()
+    devm = vb.DeviceModel(synth.make_model(cfg, 2))
+    ctx = vb.vlac_create(vb.make_config(cfg, 2), devm.weights)
+    cache = vb.vlac_cache_alloc(ctx, 2)
+    try:
+        rng = np.random.default_rng(4)
+        feats = vb.upload_bf16(synth.f32_to_bf16(rng.standard_normal((2, cfg.n_vision, cfg.hidden), dtype=np.float32)))
+        frames = torch.from_numpy(np.repeat(synth.rerandomised_pair(cfg, 2, 13)[0][None], 2, 0)).to("cuda").contiguous()
+        ids = torch.from_numpy(np.concatenate([synth.make_prompt_ids(cfg, 1)] * 2)).to("cuda")
+        tokens = torch.zeros((2, cfg.n_action), dtype=torch.int32, device="cuda")
+        pages = vb.Pages.empty(cfg.n_layers, 40, 16, cfg.n_heads, cfg.head_dim, 2, 8)
+        st, st2, L = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"), cfg.seq_len
+        vb.vlac_pages_resize(pages, dev([0, 1]), dev([L, L]), st2)
+
+        def codes(n=L):
+            out = []
+            for seq in range(2):
+                vb.vlac_pages_from_cache(pages, cache, seq, seq, n, st)
+                out.append(st.item())
+            return out
+
+        step = lambda full, params=None: vb.vlac_step(ctx, cache, frames, feats, ids, params, full, tokens)
+        pruned = lambda keep: vb.vlac_step_pruned(ctx, cache, frames, feats, ids, 1, keep, tokens)
+        reuse, _keep = vb.make_params(top_k=32, alpha_override=[0.5, 1.0])
+        step(False, reuse)
+        assert codes() == [0, 0]
+        pruned(24)
+        assert codes() == [-2, -2] and codes(cfg.n_text_pre) == [0, 0]
+        before = pages.k.clone()
+        assert codes() == [-2, -2] and torch.equal(pages.k, before)
+        step(False, reuse)                                                # (rows of dropped positions may be reused: still not there)
+        assert codes() == [-2, -2]
+        vb.vlac_cache_reset(cache, 1)
+        step(False, reuse)
+        assert codes() == [-2, 0]
+        step(True)
+        assert codes() == [0, 0]
+        pruned(24)
+        assert codes() == [-2, -2]
+        pruned(cfg.n_vision)                                              # nothing dropped: a plain step
+        assert codes() == [0, 0]
+        pruned(24)
+        g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=s):
+            step(True)
+        assert codes() == [-2, -2]                                        # captured, not run
+        g.replay()
+        assert codes() == [0, 0]
+    finally:
+        vb.vlac_cache_free(cache)
+        vb.vlac_destroy(ctx)
