@@ -382,7 +382,8 @@ int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int s
  *   plan     n (<= VLAC_PAGES_MAX_LIST), rows of q, n_heads (a multiple of n_kv_heads, n_heads*rows < 2^29), and mem: device
  *            memory of vlac_prefix_bytes(p, n, rows, n_heads) bytes, 16-byte aligned, that holds the plan and the partial sums; a plan
  *            is made before its first attention call (or its first 256 bytes are zero: then nothing is computed), with the pool and the
- *            struct that the attention calls get, and serves one of them at a time (two captured graphs that may overlap need two)
+ *            struct that the attention calls get (a call with another table or shape computes nothing, see vlac_prefix_error), and serves
+ *            one of them at a time (two captured graphs that may overlap need two)
  *   q, out   device, the pool's type, row r at r*q_stride / r*out_stride elements (multiples of 8, at least n_heads*head_dim), 16-byte
  *            aligned;  lse  device fp32 [rows][n_heads] or NULL */
 typedef struct {
@@ -395,7 +396,8 @@ int vlac_prefix_plan(const vlac_pages* p, const vlac_prefix* plan, const int* se
 int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
                           void* out, long long out_stride, float* lse, void* stream);
 /* VLAC_ERR_TIMEOUT if a device-side bounded wait of an attention call gave up since the plan was made (its output is then not
- * valid), as vlac_device_error does for a context; reads one int back and synchronises the stream. */
+ * valid), as vlac_device_error does for a context; INVALID_ARG if a call came with another pool or struct than the plan was made with (its
+ * output was left as it was).  Reads one int back and synchronises the stream. */
 int vlac_prefix_error(const vlac_prefix* plan, void* stream);
 
 const char* vlac_status_string(int status);

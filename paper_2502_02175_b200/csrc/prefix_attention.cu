@@ -41,7 +41,8 @@ struct __align__(16) SegRec {
   int rowbase;                                  // first slot row of this segment
   int keys;                                     // keys of a unit
 };
-struct PlanHead { long long units[2]; int n_act, error; };   // error: a wait of the wide kernel gave up
+// key: what the plan was made for (see plan_key).  An attention call for anything else would read beside its tables and records, and computes nothing.
+struct __align__(16) PlanHead { long long units[2]; unsigned long long key; int n_act, error; };           // error: a wait gave up, or a call had another key
 
 struct PlanMem {
   PlanHead* head;
@@ -86,6 +87,7 @@ struct PlanArgs {
   const int *seqs, *q_ptr;
   int* status;
   void* mem;
+  unsigned long long key;
 };
 // One launch, bound by the chain of dependent reads and barriers, not by bytes: one CTA of 8 warps for few sequences with short tables, a cluster
 // of eight CTAs that reads the tables together otherwise.  8 sequences of 19 pages 4.8 us; 32 of 4132 pages 9.5 us.
@@ -267,7 +269,7 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
   const long long u_pre = units(t_pre, n_pre, keys_pre), u_suf = units(t_suf, n_suf, keys_n);
   const int g0 = at.g;
   if (mine) { s.g[tid] = g0; s.u0[NARROW][tid] = at.u[0]; s.u0[WIDE][tid] = at.u[1]; }
-  if (tid == 0) { PlanHead h = {{all.u[0], all.u[1]}, n_act, 0}; *p.head = h; }
+  if (tid == 0) { PlanHead h = {{all.u[0], all.u[1]}, a.key, n_act, 0}; *p.head = h; }
   __syncthreads();
   if (mine) {
     SeqRec q = {bad ? -1 : s.slot[tid], s.row0[tid], s.nq[tid], s.len[tid], pre > 0 ? s.g[lead] : -1, u_suf > 0 ? g0 + (u_pre > 0) : -1, 0, 0};
@@ -310,8 +312,8 @@ struct AttnArgs {
   float* lse;
   float scale2;                                 // softmax scale * log2(e)
   void* mem;
+  unsigned long long key;
 };
-
 // Weights are rounded to the 16-bit type for the product with V.  `shift`: the reference of the exponentials lies that many powers of two below the
 // maximum that moved it, so that the weights use the upper part of the type's range; sums and outputs are scaled alike, and the division by the
 // sum takes it out.  `growth`: the wide kernel moves its reference once the maximum has grown by that many.  bf16 has the exponents of fp32 and needs
@@ -457,9 +459,10 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
   pdl_trigger();
   if (!EARLY) pdl_wait();
   const int run = warp * PN_CTAS + blockIdx.x;                          // few runs: one per SM before two
+  const unsigned long long key = __ldcg(&pm.head->key);
   const long long U = __ldcg(&pm.head->units[NARROW]), G = runs(NARROW, U);
   const int g = __ldcg(&pm.first[NARROW][run]);
-  if (run >= G) { if (EARLY) pdl_wait(); return; }
+  if (run >= G || key != a.key) { if (EARLY) pdl_wait(); return; }
   Cursor cur;                                                           // pieces not yet begun
   cur.begin(pm, NARROW, run, U, G, g);
 
@@ -902,7 +905,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   pdl_trigger();
   const long long U = pm.head->units[WIDE], G = runs(WIDE, U);
   const int g_first = pm.first[WIDE][run];
-  if (run >= G) return;                                                 // uniform over the CTA
+  if (run >= G || pm.head->key != a.key) return;                        // uniform over the CTA
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(pf_smem(&tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -1295,6 +1298,10 @@ __global__ void __launch_bounds__(256, OCC) prefix_join_kernel(AttnArgs a) {
   pdl_wait();
   const PlanHead hd = *p.head;
   const SeqRec q = p.seq[blockIdx.x];
+  if (hd.key != a.key) {                                                // (0: no plan yet)
+    if (hd.key != 0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicExch(&p.head->error, VLAC_ERR_INVALID_ARG);
+    return;
+  }
   if ((int)blockIdx.x >= hd.n_act || q.slot < 0) return;                // (slot -1: refused)
   SegRec sg[2];
 #pragma unroll
@@ -1444,6 +1451,21 @@ bool small_call(const vlac_pages* p, const vlac_prefix* plan) {
   return p->n_kv_heads * tiles * blocks <= pf_runs(NARROW);
 }
 
+// 64 bits of everything that the records of a plan and the tables' extent depend on, and of the tables' address (the steps of splitmix64 by
+// Steele, Lea and Flood over one field after the other: two different calls agree by a chance of 2^-64); never 0.
+unsigned long long plan_key(const vlac_pages* p, const vlac_prefix* plan) {
+  const unsigned long long fields[] = {(unsigned long long)(uintptr_t)p->table, (unsigned)p->n_slots, (unsigned)p->max_pages, (unsigned)p->n_pages, (unsigned)p->page_size,
+                                       (unsigned)p->n_kv_heads, (unsigned)p->head_dim, (unsigned)plan->n_heads, (unsigned)plan->n, (unsigned)plan->rows};
+  unsigned long long h = 0;
+  for (const unsigned long long f : fields) {
+    h = (h ^ f) + 0x9e3779b97f4a7c15ull;
+    h = (h ^ (h >> 30)) * 0xbf58476d1ce4e5b9ull;
+    h = (h ^ (h >> 27)) * 0x94d049bb133111ebull;
+    h ^= h >> 31;
+  }
+  return h ? h : 1;
+}
+
 int plan_check(const vlac_pages* p, const vlac_prefix* plan) {
   const int rc = pages_check(p);
   if (rc != VLAC_OK) return rc;
@@ -1477,6 +1499,7 @@ int vlac_prefix_plan(const vlac_pages* p, const vlac_prefix* plan, const int* se
   a.table = p->table; a.len = p->len; a.n_slots = p->n_slots; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size;
   a.shift = pages_shift(p->page_size); a.kv_heads = p->n_kv_heads; a.ratio = plan->n_heads / p->n_kv_heads; a.head_dim = p->head_dim;
   a.n = plan->n; a.rows = plan->rows; a.n_heads = plan->n_heads; a.small = small_call(p, plan); a.seqs = seqs; a.q_ptr = q_ptr; a.status = status; a.mem = plan->mem;
+  a.key = plan_key(p, plan);
   const size_t smem = sizeof(PlanShared);
   if (plan->n <= 16 && (long long)plan->n * p->max_pages <= PL_ONE) {
     TRY(big_smem<prefix_plan_kernel<1>>((int)smem));
@@ -1495,7 +1518,7 @@ int vlac_prefix_error(const vlac_prefix* plan, void* stream) {
   int v = 0;
   VLAC_CUDA_CHECK(cudaMemcpyAsync(&v, (const char*)plan->mem + offsetof(PlanHead, error), sizeof(int), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
   VLAC_CUDA_CHECK(cudaStreamSynchronize((cudaStream_t)stream));
-  return v ? VLAC_ERR_TIMEOUT : VLAC_OK;
+  return v == VLAC_ERR_INVALID_ARG ? VLAC_ERR_INVALID_ARG : v ? VLAC_ERR_TIMEOUT : VLAC_OK;
 }
 
 int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
@@ -1512,7 +1535,7 @@ int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* pla
   a.table = p->table; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size; a.shift = pages_shift(p->page_size);
   a.kv_heads = p->n_kv_heads; a.ratio = plan->n_heads / p->n_kv_heads; a.n_heads = plan->n_heads; a.n = plan->n; a.rows = plan->rows;
   a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
-  a.scale2 = scale * 1.44269504088896f; a.mem = plan->mem;
+  a.scale2 = scale * 1.44269504088896f; a.mem = plan->mem; a.key = plan_key(p, plan);
   cudaStream_t s = (cudaStream_t)stream;
   const bool small = small_call(p, plan);
   if (p->dtype == VLAC_BF16) return p->head_dim == 128 ? launch_attention<__nv_bfloat16, 128>(a, small, s) : launch_attention<__nv_bfloat16, 64>(a, small, s);

@@ -541,3 +541,34 @@ def test_many_keys_far_behind_one(vb, kv_heads, n, members, gap, dtype):
     assert np.all(o > 3 * eo)                                                 # (the bound tells a lost sum from a kept one)
     assert np.all(np.abs(out[-1:, some].double().cpu().numpy() - o) <= eo)
     assert np.all(np.abs(lse[-1:, some].double().cpu().numpy() - l) <= el)
+
+
+@pytest.mark.parametrize("members", [2, 20], ids=["narrow", "wide"])
+def test_a_plan_for_something_else_computes_nothing(vb, members):
+    """Through the C interface: a plan's memory used with another pool, or with other numbers of sequences, rows or heads, leaves the output as it
+    was and says so; its own pool's calls are right before and behind."""
+    c = Case(vb, [(400, [(n + 1, 1) for n in range(members)])], 4, 4, 64, seed=16)
+    first = c.run(plan=(plan := vb.PrefixPlan(c.pages, members, c.rows, 4)))
+    c.check(*first)
+    p = c.pages
+    others = [vb.Pages.empty(1, 4, 16, 4, 64, 3, 2), vb.Pages(p.k, p.v, p.table.clone(), p.len, p.refs),
+              vb.Pages(p.k, p.v, p.table[:, :30].contiguous(), p.len, p.refs), vb.Pages(p.k[:, :5].contiguous(), p.v[:, :5].contiguous(), p.table, p.len, p.refs[:5])]
+    out, q = torch.full((64, 4, 64), 5.0, dtype=c.dtype, device="cuda"), torch.zeros((64, 4, 64), dtype=c.dtype, device="cuda")
+    big = torch.zeros((1 << 24,), dtype=torch.uint8, device="cuda")      # room for every form of the struct
+    big[:plan.mem.numel()] = plan.mem
+    st, seqs, ptr = c.st(members), dev(c.seqs), dev(np.concatenate([[0], np.cumsum(c.nq)]))
+
+    def call(pool, n=members, rows=c.rows, heads=4):
+        x = vb.vlac_prefix(n, rows, heads, big.data_ptr(), big.numel())
+        rc = vb.lib.vlac_prefix_attention(pool.ref, 0, vb.C.byref(x), q.data_ptr(), heads * 64, 0.125, out.data_ptr(), heads * 64, None, torch.cuda.current_stream().cuda_stream)
+        return rc, vb.lib.vlac_prefix_error(vb.C.byref(x), torch.cuda.current_stream().cuda_stream)
+
+    mine = vb.vlac_prefix(members, c.rows, 4, big.data_ptr(), big.numel())
+    for pool, other in [(o, {}) for o in others] + [(p, dict(n=members + 1)), (p, dict(n=members - 1)), (p, dict(rows=c.rows + 1)), (p, dict(heads=8))]:
+        vb.lib.vlac_prefix_plan(p.ref, vb.C.byref(mine), seqs.data_ptr(), ptr.data_ptr(), st.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        assert vb.lib.vlac_prefix_error(vb.C.byref(mine), torch.cuda.current_stream().cuda_stream) == 0
+        assert call(pool, **other) == (0, -1)
+        assert torch.all(out == 5.0)
+    vb.lib.vlac_prefix_plan(p.ref, vb.C.byref(mine), seqs.data_ptr(), ptr.data_ptr(), st.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    q[:c.rows] = c.q
+    assert call(p) == (0, 0) and torch.equal(out[:c.rows], first[0]) and torch.all(out[c.rows:] == 5.0)
