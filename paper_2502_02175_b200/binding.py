@@ -69,7 +69,7 @@ EXPORTS = ("vlac_create", "vlac_destroy", "vlac_cache_alloc", "vlac_cache_reset"
            "vlac_selftest_wait_expiry",
            "vlac_pages_work_bytes", "vlac_pages_resize", "vlac_pages_free", "vlac_pages_fork", "vlac_pages_compact", "vlac_pages_write",
            "vlac_pages_from_cache", "vlac_prefix_bytes", "vlac_prefix_plan", "vlac_prefix_attention",
-           "vlac_prefix_error")
+           "vlac_prefix_error", "vlac_selftest_prefix_wait")
 
 lib.vlac_status_string.restype = C.c_char_p
 lib.vlac_status_string.argtypes = [C.c_int]
@@ -114,6 +114,7 @@ lib.vlac_prefix_bytes.argtypes = [_P, _I, _I, _I]
 lib.vlac_prefix_plan.argtypes = [_P, _P, _P, _P, _P, _P]
 lib.vlac_prefix_error.argtypes = [_P, _P]
 lib.vlac_prefix_attention.argtypes = [_P, _I, _P, _P, _LL, C.c_float, _P, _LL, _P, _P]
+lib.vlac_selftest_prefix_wait.argtypes = [_P, _I, _P, _P, _LL, C.c_float, _P, _LL, _P, C.c_uint, C.c_uint, _P]
 
 
 class VlacError(RuntimeError):
@@ -530,6 +531,19 @@ def vlac_prefix_attention(pages: Pages, layer: int, plan: PrefixPlan, q: torch.T
 
 def vlac_prefix_error(plan: PrefixPlan) -> int:
     return int(lib.vlac_prefix_error(plan.ref, _here(plan.index)))
+
+
+def vlac_selftest_prefix_wait(pages: Pages, layer: int, plan: PrefixPlan, q: torch.Tensor, scale: float, out: torch.Tensor, lse: Optional[torch.Tensor],
+                              delay_us: int, limit_us: int) -> None:
+    """``vlac_prefix_attention`` with loads that begin late and waits that give up after ``limit_us``."""
+    dev, shape = pages.index, (plan.rows, plan.n_heads, pages.head_dim)
+    stream = _here(dev)
+    assert plan.pages is pages
+    assert lse is None or (lse.dtype is torch.float32 and lse.get_device() == dev and lse.is_contiguous() and lse.shape == shape[:2])
+    q_ptr, q_stride = _rows(q, shape, pages)
+    out_ptr, out_stride = _rows(out, shape, pages)
+    _check(lib.vlac_selftest_prefix_wait(pages.ref, layer, plan.ref, q_ptr, q_stride, scale, out_ptr, out_stride, _ptr(lse), delay_us, limit_us, stream),
+           "vlac_selftest_prefix_wait")
 
 
 # --------------------------------------------------------------------------- reading views back

@@ -745,21 +745,22 @@ __device__ __forceinline__ bool pw_try_at(unsigned bar, unsigned parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// Wait for a phase, at most PW_WAIT_LIMIT_NS; a wait that gives up (or finds that another has) returns false and marks the plan.
-__device__ __noinline__ bool pw_wait_slow(unsigned bar, unsigned parity, volatile int* abort_flag, int* error) {
+// Wait for a phase, at most `limit`; a wait that gives up (or finds that another has) returns false and marks the plan.  Its loop leaves lane by lane:
+// where instructions of the whole warp follow, the caller brings the lanes together again.
+__device__ __noinline__ bool pw_wait_slow(unsigned bar, unsigned parity, volatile int* abort_flag, int* error, unsigned long long limit) {
   const unsigned long long t0 = pw_ns();
   while (true) {
     for (int i = 0; i < 16; ++i)
       if (pw_try_at(bar, parity)) return true;
     if (*abort_flag) return false;
-    if (pw_ns() - t0 > PW_WAIT_LIMIT_NS) break;
+    if (pw_ns() - t0 > limit) break;
   }
   *abort_flag = 1;
   atomicExch(error, VLAC_ERR_TIMEOUT);
   return false;
 }
-__device__ __forceinline__ bool pw_wait(unsigned long long* bar, unsigned parity, volatile int* abort_flag, int* error) {
-  return pw_try_at(pf_smem(bar), parity) || pw_wait_slow(pf_smem(bar), parity, abort_flag, error);
+__device__ __forceinline__ bool pw_wait(unsigned long long* bar, unsigned parity, volatile int* abort_flag, int* error, unsigned long long limit) {
+  return pw_try_at(pf_smem(bar), parity) || pw_wait_slow(pf_smem(bar), parity, abort_flag, error, limit);
 }
 __device__ __forceinline__ void pw_tma(unsigned dst, const CUtensorMap* tm, int x, int y, unsigned long long* bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -871,6 +872,8 @@ struct WideArgs {
   AttnArgs a;
   int flip;                                     // 1: the scale is negative (scale2 holds its magnitude; Q's signs are flipped)
   int box;                                      // rows of a TMA box: min(page, 128)
+  unsigned delay_ns;                            // 0; the self-test holds the loads back
+  unsigned long long limit_ns;                  // a wait gives up after it
 };
 
 // QTMA: Q comes by TMA, boxes of (64 elements, the query heads of a K/V head, rows), which lie in shared memory as the stacked rows do.  Needs a
@@ -929,9 +932,10 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     const int none = a.n_pages << a.shift;                              // a row behind the pool: zeros
     int cnt = 0;
     bool ok = true;
+    if (w.delay_ns) for (const unsigned long long t0 = pw_ns(); pw_ns() - t0 < w.delay_ns;) __nanosleep(500);
     auto put = [&](const CUtensorMap* tm, int y, int x0) {
       const int s = cnt % W::SLOTS;
-      if (cnt >= W::SLOTS) ok = __all_sync(0xffffffffu, pw_wait(&empty[s], ((cnt / W::SLOTS) & 1) ^ 1, &abort_flag, error));
+      if (cnt >= W::SLOTS) ok = __all_sync(0xffffffffu, pw_wait(&empty[s], ((cnt / W::SLOTS) & 1) ^ 1, &abort_flag, error, w.limit_ns));
       if (!ok) return;
       if (first == 0 && lane == 0) pw_expect(&full[s], W::TILE);
       if (mine) pw_tma(ring + (unsigned)s * W::TILE + (unsigned)half * W::HALF + (unsigned)chunk * w.box * 128u, tm, x0 + half * 64, y, &full[s]);
@@ -960,7 +964,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     }
     if (!ok) {                                                          // given up: let what is in flight land (whoever else gave up)
       int alone = 0;
-      for (int c = max(0, cnt - W::SLOTS); c < cnt; ++c) pw_wait(&full[c % W::SLOTS], (c / W::SLOTS) & 1, &alone, error);
+      for (int c = max(0, cnt - W::SLOTS); c < cnt; ++c) pw_wait(&full[c % W::SLOTS], (c / W::SLOTS) & 1, &alone, error, PW_WAIT_LIMIT_NS);
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- products
@@ -976,7 +980,10 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     unsigned phase = 0, failed = 0;
     bool ok = true;
     auto wait_at = [&](unsigned bar, unsigned parity) {
-      if (!__all_sync(0xffffffffu, pw_try_at(bar, parity))) failed |= !pw_wait_slow(bar, parity, &abort_flag, error);       // (all lanes or none)
+      if (!__all_sync(0xffffffffu, pw_try_at(bar, parity))) {            // (all lanes or none)
+        failed |= !pw_wait_slow(bar, parity, &abort_flag, error, w.limit_ns);
+        __syncwarp();
+      }
     };
     auto still_ok = [&]() { return __all_sync(0xffffffffu, !failed); };
     auto same = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };    // tells the compiler that a value is the same in all lanes
@@ -1065,7 +1072,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     if (!ok) {
       int alone = 0;
       pw_commit(&drain, one);
-      pw_wait(&drain, 0, &alone, error);
+      pw_wait(&drain, 0, &alone, error, PW_WAIT_LIMIT_NS);
     }
     __syncwarp();
   } else if (warp >= 4) {
@@ -1114,7 +1121,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       const bool idle = row_t - lane >= p.nr;                           // a warp without rows: only its arrivals are needed
       const int step = two ? 1 : 2, first = two ? 0 : side;
       for (int i = first; i < p.n; i += step) {
-        ok = __all_sync(0xffffffffu, pw_wait(&s_full[side], n_s++ & 1, &abort_flag, error));
+        ok = __all_sync(0xffffffffu, pw_wait(&s_full[side], n_s++ & 1, &abort_flag, error, w.limit_ns));
         if (!ok) break;
         if (!idle) {
           pw_after();
@@ -1211,9 +1218,10 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       Piece pn;
       const bool more = cur.more();
       if (more) { cur.next(pm, &pn); if (!QTMA) load_q(pn); }
-      if (ok) ok = pw_wait(&o_full, pieces & 1, &abort_flag, error);
+      if (ok) ok = pw_wait(&o_full, pieces & 1, &abort_flag, error, w.limit_ns);
       ++pieces;
       ok = pw_all_ok(ok);                                               // every product of the piece is done: Q's memory is free
+      __syncwarp();
       if (!ok) break;
       if (!two) {
         red_m[side * 128 + r] = m; red_l[side * 128 + r] = l;
@@ -1414,10 +1422,10 @@ int launch_narrow(const AttnArgs& a, cudaStream_t s) {
 }
 
 template <typename T, int D>
-int launch_attention(const AttnArgs& a, bool small, cudaStream_t s) {
+int launch_attention(const AttnArgs& a, bool small, unsigned delay_ns, unsigned long long limit_ns, cudaStream_t s) {
   // more than 16 stacked rows, or the call cannot have a wide segment
   if ((long long)a.rows * a.ratio > pf_bm(NARROW) && !small) {
-    WideArgs w = {a, a.scale2 < 0.f, a.page < 128 ? a.page : 128};
+    WideArgs w = {a, a.scale2 < 0.f, a.page < 128 ? a.page : 128, delay_ns, limit_ns};
     w.a.scale2 = fmaxf(fabsf(a.scale2), 1e-30f);                        // not zero: -inf marks what is not there
     CUtensorMap tk, tv, tq;
     const int rows = a.n_pages << a.shift, cols = a.kv_heads * D;
@@ -1477,6 +1485,27 @@ int plan_check(const vlac_pages* p, const vlac_prefix* plan) {
   return VLAC_OK;
 }
 
+int attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale, void* out, long long out_stride,
+              float* lse, unsigned delay_ns, unsigned long long limit_ns, cudaStream_t s) {
+  const int rc = plan_check(p, plan);
+  if (rc != VLAC_OK) return rc;
+  if (layer < 0 || layer >= p->n_layers || !isfinite(scale)) return VLAC_ERR_INVALID_ARG;
+  if (plan->n == 0 || plan->rows == 0) return VLAC_OK;
+  const long long w = (long long)plan->n_heads * p->head_dim;
+  if (!q || !out || q_stride < w || out_stride < w || q_stride % 8 || out_stride % 8 || (((uintptr_t)q | (uintptr_t)out) & 15u) || ((uintptr_t)lse & 3u))
+    return VLAC_ERR_INVALID_ARG;
+  AttnArgs a = {};
+  a.k = (const unsigned short*)p->k + (size_t)layer * pages_layer(p); a.v = (const unsigned short*)p->v + (size_t)layer * pages_layer(p);
+  a.table = p->table; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size; a.shift = pages_shift(p->page_size);
+  a.kv_heads = p->n_kv_heads; a.ratio = plan->n_heads / p->n_kv_heads; a.n_heads = plan->n_heads; a.n = plan->n; a.rows = plan->rows;
+  a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
+  a.scale2 = scale * 1.44269504088896f; a.mem = plan->mem; a.key = plan_key(p, plan);
+  const bool small = small_call(p, plan);
+  auto launch = p->dtype == VLAC_BF16 ? (p->head_dim == 128 ? launch_attention<__nv_bfloat16, 128> : launch_attention<__nv_bfloat16, 64>)
+                                      : (p->head_dim == 128 ? launch_attention<__half, 128> : launch_attention<__half, 64>);
+  return launch(a, small, delay_ns, limit_ns, s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1523,23 +1552,13 @@ int vlac_prefix_error(const vlac_prefix* plan, void* stream) {
 
 int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
                           void* out, long long out_stride, float* lse, void* stream) {
-  const int rc = plan_check(p, plan);
-  if (rc != VLAC_OK) return rc;
-  if (layer < 0 || layer >= p->n_layers || !isfinite(scale)) return VLAC_ERR_INVALID_ARG;
-  if (plan->n == 0 || plan->rows == 0) return VLAC_OK;
-  const long long w = (long long)plan->n_heads * p->head_dim;
-  if (!q || !out || q_stride < w || out_stride < w || q_stride % 8 || out_stride % 8 || (((uintptr_t)q | (uintptr_t)out) & 15u) || ((uintptr_t)lse & 3u))
-    return VLAC_ERR_INVALID_ARG;
-  AttnArgs a = {};
-  a.k = (const unsigned short*)p->k + (size_t)layer * pages_layer(p); a.v = (const unsigned short*)p->v + (size_t)layer * pages_layer(p);
-  a.table = p->table; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size; a.shift = pages_shift(p->page_size);
-  a.kv_heads = p->n_kv_heads; a.ratio = plan->n_heads / p->n_kv_heads; a.n_heads = plan->n_heads; a.n = plan->n; a.rows = plan->rows;
-  a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
-  a.scale2 = scale * 1.44269504088896f; a.mem = plan->mem; a.key = plan_key(p, plan);
-  cudaStream_t s = (cudaStream_t)stream;
-  const bool small = small_call(p, plan);
-  if (p->dtype == VLAC_BF16) return p->head_dim == 128 ? launch_attention<__nv_bfloat16, 128>(a, small, s) : launch_attention<__nv_bfloat16, 64>(a, small, s);
-  return p->head_dim == 128 ? launch_attention<__half, 128>(a, small, s) : launch_attention<__half, 64>(a, small, s);
+  return attention(p, layer, plan, q, q_stride, scale, out, out_stride, lse, 0, PW_WAIT_LIMIT_NS, (cudaStream_t)stream);
+}
+
+int vlac_selftest_prefix_wait(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
+                              void* out, long long out_stride, float* lse, unsigned int delay_us, unsigned int limit_us, void* stream) {
+  if (delay_us > 100000 || limit_us < 1 || limit_us > 100000) return VLAC_ERR_INVALID_ARG;
+  return attention(p, layer, plan, q, q_stride, scale, out, out_stride, lse, delay_us * 1000u, limit_us * 1000ull, (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -572,3 +572,21 @@ def test_a_plan_for_something_else_computes_nothing(vb, members):
     vb.lib.vlac_prefix_plan(p.ref, vb.C.byref(mine), seqs.data_ptr(), ptr.data_ptr(), st.data_ptr(), torch.cuda.current_stream().cuda_stream)
     q[:c.rows] = c.q
     assert call(p) == (0, 0) and torch.equal(out[:c.rows], first[0]) and torch.all(out[c.rows:] == 5.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("heads,kv_heads,d", [(4, 4, 128), (4, 4, 64), (6, 2, 64), (8, 1, 128)])
+@pytest.mark.parametrize("members", [20, 150])
+def test_loads_that_come_late(vb, members, heads, kv_heads, d, dtype):
+    """Common pages that arrive a millisecond late: every wait takes its slow path, and the bits are the same."""
+    c = Case(vb, [(1500, [(2, 1)] * members)], heads, kv_heads, d, dtype=dtype, seed=17)
+    plan = vb.PrefixPlan(c.pages, members, c.rows, heads)
+    first = c.run(plan=plan)
+    c.check(*first, only=(0, members - 1))
+    out, lse = torch.zeros_like(first[0]), torch.zeros_like(first[1])
+    vb.vlac_selftest_prefix_wait(c.pages, 0, plan, c.q, c.scale, out, lse, 1000, 100000)
+    assert vb.vlac_prefix_error(plan) == 0
+    assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    for delay, limit in ((100001, 10), (0, 0), (0, 100001)):
+        with pytest.raises(vb.VlacError):
+            vb.vlac_selftest_prefix_wait(c.pages, 0, plan, c.q, c.scale, out, lse, delay, limit)
