@@ -920,6 +920,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   Cursor cur;
   cur.begin(pm, WIDE, run, U, G, g_first);
   Piece p;
+  int sent = 0;                                                         // loads: tiles this warp has asked for; products: pieces' Q
 
   if (warp < 4 && warp != 1) {
     // ---------------------------------------------------------------- loads
@@ -930,17 +931,16 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     const int n_box = 128 / w.box * W::HALVES, b = first + 3 * lane, chunk = b / W::HALVES, half = b % W::HALVES;
     const bool mine = b < n_box;
     const int none = a.n_pages << a.shift;                              // a row behind the pool: zeros
-    int cnt = 0;
     bool ok = true;
     if (w.delay_ns) for (const unsigned long long t0 = pw_ns(); pw_ns() - t0 < w.delay_ns;) __nanosleep(500);
     auto put = [&](const CUtensorMap* tm, int y, int x0) {
-      const int s = cnt % W::SLOTS;
-      if (cnt >= W::SLOTS) ok = __all_sync(0xffffffffu, pw_wait(&empty[s], ((cnt / W::SLOTS) & 1) ^ 1, &abort_flag, error, w.limit_ns));
+      const int s = sent % W::SLOTS;
+      if (sent >= W::SLOTS) ok = __all_sync(0xffffffffu, pw_wait(&empty[s], ((sent / W::SLOTS) & 1) ^ 1, &abort_flag, error, w.limit_ns));
       if (!ok) return;
       if (first == 0 && lane == 0) pw_expect(&full[s], W::TILE);
       if (mine) pw_tma(ring + (unsigned)s * W::TILE + (unsigned)half * W::HALF + (unsigned)chunk * w.box * 128u, tm, x0 + half * 64, y, &full[s]);
       __syncwarp();
-      ++cnt;
+      ++sent;
     };
     while (cur.more() && ok) {
       cur.next(pm, &p);
@@ -961,10 +961,6 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
         yp = y; y = yn;
       }
       if (ok && !two) put(&tm_v, yp, p.head * D);
-    }
-    if (!ok) {                                                          // given up: let what is in flight land (whoever else gave up)
-      int alone = 0;
-      for (int c = max(0, cnt - W::SLOTS); c < cnt; ++c) pw_wait(&full[c % W::SLOTS], (c / W::SLOTS) & 1, &alone, error, PW_WAIT_LIMIT_NS);
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- products
@@ -1027,6 +1023,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
             for (int hf = 0; hf < W::HALVES; ++hf)
               pw_tma3(q_s + t * W::TILE + hf * W::HALF, &tm_q, hf * 64, p.head * a.ratio, p.row0 + (p.rt * 256 + t * 128) / a.ratio, &q_full);
         }
+        ++sent;
         __syncwarp();
       }
       there(0);
@@ -1068,11 +1065,6 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
       }
       if (ok) pw_commit(&o_full, one);
       ++pieces;
-    }
-    if (!ok) {
-      int alone = 0;
-      pw_commit(&drain, one);
-      pw_wait(&drain, 0, &alone, error, PW_WAIT_LIMIT_NS);
     }
     __syncwarp();
   } else if (warp >= 4) {
@@ -1286,6 +1278,18 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
     pw_before();
   }
   __syncthreads();
+  if (abort_flag) {                                                     // somebody gave up (uniform): what is in flight lands first, products and copies
+    int alone = 0;
+    if (warp == 1) {
+      unsigned one;
+      asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(one));        // (the lane that issued the products)
+      pw_commit(&drain, one);
+      pw_wait(&drain, 0, &alone, error, PW_WAIT_LIMIT_NS);
+      if (QTMA && sent > 0) pw_wait(&q_full, (sent - 1) & 1, &alone, error, PW_WAIT_LIMIT_NS);
+    } else if (warp < 4)
+      for (int c = max(0, sent - W::SLOTS); c < sent; ++c) pw_wait(&full[c % W::SLOTS], (c / W::SLOTS) & 1, &alone, error, PW_WAIT_LIMIT_NS);
+    __syncwarp();
+  }
   if (warp == 1) {
     pw_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");

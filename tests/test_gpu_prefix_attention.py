@@ -590,3 +590,23 @@ def test_loads_that_come_late(vb, members, heads, kv_heads, d, dtype):
     for delay, limit in ((100001, 10), (0, 0), (0, 100001)):
         with pytest.raises(vb.VlacError):
             vb.vlac_selftest_prefix_wait(c.pages, 0, plan, c.q, c.scale, out, lse, delay, limit)
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,dtype", [(4, 4, 128, torch.bfloat16), (4, 4, 64, torch.float16), (6, 2, 64, torch.bfloat16), (8, 1, 128, torch.float16)])
+@pytest.mark.parametrize("prefix,members", [(64, 20), (1500, 20), (3000, 150)])
+def test_waits_that_give_up(vb, prefix, members, heads, kv_heads, d, dtype):
+    """Loads that begin behind the waits' limit: the call ends, the plan says so, and the next plan and call are right (products, copies and
+    tensor memory of the one that gave up are done with).  With few and many tiles for the ring, Q by TMA and by hand."""
+    c = Case(vb, [(prefix, [(2, 1)] * members)], heads, kv_heads, d, dtype=dtype, seed=18)
+    plan = vb.PrefixPlan(c.pages, members, c.rows, heads)
+    first = c.run(plan=plan)
+    c.check(*first, only=(0, members - 1))
+    out, lse = torch.zeros_like(first[0]), torch.zeros_like(first[1])
+    vb.vlac_selftest_prefix_wait(c.pages, 0, plan, c.q, c.scale, out, lse, 5000, 500)
+    assert vb.vlac_prefix_error(plan) == -5
+    vb.vlac_prefix_attention(c.pages, 0, plan, c.q, c.scale, out, lse)
+    assert vb.vlac_prefix_error(plan) == -5                              # until the next plan
+    assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    for _ in range(3):
+        again = c.run(plan=plan)                                         # (asserts that the error is gone)
+        assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
