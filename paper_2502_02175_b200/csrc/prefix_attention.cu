@@ -130,6 +130,25 @@ __device__ Sums plan_scan(Sums* part, const Sums& v, int n, Sums* total) {
   return before;
 }
 
+// What an entry says, and its code as far as it does not depend on the pages or on other entries.
+__device__ __forceinline__ int plan_entry(const PlanArgs& a, int i, int* slot, int* q0, int* q1, int* len) {
+  *q0 = a.q_ptr[i]; *q1 = a.q_ptr[i + 1]; *slot = a.seqs[i];
+  if (*q0 < 0 || *q1 > a.rows || (unsigned)*slot >= (unsigned)a.n_slots) return VLAC_ERR_INVALID_ARG;
+  *len = a.len[*slot];
+  return *len < 0 || *len > a.max_pages << a.shift ? VLAC_ERR_BAD_STATE : VLAC_OK;
+}
+
+// A plan without rows: the entries' codes are all there is to say.
+__global__ void __launch_bounds__(PL_MAX, 1) prefix_status_kernel(PlanArgs a) {
+  pdl_trigger();
+  pdl_wait();
+  const int i = threadIdx.x;
+  int slot, q0 = 0, q1 = 0, len, status = VLAC_OK;
+  if (i < a.n) status = plan_entry(a, i, &slot, &q0, &q1, &len);
+  const int broken = __syncthreads_or(i < a.n && q1 < q0);
+  if (i < a.n) a.status[i] = broken ? VLAC_ERR_INVALID_ARG : status;
+}
+
 template <int CTAS>
 __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_plan_kernel(PlanArgs a) {
   extern __shared__ __align__(16) unsigned char pl_raw[];
@@ -139,15 +158,8 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(1024, 1) prefix_p
   pdl_trigger();
   pdl_wait();
   // ---- the active sequences (rows to compute), in list order: every CTA for itself
-  int status = VLAC_OK, slot = 0, q0 = 0, q1 = 0, len = 0;
-  if (tid < a.n) {
-    q0 = a.q_ptr[tid]; q1 = a.q_ptr[tid + 1]; slot = a.seqs[tid];
-    if (q0 < 0 || q1 > a.rows || (unsigned)slot >= (unsigned)a.n_slots) status = VLAC_ERR_INVALID_ARG;
-    else {
-      len = a.len[slot];
-      if (len < 0 || len > a.max_pages << a.shift) status = VLAC_ERR_BAD_STATE;
-    }
-  }
+  int slot = 0, q0 = 0, q1 = 0, len = 0, status = VLAC_OK;
+  if (tid < a.n) status = plan_entry(a, tid, &slot, &q0, &q1, &len);
   const bool want = tid < a.n && status == VLAC_OK && q1 > q0;
   const unsigned ball = __ballot_sync(0xffffffffu, want);
   if (lane == 0) s.warps[warp] = __popc(ball);
@@ -1524,15 +1536,15 @@ int vlac_prefix_plan(const vlac_pages* p, const vlac_prefix* plan, const int* se
   const int rc = plan_check(p, plan);
   if (rc != VLAC_OK || plan->n == 0) return rc;
   if (!seqs || !q_ptr || !status) return VLAC_ERR_INVALID_ARG;
-  if (plan->rows == 0) {                          // nothing to compute; every entry is fine
-    VLAC_CUDA_CHECK(cudaMemsetAsync(status, 0, sizeof(int) * plan->n, (cudaStream_t)stream));
-    return VLAC_OK;
-  }
   PlanArgs a = {};
   a.table = p->table; a.len = p->len; a.n_slots = p->n_slots; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size;
   a.shift = pages_shift(p->page_size); a.kv_heads = p->n_kv_heads; a.ratio = plan->n_heads / p->n_kv_heads; a.head_dim = p->head_dim;
   a.n = plan->n; a.rows = plan->rows; a.n_heads = plan->n_heads; a.small = small_call(p, plan); a.seqs = seqs; a.q_ptr = q_ptr; a.status = status; a.mem = plan->mem;
   a.key = plan_key(p, plan);
+  if (plan->rows == 0) {                          // nothing to compute, and no plan memory
+    VLAC_CUDA_CHECK(launch_pdl(prefix_status_kernel, dim3(1), dim3(PL_MAX), 0, (cudaStream_t)stream, a));
+    return VLAC_OK;
+  }
   const size_t smem = sizeof(PlanShared);
   if (plan->n <= 16 && (long long)plan->n * p->max_pages <= PL_ONE) {
     TRY(big_smem<prefix_plan_kernel<1>>((int)smem));

@@ -610,3 +610,16 @@ def test_waits_that_give_up(vb, prefix, members, heads, kv_heads, d, dtype):
     for _ in range(3):
         again = c.run(plan=plan)                                         # (asserts that the error is gone)
         assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+
+
+def test_a_plan_without_rows_judges_its_entries(vb):
+    """No query rows at all: slots, lengths and pointers are looked at as ever; what a plan with rows says of the same entries without rows."""
+    c = Case(vb, [(16, [(2, 1), (3, 1), (4, 1)])])
+    c.pages.len[c.seqs[2]] = 10 ** 7
+    seqs = dev([c.seqs[0], -1, c.seqs[2], 10 ** 6, c.seqs[1]])
+    for rows, plan in ((0, vb.PrefixPlan(c.pages, 5, 0, 4)), (1, vb.PrefixPlan(c.pages, 5, 1, 4))):
+        for ptr, want in (([0, 0, 0, 0, 0, 0], [0, -1, -2, -1, 0]), ([0, 0, 0, 0, 0, 9], [0, -1, -2, -1, -1]), ([-1, 0, 0, 0, 0, 0], [-1, -1, -2, -1, 0]),
+                          ([0, -1, 0, 0, 0, 0], [-1] * 5)):
+            st = c.st(5)
+            vb.vlac_prefix_plan(c.pages, plan, seqs, dev(ptr), st)
+            assert st.tolist() == want, (rows, ptr)
