@@ -376,7 +376,8 @@ int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int s
  * infinities and NaN included.
  *
  * vlac_prefix_plan finds, from the tables, which neighbours of the list hold the same leading pages and divides the work; it is
- * called once whenever tables, lengths or q_ptr changed (once per token) and serves the attention of every layer.  List
+ * called once whenever tables, lengths or q_ptr changed (once per token) and serves the attention of every layer.  Both calls want
+ * max_pages*page_size < 2^31 - 1024 (INVALID_ARG otherwise).  List
  * sequences that share most next to one another.  A slot may be listed twice.  Status per entry as above; the rows of a refused
  * entry, and rows behind q_ptr[n], are left as they are.
  *   plan     n (<= VLAC_PAGES_MAX_LIST), rows of q, n_heads (a multiple of n_kv_heads, n_heads*rows < 2^29), and mem: device

@@ -1495,6 +1495,8 @@ int plan_check(const vlac_pages* p, const vlac_prefix* plan) {
   if (rc != VLAC_OK) return rc;
   if (!plan || plan->n < 0 || plan->rows < 0) return VLAC_ERR_INVALID_ARG;
   if (plan->n > VLAC_PAGES_MAX_LIST) return VLAC_ERR_TOO_LARGE;
+  // positions behind a sequence's end, up to a unit of keys or the page numbers that a warp fetches at once (512), are formed in 32 bits
+  if ((long long)p->max_pages * p->page_size > INT_MAX - 1024) return VLAC_ERR_INVALID_ARG;
   if (plan->n == 0 || plan->rows == 0) return VLAC_OK;
   const unsigned long long need = vlac_prefix_bytes(p, plan->n, plan->rows, plan->n_heads);
   if (need == 0 || !plan->mem || ((uintptr_t)plan->mem & 15u) || plan->bytes < need) return VLAC_ERR_INVALID_ARG;

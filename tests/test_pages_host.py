@@ -128,3 +128,11 @@ def test_mirror_keeps_its_books():
             assert np.all(h.table[s, n:] == -1)
             assert h.len[s] % 8 == 0 or h.refs[h.table[s, n - 1]] == 1      # a partly filled last page is never shared
         assert np.array_equal(held, h.refs)
+
+
+def test_tables_whose_positions_would_leave_32_bits_are_not_attended(vb):
+    """Keys are taken in units: behind the last position of a sequence there has to be room for one in an int."""
+    for page in (8, 256):
+        p = _struct(vb, page_size=page, max_pages=(2 ** 31 - 1024 + page - 1) // page, n_pages=40, work_bytes=1 << 62)
+        calls = _calls(vb, p)
+        assert calls["plan"]() == -1 and calls["attention"]() == -1
