@@ -385,6 +385,7 @@ int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int s
  *            is made before its first attention call (or its first 256 bytes are zero: then nothing is computed), with the pool and the
  *            struct that the attention calls get (a call with another table or shape computes nothing, see vlac_prefix_error), and serves
  *            one of them at a time (two captured graphs that may overlap need two)
+ *   scale    finite, also times log2(e)
  *   q, out   device, the pool's type, row r at r*q_stride / r*out_stride elements (multiples of 8, at least n_heads*head_dim), 16-byte
  *            aligned;  lse  device fp32 [rows][n_heads] or NULL */
 typedef struct {

@@ -357,7 +357,7 @@ template <> struct Half2<__half> {
 
 __device__ __forceinline__ unsigned pf_smem(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ float pf_ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-constexpr float PF_LN2 = 0.693147180559945f;
+constexpr float PF_LN2 = 0.693147180559945f, PF_LOG2E = 1.44269504088896f;
 
 // Piece of a tile that one run computes.
 struct Piece {
@@ -1507,7 +1507,7 @@ int attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const voi
               float* lse, unsigned delay_ns, unsigned long long limit_ns, cudaStream_t s) {
   const int rc = plan_check(p, plan);
   if (rc != VLAC_OK) return rc;
-  if (layer < 0 || layer >= p->n_layers || !isfinite(scale)) return VLAC_ERR_INVALID_ARG;
+  if (layer < 0 || layer >= p->n_layers || !isfinite(scale * PF_LOG2E)) return VLAC_ERR_INVALID_ARG;
   if (plan->n == 0 || plan->rows == 0) return VLAC_OK;
   const long long w = (long long)plan->n_heads * p->head_dim;
   if (!q || !out || q_stride < w || out_stride < w || q_stride % 8 || out_stride % 8 || (((uintptr_t)q | (uintptr_t)out) & 15u) || ((uintptr_t)lse & 3u))
@@ -1517,7 +1517,7 @@ int attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const voi
   a.table = p->table; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size; a.shift = pages_shift(p->page_size);
   a.kv_heads = p->n_kv_heads; a.ratio = plan->n_heads / p->n_kv_heads; a.n_heads = plan->n_heads; a.n = plan->n; a.rows = plan->rows;
   a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
-  a.scale2 = scale * 1.44269504088896f; a.mem = plan->mem; a.key = plan_key(p, plan);
+  a.scale2 = scale * PF_LOG2E; a.mem = plan->mem; a.key = plan_key(p, plan);
   const bool small = small_call(p, plan);
   auto launch = p->dtype == VLAC_BF16 ? (p->head_dim == 128 ? launch_attention<__nv_bfloat16, 128> : launch_attention<__nv_bfloat16, 64>)
                                       : (p->head_dim == 128 ? launch_attention<__half, 128> : launch_attention<__half, 64>);

@@ -136,3 +136,10 @@ def test_tables_whose_positions_would_leave_32_bits_are_not_attended(vb):
         p = _struct(vb, page_size=page, max_pages=(2 ** 31 - 1024 + page - 1) // page, n_pages=40, work_bytes=1 << 62)
         calls = _calls(vb, p)
         assert calls["plan"]() == -1 and calls["attention"]() == -1
+
+
+@pytest.mark.parametrize("scale,code", [(3.0e38, -1), (-3.0e38, -1), (2.36e38, -1), (float("-inf"), -1)])
+def test_scales_that_overflow_in_powers_of_two_are_refused(vb, scale, code):
+    """Exponentials are taken to the base 2: the scale times log2(e) has to be finite too."""
+    plan = vb.vlac_prefix(2, 2, 4, FAKE, 1 << 40)
+    assert vb.lib.vlac_prefix_attention(C.byref(_struct(vb)), 0, C.byref(plan), FAKE, 256, scale, FAKE, 256, None, None) == code
