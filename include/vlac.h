@@ -356,7 +356,7 @@ int vlac_pages_compact(const vlac_pages* p, const int* src, const int* dst, int 
  * pages that no other slot holds (BAD_STATE otherwise: vlac_pages_fork with deep = 1).
  *   row_ptr         device int32 [n + 1], 0 <= row_ptr[i] <= row_ptr[i+1] <= rows
  *   k_rows, v_rows  device, the pool's type, row r at r*k_stride / r*v_stride elements (multiples of 8, at least
- *                   n_kv_heads*head_dim), 16-byte aligned */
+ *                   n_kv_heads*head_dim), 16-byte aligned; none of the rows of the pool that the call writes */
 int vlac_pages_write(const vlac_pages* p, int layer, const int* seqs, const int* start, const int* row_ptr, int n, int rows,
                      const void* k_rows, long long k_stride, const void* v_rows, long long v_stride, int* status, void* stream);
 
@@ -387,7 +387,8 @@ int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int s
  *            one of them at a time (two captured graphs that may overlap need two)
  *   scale    finite, also times log2(e)
  *   q, out   device, the pool's type, row r at r*q_stride / r*out_stride elements (multiples of 8, at least n_heads*head_dim), 16-byte
- *            aligned;  lse  device fp32 [rows][n_heads] or NULL */
+ *            aligned;  lse  device fp32 [rows][n_heads] or NULL.  No row of out shares memory with a row of q (INVALID_ARG: queries are
+ *            still read while results are written; columns of one buffer are fine), nor with lse or the pool */
 typedef struct {
   int n, rows, n_heads;
   void* mem;

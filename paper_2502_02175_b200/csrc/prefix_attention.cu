@@ -1503,6 +1503,22 @@ int plan_check(const vlac_pages* p, const vlac_prefix* plan) {
   return VLAC_OK;
 }
 
+// Whether a row of q (row r: w bytes from q + r * qs on) and a row of out share a byte: results are written while other rows' queries are still read.
+bool rows_overlap(uintptr_t q, unsigned long long qs, uintptr_t out, unsigned long long os, unsigned long long w, int rows) {
+  const unsigned long long last = (unsigned long long)(rows - 1);
+  if (q + last * qs + w <= out || out + last * os + w <= q) return false;
+  if (qs == os) {                                 // (columns of one buffer: q's rows begin d bytes behind out's, a number of rows on)
+    const unsigned long long d = q >= out ? (q - out) % qs : (qs - (out - q) % qs) % qs;
+    return d < w || qs - d < w;
+  }
+  for (unsigned long long i = 0, j = 0; i <= last && j <= last;) {
+    if (q + i * qs + w <= out + j * os) ++i;
+    else if (out + j * os + w <= q + i * qs) ++j;
+    else return true;
+  }
+  return false;
+}
+
 int attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale, void* out, long long out_stride,
               float* lse, unsigned delay_ns, unsigned long long limit_ns, cudaStream_t s) {
   const int rc = plan_check(p, plan);
@@ -1512,6 +1528,7 @@ int attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const voi
   const long long w = (long long)plan->n_heads * p->head_dim;
   if (!q || !out || q_stride < w || out_stride < w || q_stride % 8 || out_stride % 8 || (((uintptr_t)q | (uintptr_t)out) & 15u) || ((uintptr_t)lse & 3u))
     return VLAC_ERR_INVALID_ARG;
+  if (rows_overlap((uintptr_t)q, 2ull * q_stride, (uintptr_t)out, 2ull * out_stride, 2ull * w, plan->rows)) return VLAC_ERR_INVALID_ARG;
   AttnArgs a = {};
   a.k = (const unsigned short*)p->k + (size_t)layer * pages_layer(p); a.v = (const unsigned short*)p->v + (size_t)layer * pages_layer(p);
   a.table = p->table; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size; a.shift = pages_shift(p->page_size);

@@ -623,3 +623,33 @@ def test_a_plan_without_rows_judges_its_entries(vb):
             st = c.st(5)
             vb.vlac_prefix_plan(c.pages, plan, seqs, dev(ptr), st)
             assert st.tolist() == want, (rows, ptr)
+
+
+def test_queries_and_results_in_one_buffer(vb):
+    """Rows of q and of out side by side, interleaved or with strides of their own in one buffer are right; where any two share an element the call
+    is refused and nothing is written."""
+    c = Case(vb, [(20, [(n + 1, 1) for n in range(5)])], 1, 1, 64, seed=19)
+    plan = vb.PrefixPlan(c.pages, 5, 5, 1)
+    first, _ = c.run(plan=plan)
+    rng, seen = np.random.default_rng(20), set()
+    for _ in range(400):
+        qs, os = (int(x) * 8 for x in rng.choice([8, 9, 16, 17, 24, 40], 2))
+        if rng.random() < 0.5:
+            os = qs
+        at_q, at_o = (int(x) * 8 for x in rng.integers(0, 100, 2))
+        buf = torch.full((2600,), 7.0, dtype=c.dtype, device="cuda")
+        q, out = (torch.as_strided(buf, (5, 1, 64), (s, 64, 1), at) for s, at in ((qs, at_q), (os, at_o)))
+        q.copy_(c.q)
+        used_q, used_o = (np.concatenate([np.arange(64) + at + r * s for r in range(5)]) for s, at in ((qs, at_q), (os, at_o)))
+        shared = len(np.intersect1d(used_q, used_o)) > 0
+        before, want = buf.clone(), buf.clone()
+        seen.add((shared, qs == os))
+        if shared:
+            with pytest.raises(vb.VlacError) as e:
+                vb.vlac_prefix_attention(c.pages, 0, plan, q, c.scale, out)
+            assert e.value.status == -1
+        else:
+            torch.as_strided(want, (5, 1, 64), (os, 64, 1), at_o).copy_(first)
+            vb.vlac_prefix_attention(c.pages, 0, plan, q, c.scale, out)
+        assert torch.equal(buf, before if shared else want), (qs, os, at_q, at_o)
+    assert len(seen) == 4

@@ -142,4 +142,11 @@ def test_tables_whose_positions_would_leave_32_bits_are_not_attended(vb):
 def test_scales_that_overflow_in_powers_of_two_are_refused(vb, scale, code):
     """Exponentials are taken to the base 2: the scale times log2(e) has to be finite too."""
     plan = vb.vlac_prefix(2, 2, 4, FAKE, 1 << 40)
-    assert vb.lib.vlac_prefix_attention(C.byref(_struct(vb)), 0, C.byref(plan), FAKE, 256, scale, FAKE, 256, None, None) == code
+    assert vb.lib.vlac_prefix_attention(C.byref(_struct(vb)), 0, C.byref(plan), FAKE, 256, scale, FAKE << 4, 256, None, None) == code
+
+
+def test_results_over_the_queries_are_refused(vb):
+    plan = vb.vlac_prefix(2, 3, 4, FAKE, 1 << 40)
+    for q, qs, out, os in ((FAKE, 256, FAKE, 256), (FAKE, 256, FAKE + 16, 256), (FAKE + 1024, 256, FAKE, 256), (FAKE, 512, FAKE + 256, 512), (FAKE, 256, FAKE + 1520, 1024),
+                           (FAKE + 3056, 256, FAKE, 1280), (FAKE, 1 << 40, FAKE + (1 << 42) + 496, 256)):
+        assert vb.lib.vlac_prefix_attention(C.byref(_struct(vb)), 0, C.byref(plan), q, qs, 1.0, out, os, None, None) == -1, (q, qs, out, os)
