@@ -904,7 +904,6 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   int* const error = &pm.head->error;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, run = blockIdx.x;
   unsigned char* const smem = pw_raw;
-  if (pf_smem(pw_raw) & 1023u) { if (tid == 0) atomicExch(error, VLAC_ERR_TIMEOUT); return; }        // (the swizzled tiles need it; uniform)
   const unsigned q_s = pf_smem(smem), ring = q_s + 2 * W::TILE;
   float* const red_m = reinterpret_cast<float*>(smem + W::TILE * (2 + W::SLOTS));            // [2][128] each
   float* const red_l = red_m + 256;
@@ -918,6 +917,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1) prefix_wide_kernel(const __grid
   }
   pdl_wait();
   pdl_trigger();
+  if (pf_smem(pw_raw) & 1023u) { if (tid == 0) atomicExch(error, VLAC_ERR_TIMEOUT); return; }        // (the swizzled tiles need it; uniform)
   const long long U = pm.head->units[WIDE], G = runs(WIDE, U);
   const int g_first = pm.first[WIDE][run];
   if (run >= G || pm.head->key != a.key) return;                        // uniform over the CTA
