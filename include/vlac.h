@@ -404,8 +404,8 @@ int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* pla
 int vlac_prefix_error(const vlac_prefix* plan, void* stream);
 
 /* Self-test of those waits: vlac_prefix_attention whose loads of common pages (more than 16 stacked rows) begin delay_us microseconds late
- * (0..100000) and whose waits give up after limit_us (1..100000).  With a shorter delay than limit the results are the ordinary ones; with a
- * longer one vlac_prefix_error answers TIMEOUT until the next plan, and the output is not valid. */
+ * (0..100000) and whose waits give up after limit_us (1..100000).  Where the limit covers the delay and the call's own latencies the results are
+ * the ordinary ones; with a longer delay vlac_prefix_error answers TIMEOUT until the next plan, and the output is not valid. */
 int vlac_selftest_prefix_wait(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
                               void* out, long long out_stride, float* lse, unsigned int delay_us, unsigned int limit_us, void* stream);
 

@@ -4,7 +4,8 @@
 // cluster barriers) and, where rows move, one copy launch (pages_copy_kernel) that reads the bookkeeping's result.
 // Bookkeeping is integer work on a few hundred KB; what decides it is the chain of dependent phases, which is why it is one
 // launch on one cluster and not a launch per phase (512 sequences of up to 256 pages given back or taken in a pool of 131,072: 15 us a
-// call).  Copies are bound by HBM.
+// call, of which the scattered atomics on the reference counts, through the eight SMs of the cluster, are a part that was not timed by itself).
+// Copies are bound by HBM.
 #include "pages_internal.h"
 #include "launch_util.h"
 
@@ -307,7 +308,10 @@ __global__ void __cluster_dims__(PB_CTAS, 1, 1) __launch_bounds__(PB_THREADS, 1)
 
 // The same for few entries with short tables, which a chain of cluster barriers and reads through L2 would only hold up: one CTA, everything
 // between its phases in shared memory, entries compared pair by pair, free pages searched from the lowest on until there are enough
-// (8 sequences of 35 pages given back or taken: 3.5 us a call; bound: launch and dependent reads).
+// (8 sequences of 35 pages given back or taken: 3.6 us a call; bound: launch and dependent reads).  The borders are of table entries, not of pages in
+// use, because the host knows no lengths.  One CTA / the cluster, us a call: 8 sequences of 35 pages 3.6 / 9.4, 64 of 16 6.0 / 10.4, 64 of 64 8.3 / 10.1,
+// 64 of 128 (8192 entries) 11.8 / 10.7, 64 of 256 20.1 / 10.8; 16 of 128 4.2 / 10.0, 16 of 512 10.4 / 10.8.  Short sequences in wide tables pay the
+// cluster's price: 8 of 30 pages with 2048 columns 9.5 us a call.
 constexpr int PO_THREADS = 512;
 constexpr int PO_LIST = 64;                     // entries
 constexpr int PO_ENTRIES = 8192;                // table or keep-list entries of all together
@@ -499,7 +503,7 @@ __global__ void __launch_bounds__(PO_THREADS, 1) pages_book_one_kernel(BookArgs 
 // ------------------------------------------------------------------------------------------------
 // Rows of the new pages of a fork / compaction: unit = (new page, layer, part of the page's rows, at most 32 KB of K and of V); a CTA of 256
 // threads moves it with 16-byte accesses, four of K and four of V in flight per thread.  HBM-bound: read once, written once (8 sequences of 297 rows
-// in 32 layers, 2.2 GB with the writes: 359 us with the bookkeeping, 6.2 TB/s).
+// in 32 layers, 2.2 GB with the writes: 361 us with the bookkeeping, 6.2 TB/s; pruned in place it is as long as into another slot).
 constexpr int PC_THREADS = 256;
 struct Rows16 {                                 // rows of 16-byte pieces
   int n;                                        // pieces of a row
@@ -573,7 +577,8 @@ __global__ void __launch_bounds__(PC_THREADS) pages_copy_kernel(CopyArgs a) {
 // ------------------------------------------------------------------------------------------------
 // Rows into pages.  grid (x, entries, layers): the CTAs of an entry share its rows out in groups; each checks the whole entry for
 // itself (its pages must exist and be the slot's own), so that an entry is written whole or not at all without a second launch.
-// HBM-bound (8 prompts of up to 4096 rows, 0.9 GB with the writes: 154 us, 5.8 TB/s); one row each for 64 sequences: 3.6 us.
+// HBM-bound (8 prompts of up to 4096 rows, 0.9 GB with the writes: 152 us, 5.9 TB/s; a step's prompt of 290 rows in 32 layers, 0.3 GB: 52 us, 5.8 TB/s);
+// one row each for 64 sequences: 3.6 us.
 constexpr int PR_THREADS = 256;
 constexpr int PR_ROWS = 8;                      // rows of K and of V per group
 struct WriteArgs {

@@ -20,6 +20,9 @@ namespace {
 
 // Two kernels share the segments.  Wide: common pages with more than 16 stacked rows, which every row sees whole (tcgen05).  Narrow:
 // the rest -- prefixes of few rows and every sequence's own rows, where the causal mask lies (warp-level tensor cores).
+// The border is the narrow tile's height, and measured: four prompts, 32 heads of 128, narrow / wide in us: 4 rows a prompt behind 512 positions
+// 18.2 / 22.9, behind 2048 35.4 / 39.2, behind 8192 99.7 / 99.1; 16 rows 22.2 / 24.2, 40.2 / 40.9, 103.1 / 100.8; 32 heads of 64, 16 rows: 16.2 / 21.1,
+// 22.4 / 29.5, 65.2 / 63.9.  Behind 16 rows the narrow kernel would read every key again.
 constexpr int NARROW = 0, WIDE = 1;
 constexpr int PN_WARPS = 4, PN_CTAS = 2 * 148;  // narrow: two CTAs of four warps per SM, every warp works alone
 constexpr int PW_CTAS = 148;                    // runs of the wide kernel: one CTA per SM
@@ -90,7 +93,8 @@ struct PlanArgs {
   unsigned long long key;
 };
 // One launch, bound by the chain of dependent reads and barriers, not by bytes: one CTA of 8 warps for few sequences with short tables, a cluster
-// of eight CTAs that reads the tables together otherwise.  8 sequences of 19 pages 4.8 us; 32 of 4132 pages 9.5 us.
+// of eight CTAs that reads the tables together otherwise.  8 sequences of 19 pages 4.8 us; 32 of 4132 pages 9.5 us.  One CTA / the cluster: 8 sequences of
+// 19 pages 4.8 / 6.7, 16 of 19 5.5 / 6.7, 16 of 256 7.2 / 7.4, one of 4096 5.8 / 7.2.  (Of the tables' width: 8 of 19 pages with 2048 columns 6.8 us.)
 constexpr int PL_CTAS = 8;
 constexpr int PL_MAX = VLAC_PAGES_MAX_LIST;
 constexpr int PL_ONE = 4096;                    // table entries up to which one CTA is faster
