@@ -364,7 +364,7 @@ int vlac_pages_write(const vlac_pages* p, int layer, const int* seqs, const int*
  * becomes a prefix that candidates share.  Shapes must agree (bf16 pool of the cache's layers, heads and head_dim, n_rows <= the
  * cache's L + n_action), the slot must already have n_rows rows in pages of its own.  status: device int32 [1]; BAD_STATE also where
  * vlac_step_pruned has dropped one of these positions and no step has recomputed every position of the sequence since (the layers behind the
- * pruning have no row there). */
+ * pruning have no row there; vlac_cache_write does not change what counts as dropped). */
 int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int slot, int n_rows, int* status, void* stream);
 
 /* Attention of new rows over paged sequences, the common prefix read once for all that share it.
