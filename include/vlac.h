@@ -409,6 +409,121 @@ int vlac_prefix_error(const vlac_prefix* plan, void* stream);
 int vlac_selftest_prefix_wait(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
                               void* out, long long out_stride, float* lse, unsigned int delay_us, unsigned int limit_us, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Speculative decoding over the paged pool: a tree of drafted tokens behind each sequence in one pass
+ *
+ * A token step of a caller's decoder: vlac_pages_resize makes room for the drafted rows, vlac_tree_plan and vlac_prefix_plan look at
+ * the trees and tables once; per layer vlac_pages_append rotates the new rows and puts their K and V into the pool and
+ * vlac_tree_attention lets each see the sequence and its own ancestors; vlac_logits_adjust applies penalties, biases and the grammar and
+ * picks a token for every row; vlac_tree_accept finds the path that the decoder would have taken itself, and vlac_pages_compact drops the
+ * other rows.  Nothing waits for the device; the whole step can be captured.  The rules of the paged calls hold here too; an
+ * ordinary token is a tree of one row.
+ *
+ * Rotary tables for any positions, fp32, made in 64 bits (as vlac_weights.rope_cos / rope_sin, and for vlac_pages_append):
+ *     f_i = theta^(-2i/rot_dim), i < rot_dim/2;  turns_i = original_len * f_i / (2 pi)
+ *     g_i = clamp((turns_i - turns_low) / (turns_high - turns_low), 0, 1), 0 if original_len is 0
+ *     cos[p][i] = amplitude * cos((first + p) * f_i * (g_i + (1 - g_i) / factor)),  sin alike
+ * factor stretches the positions (1: none): all frequencies alike with original_len = 0, otherwise only those that turn seldom over the
+ * length that the weights were trained for (the interpolation by parts of the YaRN paper, arXiv 2309.00071, whose attention temperature is the
+ * amplitude).
+ *   rot_dim  even, 2..256;  theta > 0, factor > 0, original_len >= 0, amplitude finite; turns_low < turns_high where original_len > 0
+ *   first >= 0, n_pos >= 0, first + n_pos <= 2^31 - 1;  cos, sin  device fp32 [n_pos][rot_dim/2] */
+typedef struct {
+  int rot_dim;
+  double theta, factor, original_len, turns_low, turns_high, amplitude;
+} vlac_rope_scaling;
+int vlac_rope_tables(const vlac_rope_scaling* r, int first, int n_pos, float* cos, float* sin, void* stream);
+
+/* How vlac_pages_append treats a head's query or key before it is stored, in this order and rounded once at the end:
+ *   q_gain, k_gain  device [head_dim] of the pool's type, or NULL: x -> x / sqrt(mean(x^2) + eps) * gain over the head's dimensions (sums in
+ *                   fp32: components beyond 10^18 overflow them)
+ *   rot_dim         0 or a multiple of 16 up to head_dim: the first rot_dim dimensions are rotated, pairs (i, i + rot_dim/2), or with
+ *                   interleaved = 1 (2i, 2i + 1):  (x, y) -> (x cos - y sin, x sin + y cos)
+ *   cos, sin        device fp32 [n_pos][rot_dim/2], 16-byte aligned (not read with rot_dim = 0) */
+typedef struct {
+  const float *cos, *sin;
+  int n_pos, rot_dim, interleaved;
+  const void *q_gain, *k_gain;
+  float eps;
+} vlac_rope;
+
+/* vlac_pages_write with the norm and rotation of `rope` on the way, for the queries of the same rows too: row r of q goes to row r of
+ * q_out, row r of k_rows and v_rows (v as it is) into the pool.
+ *   pos    device int32 [rows], the position that row r is rotated to, or NULL: the position it is written to.  An entry with a
+ *          position outside [0, n_pos) is refused (INVALID_ARG)
+ *   q      n_heads heads of head_dim a row (n_heads = 0: none, q and q_out are not looked at); strides and alignment as k_rows.  q_out may be q
+ *          itself (same stride); no other row of q_out shares memory with rows of q, k_rows or v_rows (INVALID_ARG)
+ * Other arguments, codes and refusals as vlac_pages_write; rows of refused entries and rows behind row_ptr[n] stay as they were, in q_out too. */
+int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int* start, const int* row_ptr, int n, int rows, const vlac_rope* rope,
+                      const int* pos, int n_heads, const void* q, long long q_stride, void* q_out, long long q_out_stride, const void* k_rows,
+                      long long k_stride, const void* v_rows, long long v_stride, int* status, void* stream);
+
+/* Trees of drafted tokens, one per entry of a list.
+ *   q_ptr    device int32 [n + 1]: rows q_ptr[i] .. q_ptr[i+1] (at most max_rows, 1..VLAC_TREE_MAX_ROWS) are the nq_i newest rows of slot seqs[i]
+ *   parent   device int32 [rows]: the row's parent within its entry, a row in front of it; -1: none (what it extends is the sequence)
+ * and what vlac_tree_plan makes of them (a caller may write mask itself: any bits, of its own rows too):
+ *   mask     device uint32 [rows][ceil(max_rows/32)]: bit j = the row sees row j of its entry (its ancestors and itself)
+ *   pos      device int32 [rows]: len - nq_i + depth, the position to rotate to;  entry  device int32 [rows]: the row's entry
+ * Status as for the paged calls, INVALID_ARG also for a parent out of range and nq_i > len, TOO_LARGE for nq_i > max_rows; rows of refused
+ * entries and of none get mask 0, pos -1, entry -1.  A falling q_ptr refuses all.  p and seqs may both be NULL: pos is then the depth. */
+#define VLAC_TREE_MAX_ROWS 1024
+typedef struct {
+  int n, rows, max_rows;
+  const int *q_ptr, *parent;
+  unsigned* mask;
+  int *pos, *entry;
+} vlac_tree;
+int vlac_tree_plan(const vlac_pages* p, const vlac_tree* tree, const int* seqs, int* status, void* stream);
+
+/* vlac_prefix_attention, on the same plan, with the tree's mask among the newest rows: row j of entry i sees the positions in front of
+ * len - nq_i and those len - nq_i + b whose bit b is set in its mask (b < nq_i).  tree->n and rows are the plan's; the mask is read, the rest of the
+ * tree is not.  An entry that the plan refused keeps its rows of out; one that vlac_tree_plan refused sees only what lies in front of the tree. */
+int vlac_tree_attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const vlac_tree* tree, const void* q, long long q_stride, float scale,
+                        void* out, long long out_stride, float* lse, void* stream);
+
+/* Logits before a token is picked.  For row r and token t, in this order, fp32, every step rounded once:
+ *   made = how often t was generated: in tokens[span[r][1] .. span[r][2]), and (with a tree) among drafted[] of the rows that row r sees in its mask
+ *   seen = made > 0 or t in the prompt tokens[span[r][0] .. span[r][1])
+ *   x = logits[r][t];  if seen: x = x > 0 ? x / repetition[r] : x * repetition[r]
+ *   x = x - frequency[r] * made;  if made: x = x - presence[r];  x = x + bias of t;  x = -infinity where t is not allowed
+ * out[r][t] is x in the type of the logits; picked[r] the lowest index of the largest x (before that rounding) among the allowed tokens, a NaN
+ * counting as the largest; -1 if none is allowed.
+ *   tokens      device int32 [n_tokens]; numbers outside the vocabulary are passed over (padding).  Spans of rows may overlap
+ *   span        device int32 [rows][3], or NULL: no history
+ *   repetition, frequency, presence   device fp32 [rows], each or NULL (not applied)
+ *   bias        entries bias_ptr[r] .. bias_ptr[r+1] of bias_token, bias (int32 [rows + 1], int32 / fp32 [n_bias]) for row r; of several for a token
+ *               the last stands; bias_ptr NULL: none
+ *   allow       device uint32 [n_allow][ceil(vocab/32)], bit t % 32 of word t / 32: 1 = allowed; allow_row[r] (int32 [rows]) says which one row r
+ *               goes by, -1 none; allow_row NULL: row r the r-th (n_allow >= rows).  allow NULL: all tokens are allowed
+ *   tree, drafted   the rows are the tree's (tree->rows == rows) and drafted  device int32 [rows] their tokens; both or neither
+ * The host refuses what it can see (INVALID_ARG).  status[r]: INVALID_ARG for a span, bias_ptr or allow_row out of range; such a row's out and picked
+ * stay as they were. */
+#define VLAC_FP32 2
+typedef struct {
+  const int* tokens; int n_tokens;
+  const int* span;
+  const float *repetition, *frequency, *presence;
+  const int *bias_ptr, *bias_token; const float* bias; int n_bias;
+  const unsigned* allow; const int* allow_row; int n_allow;
+  const vlac_tree* tree; const int* drafted;
+} vlac_logits_rules;
+/* logits, out  device, dtype VLAC_FP32, VLAC_BF16 or VLAC_FP16, row r at r*stride / r*out_stride elements (at least vocab; any alignment of the element,
+ *              16-byte rows are faster); out NULL: only tokens are picked; out may be logits itself (same stride), other overlaps are refused
+ * picked, status  device int32 [rows]; picked may be NULL.  rows 0..65535 (TOO_LARGE beyond), vocab 1..2^30 */
+int vlac_logits_adjust(int rows, int vocab, int dtype, const void* logits, long long stride, const vlac_logits_rules* rules, void* out,
+                       long long out_stride, int* picked, int* status, void* stream);
+
+/* The path of each tree that the decoder confirms: from the entry's first row on, to the first child whose drafted token is the token chosen at the
+ * row (drafted, chosen  device int32 [rows]).
+ *   count   [n]: rows on the path (0 for an empty or refused entry);  path  [rows]: the path's rows within the entry from q_ptr[i] on, -1 behind;
+ *   tokens  [rows]: the tokens chosen at them (the last is new), -1 behind
+ *   keep_ptr [n + 1], keep [n_keep]: the positions of slot seqs[i] that stay, for vlac_pages_compact (the rows in front of the tree, then the path;
+ *           all rows of a refused entry whose slot is sound).  keep_ptr runs on beyond n_keep where the list does not fit: those entries get
+ *           TOO_LARGE, and vlac_pages_compact refuses them.  0 <= n_keep < 2^31 - 1
+ * Status otherwise as vlac_tree_plan; of the tree only n, rows, max_rows, q_ptr and parent are looked at. */
+int vlac_tree_accept(const vlac_pages* p, const vlac_tree* tree, const int* seqs, const int* drafted, const int* chosen, int* count, int* path, int* tokens,
+                     int* keep_ptr, int* keep, int n_keep, int* status, void* stream);
+
 const char* vlac_status_string(int status);
 
 #ifdef __cplusplus

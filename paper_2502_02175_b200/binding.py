@@ -62,6 +62,25 @@ class vlac_prefix(C.Structure):
     _fields_ = [("n", C.c_int), ("rows", C.c_int), ("n_heads", C.c_int), ("mem", C.c_void_p), ("bytes", C.c_ulonglong)]
 
 
+class vlac_rope_scaling(C.Structure):
+    _fields_ = [("rot_dim", C.c_int)] + [(n, C.c_double) for n in ("theta", "factor", "original_len", "turns_low", "turns_high", "amplitude")]
+
+
+class vlac_rope(C.Structure):
+    _fields_ = [("cos", C.c_void_p), ("sin", C.c_void_p), ("n_pos", C.c_int), ("rot_dim", C.c_int), ("interleaved", C.c_int),
+                ("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("eps", C.c_float)]
+
+
+class vlac_tree(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n", "rows", "max_rows")] + [(n, C.c_void_p) for n in ("q_ptr", "parent", "mask", "pos", "entry")]
+
+
+class vlac_logits_rules(C.Structure):
+    _fields_ = [("tokens", C.c_void_p), ("n_tokens", C.c_int), ("span", C.c_void_p), ("repetition", C.c_void_p), ("frequency", C.c_void_p),
+                ("presence", C.c_void_p), ("bias_ptr", C.c_void_p), ("bias_token", C.c_void_p), ("bias", C.c_void_p), ("n_bias", C.c_int),
+                ("allow", C.c_void_p), ("allow_row", C.c_void_p), ("n_allow", C.c_int), ("tree", C.c_void_p), ("drafted", C.c_void_p)]
+
+
 EXPORTS = ("vlac_create", "vlac_destroy", "vlac_cache_alloc", "vlac_cache_reset", "vlac_cache_free",
            "vlac_cache_read", "vlac_cache_write", "vlac_select", "vlac_select_bf16", "vlac_select_import", "vlac_layer_forward",
            "vlac_step", "vlac_step_chunk", "vlac_step_pruned", "vlac_selection_view", "vlac_launch_count", "vlac_device_error", "vlac_status_string",
@@ -69,7 +88,8 @@ EXPORTS = ("vlac_create", "vlac_destroy", "vlac_cache_alloc", "vlac_cache_reset"
            "vlac_selftest_wait_expiry",
            "vlac_pages_work_bytes", "vlac_pages_resize", "vlac_pages_free", "vlac_pages_fork", "vlac_pages_compact", "vlac_pages_write",
            "vlac_pages_from_cache", "vlac_prefix_bytes", "vlac_prefix_plan", "vlac_prefix_attention",
-           "vlac_prefix_error", "vlac_selftest_prefix_wait")
+           "vlac_prefix_error", "vlac_selftest_prefix_wait",
+           "vlac_rope_tables", "vlac_pages_append", "vlac_tree_plan", "vlac_tree_attention", "vlac_tree_accept", "vlac_logits_adjust")
 
 lib.vlac_status_string.restype = C.c_char_p
 lib.vlac_status_string.argtypes = [C.c_int]
@@ -115,6 +135,12 @@ lib.vlac_prefix_plan.argtypes = [_P, _P, _P, _P, _P, _P]
 lib.vlac_prefix_error.argtypes = [_P, _P]
 lib.vlac_prefix_attention.argtypes = [_P, _I, _P, _P, _LL, C.c_float, _P, _LL, _P, _P]
 lib.vlac_selftest_prefix_wait.argtypes = [_P, _I, _P, _P, _LL, C.c_float, _P, _LL, _P, C.c_uint, C.c_uint, _P]
+lib.vlac_rope_tables.argtypes = [_P, _I, _I, _P, _P, _P]
+lib.vlac_pages_append.argtypes = [_P, _I, _P, _P, _P, _I, _I, _P, _P, _I, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _P]
+lib.vlac_tree_plan.argtypes = [_P, _P, _P, _P, _P]
+lib.vlac_tree_attention.argtypes = [_P, _I, _P, _P, _P, _LL, C.c_float, _P, _LL, _P, _P]
+lib.vlac_tree_accept.argtypes = [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P]
+lib.vlac_logits_adjust.argtypes = [_I, _I, _I, _P, _LL, _P, _P, _LL, _P, _P, _P]
 
 
 class VlacError(RuntimeError):
@@ -544,6 +570,163 @@ def vlac_selftest_prefix_wait(pages: Pages, layer: int, plan: PrefixPlan, q: tor
     out_ptr, out_stride = _rows(out, shape, pages)
     _check(lib.vlac_selftest_prefix_wait(pages.ref, layer, plan.ref, q_ptr, q_stride, scale, out_ptr, out_stride, _ptr(lse), delay_us, limit_us, stream),
            "vlac_selftest_prefix_wait")
+
+
+# --------------------------------------------------------------------------- speculative decoding over the pool
+def vlac_rope_tables(cos: torch.Tensor, sin: torch.Tensor, theta: float, first: int = 0, factor: float = 1.0, original_len: float = 0.0,
+                     turns: Sequence[float] = (1.0, 32.0), amplitude: float = 1.0) -> None:
+    """Rotary tables ``cos``, ``sin`` (fp32 ``[n_pos, rot_dim / 2]``) of the positions ``first ..``, stretched by ``factor``: all frequencies, or with
+    ``original_len`` those that turn less than ``turns`` times over that length."""
+    assert cos.dtype is torch.float32 and cos.dim() == 2 and cos.is_cuda and cos.is_contiguous()
+    assert sin.dtype is torch.float32 and sin.shape == cos.shape and sin.get_device() == cos.get_device() and sin.is_contiguous()
+    stream = _here(cos.get_device())
+    r = vlac_rope_scaling(2 * cos.shape[1], theta, factor, original_len, turns[0], turns[1], amplitude)
+    _check(lib.vlac_rope_tables(C.byref(r), first, cos.shape[0], cos.data_ptr(), sin.data_ptr(), stream), "vlac_rope_tables")
+
+
+class Rope:
+    """What ``vlac_pages_append`` does to a head: tables of ``vlac_rope_tables`` (``[n_pos, rot_dim / 2]``; ``None``: no rotation), pairs half a rotated
+    part apart or ``interleaved``, and norms of queries and keys with gains ``[head_dim]`` of the pool's type (``None``: no norm)."""
+
+    def __init__(self, cos: Optional[torch.Tensor], sin: Optional[torch.Tensor], interleaved: bool = False, q_gain: Optional[torch.Tensor] = None,
+                 k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        assert (cos is None) == (sin is None)
+        self.tensors = [t for t in (cos, sin, q_gain, k_gain) if t is not None]
+        for t in (cos, sin):
+            assert t is None or (t.dtype is torch.float32 and t.dim() == 2 and t.is_contiguous() and t.shape == cos.shape)
+        for t in (q_gain, k_gain):
+            assert t is None or (t.dim() == 1 and t.is_contiguous())
+        assert all(t.is_cuda and t.device == self.tensors[0].device for t in self.tensors)
+        self.index = self.tensors[0].get_device() if self.tensors else None
+        self.gains = [t for t in (q_gain, k_gain) if t is not None]
+        n_pos, half = (0, 0) if cos is None else cos.shape
+        self.struct = vlac_rope(_ptr(cos), _ptr(sin), n_pos, 2 * half, int(bool(interleaved)), _ptr(q_gain), _ptr(k_gain), eps)
+        self.ref = C.byref(self.struct)
+        self.pools = set()                                       # pools (type, head width, device) that it has been seen to fit
+
+    def fits(self, pages: Pages) -> bool:
+        return self.index in (None, pages.index) and all(t.dtype is pages.dtype and t.shape[0] == pages.head_dim for t in self.gains)
+
+
+def vlac_pages_append(pages: Pages, layer: int, seqs: torch.Tensor, start: Optional[torch.Tensor], row_ptr: torch.Tensor, rope: Rope,
+                      pos: Optional[torch.Tensor], q: Optional[torch.Tensor], q_out: Optional[torch.Tensor], k_rows: torch.Tensor, v_rows: torch.Tensor,
+                      status: torch.Tensor) -> None:
+    """``vlac_pages_write`` with ``rope`` on the way: ``k_rows`` normalised and rotated to ``pos`` (``None``: where they are written) into the pool, the queries
+    ``q`` ``[rows, n_heads, head_dim]`` of the same rows into ``q_out`` (may be ``q``)."""
+    n, dev, rows = seqs.size(0), pages.index, k_rows.size(0)
+    stream, shape = _here(dev), (rows, pages.n_kv_heads, pages.head_dim)
+    key = (pages.dtype, pages.head_dim, dev)
+    if key not in rope.pools:
+        assert rope.fits(pages)
+        rope.pools.add(key)
+    k_ptr, k_stride = _rows(k_rows, shape, pages)
+    v_ptr, v_stride = _rows(v_rows, shape, pages)
+    heads, q_ptr, q_stride, o_ptr, o_stride = 0, None, 0, None, 0
+    if q is not None:
+        heads = q.size(1)
+        q_ptr, q_stride = _rows(q, (rows, heads, pages.head_dim), pages)
+        o_ptr, o_stride = _rows(q_out, (rows, heads, pages.head_dim), pages)
+    _check(lib.vlac_pages_append(pages.ref, layer, _ints(seqs, n, dev), None if start is None else _ints(start, n, dev), _ints(row_ptr, n + 1, dev), n, rows,
+                                 rope.ref, None if pos is None else _ints(pos, rows, dev), heads, q_ptr, q_stride, o_ptr, o_stride, k_ptr, k_stride, v_ptr, v_stride,
+                                 _ints(status, n, dev), stream), "vlac_pages_append")
+
+
+class Tree:
+    """Trees of drafted tokens: ``q_ptr`` int32 ``[n + 1]``, ``parent`` int32 ``[rows]`` (within the entry, -1: none), at most ``max_rows`` rows each; and what
+    ``vlac_tree_plan`` makes of them: ``mask`` int32 ``[rows, words]``, ``pos``, ``entry`` int32 ``[rows]``."""
+
+    def __init__(self, q_ptr: torch.Tensor, parent: torch.Tensor, max_rows: int):
+        assert q_ptr.is_cuda and parent.get_device() == q_ptr.get_device()
+        for t in (q_ptr, parent):
+            assert t.dtype is torch.int32 and t.dim() == 1 and t.is_contiguous()
+        assert q_ptr.shape[0] >= 1 and 1 <= max_rows <= 1024
+        self.q_ptr, self.parent, self.n, self.rows, self.index = q_ptr, parent, q_ptr.shape[0] - 1, parent.shape[0], q_ptr.get_device()
+        self.mask = torch.zeros((self.rows, -(-max_rows // 32)), dtype=torch.int32, device=q_ptr.device)
+        self.pos, self.entry = (torch.full((self.rows,), -1, dtype=torch.int32, device=q_ptr.device) for _ in range(2))
+        self.struct = vlac_tree(self.n, self.rows, max_rows, *(t.data_ptr() for t in (q_ptr, parent, self.mask, self.pos, self.entry)))
+        self.ref = C.byref(self.struct)
+
+
+def vlac_tree_plan(pages: Optional[Pages], tree: Tree, seqs: Optional[torch.Tensor], status: torch.Tensor) -> None:
+    """Masks, positions and entries of the trees' rows; without a pool (``None`` twice) positions are depths."""
+    dev, n = tree.index, tree.n
+    stream = _here(dev)
+    assert pages is None or pages.index == dev
+    _check(lib.vlac_tree_plan(None if pages is None else pages.ref, tree.ref, None if seqs is None else _ints(seqs, n, dev), _ints(status, n, dev), stream),
+           "vlac_tree_plan")
+
+
+def vlac_tree_attention(pages: Pages, layer: int, plan: PrefixPlan, tree: Tree, q: torch.Tensor, scale: float, out: torch.Tensor,
+                        lse: Optional[torch.Tensor] = None) -> None:
+    """``vlac_prefix_attention`` with the trees' masks among the newest rows of each entry."""
+    dev, shape = pages.index, (plan.rows, plan.n_heads, pages.head_dim)
+    stream = _here(dev)
+    assert plan.pages is pages and tree.index == dev
+    assert lse is None or (lse.dtype is torch.float32 and lse.get_device() == dev and lse.is_contiguous() and lse.shape == shape[:2])
+    q_ptr, q_stride = _rows(q, shape, pages)
+    out_ptr, out_stride = _rows(out, shape, pages)
+    _check(lib.vlac_tree_attention(pages.ref, layer, plan.ref, tree.ref, q_ptr, q_stride, scale, out_ptr, out_stride, _ptr(lse), stream), "vlac_tree_attention")
+
+
+def vlac_tree_accept(pages: Pages, tree: Tree, seqs: torch.Tensor, drafted: torch.Tensor, chosen: torch.Tensor, count: torch.Tensor, path: torch.Tensor,
+                     tokens: torch.Tensor, keep_ptr: torch.Tensor, keep: torch.Tensor, status: torch.Tensor) -> None:
+    """The path of each tree whose ``drafted`` tokens are those ``chosen`` at the rows in front of them, and the keep lists for ``vlac_pages_compact``."""
+    dev, n, rows, n_keep = pages.index, tree.n, tree.rows, keep.size(0)
+    stream = _here(dev)
+    assert tree.index == dev
+    _check(lib.vlac_tree_accept(pages.ref, tree.ref, _ints(seqs, n, dev), _ints(drafted, rows, dev), _ints(chosen, rows, dev), _ints(count, n, dev),
+                                _ints(path, rows, dev), _ints(tokens, rows, dev), _ints(keep_ptr, n + 1, dev), _ints(keep, n_keep, dev), n_keep,
+                                _ints(status, n, dev), stream), "vlac_tree_accept")
+
+
+class LogitsRules:
+    """What ``vlac_logits_adjust`` does to ``rows`` rows of ``vocab`` logits; everything is optional.
+
+    ``history`` int32 tokens and ``span`` int32 ``[rows, 3]`` (prompt from, generated from, end); ``repetition``, ``frequency``, ``presence`` fp32 ``[rows]``;
+    ``bias_ptr`` int32 ``[rows + 1]``, ``bias_token`` int32, ``bias`` fp32; ``allow`` int32 words ``[n, ceil(vocab / 32)]`` (bit = allowed) and ``allow_row`` int32
+    ``[rows]`` (-1: all allowed); ``tree`` and the ``drafted`` int32 tokens of its rows.
+    """
+
+    def __init__(self, rows: int, vocab: int, history: Optional[torch.Tensor] = None, span: Optional[torch.Tensor] = None,
+                 repetition: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                 bias_ptr: Optional[torch.Tensor] = None, bias_token: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                 allow: Optional[torch.Tensor] = None, allow_row: Optional[torch.Tensor] = None, tree: Optional[Tree] = None,
+                 drafted: Optional[torch.Tensor] = None):
+        self.rows, self.vocab, self.tree = rows, vocab, tree
+        self.tensors = [t for t in (history, span, repetition, frequency, presence, bias_ptr, bias_token, bias, allow, allow_row, drafted) if t is not None]
+        assert all(t.is_cuda and t.is_contiguous() and t.device == self.tensors[0].device for t in self.tensors)
+        self.index = self.tensors[0].get_device() if self.tensors else None
+        for t, shape in ((span, (rows, 3)), (bias_ptr, (rows + 1,)), (allow_row, (rows,)), (drafted, (rows,))):
+            assert t is None or (t.dtype is torch.int32 and t.shape == shape)
+        for t in (repetition, frequency, presence):
+            assert t is None or (t.dtype is torch.float32 and t.shape == (rows,))
+        assert (span is None) == (history is None) and (history is None or (history.dtype is torch.int32 and history.dim() == 1))
+        assert (bias_ptr is None) == (bias_token is None) == (bias is None)
+        assert bias is None or (bias.dtype is torch.float32 and bias_token.dtype is torch.int32 and bias.dim() == 1 and bias.shape == bias_token.shape)
+        assert allow is None or (allow.dtype is torch.int32 and allow.dim() == 2 and allow.shape[1] == -(-vocab // 32))
+        assert allow_row is None or allow is not None
+        assert (tree is None) == (drafted is None) and (tree is None or (tree.rows == rows and tree.index == self.index))
+        count = lambda t: 0 if t is None else t.shape[0]  # noqa: E731
+        self.struct = vlac_logits_rules(_ptr(history), count(history), _ptr(span), _ptr(repetition), _ptr(frequency), _ptr(presence), _ptr(bias_ptr), _ptr(bias_token),
+                                        _ptr(bias), count(bias), _ptr(allow), _ptr(allow_row), count(allow),
+                                        None if tree is None else C.addressof(tree.struct), _ptr(drafted))
+        self.ref = C.byref(self.struct)
+
+
+_LOGITS_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def vlac_logits_adjust(logits: torch.Tensor, rules: LogitsRules, out: Optional[torch.Tensor], picked: Optional[torch.Tensor], status: torch.Tensor) -> None:
+    """``rules`` applied to ``logits`` ``[rows, vocab]`` (fp32, bf16 or fp16, any row stride) into ``out`` (``None``: not kept; may be ``logits``), the best allowed token of
+    each row into ``picked`` (int32, ``None``: not wanted)."""
+    dev, shape = logits.get_device(), (rules.rows, rules.vocab)
+    stream = _here(dev)
+    assert rules.index in (None, dev) and logits.shape == shape and logits.stride(1) == 1
+    assert out is None or (out.dtype is logits.dtype and out.get_device() == dev and out.shape == shape and out.stride(1) == 1)
+    wide = max(rules.vocab, 1)
+    _check(lib.vlac_logits_adjust(shape[0], shape[1], _LOGITS_TYPES[logits.dtype], logits.data_ptr(), logits.stride(0) if shape[0] > 1 else wide, rules.ref, _ptr(out),
+                                  0 if out is None else out.stride(0) if shape[0] > 1 else wide, None if picked is None else _ints(picked, shape[0], dev),
+                                  _ints(status, shape[0], dev), stream), "vlac_logits_adjust")
 
 
 # --------------------------------------------------------------------------- reading views back

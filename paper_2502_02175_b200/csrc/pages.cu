@@ -651,21 +651,9 @@ __global__ void __launch_bounds__(PR_THREADS) pages_write_kernel(WriteArgs a) {
   }
 }
 
-int sm_count(int* out) {
-  int dev = 0;
-  VLAC_CUDA_CHECK(cudaGetDevice(&dev));
-  VLAC_CUDA_CHECK(cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev));
-  return VLAC_OK;
-}
-
 Rows16 rows16(const vlac_pages* p) {
   const int n = (int)(pages_row(p) / 8);
   return {n, n & (n - 1) ? -1 : pages_shift(n)};
-}
-
-int list_check(int n) {
-  if (n < 0) return VLAC_ERR_INVALID_ARG;
-  return n > VLAC_PAGES_MAX_LIST ? VLAC_ERR_TOO_LARGE : VLAC_OK;
 }
 
 int book(const vlac_pages* p, int op, const int* src, const int* dst, const int* lens, int n, int deep, const int* keep_ptr,

@@ -1,8 +1,9 @@
-// Shared by the translation units of the paged K/V pool (pages.cu) and of the attention that reads it
-// (prefix_attention.cu).
+// Shared by the translation units of the paged K/V pool (pages.cu), of what appends to it (rotary.cu), of the attention that reads it
+// (prefix_attention.cu) and of the trees of drafted tokens over it (tree.cu).
 #pragma once
 #include "vlac_internal.h"
 #include <limits.h>
+#include <atomic>
 
 static inline int pages_shift(int page_size) {
   int s = 0;
@@ -24,6 +25,46 @@ static inline int pages_check(const vlac_pages* p) {
   if ((long long)p->n_pages * p->page_size > INT_MAX || (long long)p->max_pages * p->page_size > INT_MAX) return VLAC_ERR_INVALID_ARG;
   if (p->work_bytes < vlac_pages_work_bytes(p)) return VLAC_ERR_INVALID_ARG;
   return VLAC_OK;
+}
+
+static inline int list_check(int n) {
+  if (n < 0) return VLAC_ERR_INVALID_ARG;
+  return n > VLAC_PAGES_MAX_LIST ? VLAC_ERR_TOO_LARGE : VLAC_OK;
+}
+
+static inline int sm_count(int* out) {
+  int dev = 0;
+  VLAC_CUDA_CHECK(cudaGetDevice(&dev));
+  VLAC_CUDA_CHECK(cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev));
+  return VLAC_OK;
+}
+
+// Dynamic shared memory beyond 48 KB is asked for once per device and kernel.
+template <auto kernel> static inline int big_smem(int bytes) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  VLAC_CUDA_CHECK(cudaGetDevice(&dev));
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_acquire) & bit) return VLAC_OK;
+  VLAC_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  done.fetch_or(bit, std::memory_order_release);
+  return VLAC_OK;
+}
+
+// Whether a row of q (row r: wq bytes from q + r * qs on) and a row of out (wo bytes) share a byte: results are written while other rows are still read.
+static inline bool rows_overlap(uintptr_t q, unsigned long long qs, uintptr_t out, unsigned long long os, unsigned long long wq, unsigned long long wo, int rows) {
+  const unsigned long long last = (unsigned long long)(rows - 1);
+  if (q + last * qs + wq <= out || out + last * os + wo <= q) return false;
+  if (qs == os) {                                 // (columns of one buffer: q's rows begin d bytes behind out's, a number of rows on)
+    const unsigned long long d = q >= out ? (q - out) % qs : (qs - (out - q) % qs) % qs;
+    return d < wo || qs - d < wq;
+  }
+  for (unsigned long long i = 0, j = 0; i <= last && j <= last;) {
+    if (q + i * qs + wq <= out + j * os) ++i;
+    else if (out + j * os + wo <= q + i * qs) ++j;
+    else return true;
+  }
+  return false;
 }
 
 // elements of one K (or V) row of the pool, and of one layer

@@ -14,7 +14,6 @@
 #include <math.h>
 #include <stddef.h>
 #include <algorithm>
-#include <atomic>
 
 namespace {
 
@@ -329,6 +328,7 @@ struct AttnArgs {
   float scale2;                                 // softmax scale * log2(e)
   void* mem;
   unsigned long long key;
+  const unsigned* mask; int words;              // a tree's: which of its entry's newest rows each row of q sees, or NULL
 };
 // Weights are rounded to the 16-bit type for the product with V.  `shift`: the reference of the exponentials lies that many powers of two below the
 // maximum that moved it, so that the weights use the upper part of the type's range; sums and outputs are scaled alike, and the division by the
@@ -366,7 +366,7 @@ constexpr float PF_LN2 = 0.693147180559945f, PF_LOG2E = 1.44269504088896f;
 // Piece of a tile that one run computes.
 struct Piece {
   int slot, head, rt, nr;                       // table; K/V head; tile; valid stacked rows
-  int row0, key0, key1, lim0;                   // q row of stacked row 0 of the segment; keys [key0, key1); see lim0 below
+  int row0, key0, key1, lim0;                   // q row of stacked row 0 of the segment; keys [key0, key1); see lim0 below (with a tree: its first position + 1)
   int n;                                        // key blocks (steps) of the piece
   int direct;
   size_t slot0;                                 // slot row of the tile's first row
@@ -464,7 +464,9 @@ __device__ __forceinline__ bool any_nonfinite(uint4 x) {
 
 // EARLY: behind the wide kernel of the same call, of which it reads nothing.  That kernel lets its successor start only once it has seen the plan
 // complete, so the CTAs here begin as SMs come free and wait for its end before their own (what comes after reads both).
-template <typename T, int D, bool EARLY>
+// TREE: a row sees all positions in front of its entry's newest rows and, of those, what its mask says.  The words are asked for before the scores are
+// formed, in the steps that reach the newest rows alone.
+template <typename T, int D, bool EARLY, bool TREE>
 __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArgs a) {
   using N = Narrow<D>;
   constexpr int STEP = N::STEP, NB = STEP / 16;                         // blocks of 16 keys in a step
@@ -565,6 +567,8 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
   float o[D / 8][4], m[2], l[2];                                        // the lane's two rows: lane / 4 and lane / 4 + 8
   unsigned qf[D / 16][4];
   int c_left = 0, key_lo = 0, key1 = 0, lim[2] = {0, 0}, lim_min = 0;
+  const unsigned* mrow[2] = {nullptr, nullptr};                         // TREE: the masks of the lane's two rows (NULL: sees all)
+  int t0 = 0;                                                           // and the position of the entry's first newest row
   while (true) {
     while (l_cnt - c_cnt < PN_STAGES && issue()) {}
     if (l_cnt == c_cnt) break;
@@ -581,10 +585,15 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int x = (lane >> 2) + 8 * r;
-        lim[r] = p.lim0 == INT_MIN || x >= p.nr ? key1 : min(key1, p.lim0 + (p.rt * 16 + x) / a.ratio);
+        if (TREE) {
+          lim[r] = key1;
+          mrow[r] = p.lim0 == INT_MIN || x >= p.nr ? nullptr : a.mask + (size_t)(p.row0 + (p.rt * 16 + x) / a.ratio) * a.words;
+        } else
+          lim[r] = p.lim0 == INT_MIN || x >= p.nr ? key1 : min(key1, p.lim0 + (p.rt * 16 + x) / a.ratio);
         m[r] = -INFINITY; l[r] = 0.f;
       }
-      lim_min = p.lim0 == INT_MIN ? key1 : min(key1, p.lim0 + p.rt * 16 / a.ratio);
+      lim_min = p.lim0 == INT_MIN ? key1 : min(key1, TREE ? p.lim0 - 1 : p.lim0 + p.rt * 16 / a.ratio);
+      if (TREE && p.lim0 != INT_MIN) t0 = p.lim0 - 1;
 #pragma unroll
       for (int j = 0; j < D / 8; ++j) { o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f; }
 #pragma unroll
@@ -598,6 +607,16 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
     }
     unsigned char* const k_p = base_p + N::Q_TILE + (c_cnt % PN_STAGES) * 2 * N::TILE;
     const unsigned k_s = pf_smem(k_p), v_s = k_s + N::TILE;
+    const bool masked = key_lo + STEP > lim_min;                        // some row does not see the whole step
+    unsigned mw[2][2] = {{~0u, ~0u}, {~0u, ~0u}};                       // TREE: the two words of each row's mask that the step's keys lie in
+    if (TREE && masked) {
+      const int w = (key_lo - t0) >> 5;
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (mrow[r] && w + e >= 0) mw[r][e] = w + e < a.words ? __ldcg(mrow[r] + w + e) : 0u;
+    }
     float s[2 * NB][4];
 #pragma unroll
     for (int j = 0; j < 2 * NB; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
@@ -613,14 +632,21 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
         Half2<T>::mma(s[2 * b + 1], qf[ks], f[2], f[3]);
       }
     }
-    const bool masked = key_lo + STEP > lim_min;                        // some row does not see the whole step
+    unsigned seen[2] = {~0u, ~0u};                                      // TREE: the keys of the step that each row sees
+    if (TREE && masked)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        seen[r] = __funnelshift_r(mw[r][0], mw[r][1], (key_lo - t0) & 31);
+        if (key1 - key_lo < 32) seen[r] &= (1u << (key1 - key_lo)) - 1u;                  // (key1 > key_lo)
+      }
     float bm[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int j = 0; j < 2 * NB; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float x = s[j][e] * a.scale2;
-        if (masked && key_lo + j * 8 + 2 * (lane & 3) + (e & 1) >= lim[e >> 1]) x = -INFINITY;
+        const int key = j * 8 + 2 * (lane & 3) + (e & 1);
+        if (masked && (TREE ? !(seen[e >> 1] >> key & 1) : key_lo + key >= lim[e >> 1])) x = -INFINITY;
         s[j][e] = x;
         bm[e >> 1] = fmaxf(bm[e >> 1], x);
       }
@@ -649,7 +675,7 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
       pf[j >> 1][(j & 1) * 2] = Half2<T>::pack(p0, p1);
       pf[j >> 1][(j & 1) * 2 + 1] = Half2<T>::pack(p2, p3);
     }
-    if (masked && lim_min < key1) {
+    if (masked && (TREE || lim_min < key1)) {
       // a row does not see some key of this step: infinities and NaN of such a V row must not reach it as 0 * inf
       bool bad = false;
       for (int i = lane; i < N::TILE / 16; i += 32) bad |= any_nonfinite<T>(*reinterpret_cast<const uint4*>(k_p + N::TILE + i * 16));
@@ -663,8 +689,8 @@ __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArg
               const unsigned short x =
                   *reinterpret_cast<const unsigned short*>(k_p + N::TILE + (col >> 6) * N::HALF + pf_swz(key, (col & 63) >> 3) + (col & 7) * 2);
               if ((x & Half2<T>::exp_mask) == Half2<T>::exp_mask) {
-                if (key_lo + key < lim[0]) o[j][e] += Half2<T>::value(x);
-                if (key_lo + key < lim[1]) o[j][2 + e] += Half2<T>::value(x);
+                if (TREE ? seen[0] >> key & 1 : key_lo + key < lim[0]) o[j][e] += Half2<T>::value(x);
+                if (TREE ? seen[1] >> key & 1 : key_lo + key < lim[1]) o[j][2 + e] += Half2<T>::value(x);
               }
             }
         __syncwarp();
@@ -1414,17 +1440,6 @@ __global__ void __launch_bounds__(256, OCC) prefix_join_kernel(AttnArgs a) {
   }
 }
 
-// Dynamic shared memory beyond 48 KB is asked for once per device and kernel.
-template <auto kernel> int big_smem(int bytes) {
-  static std::atomic<unsigned long long> done{0};
-  int dev = 0;
-  VLAC_CUDA_CHECK(cudaGetDevice(&dev));
-  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
-  if (done.load(std::memory_order_acquire) & bit) return VLAC_OK;
-  VLAC_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-  done.fetch_or(bit, std::memory_order_release);
-  return VLAC_OK;
-}
 #define TRY(x) do { const int rc__ = (x); if (rc__ != VLAC_OK) return rc__; } while (0)
 
 template <typename T, int D, bool QTMA>
@@ -1434,10 +1449,10 @@ int launch_wide(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap&
   return VLAC_OK;
 }
 
-template <typename T, int D, bool EARLY>
+template <typename T, int D, bool EARLY, bool TREE>
 int launch_narrow(const AttnArgs& a, cudaStream_t s) {
-  TRY((big_smem<prefix_narrow_kernel<T, D, EARLY>>(Narrow<D>::SMEM)));
-  VLAC_CUDA_CHECK(launch_pdl(prefix_narrow_kernel<T, D, EARLY>, dim3(PN_CTAS), dim3(PN_WARPS * 32), Narrow<D>::SMEM, s, a));
+  TRY((big_smem<prefix_narrow_kernel<T, D, EARLY, TREE>>(Narrow<D>::SMEM)));
+  VLAC_CUDA_CHECK(launch_pdl(prefix_narrow_kernel<T, D, EARLY, TREE>, dim3(PN_CTAS), dim3(PN_WARPS * 32), Narrow<D>::SMEM, s, a));
   return VLAC_OK;
 }
 
@@ -1456,9 +1471,9 @@ int launch_attention(const AttnArgs& a, bool small, unsigned delay_ns, unsigned 
       TRY((launch_wide<T, D, true>(tk, tv, tq, w, s)));
     } else
       TRY((launch_wide<T, D, false>(tk, tv, tk, w, s)));
-    TRY((launch_narrow<T, D, true>(a, s)));
+    TRY((a.mask ? launch_narrow<T, D, true, true>(a, s) : launch_narrow<T, D, true, false>(a, s)));
   } else
-    TRY((launch_narrow<T, D, false>(a, s)));
+    TRY((a.mask ? launch_narrow<T, D, false, true>(a, s) : launch_narrow<T, D, false, false>(a, s)));
   // an item a CTA while the GPU holds them in two waves, else an item a warp (what an item costs is the chain of its reads): 32 rows behind
   // 32,768 positions of 8 heads 33 us against 46, but 1024 items behind 65,600 84 against 79
   const long long items = (long long)a.rows * a.n_heads, mean = (items + a.n - 1) / a.n;
@@ -1507,33 +1522,20 @@ int plan_check(const vlac_pages* p, const vlac_prefix* plan) {
   return VLAC_OK;
 }
 
-// Whether a row of q (row r: w bytes from q + r * qs on) and a row of out share a byte: results are written while other rows' queries are still read.
-bool rows_overlap(uintptr_t q, unsigned long long qs, uintptr_t out, unsigned long long os, unsigned long long w, int rows) {
-  const unsigned long long last = (unsigned long long)(rows - 1);
-  if (q + last * qs + w <= out || out + last * os + w <= q) return false;
-  if (qs == os) {                                 // (columns of one buffer: q's rows begin d bytes behind out's, a number of rows on)
-    const unsigned long long d = q >= out ? (q - out) % qs : (qs - (out - q) % qs) % qs;
-    return d < w || qs - d < w;
-  }
-  for (unsigned long long i = 0, j = 0; i <= last && j <= last;) {
-    if (q + i * qs + w <= out + j * os) ++i;
-    else if (out + j * os + w <= q + i * qs) ++j;
-    else return true;
-  }
-  return false;
-}
-
-int attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale, void* out, long long out_stride,
-              float* lse, unsigned delay_ns, unsigned long long limit_ns, cudaStream_t s) {
+int attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const vlac_tree* tree, const void* q, long long q_stride, float scale, void* out,
+              long long out_stride, float* lse, unsigned delay_ns, unsigned long long limit_ns, cudaStream_t s) {
   const int rc = plan_check(p, plan);
   if (rc != VLAC_OK) return rc;
+  if (tree && (tree->n != plan->n || tree->rows != plan->rows || tree->max_rows < 1 || tree->max_rows > VLAC_TREE_MAX_ROWS)) return VLAC_ERR_INVALID_ARG;
   if (layer < 0 || layer >= p->n_layers || !isfinite(scale * PF_LOG2E)) return VLAC_ERR_INVALID_ARG;
   if (plan->n == 0 || plan->rows == 0) return VLAC_OK;
   const long long w = (long long)plan->n_heads * p->head_dim;
   if (!q || !out || q_stride < w || out_stride < w || q_stride % 8 || out_stride % 8 || (((uintptr_t)q | (uintptr_t)out) & 15u) || ((uintptr_t)lse & 3u))
     return VLAC_ERR_INVALID_ARG;
-  if (rows_overlap((uintptr_t)q, 2ull * q_stride, (uintptr_t)out, 2ull * out_stride, 2ull * w, plan->rows)) return VLAC_ERR_INVALID_ARG;
+  if (rows_overlap((uintptr_t)q, 2ull * q_stride, (uintptr_t)out, 2ull * out_stride, 2ull * w, 2ull * w, plan->rows)) return VLAC_ERR_INVALID_ARG;
+  if (tree && (!tree->mask || (uintptr_t)tree->mask & 3u)) return VLAC_ERR_INVALID_ARG;
   AttnArgs a = {};
+  if (tree) { a.mask = tree->mask; a.words = (tree->max_rows + 31) / 32; }
   a.k = (const unsigned short*)p->k + (size_t)layer * pages_layer(p); a.v = (const unsigned short*)p->v + (size_t)layer * pages_layer(p);
   a.table = p->table; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size; a.shift = pages_shift(p->page_size);
   a.kv_heads = p->n_kv_heads; a.ratio = plan->n_heads / p->n_kv_heads; a.n_heads = plan->n_heads; a.n = plan->n; a.rows = plan->rows;
@@ -1591,13 +1593,19 @@ int vlac_prefix_error(const vlac_prefix* plan, void* stream) {
 
 int vlac_prefix_attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
                           void* out, long long out_stride, float* lse, void* stream) {
-  return attention(p, layer, plan, q, q_stride, scale, out, out_stride, lse, 0, PW_WAIT_LIMIT_NS, (cudaStream_t)stream);
+  return attention(p, layer, plan, nullptr, q, q_stride, scale, out, out_stride, lse, 0, PW_WAIT_LIMIT_NS, (cudaStream_t)stream);
+}
+
+int vlac_tree_attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const vlac_tree* tree, const void* q, long long q_stride, float scale,
+                        void* out, long long out_stride, float* lse, void* stream) {
+  if (!tree) return VLAC_ERR_INVALID_ARG;
+  return attention(p, layer, plan, tree, q, q_stride, scale, out, out_stride, lse, 0, PW_WAIT_LIMIT_NS, (cudaStream_t)stream);
 }
 
 int vlac_selftest_prefix_wait(const vlac_pages* p, int layer, const vlac_prefix* plan, const void* q, long long q_stride, float scale,
                               void* out, long long out_stride, float* lse, unsigned int delay_us, unsigned int limit_us, void* stream) {
   if (delay_us > 100000 || limit_us < 1 || limit_us > 100000) return VLAC_ERR_INVALID_ARG;
-  return attention(p, layer, plan, q, q_stride, scale, out, out_stride, lse, delay_us * 1000u, limit_us * 1000ull, (cudaStream_t)stream);
+  return attention(p, layer, plan, nullptr, q, q_stride, scale, out, out_stride, lse, delay_us * 1000u, limit_us * 1000ull, (cudaStream_t)stream);
 }
 
 }  // extern "C"

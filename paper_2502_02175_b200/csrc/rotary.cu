@@ -1,0 +1,287 @@
+// Rotary tables, and new rows on their way into the paged pool: norm of each head's queries and keys, rotation, append.
+#include "pages_internal.h"
+#include "launch_util.h"
+#include <cuda_fp16.h>
+#include <math.h>
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ tables
+// Angles are kept as turns (angle / 2 pi): the whole turns of a far position fall away exactly before a sine is taken.  Turns per position come
+// from the host as a pair of doubles (from its extended type); a thread takes one frequency and a run of positions: one sine and cosine in
+// 64 bits for the first, then a rotation by the angle of one position each (four products in 64 bits; the error grows by about 2^-53 a step).
+constexpr int RT_MAX = 256, RT_RUN = 16, RT_THREADS = 256;
+struct TableArgs {
+  double turns[RT_MAX / 2], rest[RT_MAX / 2];   // per position; what the double leaves of it
+  double amplitude;
+  int half, first, n_pos;
+  float *cos, *sin;
+};
+
+__device__ __forceinline__ void turn_sincos(double pos, double t, double rest, double* s, double* c) {
+  const double whole = pos * t, low = fma(pos, t, -whole) + pos * rest;
+  sincospi(2.0 * ((whole - rint(whole)) + low), s, c);
+}
+
+__global__ void __launch_bounds__(RT_THREADS) rope_tables_kernel(const __grid_constant__ TableArgs a) {
+  pdl_trigger();
+  pdl_wait();
+  const long long u = (long long)blockIdx.x * RT_THREADS + threadIdx.x;
+  const int i = (int)(u % a.half);
+  const long long p0 = u / a.half * RT_RUN;
+  if (p0 >= a.n_pos) return;
+  double s, c, ds, dc;
+  turn_sincos((double)(a.first + p0), a.turns[i], a.rest[i], &s, &c);
+  turn_sincos(1.0, a.turns[i], a.rest[i], &ds, &dc);
+  const int n = (int)min((long long)RT_RUN, a.n_pos - p0);
+  float *co = a.cos + (size_t)p0 * a.half + i, *so = a.sin + (size_t)p0 * a.half + i;
+  for (int p = 0; p < n; ++p) {
+    co[(size_t)p * a.half] = (float)(a.amplitude * c);
+    so[(size_t)p * a.half] = (float)(a.amplitude * s);
+    const double t = c * dc - s * ds;
+    s = s * dc + c * ds;
+    c = t;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ append
+constexpr int AP_THREADS = 256, AP_WARPS = AP_THREADS / 32, AP_BATCH = 4;
+struct AppendArgs {
+  void *k, *v;                                  // the layer
+  const int *table, *len, *refs;
+  int n_slots, max_pages, n_pages, page, shift, rows;
+  const int *seqs, *start, *row_ptr, *pos;
+  int heads, kv_heads;
+  const float *cos, *sin;
+  int n_pos, rot;
+  const void *q_gain, *k_gain;
+  float eps;
+  const void *q, *kin, *vin; void* qout;
+  long long q_stride, qout_stride, k_stride, v_stride;
+  int* status;
+  int split;                                    // warps that share a row: 1, 2, 4 or 8
+};
+
+template <typename T> struct Pair16;
+template <> struct Pair16<__nv_bfloat16> {
+  static __device__ __forceinline__ float2 two(unsigned x) { return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+  static __device__ __forceinline__ unsigned pack(float lo, float hi) { __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<unsigned*>(&v); }
+};
+template <> struct Pair16<__half> {
+  static __device__ __forceinline__ float2 two(unsigned x) { return __half22float2(*reinterpret_cast<__half2*>(&x)); }
+  static __device__ __forceinline__ unsigned pack(float lo, float hi) { __half2 v = __floats2half2_rn(lo, hi); return *reinterpret_cast<unsigned*>(&v); }
+};
+
+// grid (x, entries).  A lane holds 8 neighbouring elements of a head, a warp two heads of 128 or four of 64 at a time, all of one row, so that a
+// lane's cosines and sines stay in registers for the whole row; the partner of a half-layout pair comes from another lane.
+// Each CTA checks the whole entry for itself (its pages and positions), so that an entry is written whole or not at all without a second launch.
+template <typename T, int D, bool INTER, bool NORM>
+__global__ void __launch_bounds__(AP_THREADS) pages_append_kernel(AppendArgs a) {
+  constexpr int LANES = D / 8, PER = 32 / LANES;                        // lanes of a head; heads of a warp
+  const int tid = threadIdx.x, i = blockIdx.y, warp = tid >> 5, lane = tid & 31;
+  pdl_trigger();
+  pdl_wait();
+  const int slot = a.seqs[i], r0 = a.row_ptr[i], r1 = a.row_ptr[i + 1];
+  int code = 0, at0 = 0;
+  if ((unsigned)slot >= (unsigned)a.n_slots || r0 < 0 || r1 < r0 || r1 > a.rows) code = VLAC_ERR_INVALID_ARG;
+  else {
+    const int len = a.len[slot];
+    if (len < 0 || len > a.max_pages << a.shift) code = VLAC_ERR_BAD_STATE;
+    else {
+      at0 = a.start ? a.start[i] : len - (r1 - r0);
+      if (at0 < 0 || (long long)at0 + (r1 - r0) > len) code = VLAC_ERR_INVALID_ARG;
+      else if (a.rot && !a.pos && r1 > r0 && at0 + (r1 - r0) > a.n_pos) code = VLAC_ERR_INVALID_ARG;
+    }
+  }
+  // (uniform so far) an earlier entry with the same slot stands; positions have a row in the tables; pages exist and are the slot's own
+  int wrong = 0, bad = 0;
+  for (int j = tid; j < i; j += AP_THREADS) wrong |= a.seqs[j] == slot;
+  const int* t = a.table + (size_t)(code == 0 ? slot : 0) * a.max_pages;
+  if (code == 0 && r1 > r0) {
+    for (int j = (at0 >> a.shift) + tid; j <= (at0 + r1 - r0 - 1) >> a.shift; j += AP_THREADS) {
+      const int p = t[j];
+      bad |= (unsigned)p >= (unsigned)a.n_pages || a.refs[p] != 1;
+    }
+    if (a.pos && a.rot) for (int j = r0 + tid; j < r1; j += AP_THREADS) wrong |= (unsigned)a.pos[j] >= (unsigned)a.n_pos;
+  }
+  if (__syncthreads_or(wrong)) code = VLAC_ERR_INVALID_ARG;
+  if (__syncthreads_or(bad) && code == 0) code = VLAC_ERR_BAD_STATE;
+  if (tid == 0 && blockIdx.x == 0) a.status[i] = code;
+  if (code != 0) return;
+
+  const int c = lane % LANES, half16 = a.rot / 16, el = c * 8;          // the lane's 16-byte piece of a head; pieces of half the rotated part
+  const bool turned = el < a.rot;
+  const int partner = INTER || !turned ? lane : c < half16 ? lane + half16 : lane - half16;
+  float qg[8], kg[8];
+  if (NORM) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qg[e] = kg[e] = 1.f;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const void* g = s ? a.k_gain : a.q_gain;
+      if (!g) continue;
+      uint4 x = *reinterpret_cast<const uint4*>((const T*)g + el);
+      const unsigned w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { const float2 f = Pair16<T>::two(w[e]); (s ? kg : qg)[2 * e] = f.x; (s ? kg : qg)[2 * e + 1] = f.y; }
+    }
+  }
+  const int all = a.heads + 2 * a.kv_heads, step = PER * a.split, per_cta = AP_WARPS / a.split;
+  const int first = (warp % a.split) * PER + lane / LANES;              // first head of this lane
+  for (int r = r0 + blockIdx.x * per_cta + warp / a.split; r < r1; r += gridDim.x * per_cta) {
+    const int at = at0 + (r - r0);
+    const size_t pool = (((size_t)t[at >> a.shift] << a.shift) + (at & (a.page - 1))) * ((size_t)a.kv_heads * D) + el;
+    float cs[8], sn[8];                                                 // (interleaved: four of each)
+    if (turned) {
+      const size_t row = (size_t)(a.pos ? a.pos[r] : at) * (a.rot / 2) + (INTER ? el / 2 : c < half16 ? el : el - a.rot / 2);
+#pragma unroll
+      for (int e = 0; e < (INTER ? 4 : 8); e += 4) {
+        *reinterpret_cast<float4*>(cs + e) = *reinterpret_cast<const float4*>(a.cos + row + e);
+        *reinterpret_cast<float4*>(sn + e) = *reinterpret_cast<const float4*>(a.sin + row + e);
+      }
+    }
+    const T* qi = (const T*)a.q + (size_t)r * a.q_stride + el;
+    const T *ki = (const T*)a.kin + (size_t)r * a.k_stride + el, *vi = (const T*)a.vin + (size_t)r * a.v_stride + el;
+    T* qo = (T*)a.qout + (size_t)r * a.qout_stride + el;
+    for (int h0 = first; h0 - lane / LANES < all; h0 += step * AP_BATCH) {               // (uniform over the warp)
+      uint4 x[AP_BATCH];
+#pragma unroll
+      for (int b = 0; b < AP_BATCH; ++b) {
+        const int h = h0 + b * step;
+        x[b] = make_uint4(0, 0, 0, 0);
+        if (h < all) x[b] = *reinterpret_cast<const uint4*>(h < a.heads ? qi + (size_t)h * D : h < a.heads + a.kv_heads ? ki + (size_t)(h - a.heads) * D
+                                                                                               : vi + (size_t)(h - a.heads - a.kv_heads) * D);
+      }
+#pragma unroll
+      for (int b = 0; b < AP_BATCH; ++b) {
+        const int h = h0 + b * step;
+        if (h - lane / LANES >= all) break;                             // (uniform)
+        const bool is_q = h < a.heads, is_v = h >= a.heads + a.kv_heads;
+        if (!__all_sync(0xffffffffu, is_v)) {
+          float f[8];
+          const unsigned w[4] = {x[b].x, x[b].y, x[b].z, x[b].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { const float2 y = Pair16<T>::two(w[e]); f[2 * e] = y.x; f[2 * e + 1] = y.y; }
+          if (NORM) {
+            float ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            const float inv = rsqrtf(ss * (1.f / D) + a.eps);
+            if ((is_q ? a.q_gain : a.k_gain) != nullptr)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) f[e] = f[e] * inv * (is_q ? qg[e] : kg[e]);
+          }
+          if (INTER) {
+            if (turned)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float u = f[2 * e], v = f[2 * e + 1];
+                f[2 * e] = u * cs[e] - v * sn[e];
+                f[2 * e + 1] = u * sn[e] + v * cs[e];
+              }
+          } else if (a.rot) {                                           // (uniform)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float y = __shfl_sync(0xffffffffu, f[e], partner);
+              if (turned) f[e] = c < half16 ? f[e] * cs[e] - y * sn[e] : y * sn[e] + f[e] * cs[e];
+            }
+          }
+          if (!is_v) x[b] = make_uint4(Pair16<T>::pack(f[0], f[1]), Pair16<T>::pack(f[2], f[3]), Pair16<T>::pack(f[4], f[5]), Pair16<T>::pack(f[6], f[7]));
+        }
+        if (h < all) {
+          T* to = is_q ? qo + (size_t)h * D : (T*)(is_v ? a.v : a.k) + pool + (size_t)(h - a.heads - (is_v ? a.kv_heads : 0)) * D;
+          *reinterpret_cast<uint4*>(to) = x[b];
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int D>
+int launch_append(const AppendArgs& a, bool inter, bool norm, dim3 grid, cudaStream_t s) {
+  auto kernel = inter ? (norm ? pages_append_kernel<T, D, true, true> : pages_append_kernel<T, D, true, false>)
+                      : (norm ? pages_append_kernel<T, D, false, true> : pages_append_kernel<T, D, false, false>);
+  VLAC_CUDA_CHECK(launch_pdl(kernel, grid, dim3(AP_THREADS), 0, s, a));
+  return VLAC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int vlac_rope_tables(const vlac_rope_scaling* r, int first, int n_pos, float* cos, float* sin, void* stream) {
+  if (!r || r->rot_dim < 2 || r->rot_dim > RT_MAX || r->rot_dim % 2 || first < 0 || n_pos < 0 || (long long)first + n_pos > INT_MAX) return VLAC_ERR_INVALID_ARG;
+  if (!(r->theta > 0) || !isfinite(r->theta) || !(r->factor > 0) || !isfinite(r->factor) || !(r->original_len >= 0) || !isfinite(r->original_len) ||
+      !isfinite(r->amplitude))
+    return VLAC_ERR_INVALID_ARG;
+  if (r->original_len > 0 && !(r->turns_low < r->turns_high)) return VLAC_ERR_INVALID_ARG;
+  if (n_pos == 0) return VLAC_OK;
+  if (!cos || !sin || ((uintptr_t)cos | (uintptr_t)sin) & 3u) return VLAC_ERR_INVALID_ARG;
+  TableArgs a = {};
+  a.half = r->rot_dim / 2; a.first = first; a.n_pos = n_pos; a.cos = cos; a.sin = sin; a.amplitude = r->amplitude;
+  const long double two_pi = 6.283185307179586476925286766559005768L;
+  for (int i = 0; i < a.half; ++i) {
+    const long double f = powl((long double)r->theta, -2.0L * i / r->rot_dim), turns = r->original_len * f / two_pi;
+    long double g = 0.0L;
+    if (r->original_len > 0) {
+      g = (turns - r->turns_low) / ((long double)r->turns_high - r->turns_low);
+      g = g < 0.0L ? 0.0L : g > 1.0L ? 1.0L : g;
+    }
+    const long double per = f * (g + (1.0L - g) / r->factor) / two_pi;
+    a.turns[i] = (double)per;
+    a.rest[i] = (double)(per - a.turns[i]);
+  }
+  const long long units = (long long)a.half * ((n_pos + RT_RUN - 1LL) / RT_RUN), ctas = (units + RT_THREADS - 1) / RT_THREADS;
+  VLAC_CUDA_CHECK(launch_pdl(rope_tables_kernel, dim3((unsigned)ctas), dim3(RT_THREADS), 0, (cudaStream_t)stream, a));
+  return VLAC_OK;
+}
+
+int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int* start, const int* row_ptr, int n, int rows, const vlac_rope* rope,
+                      const int* pos, int n_heads, const void* q, long long q_stride, void* q_out, long long q_out_stride, const void* k_rows,
+                      long long k_stride, const void* v_rows, long long v_stride, int* status, void* stream) {
+  int rc = pages_check(p);
+  if (rc == VLAC_OK) rc = list_check(n);
+  if (rc != VLAC_OK) return rc;
+  if (layer < 0 || layer >= p->n_layers || rows < 0 || n_heads < 0 || n_heads > 65536 || !rope) return VLAC_ERR_INVALID_ARG;
+  if (rope->rot_dim < 0 || rope->rot_dim > p->head_dim || rope->rot_dim % 16 || (rope->interleaved != 0 && rope->interleaved != 1) || rope->n_pos < 0)
+    return VLAC_ERR_INVALID_ARG;
+  if (rope->rot_dim && (!rope->cos || !rope->sin || ((uintptr_t)rope->cos | (uintptr_t)rope->sin) & 15u)) return VLAC_ERR_INVALID_ARG;
+  if (((uintptr_t)rope->q_gain | (uintptr_t)rope->k_gain) & 15u) return VLAC_ERR_INVALID_ARG;
+  if ((rope->q_gain || rope->k_gain) && !(rope->eps >= 0.f && isfinite(rope->eps))) return VLAC_ERR_INVALID_ARG;
+  if (n == 0) return VLAC_OK;
+  if (!seqs || !row_ptr || !status || (rows > 0 && (!k_rows || !v_rows))) return VLAC_ERR_INVALID_ARG;
+  const long long w = (long long)pages_row(p), wq = (long long)n_heads * p->head_dim;
+  if (k_stride < w || v_stride < w || k_stride % 8 || v_stride % 8 || (((uintptr_t)k_rows | (uintptr_t)v_rows) & 15u)) return VLAC_ERR_INVALID_ARG;
+  if (n_heads > 0 && rows > 0) {
+    if (!q || !q_out || q_stride < wq || q_out_stride < wq || q_stride % 8 || q_out_stride % 8 || (((uintptr_t)q | (uintptr_t)q_out) & 15u))
+      return VLAC_ERR_INVALID_ARG;
+    if (!(q == q_out && q_stride == q_out_stride) && rows_overlap((uintptr_t)q, 2ull * q_stride, (uintptr_t)q_out, 2ull * q_out_stride, 2ull * wq, 2ull * wq, rows))
+      return VLAC_ERR_INVALID_ARG;
+    if (rows_overlap((uintptr_t)k_rows, 2ull * k_stride, (uintptr_t)q_out, 2ull * q_out_stride, 2ull * w, 2ull * wq, rows) ||
+        rows_overlap((uintptr_t)v_rows, 2ull * v_stride, (uintptr_t)q_out, 2ull * q_out_stride, 2ull * w, 2ull * wq, rows))
+      return VLAC_ERR_INVALID_ARG;
+  }
+  int n_sm = 0;
+  rc = sm_count(&n_sm);
+  if (rc != VLAC_OK) return rc;
+  AppendArgs a = {};
+  a.k = (unsigned short*)p->k + (size_t)layer * pages_layer(p); a.v = (unsigned short*)p->v + (size_t)layer * pages_layer(p);
+  a.table = p->table; a.len = p->len; a.refs = p->refs; a.n_slots = p->n_slots; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size;
+  a.shift = pages_shift(p->page_size); a.rows = rows; a.seqs = seqs; a.start = start; a.row_ptr = row_ptr; a.pos = pos; a.heads = n_heads; a.kv_heads = p->n_kv_heads;
+  a.cos = rope->cos; a.sin = rope->sin; a.n_pos = rope->n_pos; a.rot = rope->rot_dim; a.q_gain = rope->q_gain; a.k_gain = rope->k_gain; a.eps = rope->eps;
+  a.q = q; a.kin = k_rows; a.vin = v_rows; a.qout = q_out; a.q_stride = q_stride; a.qout_stride = q_out_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+  a.status = status;
+  a.split = 1;
+  while (a.split < AP_WARPS && (long long)rows * a.split < n_sm * 64ll) a.split *= 2;
+  // enough CTAs for the whole GPU; no more per entry than one entry could use
+  const int per = AP_WARPS / a.split, groups = (rows + per - 1) / per, spread = (n_sm * 8 + n - 1) / n;
+  const dim3 grid(groups < 1 ? 1 : groups < spread ? groups : spread, n);
+  const bool norm = rope->q_gain || rope->k_gain;
+  auto launch = p->dtype == VLAC_BF16 ? (p->head_dim == 128 ? launch_append<__nv_bfloat16, 128> : launch_append<__nv_bfloat16, 64>)
+                                      : (p->head_dim == 128 ? launch_append<__half, 128> : launch_append<__half, 64>);
+  return launch(a, rope->interleaved, norm, grid, (cudaStream_t)stream);
+}
+
+}  // extern "C"
