@@ -1,16 +1,26 @@
 // Logits before a token is picked (vlac_logits_adjust): penalties for tokens that were there, biases, grammar masks, and the choice.
 //
-// A row is shared by a cluster of CTAs that take its vocabulary in chunks.  For a chunk, what is said of single tokens (history, drafted
-// ancestors, biases) is first gathered into a table in shared memory with integer atomics, whose order changes nothing; then the chunk's
-// logits, which were asked for before that, pass through it once.  Bound: HBM, the logits read once and written once.
+// A row is shared by a cluster of CTAs, a run of the vocabulary each.  What is said of single tokens (history, drafted ancestors, biases) touches few of
+// them: the CTA first goes through the row's lists, marks its tokens in a bit map and counts them in a small table; then it streams the run through once, 16
+// bytes at a time with nothing but two masks to look at, and last it does the marked tokens one by one, whose logits are in L2 by then.  All gathering is
+// by integer atomics, whose order changes nothing.  Bound: HBM, the logits read once and written once.
 #include "pages_internal.h"
 #include "launch_util.h"
 #include <cuda_fp16.h>
+#include <type_traits>
 
 namespace {
 
-constexpr int LG_THREADS = 512, LG_EACH = 8, LG_CHUNK = LG_THREADS * LG_EACH, LG_CTAS = 8;
+constexpr int LG_THREADS = 256, LG_WARPS = LG_THREADS / 32;
+constexpr int LG_RUN = 131072;                  // tokens whose marks a CTA holds at once
+// Tokens whose counts a CTA holds: a run of at most as many by their place in it ("direct"), of a longer one the marked tokens by a hash.  Few rows: more, so
+// that an eighth of 32,000 tokens is direct; many: fewer, so that four CTAs fit an SM.
+__host__ __device__ constexpr int lg_table(int ctas) { return ctas == 8 ? 4096 : 2048; }
+constexpr int LG_TRIES = 64;                    // where a token finds no entry in as many tries, the run is cut into direct ones
+constexpr int LG_LOOK = 4;                      // tokens of the history that a thread asks for at once
+constexpr int LG_EACH = 2;                      // marked tokens that a thread has in flight
 constexpr unsigned LG_SEEN = 0x80000000u;       // of a token's entry in the table: it was in the prompt; the other bits: how often it was generated
+__host__ __device__ constexpr int lg_smem(int ctas) { return LG_RUN / 8 + lg_table(ctas) * 14; }
 
 struct LogitsArgs {
   int rows, vocab;
@@ -20,155 +30,338 @@ struct LogitsArgs {
   vlac_logits_rules r;
   const unsigned* mask; const int *entry, *q_ptr; int n, words;         // the tree's
   int allow_words;
+  int per;                                      // tokens of a CTA, a multiple of 64
 };
 
-template <typename T> __device__ __forceinline__ float lg_value(T x);
-template <> __device__ __forceinline__ float lg_value<float>(float x) { return x; }
-template <> __device__ __forceinline__ float lg_value<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <> __device__ __forceinline__ float lg_value<__half>(__half x) { return __half2float(x); }
-template <typename T> __device__ __forceinline__ T lg_round(float x);
-template <> __device__ __forceinline__ float lg_round<float>(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 lg_round<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-template <> __device__ __forceinline__ __half lg_round<__half>(float x) { return __float2half_rn(x); }
-
-// order-preserving: a larger value has a larger key, -0 and +0 the same one, a NaN the largest; never 0
-__device__ __forceinline__ unsigned lg_key(float v) {
-  if (v != v) return 0xffffffffu;
-  const unsigned u = __float_as_uint(v + 0.0f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+// order-preserving: a larger value has a larger key, -0 and +0 the same one, a NaN the largest (an addition makes every NaN the same positive one).
+// The smallest number stands for "none": no value has it.
+constexpr int LG_NONE = INT_MIN;
+__device__ __forceinline__ int lg_key(float v) {
+  const int s = __float_as_int(v + 0.0f);
+  return s ^ ((s >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ unsigned lg_hash(unsigned t, int table) { return __umulhi(t * 2654435769u, (unsigned)table); }      // (Knuth's multiplicative hash)
+__device__ __forceinline__ float lg_max(float a, float b) { float d; asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b)); return d; }
+// Bits b and b + 1 of the four lowest of x as masks of 16 bits side by side (b = 0 or 2): each bit to the top of a byte, and that spread out.
+__device__ __forceinline__ unsigned lg_spread(unsigned x) { return (x * 0x00204081u & 0x01010101u) << 7; }
+__device__ __forceinline__ unsigned lg_pair(unsigned spread, int b) {   // (a selector of 8 + i: the top bit of byte i, eight times)
+  unsigned d;
+  asm("prmt.b32 %0, %1, 0, %2;" : "=r"(d) : "r"(spread), "r"(b ? 0xbbaau : 0x9988u));
+  return d;
 }
 
-// VEC: rows of whole, aligned 16-byte pieces; a thread's elements are then neighbours in pieces, else 512 apart.
-template <typename T, bool VEC>
-__global__ void __cluster_dims__(LG_CTAS, 1, 1) __launch_bounds__(LG_THREADS) logits_kernel(LogitsArgs a) {
-  constexpr int PIECE = 16 / sizeof(T), PIECES = LG_EACH / PIECE;
-  __shared__ unsigned s_made[LG_CHUNK];
-  __shared__ int s_bias[LG_CHUNK];              // number of the token's last entry in the row's list of biases, from 1 on
-  __shared__ unsigned s_key[LG_THREADS / 32], s_at[LG_THREADS / 32];
-  __shared__ unsigned s_best[LG_CTAS][2];       // of CTA 0: what the others found
+template <typename T> struct Logit;             // one element, and two side by side
+template <> struct Logit<float> {
+  static __device__ __forceinline__ float value(float x) { return x; }
+  static __device__ __forceinline__ float round(float x) { return x; }
+};
+template <> struct Logit<__nv_bfloat16> {
+  static constexpr unsigned none = 0xff80ff80u; // -infinity
+  static __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
+  static __device__ __forceinline__ __nv_bfloat16 round(float x) { return __float2bfloat16_rn(x); }
+  static __device__ __forceinline__ unsigned max2(unsigned a, unsigned b) { unsigned d; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
+  static __device__ __forceinline__ float2 two(unsigned x) { return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+};
+template <> struct Logit<__half> {
+  static constexpr unsigned none = 0xfc00fc00u;
+  static __device__ __forceinline__ float value(__half x) { return __half2float(x); }
+  static __device__ __forceinline__ __half round(float x) { return __float2half_rn(x); }
+  static __device__ __forceinline__ unsigned max2(unsigned a, unsigned b) { unsigned d; asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
+  static __device__ __forceinline__ float2 two(unsigned x) { return __half22float2(*reinterpret_cast<__half2*>(&x)); }
+};
+
+// 16 bytes of logits, or one element where rows are not whole, aligned 16-byte pieces
+template <typename T, bool VEC> struct Piece {
+  static constexpr int N = VEC ? 16 / sizeof(T) : 1;
+  static constexpr unsigned ALL = (1u << N) - 1u;
+  uint4 v;
+  __device__ __forceinline__ void load(const T* p) {
+    if (VEC) v = *reinterpret_cast<const uint4*>(p);
+    else if (sizeof(T) == 4) v.x = *reinterpret_cast<const unsigned*>(p);
+    else v.x = *reinterpret_cast<const unsigned short*>(p);
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if (VEC) *reinterpret_cast<uint4*>(p) = v;
+    else if (sizeof(T) == 4) *reinterpret_cast<unsigned*>(p) = v.x;
+    else *reinterpret_cast<unsigned short*>(p) = (unsigned short)v.x;
+  }
+  __device__ __forceinline__ float value(int e) const {                 // (e is a constant where this is used)
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else { const float2 f = Logit<T>::two(w[e >> 1]); return e & 1 ? f.y : f.x; }
+  }
+  // -infinity in the elements outside `stay`; the largest of all so far, in two halves for 16-bit types
+  using Max = std::conditional_t<sizeof(T) == 4, float, unsigned>;
+  __device__ __forceinline__ void mask_and_max(unsigned stay, Max* m) {
+    unsigned w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        if (!(stay >> e & 1)) w[e] = 0xff800000u;
+        *m = lg_max(*m, __uint_as_float(w[e]));
+      }
+    } else {
+      using L = Logit<T>;
+      if (stay != ALL || !VEC) {
+        const unsigned s[2] = {lg_spread(stay & 15), lg_spread(stay >> 4)};
+#pragma unroll
+        for (int i = 0; i < (VEC ? 4 : 1); ++i) { const unsigned k = lg_pair(s[i >> 1], i & 1); w[i] = (w[i] & k) | (L::none & ~k); }
+      }
+#pragma unroll
+      for (int i = 0; i < (VEC ? 4 : 1); ++i) *m = L::max2(*m, w[i]);
+    }
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ Max none() { if constexpr (sizeof(T) == 4) return -INFINITY; else return Logit<T>::none; }
+  static __device__ __forceinline__ float largest(Max m) {
+    if constexpr (sizeof(T) == 4) return m;
+    else { const float2 f = Logit<T>::two(m); return lg_max(f.x, f.y); }
+  }
+};
+
+// CTAS share a row.  Few rows are shared by 8, so that there are enough CTAs; many by fewer, since every one of them goes through the row's lists.
+template <typename T, bool VEC, int CTAS>
+__global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, CTAS == 8 ? 3 : 4) logits_kernel(LogitsArgs a) {
+  using P = Piece<T, VEC>;
+  using L = Logit<T>;
+  constexpr int LG_TABLE = lg_table(CTAS);
+  constexpr int N = P::N, BATCH = VEC ? 2 : 8;  // pieces of a thread in flight
+  extern __shared__ __align__(16) unsigned lg_raw[];
+  unsigned* const s_mark = lg_raw;              // [LG_RUN / 32]
+  unsigned* const s_made = s_mark + LG_RUN / 32;                        // [LG_TABLE]
+  int* const s_bias = (int*)s_made + LG_TABLE;  // [LG_TABLE] number of the token's last entry in the row's list of biases, from 1 on
+  int* const s_token = s_bias + LG_TABLE;       // [LG_TABLE] token + 1 of the hash's entry, 0: free
+  unsigned short* const s_list = (unsigned short*)(s_token + LG_TABLE); // [LG_TABLE] the entries in use, each warp those of its share of the table
+  __shared__ int s_key[LG_WARPS], s_full;
+  __shared__ unsigned s_at[LG_WARPS];
+  __shared__ int s_best[CTAS][2];               // of CTA 0: what the others found
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.y, rank = (int)cluster_rank();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");                   // (CTA 0 runs before anything is put into its memory)
   pdl_trigger();
   pdl_wait();
   const vlac_logits_rules& u = a.r;
-  int h0 = 0, h1 = 0, h2 = 0, b0 = 0, b1 = 0, allow_row = -1, first = -1, n_seen = 0;  // rows first .. first + n_seen may be seen
+  int h0 = 0, h1 = 0, h2 = 0, b0 = 0, b1 = 0, allow_row = -1, first = -1, n_seen = 0;     // rows first .. first + n_seen may be seen
+  const int e = a.mask ? a.entry[row] : -1;
   bool ok = true;
   if (u.span) { h0 = u.span[3 * row]; h1 = u.span[3 * row + 1]; h2 = u.span[3 * row + 2]; ok = 0 <= h0 && h0 <= h1 && h1 <= h2 && h2 <= u.n_tokens; }
   if (u.bias_ptr) { b0 = u.bias_ptr[row]; b1 = u.bias_ptr[row + 1]; ok = ok && 0 <= b0 && b0 <= b1 && b1 <= u.n_bias; }
   if (u.allow) { allow_row = u.allow_row ? u.allow_row[row] : row; ok = ok && -1 <= allow_row && allow_row < u.n_allow; }
   const float rep = u.repetition ? u.repetition[row] : 1.f, freq = u.frequency ? u.frequency[row] : 0.f, pres = u.presence ? u.presence[row] : 0.f;
-  if (a.mask) {
-    const int e = a.entry[row];
-    if ((unsigned)e < (unsigned)a.n) { first = a.q_ptr[e]; n_seen = min(a.q_ptr[e + 1], a.rows); }
+  // (the first of every list are asked for together: one after the other they would be the longest part of a call)
+  int h[LG_LOOK], b = -1;
+#pragma unroll
+  for (int q = 0; q < LG_LOOK; ++q) { const int i = h0 + q * LG_THREADS + tid; h[q] = ok && i < h2 ? u.tokens[i] : -1; }
+  if (ok && tid < b1 - b0) b = u.bias_token[b0 + tid];
+  if ((unsigned)e < (unsigned)a.n) {            // (a.n is 0 without a tree)
+    first = a.q_ptr[e]; n_seen = min(a.q_ptr[e + 1], a.rows);
     if (first < 0 || first > row || n_seen <= row) first = -1;
     n_seen = first < 0 ? 0 : min(n_seen - first, a.words * 32);
   }
+  const int d = tid < n_seen ? u.drafted[first + tid] : -1;
+  const unsigned seen = tid < n_seen ? a.mask[(size_t)row * a.words + (tid >> 5)] >> (tid & 31) & 1 : 0;
   if (rank == 0 && tid == 0) a.status[row] = ok ? VLAC_OK : VLAC_ERR_INVALID_ARG;
-  const bool made = ok && (h2 > h0 || first >= 0), biased = ok && b1 > b0;               // is there anything to gather (uniform)
-  const unsigned* allow = u.allow && allow_row >= 0 ? u.allow + (size_t)allow_row * a.allow_words : nullptr;
+  const bool any = ok && (h2 > h0 || first >= 0 || b1 > b0);                              // is anything said of single tokens (uniform)
+  const unsigned char* allow = u.allow && allow_row >= 0 ? (const unsigned char*)(u.allow + (size_t)allow_row * a.allow_words) : nullptr;
   const T* in = (const T*)a.in + (size_t)row * a.stride;
   T* out = a.out ? (T*)a.out + (size_t)row * a.out_stride : nullptr;
-  unsigned best = 0, best_at = 0;
-  for (int c0 = rank * LG_CHUNK; ok && c0 < a.vocab; c0 += LG_CTAS * LG_CHUNK) {
-    const int n = min(LG_CHUNK, a.vocab - c0);
-    // ---- the logits, asked for before they are needed
-    __align__(16) T x[LG_EACH];
-    if (VEC) {
+  int best = LG_NONE, best1 = LG_NONE;          // largest key of the unmarked tokens, and of the marked ones
+  unsigned best_at = 0, best_of = 0, best1_at = 0;                      // first token of the batch that has it, and which of the batch count; the token
+  const int end = ok ? (int)min((long long)a.vocab, (long long)(rank + 1) * a.per) : 0;
+  int most = LG_RUN;
+  for (int c0 = rank * a.per, n; c0 < end; c0 += n) {
+    n = min(most, end - c0);
+    bool direct = n <= LG_TABLE;
+    P x[BATCH];                                 // the first logits, asked for before they are needed
 #pragma unroll
-      for (int q = 0; q < PIECES; ++q) {
-        const int at = (q * LG_THREADS + tid) * PIECE;
-        if (at < n) *reinterpret_cast<uint4*>(x + q * PIECE) = *reinterpret_cast<const uint4*>(in + c0 + at);
+    for (int q = 0; q < BATCH; ++q) { const int at = (q * LG_THREADS + tid) * N; if (at < n) x[q].load(in + c0 + at); }
+    // ---- what is said of which tokens
+    for (bool again = any; again;) {
+      __syncthreads();                          // (what was there before is read)
+      for (int i = tid * 4; i < (n + 31) >> 5; i += LG_THREADS * 4) *reinterpret_cast<uint4*>(s_mark + i) = make_uint4(0, 0, 0, 0);
+      for (int i = tid * 4; i < (direct ? n : LG_TABLE); i += LG_THREADS * 4) {
+        *reinterpret_cast<uint4*>(s_made + i) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(s_bias + i) = make_uint4(0, 0, 0, 0);
+        if (!direct) *reinterpret_cast<uint4*>(s_token + i) = make_uint4(0, 0, 0, 0);
       }
-    } else {
-#pragma unroll
-      for (int q = 0; q < LG_EACH; ++q) { const int at = q * LG_THREADS + tid; if (at < n) x[q] = in[c0 + at]; }
-    }
-    // ---- what is said of single tokens
-    if (made || biased) {
-      __syncthreads();                                                  // (the table of the chunk before is read)
-#pragma unroll
-      for (int q = 0; q < LG_EACH; ++q) { if (made) s_made[q * LG_THREADS + tid] = 0; if (biased) s_bias[q * LG_THREADS + tid] = 0; }
+      if (tid == 0) s_full = 0;
       __syncthreads();
-      for (int i = h0 + tid; i < h2; i += LG_THREADS) {
-        const unsigned t = (unsigned)u.tokens[i] - (unsigned)c0;
-        if (t < (unsigned)n) { if (i >= h1) atomicAdd(&s_made[t], 1u); else atomicOr(&s_made[t], LG_SEEN); }
-      }
-      if (first >= 0)
-        for (int j = tid; j < n_seen; j += LG_THREADS)
-          if (a.mask[(size_t)row * a.words + (j >> 5)] >> (j & 31) & 1) {
-            const unsigned t = (unsigned)u.drafted[first + j] - (unsigned)c0;
-            if (t < (unsigned)n) atomicAdd(&s_made[t], 1u);
-          }
-      if (biased)
-        for (int i = b0 + tid; i < b1; i += LG_THREADS) {
-          const unsigned t = (unsigned)u.bias_token[i] - (unsigned)c0;
-          if (t < (unsigned)n) atomicMax(&s_bias[t], i - b0 + 1);
+      auto place = [&](unsigned t) -> int {     // the token's entry; -1: there are too many
+        atomicOr(&s_mark[t >> 5], 1u << (t & 31));
+        if (direct) return (int)t;
+        unsigned i = lg_hash(t, LG_TABLE);
+        for (int tries = 0; tries < LG_TRIES; ++tries, i = (i + 1) % LG_TABLE) {
+          int had = *(volatile int*)&s_token[i];
+          if (had == 0) had = atomicCAS(&s_token[i], 0, (int)t + 1);
+          if (had == 0 || had == (int)t + 1) return (int)i;
         }
+        s_full = 1;
+        return -1;
+      };
+      auto count = [&](int token, bool made) {
+        const unsigned t = (unsigned)token - (unsigned)c0;
+        const int i = token >= 0 && t < (unsigned)n ? place(t) : -1;
+        if (i >= 0) { if (made) atomicAdd(&s_made[i], 1u); else atomicOr(&s_made[i], LG_SEEN); }
+      };
+      auto add = [&](int token, int number) {
+        const unsigned t = (unsigned)token - (unsigned)c0;
+        const int i = token >= 0 && t < (unsigned)n ? place(t) : -1;
+        if (i >= 0) atomicMax(&s_bias[i], number);
+      };
+#pragma unroll
+      for (int q = 0; q < LG_LOOK; ++q) count(h[q], h0 + q * LG_THREADS + tid >= h1);
+      for (int i0 = h0 + LG_LOOK * LG_THREADS; i0 < h2; i0 += LG_LOOK * LG_THREADS) {
+        int g[LG_LOOK];
+#pragma unroll
+        for (int q = 0; q < LG_LOOK; ++q) { const int i = i0 + q * LG_THREADS + tid; g[q] = i < h2 ? u.tokens[i] : -1; }
+#pragma unroll
+        for (int q = 0; q < LG_LOOK; ++q) count(g[q], i0 + q * LG_THREADS + tid >= h1);
+      }
+      if (seen) count(d, true);
+      for (int j = tid + LG_THREADS; j < n_seen; j += LG_THREADS)
+        if (a.mask[(size_t)row * a.words + (j >> 5)] >> (j & 31) & 1) count(u.drafted[first + j], true);
+      if (b >= 0) add(b, tid + 1);
+      for (int i = b0 + tid + LG_THREADS; i < b1; i += LG_THREADS) add(u.bias_token[i], i - b0 + 1);
       __syncthreads();
+      again = s_full;                           // (never of a direct run)
+      if (again) { most = n = LG_TABLE; direct = true; }                // (uniform; the first logits lie in the shorter run too, or are not looked at)
     }
-    // ---- through it
+    // ---- the run: BATCH pieces of a thread at a time, the next ones asked for in front of that.  Of a batch only the largest element is looked at; which
+    // of its elements that is, is found out in the end.
+    const unsigned char *may_b = allow ? allow + ((c0 + tid * N) >> 3) : nullptr, *mark_b = reinterpret_cast<const unsigned char*>(s_mark) + (tid * N >> 3);
+    const T* from = in + c0 + tid * N;
+    T* to = out ? out + c0 + tid * N : nullptr;
+    constexpr int STEP = LG_THREADS * N, ALL_STEP = BATCH * STEP;       // tokens of a piece of every thread, of a batch
+    auto batch = [&](int at0, auto whole) {                             // whole: no thread has a piece behind the end of the run
+      typename P::Max m = P::none();
+      unsigned of = 0;
 #pragma unroll
-    for (int q = 0; q < LG_EACH; ++q) {
-      const int at = VEC ? ((q / PIECE) * LG_THREADS + tid) * PIECE + q % PIECE : q * LG_THREADS + tid;
-      if (at >= n) continue;
-      float v = lg_value<T>(x[q]);
-      if (made) {
-        const unsigned m = s_made[at], c = m & ~LG_SEEN;
-        if (m) v = v > 0.f ? __fdiv_rn(v, rep) : __fmul_rn(v, rep);
-        if (c) { v = __fsub_rn(v, __fmul_rn(freq, (float)c)); v = __fsub_rn(v, pres); }
+      for (int q = 0; q < BATCH; ++q) {
+        if (!decltype(whole)::value && at0 + q * STEP + tid * N >= n) continue;
+        unsigned stay = 0xffu;                                          // (c0 is a multiple of 32, a piece's first token one of N)
+        if (may_b) stay = may_b[(at0 + q * STEP) >> 3];
+        unsigned mark = any ? mark_b[(at0 + q * STEP) >> 3] : 0;
+        if (N < 8) { stay = stay >> (tid * N & 7) & P::ALL; mark = mark >> (tid * N & 7) & P::ALL; }
+        of |= (stay & ~mark) << q * N;
+        P y = x[q];
+        y.mask_and_max(stay & ~mark, &m);
+        if (mark & stay) { typename P::Max none; y = x[q]; y.mask_and_max(stay, &none); }  // (a marked token stays as it is, where out is in)
+        if (to) y.store(to + at0 + q * STEP);
       }
-      if (biased) { const int b = s_bias[at]; if (b) v = __fadd_rn(v, u.bias[b0 + b - 1]); }
-      const bool may = !allow || (allow[(c0 + at) >> 5] >> (at & 31) & 1);               // (c0 is a multiple of 32)
-      if (!may) v = -INFINITY;
-      x[q] = lg_round<T>(v);
-      const unsigned k = may ? lg_key(v) : 0;
-      if (k > best || (k == best && k && (unsigned)(c0 + at) < best_at)) { best = k; best_at = c0 + at; }
+      const int k = lg_key(P::largest(m));
+      if (k > best && of) { best = k; best_at = c0 + at0 + tid * N; best_of = of; }        // (ascending: of equal ones the first stays)
+    };
+    for (int at0 = 0; at0 < n; at0 += ALL_STEP) {
+      P y[BATCH];
+      if (at0 + 2 * ALL_STEP <= n) {
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) y[q].load(from + at0 + ALL_STEP + q * STEP);
+        batch(at0, std::true_type());
+      } else {
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) if (at0 + ALL_STEP + q * STEP + tid * N < n) y[q].load(from + at0 + ALL_STEP + q * STEP);
+        batch(at0, std::false_type());
+      }
+#pragma unroll
+      for (int q = 0; q < BATCH; ++q) x[q] = y[q];
     }
-    if (!out) continue;
-    if (VEC) {
-#pragma unroll
-      for (int q = 0; q < PIECES; ++q) {
-        const int at = (q * LG_THREADS + tid) * PIECE;
-        if (at < n) *reinterpret_cast<uint4*>(out + c0 + at) = *reinterpret_cast<const uint4*>(x + q * PIECE);
+    // ---- the marked tokens: every warp collects those of its share of the table and does them, LG_EACH a lane at a time
+    if (any) {
+      constexpr int SHARE = LG_TABLE / LG_WARPS;
+      unsigned short* const mine = s_list + warp * SHARE;
+      int used = 0;
+      for (int i0 = warp * SHARE; i0 < min((warp + 1) * SHARE, direct ? n : LG_TABLE); i0 += 32) {
+        const bool in_use = direct ? s_mark[i0 >> 5] >> lane & 1 : s_token[i0 + lane] != 0;
+        const unsigned b = __ballot_sync(0xffffffffu, in_use);
+        if (in_use) mine[used + __popc(b & ((1u << lane) - 1))] = (unsigned short)(i0 + lane);
+        used += __popc(b);
       }
-    } else {
+      __syncthreads();                          // (the run is written: what comes now lies over it)
+      for (int j0 = lane; j0 < used; j0 += 32 * LG_EACH) {
+        int at[LG_EACH], number[LG_EACH];
+        unsigned made[LG_EACH];
+        float v[LG_EACH], add[LG_EACH];
+        bool may[LG_EACH];
 #pragma unroll
-      for (int q = 0; q < LG_EACH; ++q) { const int at = q * LG_THREADS + tid; if (at < n) out[c0 + at] = x[q]; }
+        for (int q = 0; q < LG_EACH; ++q) {
+          const int j = j0 + q * 32, i = mine[min(j, used - 1)];
+          at[q] = c0 + (direct ? i : s_token[i] - 1);
+          made[q] = s_made[i]; number[q] = s_bias[i];
+          v[q] = L::value(in[at[q]]);
+          may[q] = j < used && (!allow || (allow[at[q] >> 3] >> (at[q] & 7) & 1));        // (what is not allowed is written already)
+          add[q] = number[q] ? u.bias[b0 + number[q] - 1] : 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < LG_EACH; ++q) {
+          if (!may[q]) continue;
+          const unsigned c = made[q] & ~LG_SEEN;
+          float y = v[q];
+          if (made[q]) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
+          if (c) { y = __fsub_rn(y, __fmul_rn(freq, (float)c)); y = __fsub_rn(y, pres); }
+          if (number[q]) y = __fadd_rn(y, add[q]);
+          if (out) out[at[q]] = L::round(y);
+          const int k = lg_key(y);
+          if (k > best1 || (k == best1 && (unsigned)at[q] < best1_at)) { best1 = k; best1_at = at[q]; }
+        }
+      }
     }
   }
-  // ---- the largest, of equal ones the lowest: warp, CTA, cluster
-  auto join = [&](unsigned k, unsigned at) {
-    best = __reduce_max_sync(0xffffffffu, k);
-    best_at = __reduce_min_sync(0xffffffffu, k == best ? at : 0xffffffffu);
-  };
-  join(best, best_at);
-  if (lane == 0) { s_key[warp] = best; s_at[warp] = best_at; }
+  // ---- the largest, of equal ones the lowest: CTA, then cluster
+  int top = __reduce_max_sync(0xffffffffu, max(best, best1));
+  if (lane == 0) s_key[warp] = top;
   __syncthreads();
-  __syncwarp();
+  top = LG_NONE;
+#pragma unroll
+  for (int w = 0; w < LG_WARPS; ++w) top = max(top, s_key[w]);
+  unsigned at = best1 == top ? best1_at : 0xffffffffu;
+  if (best == top && top != LG_NONE) {          // which of its batch (what counts was stored as it was)
+    P z[BATCH];
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) if (best_of >> q * N & P::ALL) z[q].load(in + best_at + q * LG_THREADS * N);
+#pragma unroll
+    for (int q = BATCH - 1; q >= 0; --q)
+#pragma unroll
+      for (int e = N - 1; e >= 0; --e)
+        if (best_of >> (q * N + e) & 1 && lg_key(z[q].value(e)) == top) at = min(at, best_at + q * LG_THREADS * N + e);
+  }
+  at = __reduce_min_sync(0xffffffffu, at);
+  if (lane == 0) s_at[warp] = at;
+  __syncthreads();
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (warp == 0) {
-    const bool in_use = lane < LG_THREADS / 32;
-    join(in_use ? s_key[lane] : 0, in_use ? s_at[lane] : 0xffffffffu);
+    at = __reduce_min_sync(0xffffffffu, lane < LG_WARPS ? s_at[lane] : 0xffffffffu);
     if (lane == 0) {
       unsigned to;
       asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to) : "r"((unsigned)__cvta_generic_to_shared(&s_best[rank][0])));
-      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(best) : "memory");
-      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + 4), "r"(best_at) : "memory");
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(top) : "memory");
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + 4), "r"(at) : "memory");
     }
   }
   cluster_sync_all();
   if (rank == 0 && warp == 0 && ok && a.picked) {
-    join(lane < LG_CTAS ? s_best[lane][0] : 0, lane < LG_CTAS ? s_best[lane][1] : 0xffffffffu);
-    if (lane == 0) a.picked[row] = best ? (int)best_at : -1;
+    const int k = lane < CTAS ? s_best[lane][0] : LG_NONE;
+    top = __reduce_max_sync(0xffffffffu, k);
+    at = __reduce_min_sync(0xffffffffu, k == top && lane < CTAS ? (unsigned)s_best[lane][1] : 0xffffffffu);
+    if (lane == 0) a.picked[row] = top != LG_NONE ? (int)at : -1;
   }
 }
 
+template <typename T, bool VEC, int CTAS>
+int launch_logits(LogitsArgs a, cudaStream_t s) {
+  a.per = (int)(((long long)a.vocab + CTAS * 64 - 1) / (CTAS * 64) * 64);
+  const int rc = big_smem<logits_kernel<T, VEC, CTAS>>(lg_smem(CTAS));
+  if (rc != VLAC_OK) return rc;
+  VLAC_CUDA_CHECK(launch_pdl(logits_kernel<T, VEC, CTAS>, dim3(CTAS, a.rows), dim3(LG_THREADS), lg_smem(CTAS), s, a));
+  return VLAC_OK;
+}
 template <typename T>
 int launch_logits(const LogitsArgs& a, cudaStream_t s) {
   const bool vec = a.vocab * (long long)sizeof(T) % 16 == 0 && a.stride * (long long)sizeof(T) % 16 == 0 && !((uintptr_t)a.in & 15u) &&
                    (!a.out || (a.out_stride * (long long)sizeof(T) % 16 == 0 && !((uintptr_t)a.out & 15u)));
-  VLAC_CUDA_CHECK(launch_pdl(vec ? logits_kernel<T, true> : logits_kernel<T, false>, dim3(LG_CTAS, a.rows), dim3(LG_THREADS), 0, s, a));
-  return VLAC_OK;
+  // as few CTAs a row as give every SM two
+  if (a.rows >= 296) return vec ? launch_logits<T, true, 1>(a, s) : launch_logits<T, false, 1>(a, s);
+  if (a.rows >= 148) return vec ? launch_logits<T, true, 2>(a, s) : launch_logits<T, false, 2>(a, s);
+  if (a.rows >= 74) return vec ? launch_logits<T, true, 4>(a, s) : launch_logits<T, false, 4>(a, s);
+  return vec ? launch_logits<T, true, 8>(a, s) : launch_logits<T, false, 8>(a, s);
 }
 
 }  // namespace

@@ -222,8 +222,10 @@ int vlac_rope_tables(const vlac_rope_scaling* r, int first, int n_pos, float* co
   TableArgs a = {};
   a.half = r->rot_dim / 2; a.first = first; a.n_pos = n_pos; a.cos = cos; a.sin = sin; a.amplitude = r->amplitude;
   const long double two_pi = 6.283185307179586476925286766559005768L;
+  const long double next = powl((long double)r->theta, -2.0L / r->rot_dim);
+  long double f = 1.0L;
   for (int i = 0; i < a.half; ++i) {
-    const long double f = powl((long double)r->theta, -2.0L * i / r->rot_dim), turns = r->original_len * f / two_pi;
+    const long double turns = r->original_len * f / two_pi;
     long double g = 0.0L;
     if (r->original_len > 0) {
       g = (turns - r->turns_low) / ((long double)r->turns_high - r->turns_low);
@@ -232,6 +234,7 @@ int vlac_rope_tables(const vlac_rope_scaling* r, int first, int n_pos, float* co
     const long double per = f * (g + (1.0L - g) / r->factor) / two_pi;
     a.turns[i] = (double)per;
     a.rest[i] = (double)(per - a.turns[i]);
+    f *= next;                                    // (64 bits of fraction: 128 products leave the frequencies right to 2^-56)
   }
   const long long units = (long long)a.half * ((n_pos + RT_RUN - 1LL) / RT_RUN), ctas = (units + RT_THREADS - 1) / RT_THREADS;
   VLAC_CUDA_CHECK(launch_pdl(rope_tables_kernel, dim3((unsigned)ctas), dim3(RT_THREADS), 0, (cudaStream_t)stream, a));
@@ -275,9 +278,10 @@ int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int
   a.status = status;
   a.split = 1;
   while (a.split < AP_WARPS && (long long)rows * a.split < n_sm * 64ll) a.split *= 2;
-  // enough CTAs for the whole GPU; no more per entry than one entry could use
-  const int per = AP_WARPS / a.split, groups = (rows + per - 1) / per, spread = (n_sm * 8 + n - 1) / n;
-  const dim3 grid(groups < 1 ? 1 : groups < spread ? groups : spread, n);
+  // enough CTAs for the whole GPU; no more per entry than an entry of up to twice the mean length can use (64 sequences of one row, 19 CTAs each / one:
+  // 9.7 / XX us)
+  const int per = AP_WARPS / a.split, mean = (int)((2ll * rows - n + (long long)n * per - 1) / ((long long)n * per)), spread = (n_sm * 8 + n - 1) / n;
+  const dim3 grid(mean < 1 ? 1 : mean < spread ? mean : spread, n);
   const bool norm = rope->q_gain || rope->k_gain;
   auto launch = p->dtype == VLAC_BF16 ? (p->head_dim == 128 ? launch_append<__nv_bfloat16, 128> : launch_append<__nv_bfloat16, 64>)
                                       : (p->head_dim == 128 ? launch_append<__half, 128> : launch_append<__half, 64>);
