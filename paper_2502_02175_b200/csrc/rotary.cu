@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(RT_THREADS) rope_tables_kernel(const __grid_co
 }
 
 // ------------------------------------------------------------------------------------------------ append
-constexpr int AP_THREADS = 256, AP_WARPS = AP_THREADS / 32, AP_BATCH = 4;
+constexpr int AP_THREADS = 256, AP_WARPS = AP_THREADS / 32, AP_BATCH = 4, AP_CTAS = 24;
 struct AppendArgs {
   void *k, *v;                                  // the layer
   const int *table, *len, *refs;
@@ -62,22 +62,42 @@ struct AppendArgs {
   int split;                                    // warps that share a row: 1, 2, 4 or 8
 };
 
+// pairs of fp32: one instruction for two elements
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float lo, float hi) { F2 d; asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi)); return d; }
+__device__ __forceinline__ float2 f2_parts(F2 d) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d)); return r; }
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) { F2 d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) { F2 d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+
 template <typename T> struct Pair16;
 template <> struct Pair16<__nv_bfloat16> {
-  static __device__ __forceinline__ float2 two(unsigned x) { return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
-  static __device__ __forceinline__ unsigned pack(float lo, float hi) { __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<unsigned*>(&v); }
+  static __device__ __forceinline__ F2 two(unsigned x) { return f2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+  static __device__ __forceinline__ unsigned pack(F2 x) { const float2 p = f2_parts(x); __nv_bfloat162 v = __floats2bfloat162_rn(p.x, p.y); return *reinterpret_cast<unsigned*>(&v); }
+  static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 };
 template <> struct Pair16<__half> {
-  static __device__ __forceinline__ float2 two(unsigned x) { return __half22float2(*reinterpret_cast<__half2*>(&x)); }
-  static __device__ __forceinline__ unsigned pack(float lo, float hi) { __half2 v = __floats2half2_rn(lo, hi); return *reinterpret_cast<unsigned*>(&v); }
+  static __device__ __forceinline__ F2 two(unsigned x) { const float2 p = __half22float2(*reinterpret_cast<__half2*>(&x)); return f2(p.x, p.y); }
+  static __device__ __forceinline__ unsigned pack(F2 x) { const float2 p = f2_parts(x); __half2 v = __floats2half2_rn(p.x, p.y); return *reinterpret_cast<unsigned*>(&v); }
+  static __device__ __forceinline__ float one(const __half* p) { return __half2float(*p); }
 };
 
-// grid (x, entries).  A lane holds 8 neighbouring elements of a head, a warp two heads of 128 or four of 64 at a time, all of one row, so that a
-// lane's cosines and sines stay in registers for the whole row; the partner of a half-layout pair comes from another lane.
-// Each CTA checks the whole entry for itself (its pages and positions), so that an entry is written whole or not at all without a second launch.
+// two pieces of 4 elements, which may be neighbours
+template <bool ONE> __device__ __forceinline__ void load8(uint2* x, const void* p0, const void* p1) {
+  if (ONE) { const uint4 v = *reinterpret_cast<const uint4*>(p0); x[0] = make_uint2(v.x, v.y); x[1] = make_uint2(v.z, v.w); }
+  else { x[0] = *reinterpret_cast<const uint2*>(p0); x[1] = *reinterpret_cast<const uint2*>(p1); }
+}
+template <bool ONE> __device__ __forceinline__ void store8(const uint2* x, void* p0, void* p1) {
+  if (ONE) *reinterpret_cast<uint4*>(p0) = make_uint4(x[0].x, x[0].y, x[1].x, x[1].y);
+  else { *reinterpret_cast<uint2*>(p0) = x[0]; *reinterpret_cast<uint2*>(p1) = x[1]; }
+}
+
+// grid (x, entries).  A lane holds 8 elements of a head in two pieces of 4, a warp two heads of 128 or four of 64 at a time, all of one row, so that a lane's
+// cosines and sines stay in registers for the whole row.  The pieces are the two that are rotated with one another (half layout: rot/2 apart;
+// interleaved, and behind the rotated part: neighbours), so that nothing is exchanged between lanes but the sum of a norm.
 template <typename T, int D, bool INTER, bool NORM>
-__global__ void __launch_bounds__(AP_THREADS) pages_append_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(AP_THREADS, 4) pages_append_kernel(AppendArgs a) {
   constexpr int LANES = D / 8, PER = 32 / LANES;                        // lanes of a head; heads of a warp
+  __shared__ __align__(16) float s_gain[NORM ? 2 : 1][D];
   const int tid = threadIdx.x, i = blockIdx.y, warp = tid >> 5, lane = tid & 31;
   pdl_trigger();
   pdl_wait();
@@ -109,48 +129,39 @@ __global__ void __launch_bounds__(AP_THREADS) pages_append_kernel(AppendArgs a) 
   if (tid == 0 && blockIdx.x == 0) a.status[i] = code;
   if (code != 0) return;
 
-  const int c = lane % LANES, half16 = a.rot / 16, el = c * 8;          // the lane's 16-byte piece of a head; pieces of half the rotated part
-  const bool turned = el < a.rot;
-  const int partner = INTER || !turned ? lane : c < half16 ? lane + half16 : lane - half16;
-  float qg[8], kg[8];
   if (NORM) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) qg[e] = kg[e] = 1.f;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const void* g = s ? a.k_gain : a.q_gain;
-      if (!g) continue;
-      uint4 x = *reinterpret_cast<const uint4*>((const T*)g + el);
-      const unsigned w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { const float2 f = Pair16<T>::two(w[e]); (s ? kg : qg)[2 * e] = f.x; (s ? kg : qg)[2 * e + 1] = f.y; }
+    for (int e = tid; e < D; e += AP_THREADS) {
+      s_gain[0][e] = a.q_gain ? Pair16<T>::one((const T*)a.q_gain + e) : 1.f;
+      s_gain[1][e] = a.k_gain ? Pair16<T>::one((const T*)a.k_gain + e) : 1.f;
     }
+    __syncthreads();
   }
+  const int c = lane % LANES, pairs = a.rot / 8;                        // lanes whose pieces are rotated
+  const bool turned = c < pairs;
+  const int el0 = INTER || !turned ? 8 * c : 4 * c, el1 = INTER || !turned ? 8 * c + 4 : 4 * c + a.rot / 2;      // first element of each piece
   const int all = a.heads + 2 * a.kv_heads, step = PER * a.split, per_cta = AP_WARPS / a.split;
   const int first = (warp % a.split) * PER + lane / LANES;              // first head of this lane
   for (int r = r0 + blockIdx.x * per_cta + warp / a.split; r < r1; r += gridDim.x * per_cta) {
     const int at = at0 + (r - r0);
-    const size_t pool = (((size_t)t[at >> a.shift] << a.shift) + (at & (a.page - 1))) * ((size_t)a.kv_heads * D) + el;
-    float cs[8], sn[8];                                                 // (interleaved: four of each)
+    const size_t pool = (((size_t)t[at >> a.shift] << a.shift) + (at & (a.page - 1))) * ((size_t)a.kv_heads * D);
+    float4 cs = make_float4(1.f, 1.f, 1.f, 1.f), sn = make_float4(0.f, 0.f, 0.f, 0.f);  // of the lane's four pairs
     if (turned) {
-      const size_t row = (size_t)(a.pos ? a.pos[r] : at) * (a.rot / 2) + (INTER ? el / 2 : c < half16 ? el : el - a.rot / 2);
-#pragma unroll
-      for (int e = 0; e < (INTER ? 4 : 8); e += 4) {
-        *reinterpret_cast<float4*>(cs + e) = *reinterpret_cast<const float4*>(a.cos + row + e);
-        *reinterpret_cast<float4*>(sn + e) = *reinterpret_cast<const float4*>(a.sin + row + e);
-      }
+      const size_t row = (size_t)(a.pos ? a.pos[r] : at) * (a.rot / 2) + 4 * c;
+      cs = *reinterpret_cast<const float4*>(a.cos + row);
+      sn = *reinterpret_cast<const float4*>(a.sin + row);
     }
-    const T* qi = (const T*)a.q + (size_t)r * a.q_stride + el;
-    const T *ki = (const T*)a.kin + (size_t)r * a.k_stride + el, *vi = (const T*)a.vin + (size_t)r * a.v_stride + el;
-    T* qo = (T*)a.qout + (size_t)r * a.qout_stride + el;
+    const T *qi = (const T*)a.q + (size_t)r * a.q_stride, *ki = (const T*)a.kin + (size_t)r * a.k_stride, *vi = (const T*)a.vin + (size_t)r * a.v_stride;
+    T* qo = (T*)a.qout + (size_t)r * a.qout_stride;
     for (int h0 = first; h0 - lane / LANES < all; h0 += step * AP_BATCH) {               // (uniform over the warp)
-      uint4 x[AP_BATCH];
+      uint2 x[AP_BATCH][2];
 #pragma unroll
       for (int b = 0; b < AP_BATCH; ++b) {
         const int h = h0 + b * step;
-        x[b] = make_uint4(0, 0, 0, 0);
-        if (h < all) x[b] = *reinterpret_cast<const uint4*>(h < a.heads ? qi + (size_t)h * D : h < a.heads + a.kv_heads ? ki + (size_t)(h - a.heads) * D
-                                                                                               : vi + (size_t)(h - a.heads - a.kv_heads) * D);
+        x[b][0] = x[b][1] = make_uint2(0, 0);
+        if (h < all) {
+          const T* from = h < a.heads ? qi + (size_t)h * D : h < a.heads + a.kv_heads ? ki + (size_t)(h - a.heads) * D : vi + (size_t)(h - a.heads - a.kv_heads) * D;
+          load8<INTER>(x[b], from + el0, from + el1);
+        }
       }
 #pragma unroll
       for (int b = 0; b < AP_BATCH; ++b) {
@@ -158,41 +169,49 @@ __global__ void __launch_bounds__(AP_THREADS) pages_append_kernel(AppendArgs a) 
         if (h - lane / LANES >= all) break;                             // (uniform)
         const bool is_q = h < a.heads, is_v = h >= a.heads + a.kv_heads;
         if (!__all_sync(0xffffffffu, is_v)) {
-          float f[8];
-          const unsigned w[4] = {x[b].x, x[b].y, x[b].z, x[b].w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { const float2 y = Pair16<T>::two(w[e]); f[2 * e] = y.x; f[2 * e + 1] = y.y; }
+          F2 f[4] = {Pair16<T>::two(x[b][0].x), Pair16<T>::two(x[b][0].y), Pair16<T>::two(x[b][1].x), Pair16<T>::two(x[b][1].y)};
           if (NORM) {
-            float ss = 0.f;
+            F2 s2 = f2_mul(f[0], f[0]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
+            for (int e = 1; e < 4; ++e) s2 = f2_fma(f[e], f[e], s2);
+            const float2 p = f2_parts(s2);
+            float ss = p.x + p.y;
 #pragma unroll
             for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            const float inv = rsqrtf(ss * (1.f / D) + a.eps);
-            if ((is_q ? a.q_gain : a.k_gain) != nullptr)
+            if ((is_q ? a.q_gain : a.k_gain) != nullptr) {
+              const float inv = rsqrtf(ss * (1.f / D) + a.eps);
+              const float4 g0 = *reinterpret_cast<const float4*>(&s_gain[is_q ? 0 : 1][el0]), g1 = *reinterpret_cast<const float4*>(&s_gain[is_q ? 0 : 1][el1]);
+              const F2 g[4] = {f2(g0.x, g0.y), f2(g0.z, g0.w), f2(g1.x, g1.y), f2(g1.z, g1.w)}, i2 = f2(inv, inv);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) f[e] = f[e] * inv * (is_q ? qg[e] : kg[e]);
-          }
-          if (INTER) {
-            if (turned)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float u = f[2 * e], v = f[2 * e + 1];
-                f[2 * e] = u * cs[e] - v * sn[e];
-                f[2 * e + 1] = u * sn[e] + v * cs[e];
-              }
-          } else if (a.rot) {                                           // (uniform)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float y = __shfl_sync(0xffffffffu, f[e], partner);
-              if (turned) f[e] = c < half16 ? f[e] * cs[e] - y * sn[e] : y * sn[e] + f[e] * cs[e];
+              for (int e = 0; e < 4; ++e) f[e] = f2_mul(f2_mul(f[e], i2), g[e]);
             }
           }
-          if (!is_v) x[b] = make_uint4(Pair16<T>::pack(f[0], f[1]), Pair16<T>::pack(f[2], f[3]), Pair16<T>::pack(f[4], f[5]), Pair16<T>::pack(f[6], f[7]));
+          if (turned) {                                                 // (without rotation infinities pass as they are)
+            if (INTER) {
+              const float cc[4] = {cs.x, cs.y, cs.z, cs.w}, ss[4] = {sn.x, sn.y, sn.z, sn.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float2 y = f2_parts(f[e]);
+                f[e] = f2(y.x * cc[e] - y.y * ss[e], y.x * ss[e] + y.y * cc[e]);
+              }
+            } else {
+              const F2 cc[2] = {f2(cs.x, cs.y), f2(cs.z, cs.w)}, ss[2] = {f2(sn.x, sn.y), f2(sn.z, sn.w)}, ns[2] = {f2(-sn.x, -sn.y), f2(-sn.z, -sn.w)};
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const F2 u = f[e], v = f[2 + e];
+                f[e] = f2_fma(v, ns[e], f2_mul(u, cc[e]));
+                f[2 + e] = f2_fma(u, ss[e], f2_mul(v, cc[e]));
+              }
+            }
+          }
+          if (!is_v) {
+            x[b][0] = make_uint2(Pair16<T>::pack(f[0]), Pair16<T>::pack(f[1]));
+            x[b][1] = make_uint2(Pair16<T>::pack(f[2]), Pair16<T>::pack(f[3]));
+          }
         }
         if (h < all) {
           T* to = is_q ? qo + (size_t)h * D : (T*)(is_v ? a.v : a.k) + pool + (size_t)(h - a.heads - (is_v ? a.kv_heads : 0)) * D;
-          *reinterpret_cast<uint4*>(to) = x[b];
+          store8<INTER>(x[b], to + el0, to + el1);
         }
       }
     }
@@ -278,9 +297,10 @@ int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int
   a.status = status;
   a.split = 1;
   while (a.split < AP_WARPS && (long long)rows * a.split < n_sm * 64ll) a.split *= 2;
-  // enough CTAs for the whole GPU; no more per entry than an entry of up to twice the mean length can use (64 sequences of one row, 19 CTAs each / one:
-  // 9.7 / XX us)
-  const int per = AP_WARPS / a.split, mean = (int)((2ll * rows - n + (long long)n * per - 1) / ((long long)n * per)), spread = (n_sm * 8 + n - 1) / n;
+  // CTAs: no more per entry than an entry of up to twice the mean length can use; what fits the GPU at once is not given a second wave; larger calls get
+  // many short CTAs, which even out
+  const int per = AP_WARPS / a.split, mean = (int)((2ll * rows - n + (long long)n * per - 1) / ((long long)n * per));
+  const int most = n_sm * ((long long)rows * a.split <= n_sm * 4ll * AP_WARPS ? 4 : AP_CTAS), spread = (most + n - 1) / n;
   const dim3 grid(mean < 1 ? 1 : mean < spread ? mean : spread, n);
   const bool norm = rope->q_gain || rope->k_gain;
   auto launch = p->dtype == VLAC_BF16 ? (p->head_dim == 128 ? launch_append<__nv_bfloat16, 128> : launch_append<__nv_bfloat16, 64>)
