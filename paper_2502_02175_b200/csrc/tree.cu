@@ -17,24 +17,25 @@ struct TreeArgs {
   int *pos, *entry, *status;
 };
 
-// What an entry says, and its code as far as it does not depend on its rows or on other entries.
-__device__ __forceinline__ int tree_entry(const TreeArgs& a, int i, int* q0, int* q1, int* len) {
-  *q0 = a.q_ptr[i]; *q1 = a.q_ptr[i + 1];
-  *len = INT_MAX;
-  int code = VLAC_OK;
-  if (a.len) {
-    const int slot = a.seqs[i];
-    if ((unsigned)slot >= (unsigned)a.n_slots) code = VLAC_ERR_INVALID_ARG;
-    else {
-      *len = a.len[slot];
-      if (*len < 0 || *len > a.most) code = VLAC_ERR_BAD_STATE;
-    }
-    if (code != VLAC_OK) *len = -1;
+// What an entry says.  Its rows can be read as soon as q0 and q1 are known to be sound, before the slot's length is there: one chain of reads less.
+struct TreeEntry {
+  int q0, q1, slot, nq;                         // nq: 0 where the rows cannot be read
+  __device__ __forceinline__ TreeEntry(const TreeArgs& a, int i) {
+    q0 = a.q_ptr[i]; q1 = a.q_ptr[i + 1]; slot = a.len ? a.seqs[i] : 0;
+    nq = q0 >= 0 && q1 >= q0 && q1 <= a.rows && q1 - q0 <= a.max_rows ? q1 - q0 : 0;
   }
-  if (code == VLAC_OK && (*q0 < 0 || *q1 > a.rows || *q1 < *q0 || *q1 - *q0 > *len)) code = VLAC_ERR_INVALID_ARG;
-  if (code == VLAC_OK && *q1 - *q0 > a.max_rows) code = VLAC_ERR_TOO_LARGE;
-  return code;
-}
+  // The code as far as it does not depend on the rows or on other entries; the slot's length, -1 where there is none.
+  __device__ __forceinline__ int code(const TreeArgs& a, int* len) const {
+    *len = INT_MAX;
+    if (a.len) {
+      *len = (unsigned)slot < (unsigned)a.n_slots ? a.len[slot] : -1;
+      if ((unsigned)slot >= (unsigned)a.n_slots) return VLAC_ERR_INVALID_ARG;
+      if (*len < 0 || *len > a.most) { *len = -1; return VLAC_ERR_BAD_STATE; }
+    }
+    if (q0 < 0 || q1 > a.rows || q1 < q0 || q1 - q0 > *len) return VLAC_ERR_INVALID_ARG;
+    return q1 - q0 > a.max_rows ? VLAC_ERR_TOO_LARGE : VLAC_OK;
+  }
+};
 
 __device__ __forceinline__ void tree_blank(const TreeArgs& a, int from, int to) {
   for (int r = from + threadIdx.x; r < to; r += TP_THREADS) { a.pos[r] = -1; a.entry[r] = -1; }
@@ -49,32 +50,30 @@ __global__ void __launch_bounds__(TP_THREADS) tree_plan_kernel(TreeArgs a) {
   pdl_trigger();
   pdl_wait();
   int broken = 0;
-  for (int j = tid; j < a.n; j += TP_THREADS) broken |= a.q_ptr[j + 1] < a.q_ptr[j];
-  broken = __syncthreads_or(broken);                                    // rows would overlap: all are refused
+  for (int j = tid; j < a.n; j += TP_THREADS) broken |= a.q_ptr[j + 1] < a.q_ptr[j];      // rows would overlap: all are refused
   if (i == a.n) {
-    const int first = broken ? a.rows : min(max(a.q_ptr[0], 0), a.rows), last = broken ? a.rows : min(max(a.q_ptr[a.n], 0), a.rows);
+    const int q_first = a.q_ptr[0], q_last = a.q_ptr[a.n];
+    broken = __syncthreads_or(broken);
+    const int first = broken ? a.rows : min(max(q_first, 0), a.rows), last = broken ? a.rows : min(max(q_last, 0), a.rows);
     tree_blank(a, 0, first);
     tree_blank(a, last, a.rows);
     return;
   }
-  if (broken) {
-    if (tid == 0) a.status[i] = VLAC_ERR_INVALID_ARG;
-    return;
+  const TreeEntry e(a, i);
+  const int q0 = e.q0, nq = e.nq;
+  int bad = 0, len;
+  for (int j = tid; j < nq; j += TP_THREADS) {
+    const int p = a.parent[q0 + j];
+    s_parent[j] = p;
+    bad |= p < -1 || p >= j;
   }
-  int q0, q1, len;
-  int code = tree_entry(a, i, &q0, &q1, &len);
-  const int nq = code == VLAC_OK ? q1 - q0 : 0;
-  int bad = 0;
-  if (code == VLAC_OK)
-    for (int j = tid; j < nq; j += TP_THREADS) {
-      const int p = a.parent[q0 + j];
-      s_parent[j] = p;
-      bad |= p < -1 || p >= j;
-    }
-  if (__syncthreads_or(bad)) code = VLAC_ERR_INVALID_ARG;
+  int code = e.code(a, &len);
+  broken = __syncthreads_or(broken);
+  if (__syncthreads_or(bad) && code == VLAC_OK) code = VLAC_ERR_INVALID_ARG;
+  if (broken) code = VLAC_ERR_INVALID_ARG;
   if (tid == 0) a.status[i] = code;
   if (code != VLAC_OK) {
-    tree_blank(a, min(max(q0, 0), a.rows), min(max(q1, 0), a.rows));
+    if (!broken) tree_blank(a, min(max(q0, 0), a.rows), min(max(e.q1, 0), a.rows));
     return;
   }
   for (int j = tid; j < nq; j += TP_THREADS) {
@@ -116,22 +115,20 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(TA_THREADS, 1) tr
   const int broken = __syncthreads_or(tid < t.n && t.q_ptr[min(tid, t.n - 1) + 1] < t.q_ptr[min(tid, t.n - 1)]);
   int* const next = ta_next + warp * t.max_rows;
   for (int i = warp * CTAS + rank; i < t.n; i += TA_WARPS * CTAS) {
-    int q0, q1, len;
-    int code = tree_entry(t, i, &q0, &q1, &len);
-    if (broken) code = VLAC_ERR_INVALID_ARG;
-    const int nq = code == VLAC_OK ? q1 - q0 : 0;
-    if (code == VLAC_OK) {
-      for (int j = lane; j < nq; j += 32) next[j] = INT_MAX;
-      __syncwarp();
-      bool bad = false;
-      for (int j = lane; j < nq; j += 32) {
-        const int p = t.parent[q0 + j];
-        bad |= p < -1 || p >= j;
-        if (p >= 0 && p < j && a.drafted[q0 + j] == a.chosen[q0 + p]) atomicMin(&next[p], j);
-      }
-      if (__any_sync(0xffffffffu, bad)) code = VLAC_ERR_INVALID_ARG;
-      __syncwarp();
+    const TreeEntry e(t, i);
+    const int q0 = e.q0, q1 = e.q1, nq = e.nq;
+    for (int j = lane; j < nq; j += 32) next[j] = INT_MAX;
+    __syncwarp();
+    bool bad = false;
+    for (int j = lane; j < nq; j += 32) {
+      const int p = t.parent[q0 + j], d = a.drafted[q0 + j];
+      bad |= p < -1 || p >= j;
+      if (p >= 0 && p < j && d == a.chosen[q0 + p]) atomicMin(&next[p], j);
     }
+    int len, code = e.code(t, &len);
+    if (broken) code = VLAC_ERR_INVALID_ARG;
+    if (__any_sync(0xffffffffu, bad) && code == VLAC_OK) code = VLAC_ERR_INVALID_ARG;
+    __syncwarp();
     int count = 0;
     if (code == VLAC_OK) {
       int cur = nq > 0 ? 0 : INT_MAX;
