@@ -426,7 +426,8 @@ int vlac_selftest_prefix_wait(const vlac_pages* p, int layer, const vlac_prefix*
  * factor stretches the positions (1: none): all frequencies alike with original_len = 0, otherwise only those that turn seldom over the
  * length that the weights were trained for (the interpolation by parts of the YaRN paper, arXiv 2309.00071, whose attention temperature is the
  * amplitude).
- *   rot_dim  even, 2..256;  theta > 0, factor > 0, original_len >= 0, amplitude finite; turns_low < turns_high where original_len > 0
+ *   rot_dim  even, 2..256;  theta > 0, factor > 0, original_len >= 0, amplitude finite; turns_low < turns_high where original_len > 0; no frequency
+ *            of 65536 turns a position or more (an angle is right to its own size times 2^-63)
  *   first >= 0, n_pos >= 0, first + n_pos <= 2^31 - 1;  cos, sin  device fp32 [n_pos][rot_dim/2] */
 typedef struct {
   int rot_dim;
@@ -450,10 +451,10 @@ typedef struct {
 /* vlac_pages_write with the norm and rotation of `rope` on the way, for the queries of the same rows too: row r of q goes to row r of
  * q_out, row r of k_rows and v_rows (v as it is) into the pool.
  *   pos    device int32 [rows], the position that row r is rotated to, or NULL: the position it is written to.  An entry with a
- *          position outside [0, n_pos) is refused (INVALID_ARG)
+ *          position outside [0, n_pos) is refused (INVALID_ARG); without rotation positions are not looked at
  *   q      n_heads heads of head_dim a row (n_heads = 0: none, q and q_out are not looked at); strides and alignment as k_rows.  q_out may be q
- *          itself (same stride); no other row of q_out shares memory with rows of q, k_rows or v_rows (INVALID_ARG)
- * Other arguments, codes and refusals as vlac_pages_write; rows of refused entries and rows behind row_ptr[n] stay as they were, in q_out too. */
+ *          itself (same stride); no other row of q_out shares memory with rows of q, k_rows or v_rows (INVALID_ARG), nor with the pool
+ * A row_ptr that falls refuses all.  Other arguments, codes and refusals as vlac_pages_write; rows of refused entries and rows behind row_ptr[n] stay as they were, in q_out too. */
 int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int* start, const int* row_ptr, int n, int rows, const vlac_rope* rope,
                       const int* pos, int n_heads, const void* q, long long q_stride, void* q_out, long long q_out_stride, const void* k_rows,
                       long long k_stride, const void* v_rows, long long v_stride, int* status, void* stream);
@@ -488,7 +489,8 @@ int vlac_tree_attention(const vlac_pages* p, int layer, const vlac_prefix* plan,
  *   x = x - frequency[r] * made;  if made: x = x - presence[r];  x = x + bias of t;  x = -infinity where t is not allowed
  * out[r][t] is x in the type of the logits; picked[r] the lowest index of the largest x (before that rounding) among the allowed tokens, a NaN
  * counting as the largest; -1 if none is allowed.
- *   tokens      device int32 [n_tokens]; numbers outside the vocabulary are passed over (padding).  Spans of rows may overlap
+ *   tokens      device int32 [n_tokens] (up to 2^30, n_bias too).  Spans of rows may overlap.  Here, in bias_token and in drafted, numbers outside the
+ *               vocabulary are passed over (padding)
  *   span        device int32 [rows][3], or NULL: no history
  *   repetition, frequency, presence   device fp32 [rows], each or NULL (not applied)
  *   bias        entries bias_ptr[r] .. bias_ptr[r+1] of bias_token, bias (int32 [rows + 1], int32 / fp32 [n_bias]) for row r; of several for a token
@@ -514,7 +516,7 @@ int vlac_logits_adjust(int rows, int vocab, int dtype, const void* logits, long 
                        long long out_stride, int* picked, int* status, void* stream);
 
 /* The path of each tree that the decoder confirms: from the entry's first row on, to the first child whose drafted token is the token chosen at the
- * row (drafted, chosen  device int32 [rows]).
+ * row (drafted, chosen  device int32 [rows]; a negative number is no token and confirms nothing).
  *   count   [n]: rows on the path (0 for an empty or refused entry);  path  [rows]: the path's rows within the entry from q_ptr[i] on, -1 behind;
  *   tokens  [rows]: the tokens chosen at them (the last is new), -1 behind
  *   keep_ptr [n + 1], keep [n_keep]: the positions of slot seqs[i] that stay, for vlac_pages_compact (the rows in front of the tree, then the path;

@@ -721,8 +721,8 @@ def vlac_logits_adjust(logits: torch.Tensor, rules: LogitsRules, out: Optional[t
     each row into ``picked`` (int32, ``None``: not wanted)."""
     dev, shape = logits.get_device(), (rules.rows, rules.vocab)
     stream = _here(dev)
-    assert rules.index in (None, dev) and logits.shape == shape and logits.stride(1) == 1
-    assert out is None or (out.dtype is logits.dtype and out.get_device() == dev and out.shape == shape and out.stride(1) == 1)
+    assert rules.index in (None, dev) and logits.shape == shape and (shape[1] == 1 or logits.stride(1) == 1)
+    assert out is None or (out.dtype is logits.dtype and out.get_device() == dev and out.shape == shape and (shape[1] == 1 or out.stride(1) == 1))
     wide = max(rules.vocab, 1)
     _check(lib.vlac_logits_adjust(shape[0], shape[1], _LOGITS_TYPES[logits.dtype], logits.data_ptr(), logits.stride(0) if shape[0] > 1 else wide, rules.ref, _ptr(out),
                                   0 if out is None else out.stride(0) if shape[0] > 1 else wide, None if picked is None else _ints(picked, shape[0], dev),

@@ -11,7 +11,6 @@
 
 namespace {
 
-constexpr int LG_THREADS = 256, LG_WARPS = LG_THREADS / 32;
 constexpr int LG_RUN = 131072;                  // tokens whose marks a CTA holds at once
 // Tokens whose counts a CTA holds: a run of at most as many by their place in it ("direct"), of a longer one the marked tokens by a hash.  Few rows: more, so
 // that an eighth of 32,000 tokens is direct; many: fewer, so that four CTAs fit an SM.
@@ -19,6 +18,7 @@ __host__ __device__ constexpr int lg_table(int ctas) { return ctas == 8 ? 4096 :
 constexpr int LG_TRIES = 64;                    // where a token finds no entry in as many tries, the run is cut into direct ones
 constexpr int LG_LOOK = 4;                      // tokens of the history that a thread asks for at once
 constexpr int LG_EACH = 2;                      // marked tokens that a thread has in flight
+constexpr int LG_SMS = 148;
 constexpr unsigned LG_SEEN = 0x80000000u;       // of a token's entry in the table: it was in the prompt; the other bits: how often it was generated
 __host__ __device__ constexpr int lg_smem(int ctas) { return LG_RUN / 8 + lg_table(ctas) * 14; }
 
@@ -120,11 +120,11 @@ template <typename T, bool VEC> struct Piece {
 };
 
 // CTAS share a row.  Few rows are shared by 8, so that there are enough CTAs; many by fewer, since every one of them goes through the row's lists.
-template <typename T, bool VEC, int CTAS>
-__global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, CTAS == 8 ? 3 : 4) logits_kernel(LogitsArgs a) {
+template <typename T, bool VEC, int CTAS, int LG_THREADS>
+__global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, LG_THREADS > 256 ? 1 : CTAS == 8 ? 3 : 4) logits_kernel(LogitsArgs a) {
   using P = Piece<T, VEC>;
   using L = Logit<T>;
-  constexpr int LG_TABLE = lg_table(CTAS);
+  constexpr int LG_TABLE = lg_table(CTAS), LG_WARPS = LG_THREADS / 32;
   constexpr int N = P::N, BATCH = VEC ? 2 : 8;  // pieces of a thread in flight
   extern __shared__ __align__(16) unsigned lg_raw[];
   unsigned* const s_mark = lg_raw;              // [LG_RUN / 32]
@@ -345,23 +345,26 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, CTAS 
   }
 }
 
-template <typename T, bool VEC, int CTAS>
-int launch_logits(LogitsArgs a, cudaStream_t s) {
+template <typename T, int CTAS, int THREADS>
+int launch_logits(LogitsArgs a, bool vec, cudaStream_t s) {
   a.per = (int)(((long long)a.vocab + CTAS * 64 - 1) / (CTAS * 64) * 64);
-  const int rc = big_smem<logits_kernel<T, VEC, CTAS>>(lg_smem(CTAS));
+  const int rc = vec ? big_smem<logits_kernel<T, true, CTAS, THREADS>>(lg_smem(CTAS)) : big_smem<logits_kernel<T, false, CTAS, THREADS>>(lg_smem(CTAS));
   if (rc != VLAC_OK) return rc;
-  VLAC_CUDA_CHECK(launch_pdl(logits_kernel<T, VEC, CTAS>, dim3(CTAS, a.rows), dim3(LG_THREADS), lg_smem(CTAS), s, a));
+  VLAC_CUDA_CHECK(launch_pdl(vec ? logits_kernel<T, true, CTAS, THREADS> : logits_kernel<T, false, CTAS, THREADS>, dim3(CTAS, a.rows), dim3(THREADS), lg_smem(CTAS), s, a));
   return VLAC_OK;
 }
 template <typename T>
 int launch_logits(const LogitsArgs& a, cudaStream_t s) {
   const bool vec = a.vocab * (long long)sizeof(T) % 16 == 0 && a.stride * (long long)sizeof(T) % 16 == 0 && !((uintptr_t)a.in & 15u) &&
                    (!a.out || (a.out_stride * (long long)sizeof(T) % 16 == 0 && !((uintptr_t)a.out & 15u)));
-  // as few CTAs a row as give every SM two
-  if (a.rows >= 296) return vec ? launch_logits<T, true, 1>(a, s) : launch_logits<T, false, 1>(a, s);
-  if (a.rows >= 148) return vec ? launch_logits<T, true, 2>(a, s) : launch_logits<T, false, 2>(a, s);
-  if (a.rows >= 74) return vec ? launch_logits<T, true, 4>(a, s) : launch_logits<T, false, 4>(a, s);
-  return vec ? launch_logits<T, true, 8>(a, s) : launch_logits<T, false, 8>(a, s);
+  // The GPU holds 3 CTAs with the large table an SM, 4 of the others.  As few a row as fill three quarters of its places, since each goes through the row's
+  // lists: 310 rows of 50,000 with histories of 3000, one / two a row 39 / 29 us; 512 of 128,000 81 / 81 (without lists 51 / 54); 140 of 50,000 in fp32,
+  // two / four 31 / 25; 60 of them, eight (a second wave) / four 24 / 19.  Where not every SM has one, CTAs of 512 threads (one row of 260,000 11.6 -> 9.6).
+  if (a.rows >= 3 * LG_SMS) return launch_logits<T, 1, 256>(a, vec, s);
+  if (a.rows >= 3 * LG_SMS / 2) return launch_logits<T, 2, 256>(a, vec, s);
+  if (a.rows > 3 * LG_SMS / 8) return launch_logits<T, 4, 256>(a, vec, s);
+  if (a.rows > LG_SMS / 8) return launch_logits<T, 8, 256>(a, vec, s);
+  return launch_logits<T, 8, 512>(a, vec, s);
 }
 
 }  // namespace
@@ -371,7 +374,7 @@ extern "C" int vlac_logits_adjust(int rows, int vocab, int dtype, const void* lo
   if (rows < 0 || vocab < 1 || vocab > 1 << 30 || (dtype != VLAC_FP32 && dtype != VLAC_BF16 && dtype != VLAC_FP16) || !rules) return VLAC_ERR_INVALID_ARG;
   if (rows > 65535) return VLAC_ERR_TOO_LARGE;
   const vlac_logits_rules& u = *rules;
-  if (u.n_tokens < 0 || u.n_bias < 0 || u.n_allow < 0 || (u.span && u.n_tokens > 0 && !u.tokens)) return VLAC_ERR_INVALID_ARG;
+  if (u.n_tokens < 0 || u.n_tokens > 1 << 30 || u.n_bias < 0 || u.n_bias > 1 << 30 || u.n_allow < 0 || (u.span && u.n_tokens > 0 && !u.tokens)) return VLAC_ERR_INVALID_ARG;
   if (u.bias_ptr && u.n_bias > 0 && (!u.bias_token || !u.bias)) return VLAC_ERR_INVALID_ARG;
   if (u.allow && !u.allow_row && u.n_allow < rows) return VLAC_ERR_INVALID_ARG;
   if ((u.tree == nullptr) != (u.drafted == nullptr)) return VLAC_ERR_INVALID_ARG;

@@ -49,7 +49,7 @@ constexpr int AP_THREADS = 256, AP_WARPS = AP_THREADS / 32, AP_BATCH = 4, AP_CTA
 struct AppendArgs {
   void *k, *v;                                  // the layer
   const int *table, *len, *refs;
-  int n_slots, max_pages, n_pages, page, shift, rows;
+  int n_slots, max_pages, n_pages, page, shift, n, rows;
   const int *seqs, *start, *row_ptr, *pos;
   int heads, kv_heads;
   const float *cos, *sin;
@@ -114,8 +114,9 @@ __global__ void __launch_bounds__(AP_THREADS, 4) pages_append_kernel(AppendArgs 
     }
   }
   // (uniform so far) an earlier entry with the same slot stands; positions have a row in the tables; pages exist and are the slot's own
-  int wrong = 0, bad = 0;
+  int wrong = 0, bad = 0, falls = 0;
   for (int j = tid; j < i; j += AP_THREADS) wrong |= a.seqs[j] == slot;
+  for (int j = tid; j < a.n; j += AP_THREADS) falls |= a.row_ptr[j + 1] < a.row_ptr[j];    // entries would share rows of q: all are refused
   const int* t = a.table + (size_t)(code == 0 ? slot : 0) * a.max_pages;
   if (code == 0 && r1 > r0) {
     for (int j = (at0 >> a.shift) + tid; j <= (at0 + r1 - r0 - 1) >> a.shift; j += AP_THREADS) {
@@ -126,6 +127,7 @@ __global__ void __launch_bounds__(AP_THREADS, 4) pages_append_kernel(AppendArgs 
   }
   if (__syncthreads_or(wrong)) code = VLAC_ERR_INVALID_ARG;
   if (__syncthreads_or(bad) && code == 0) code = VLAC_ERR_BAD_STATE;
+  if (__syncthreads_or(falls)) code = VLAC_ERR_INVALID_ARG;
   if (tid == 0 && blockIdx.x == 0) a.status[i] = code;
   if (code != 0) return;
 
@@ -251,6 +253,7 @@ int vlac_rope_tables(const vlac_rope_scaling* r, int first, int n_pos, float* co
       g = g < 0.0L ? 0.0L : g > 1.0L ? 1.0L : g;
     }
     const long double per = f * (g + (1.0L - g) / r->factor) / two_pi;
+    if (!(per < 65536.0L)) return VLAC_ERR_INVALID_ARG;
     a.turns[i] = (double)per;
     a.rest[i] = (double)(per - a.turns[i]);
     f *= next;                                    // (64 bits of fraction: 128 products leave the frequencies right to 2^-56)
@@ -291,7 +294,7 @@ int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int
   AppendArgs a = {};
   a.k = (unsigned short*)p->k + (size_t)layer * pages_layer(p); a.v = (unsigned short*)p->v + (size_t)layer * pages_layer(p);
   a.table = p->table; a.len = p->len; a.refs = p->refs; a.n_slots = p->n_slots; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.page = p->page_size;
-  a.shift = pages_shift(p->page_size); a.rows = rows; a.seqs = seqs; a.start = start; a.row_ptr = row_ptr; a.pos = pos; a.heads = n_heads; a.kv_heads = p->n_kv_heads;
+  a.shift = pages_shift(p->page_size); a.n = n; a.rows = rows; a.seqs = seqs; a.start = start; a.row_ptr = row_ptr; a.pos = pos; a.heads = n_heads; a.kv_heads = p->n_kv_heads;
   a.cos = rope->cos; a.sin = rope->sin; a.n_pos = rope->n_pos; a.rot = rope->rot_dim; a.q_gain = rope->q_gain; a.k_gain = rope->k_gain; a.eps = rope->eps;
   a.q = q; a.kin = k_rows; a.vin = v_rows; a.qout = q_out; a.q_stride = q_stride; a.qout_stride = q_out_stride; a.k_stride = k_stride; a.v_stride = v_stride;
   a.status = status;

@@ -123,7 +123,7 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(TA_THREADS, 1) tr
     for (int j = lane; j < nq; j += 32) {
       const int p = t.parent[q0 + j], d = a.drafted[q0 + j];
       bad |= p < -1 || p >= j;
-      if (p >= 0 && p < j && d == a.chosen[q0 + p]) atomicMin(&next[p], j);
+      if (p >= 0 && p < j && d >= 0 && d == a.chosen[q0 + p]) atomicMin(&next[p], j);
     }
     int len, code = e.code(t, &len);
     if (broken) code = VLAC_ERR_INVALID_ARG;

@@ -102,7 +102,7 @@ def accept(parent, drafted, chosen):
     got = [0] if len(parent) else []
     while got:
         r = got[-1]
-        nxt = [c for c in range(r + 1, len(parent)) if parent[c] == r and drafted[c] == chosen[r]]
+        nxt = [c for c in range(r + 1, len(parent)) if parent[c] == r and drafted[c] == chosen[r] and chosen[r] >= 0]
         if not nxt:
             break
         got.append(nxt[0])

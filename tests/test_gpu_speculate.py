@@ -180,6 +180,28 @@ def test_append_refusals_on_the_device(vb):
         a.check(q_out, before, pos=pos, skip=(bad,))
 
 
+def test_append_lists_that_fall(vb):
+    """A falling row_ptr would rotate rows twice: nothing is done; entries that run out of the rows, and none at all."""
+    a = Append(vb, [40, 33, 20], [9, 4, 5], 4, 2, 64, rot=64, seed=4)
+    before, ptr = (host(a.pages.k), host(a.pages.v)), a.ptr
+    for bad, want in (([0, 9, 4, 18], [-1] * 3), ([0, 2, 4, 19], None), ([-1, 2, 2, 2], None)):
+        a.ptr = np.array(bad)
+        q_out, st = a.run()
+        if want is None:
+            assert st.tolist()[0 if bad[0] < 0 else 2] == -1
+            q_out, st = a.run(seqs=[9, 9, 9])
+            assert set(st.tolist()) == {-1}
+        else:
+            assert st.tolist() == want and torch.equal(a.pages.k.double().cpu(), torch.from_numpy(before[0])) and torch.equal(a.pages.v.double().cpu(), torch.from_numpy(before[1]))
+        assert torch.all(q_out == 5)
+    st = ints(0)
+    vb.vlac_pages_append(a.pages, 0, dev([]), None, dev([0]), a.rope, None, a.q, a.q.clone(), a.k, a.v, st)
+    a.ptr, a.rows = ptr, 0
+    none, st = a.q[:0], ints(3)
+    vb.vlac_pages_append(a.pages, 0, dev(range(3)), None, dev([0] * 4), a.rope, None, none, none, a.k[:0], a.v[:0], st)
+    assert st.tolist() == [0, 0, 0]
+
+
 def test_append_far_pages_and_layers(vb):
     """Element offsets beyond 2^31 in K and V of the last layer, table rows beyond 2^31 bytes."""
     n_pages, kv, d = 5000, 16, 64
@@ -408,7 +430,7 @@ def test_accept(vb, nq, front):
     parents = [ref.random_tree(n, rng, 3) for n in nq]
     rows, lens = sum(nq), [a + b for a, b in zip(nq, front)]
     for likely in (1, 2, 1000):
-        drafted, chosen = rng.integers(0, likely, rows), rng.integers(0, likely, rows)
+        drafted, chosen = rng.integers(-1 if likely == 2 else 0, likely, rows), rng.integers(-1 if likely == 2 else 0, likely, rows)   # (-1: no token)
         got = accept(vb, nq, lens, parents, drafted, chosen, room=3)
         keep, r = [], 0
         assert got["status"] == [0] * len(nq) and got["keep_ptr"][0] == 0
@@ -568,6 +590,22 @@ def test_logits_long_history_and_many_rows(vb):
     for rows, vocab, hist, tree in ((300, 3000, 3000, [64] * 4 + [44]), (40, 150000, 5000, [40])):
         c = Logits(vb, rows, vocab, torch.bfloat16, seed=rows, hist=hist, bias=40, tree=tree)
         c.check(*c.run(), only=range(0, rows, 13))
+
+
+@pytest.mark.parametrize("rows,dtype", [(3, torch.float32), (20, torch.bfloat16), (60, torch.float16), (230, torch.bfloat16), (450, torch.bfloat16)])
+def test_logits_more_marks_than_the_table_holds(vb, rows, dtype):
+    """Histories of many different tokens, and of one token many times: tables overflow, runs are cut, counts are exact."""
+    vocab = 140000 if rows < 100 else 20000
+    c = Logits(vb, rows, vocab, dtype, seed=rows, hist=9000, bias=60, tree=[rows] if rows < 100 else [50] * (rows // 50) + ([rows % 50] if rows % 50 else []))
+    c.history[:] = np.random.default_rng(rows).integers(0, vocab, len(c.history))
+    c.history[5000:9000] = 77
+    c.kw["history"].copy_(dev(c.history))
+    c.span[:, 2] = np.minimum(c.span[:, 1] + 8000, 18000)
+    c.span[:, 0] = np.maximum(c.span[:, 1] - 6000, 0)
+    c.kw["span"].copy_(dev(c.span))
+    again = c.x.clone()
+    c.check(*c.run(x=again, out=again), only=range(0, rows, max(1, rows // 7)))
+    c.check(*c.run(), only=range(1, rows, max(1, rows // 5)))
 
 
 def test_logits_refused_rows(vb):

@@ -46,7 +46,7 @@ def test_impossible_pools(vb, over):
 def test_tables(vb):
     good = dict(rot_dim=64, theta=1e4, factor=1.0, original_len=0.0, turns_low=1.0, turns_high=32.0, amplitude=1.0)
     call = lambda first=0, n=4, cos=FAKE, sin=FAKE, **o: vb.lib.vlac_rope_tables(C.byref(vb.vlac_rope_scaling(**dict(good, **o))), first, n, cos, sin, None)  # noqa: E731
-    for bad in (dict(rot_dim=0), dict(rot_dim=3), dict(rot_dim=258), dict(theta=0.0), dict(theta=float("nan")), dict(theta=float("inf")), dict(factor=0.0), dict(factor=-1.0),
+    for bad in (dict(rot_dim=0), dict(rot_dim=3), dict(rot_dim=258), dict(theta=0.0), dict(theta=float("nan")), dict(theta=float("inf")), dict(theta=1e-30), dict(factor=1e-9), dict(factor=0.0), dict(factor=-1.0),
                 dict(original_len=-1.0), dict(original_len=float("inf")), dict(original_len=64.0, turns_low=2.0, turns_high=2.0), dict(amplitude=float("nan")), dict(first=-1), dict(n=-1),
                 dict(first=2 ** 31 - 2, n=3), dict(cos=None), dict(sin=None), dict(cos=FAKE + 2)):
         assert call(**bad) == INVALID, bad
@@ -100,7 +100,7 @@ def test_logits(vb):
     call.keep = {}
     for bad in (dict(rows=-1), dict(vocab=0), dict(vocab=2 ** 30 + 1, stride=2 ** 31), dict(dtype=3), dict(dtype=-1), dict(x=None), dict(x=FAKE + 2), dict(out=SIDE + 1), dict(stride=99),
                 dict(out_stride=99), dict(status=None), dict(picked=FAKE + 2), dict(status=FAKE + 1), dict(rules=False), dict(out=FAKE + 4), dict(out=FAKE, out_stride=101),
-                dict(span=FAKE, n_tokens=3), dict(n_tokens=-1), dict(n_bias=-1), dict(n_allow=-1), dict(bias_ptr=FAKE, n_bias=2, bias=FAKE), dict(bias_ptr=FAKE, n_bias=2, bias_token=FAKE),
+                dict(span=FAKE, n_tokens=3), dict(n_tokens=-1), dict(n_tokens=2 ** 30 + 1), dict(n_bias=-1), dict(n_bias=2 ** 30 + 1), dict(n_allow=-1), dict(bias_ptr=FAKE, n_bias=2, bias=FAKE), dict(bias_ptr=FAKE, n_bias=2, bias_token=FAKE),
                 dict(allow=FAKE, n_allow=3), dict(allow=FAKE + 2, n_allow=4), dict(span=FAKE + 1), dict(repetition=FAKE + 2), dict(tree=tree()), dict(drafted=FAKE),
                 dict(tree=tree(rows=5), drafted=FAKE), dict(tree=tree(n=1025), drafted=FAKE), dict(tree=tree(max_rows=0), drafted=FAKE), dict(tree=tree(mask=None), drafted=FAKE),
                 dict(tree=tree(entry=None), drafted=FAKE), dict(tree=tree(q_ptr=FAKE + 2), drafted=FAKE)):
@@ -113,7 +113,7 @@ def test_host_forms():
     """The references' own arithmetic, by hand."""
     assert ref.path([-1, 0, 0, 2, 1], 3) == [3, 2, 0]
     assert ref.accept([-1, 0, 0, 2, 2, 1], [0, 5, 6, 7, 8, 9], [6, 0, 8, 0, 1, 0]) == [0, 2, 4]
-    assert ref.accept([-1, 0, 0], [0, 5, 5], [5, 1, 1]) == [0, 1]
+    assert ref.accept([-1, 0, 0], [0, 5, 5], [5, 1, 1]) == [0, 1] and ref.accept([-1, 0], [0, -1], [-1, 0]) == [0]
     x, at = ref.logits(np.array([2.0, -2.0, 1.0, 4.0], np.float32), [0, 99], [1, 1], 2.0, 0.5, 0.25, [(2, 9.0), (2, 1.0)], np.array([1, 1, 1, 0], bool))
     assert x.tolist() == [1.0, -5.25, 2.0, -np.inf] and at == 2
     assert ref.logits(np.zeros(3, np.float32), [], [], 1, 0, 0, [], np.zeros(3, bool))[1] == -1
