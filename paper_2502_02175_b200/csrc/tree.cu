@@ -99,6 +99,9 @@ struct AcceptArgs {
   int n_keep;
 };
 constexpr int TA_CTAS = 8, TA_THREADS = 1024, TA_WARPS = TA_THREADS / 32;
+// One CTA / the cluster, us a call: 8 entries of 25 rows behind 300 positions 4.8 / 5.5, behind 4000 6.9 / 6.2; 32 of 61 behind 500 6.9 / 6.3; one behind 65,000
+// 11.0 / 6.2; 100 of 250 behind 300 22.6 / 9.5.
+constexpr int TA_ONE = 16, TA_SHORT = 8192;     // entries, positions that stay
 static_assert(TA_THREADS >= VLAC_PAGES_MAX_LIST, "one thread per list entry");
 
 // One launch.  A warp an entry: every row that its parent's choice fits bids for being the parent's successor, the lowest wins, and the path follows the
@@ -235,7 +238,7 @@ int vlac_tree_accept(const vlac_pages* p, const vlac_tree* tree, const int* seqs
   if (!seqs || !count || !keep_ptr || !status || (n_keep > 0 && !keep) || (tree->rows > 0 && (!drafted || !chosen || !path || !tokens))) return VLAC_ERR_INVALID_ARG;
   AcceptArgs a = {tree_args(p, tree, seqs, status), drafted, chosen, count, path, tokens, keep_ptr, keep, n_keep};
   const int smem = TA_WARPS * tree->max_rows * 4;                       // at most 128 KB
-  if (tree->n <= TA_WARPS && n_keep <= 16384) {
+  if (tree->n <= TA_ONE && n_keep <= TA_SHORT) {
     if (smem > 32768) { rc = big_smem<tree_accept_kernel<1>>(TA_WARPS * VLAC_TREE_MAX_ROWS * 4); if (rc != VLAC_OK) return rc; }
     VLAC_CUDA_CHECK(launch_pdl(tree_accept_kernel<1>, dim3(1), dim3(TA_THREADS), smem, (cudaStream_t)stream, a));
   } else {
