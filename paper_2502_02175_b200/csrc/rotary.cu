@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(RT_THREADS) rope_tables_kernel(const __grid_co
 }
 
 // ------------------------------------------------------------------------------------------------ append
-constexpr int AP_THREADS = 256, AP_WARPS = AP_THREADS / 32, AP_BATCH = 4, AP_CTAS = 24;
+constexpr int AP_THREADS = 256, AP_WARPS = AP_THREADS / 32, AP_BATCH = 6, AP_CTAS = 24;
 struct AppendArgs {
   void *k, *v;                                  // the layer
   const int *table, *len, *refs;
@@ -142,9 +142,11 @@ __global__ void __launch_bounds__(AP_THREADS, 4) pages_append_kernel(AppendArgs 
   const int c = lane % LANES, pairs = a.rot / 8;                        // lanes whose pieces are rotated
   const bool turned = c < pairs;
   const int el0 = INTER || !turned ? 8 * c : 4 * c, el1 = INTER || !turned ? 8 * c + 4 : 4 * c + a.rot / 2;      // first element of each piece
-  const int all = a.heads + 2 * a.kv_heads, step = PER * a.split, per_cta = AP_WARPS / a.split;
-  const int first = (warp % a.split) * PER + lane / LANES;              // first head of this lane
-  for (int r = r0 + blockIdx.x * per_cta + warp / a.split; r < r1; r += gridDim.x * per_cta) {
+  const size_t lane0 = (size_t)(lane / LANES) * D + el0, lane1 = (size_t)(lane / LANES) * D + el1;
+  // A warp's share of a row: slots of PER heads, those of q, of k, of v, the same for all its lanes (the compiler is told)
+  const int w = __shfl_sync(0xffffffffu, warp, 0), per_cta = AP_WARPS / a.split;
+  const int nq = (a.heads + PER - 1) / PER, nk = (a.kv_heads + PER - 1) / PER, slots = nq + 2 * nk;
+  for (int r = r0 + blockIdx.x * per_cta + w / a.split; r < r1; r += gridDim.x * per_cta) {
     const int at = at0 + (r - r0);
     const size_t pool = (((size_t)t[at >> a.shift] << a.shift) + (at & (a.page - 1))) * ((size_t)a.kv_heads * D);
     float4 cs = make_float4(1.f, 1.f, 1.f, 1.f), sn = make_float4(0.f, 0.f, 0.f, 0.f);  // of the lane's four pairs
@@ -154,26 +156,23 @@ __global__ void __launch_bounds__(AP_THREADS, 4) pages_append_kernel(AppendArgs 
       sn = *reinterpret_cast<const float4*>(a.sin + row);
     }
     const T *qi = (const T*)a.q + (size_t)r * a.q_stride, *ki = (const T*)a.kin + (size_t)r * a.k_stride, *vi = (const T*)a.vin + (size_t)r * a.v_stride;
-    T* qo = (T*)a.qout + (size_t)r * a.qout_stride;
-    for (int h0 = first; h0 - lane / LANES < all; h0 += step * AP_BATCH) {               // (uniform over the warp)
+    T *qo = (T*)a.qout + (size_t)r * a.qout_stride, *ko = (T*)a.k + pool, *vo = (T*)a.v + pool;
+    for (int s0 = w % a.split; s0 < slots; s0 += a.split * AP_BATCH) {
       uint2 x[AP_BATCH][2];
 #pragma unroll
       for (int b = 0; b < AP_BATCH; ++b) {
-        const int h = h0 + b * step;
-        x[b][0] = x[b][1] = make_uint2(0, 0);
-        if (h < all) {
-          const T* from = h < a.heads ? qi + (size_t)h * D : h < a.heads + a.kv_heads ? ki + (size_t)(h - a.heads) * D : vi + (size_t)(h - a.heads - a.kv_heads) * D;
-          load8<INTER>(x[b], from + el0, from + el1);
-        }
+        const int s = s0 + b * a.split, kind = s < nq ? 0 : s < nq + nk ? 1 : 2, h = (kind == 0 ? s : kind == 1 ? s - nq : s - nq - nk) * PER;
+        const T* from = (kind == 0 ? qi : kind == 1 ? ki : vi) + (size_t)h * D;
+        if (s < slots && h + lane / LANES < (kind == 0 ? a.heads : a.kv_heads)) load8<INTER>(x[b], from + lane0, from + lane1);
+        else x[b][0] = x[b][1] = make_uint2(0, 0);
       }
 #pragma unroll
       for (int b = 0; b < AP_BATCH; ++b) {
-        const int h = h0 + b * step;
-        if (h - lane / LANES >= all) break;                             // (uniform)
-        const bool is_q = h < a.heads, is_v = h >= a.heads + a.kv_heads;
-        if (!__all_sync(0xffffffffu, is_v)) {
+        const int s = s0 + b * a.split, kind = s < nq ? 0 : s < nq + nk ? 1 : 2, h = (kind == 0 ? s : kind == 1 ? s - nq : s - nq - nk) * PER;
+        if (s >= slots) break;
+        if (kind < 2) {
           F2 f[4] = {Pair16<T>::two(x[b][0].x), Pair16<T>::two(x[b][0].y), Pair16<T>::two(x[b][1].x), Pair16<T>::two(x[b][1].y)};
-          if (NORM) {
+          if (NORM && (kind == 0 ? a.q_gain : a.k_gain) != nullptr) {
             F2 s2 = f2_mul(f[0], f[0]);
 #pragma unroll
             for (int e = 1; e < 4; ++e) s2 = f2_fma(f[e], f[e], s2);
@@ -181,13 +180,11 @@ __global__ void __launch_bounds__(AP_THREADS, 4) pages_append_kernel(AppendArgs 
             float ss = p.x + p.y;
 #pragma unroll
             for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            if ((is_q ? a.q_gain : a.k_gain) != nullptr) {
-              const float inv = rsqrtf(ss * (1.f / D) + a.eps);
-              const float4 g0 = *reinterpret_cast<const float4*>(&s_gain[is_q ? 0 : 1][el0]), g1 = *reinterpret_cast<const float4*>(&s_gain[is_q ? 0 : 1][el1]);
-              const F2 g[4] = {f2(g0.x, g0.y), f2(g0.z, g0.w), f2(g1.x, g1.y), f2(g1.z, g1.w)}, i2 = f2(inv, inv);
+            const float inv = rsqrtf(ss * (1.f / D) + a.eps);
+            const float4 g0 = *reinterpret_cast<const float4*>(&s_gain[kind][el0]), g1 = *reinterpret_cast<const float4*>(&s_gain[kind][el1]);
+            const F2 g[4] = {f2(g0.x, g0.y), f2(g0.z, g0.w), f2(g1.x, g1.y), f2(g1.z, g1.w)}, i2 = f2(inv, inv);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) f[e] = f2_mul(f2_mul(f[e], i2), g[e]);
-            }
+            for (int e = 0; e < 4; ++e) f[e] = f2_mul(f2_mul(f[e], i2), g[e]);
           }
           if (turned) {                                                 // (without rotation infinities pass as they are)
             if (INTER) {
@@ -207,15 +204,11 @@ __global__ void __launch_bounds__(AP_THREADS, 4) pages_append_kernel(AppendArgs 
               }
             }
           }
-          if (!is_v) {
-            x[b][0] = make_uint2(Pair16<T>::pack(f[0]), Pair16<T>::pack(f[1]));
-            x[b][1] = make_uint2(Pair16<T>::pack(f[2]), Pair16<T>::pack(f[3]));
-          }
+          x[b][0] = make_uint2(Pair16<T>::pack(f[0]), Pair16<T>::pack(f[1]));
+          x[b][1] = make_uint2(Pair16<T>::pack(f[2]), Pair16<T>::pack(f[3]));
         }
-        if (h < all) {
-          T* to = is_q ? qo + (size_t)h * D : (T*)(is_v ? a.v : a.k) + pool + (size_t)(h - a.heads - (is_v ? a.kv_heads : 0)) * D;
-          store8<INTER>(x[b], to + el0, to + el1);
-        }
+        T* to = (kind == 0 ? qo : kind == 1 ? ko : vo) + (size_t)h * D;
+        if (h + lane / LANES < (kind == 0 ? a.heads : a.kv_heads)) store8<INTER>(x[b], to + lane0, to + lane1);
       }
     }
   }
