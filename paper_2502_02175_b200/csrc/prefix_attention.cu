@@ -465,7 +465,9 @@ __device__ __forceinline__ bool any_nonfinite(uint4 x) {
 // EARLY: behind the wide kernel of the same call, of which it reads nothing.  That kernel lets its successor start only once it has seen the plan
 // complete, so the CTAs here begin as SMs come free and wait for its end before their own (what comes after reads both).
 // TREE: a row sees all positions in front of its entry's newest rows and, of those, what its mask says.  The words are asked for before the scores are
-// formed, in the steps that reach the newest rows alone.
+// formed, in the steps that reach the newest rows alone.  The pages in front are the wide kernel's as ever, so that a tree costs what its rows cost as a
+// chunk: 16 trees of up to 61 rows, 32 heads of 128, behind 8208 positions 254 us (6.2 TB/s) + 24 here; four of up to 64 rows with 8 K/V heads behind 65,600
+// 178 us (its softmax chain) + 11.  Bound here: the chain of a step (16 rows by 16 keys: 340 instructions), two warps a scheduler.
 template <typename T, int D, bool EARLY, bool TREE>
 __global__ void __launch_bounds__(PN_WARPS * 32, 2) prefix_narrow_kernel(AttnArgs a) {
   using N = Narrow<D>;

@@ -10,6 +10,7 @@ namespace {
 // Angles are kept as turns (angle / 2 pi): the whole turns of a far position fall away exactly before a sine is taken.  Turns per position come
 // from the host as a pair of doubles (from its extended type); a thread takes one frequency and a run of positions: one sine and cosine in
 // 64 bits for the first, then a rotation by the angle of one position each (four products in 64 bits; the error grows by about 2^-53 a step).
+// Bound: the stores (262,144 positions of 128 dimensions, 134 MB: 21.6 us, 6.2 TB/s); a table of 2048 positions is a launch (2.8 us).
 constexpr int RT_MAX = 256, RT_THREADS = 256;
 struct TableArgs {
   double turns[RT_MAX / 2], rest[RT_MAX / 2];   // per position; what the double leaves of it
@@ -94,7 +95,11 @@ template <bool ONE> __device__ __forceinline__ void store8(const uint2* x, void*
 
 // grid (x, entries).  A lane holds 8 elements of a head in two pieces of 4, a warp two heads of 128 or four of 64 at a time, all of one row, so that a lane's
 // cosines and sines stay in registers for the whole row.  The pieces are the two that are rotated with one another (half layout: rot/2 apart;
-// interleaved, and behind the rotated part: neighbours), so that nothing is exchanged between lanes but the sum of a norm.
+// interleaved, and behind the rotated part: neighbours), so that nothing is exchanged between lanes but the sum of a norm.  (With pieces of 8 neighbours and
+// the partner's values by shuffles 96 heads of 128 took 260 us a 1.45 GB call against 201, 48 of 64 111 against 66.)  Each CTA checks the whole entry for
+// itself, so that an entry is written whole or not at all without a second launch.  Bound: HBM where heads are 128 wide and only rotated (201 us, 7.2 TB/s of
+// algorithmic bytes, part of the writes still in L2), the instructions beside it with norms (fp16, interleaved quarter, 0.63 GB: 113 us, 5.6 TB/s, 72 % of the
+// issue slots); one row each for 64 sequences 4.8 us, launch and dependent reads.
 template <typename T, int D, bool INTER, bool NORM>
 __global__ void __launch_bounds__(AP_THREADS, 4) pages_append_kernel(AppendArgs a) {
   constexpr int LANES = D / 8, PER = 32 / LANES;                        // lanes of a head; heads of a warp
@@ -297,8 +302,8 @@ int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int
   a.status = status;
   a.split = 1;
   while (a.split < AP_WARPS && (long long)rows * a.split < n_sm * 64ll) a.split *= 2;
-  // CTAs: no more per entry than an entry of up to twice the mean length can use; what fits the GPU at once is not given a second wave; larger calls get
-  // many short CTAs, which even out
+  // CTAs: no more per entry than an entry of up to twice the mean length can use; what fits the GPU at once is not given a second wave (16 entries of 17 to 33
+  // rows, 49 / 37 CTAs each: 8.2 / 6.9 us); larger calls get many short CTAs, which even out (8, 24, 48 an SM: 131 / 124 / 127 us for 8 prompts)
   const int per = AP_WARPS / a.split, mean = (int)((2ll * rows - n + (long long)n * per - 1) / ((long long)n * per));
   const int most = n_sm * ((long long)rows * a.split <= n_sm * 4ll * AP_WARPS ? 4 : AP_CTAS), spread = (most + n - 1) / n;
   const dim3 grid(mean < 1 ? 1 : mean < spread ? mean : spread, n);
