@@ -466,7 +466,8 @@ int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int
  *   mask     device uint32 [rows][ceil(max_rows/32)]: bit j = the row sees row j of its entry (its ancestors and itself)
  *   pos      device int32 [rows]: len - nq_i + depth, the position to rotate to;  entry  device int32 [rows]: the row's entry
  * Status as for the paged calls, INVALID_ARG also for a parent out of range and nq_i > len, TOO_LARGE for nq_i > max_rows; rows of refused
- * entries and of none get mask 0, pos -1, entry -1.  A falling q_ptr refuses all.  p and seqs may both be NULL: pos is then the depth. */
+ * entries and of none get mask 0, pos -1, entry -1.  A falling q_ptr refuses all.  p and seqs may both be NULL: pos is then the depth.  mask, pos
+ * and entry serve one step at a time (two captured graphs that may overlap need two). */
 #define VLAC_TREE_MAX_ROWS 1024
 typedef struct {
   int n, rows, max_rows;
@@ -509,8 +510,8 @@ typedef struct {
   const unsigned* allow; const int* allow_row; int n_allow;
   const vlac_tree* tree; const int* drafted;
 } vlac_logits_rules;
-/* logits, out  device, dtype VLAC_FP32, VLAC_BF16 or VLAC_FP16, row r at r*stride / r*out_stride elements (at least vocab; any alignment of the element,
- *              16-byte rows are faster); out NULL: only tokens are picked; out may be logits itself (same stride), other overlaps are refused
+/* logits, out  device, dtype VLAC_FP32, VLAC_BF16 or VLAC_FP16, row r at r*stride / r*out_stride elements (at least vocab; any alignment of the element;
+ *              rows of out that lie as their logits do to 16 bytes are faster); out NULL: only tokens are picked; out may be logits itself (same stride), other overlaps are refused
  * picked, status  device int32 [rows]; picked may be NULL.  rows 0..65535 (TOO_LARGE beyond), vocab 1..2^30 */
 int vlac_logits_adjust(int rows, int vocab, int dtype, const void* logits, long long stride, const vlac_logits_rules* rules, void* out,
                        long long out_stride, int* picked, int* status, void* stream);

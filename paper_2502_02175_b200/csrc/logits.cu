@@ -32,7 +32,7 @@ struct LogitsArgs {
   vlac_logits_rules r;
   const unsigned* mask; const int *entry, *q_ptr; int n, words;         // the tree's
   int allow_words;
-  int per;                                      // tokens of a CTA, a multiple of 64
+  int per;                                      // places of a CTA, a multiple of 64
 };
 
 // order-preserving: a larger value has a larger key, -0 and +0 the same one, a NaN the largest (an addition makes every NaN the same positive one).
@@ -72,7 +72,7 @@ template <> struct Logit<__half> {
   static __device__ __forceinline__ float2 two(unsigned x) { return __half22float2(*reinterpret_cast<__half2*>(&x)); }
 };
 
-// 16 bytes of logits, or one element where rows are not whole, aligned 16-byte pieces
+// 16 bytes of logits, or one element where a row of the results is aligned otherwise than its logits
 template <typename T, bool VEC> struct Piece {
   static constexpr int N = VEC ? 16 / sizeof(T) : 1;
   static constexpr unsigned ALL = (1u << N) - 1u;
@@ -121,9 +121,14 @@ template <typename T, bool VEC> struct Piece {
   }
 };
 
+// LG_WHOLE: rows of whole, aligned 16-byte pieces.  LG_SHIFTED: a row may begin and end anywhere, its results like its logits.  Places are counted from the 16-byte boundary in front of the row, so that pieces are
+// whole and aligned; token t has place t + off.  What lies in a piece that the row does not fill (at most 7 tokens at each end) is marked and done with
+// the marked tokens (512 rows of 126,953 in bf16: 82 us, one element at a time 210).  LG_SINGLE: results that lie otherwise than their logits.
 // CTAS share a row.  Few rows are shared by 8, so that there are enough CTAs; many by fewer, since every one of them goes through the row's lists.
-template <typename T, bool VEC, int CTAS, int LG_THREADS>
+enum { LG_SINGLE = 0, LG_WHOLE = 1, LG_SHIFTED = 2 };
+template <typename T, int MODE, int CTAS, int LG_THREADS>
 __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, LG_THREADS > 256 ? 1 : CTAS == 8 ? 3 : 4) logits_kernel(LogitsArgs a) {
+  constexpr bool VEC = MODE != LG_SINGLE, SHIFTED = MODE == LG_SHIFTED;
   using P = Piece<T, VEC>;
   using L = Logit<T>;
   constexpr int LG_TABLE = lg_table(CTAS), LG_WARPS = LG_THREADS / 32;
@@ -162,22 +167,28 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, LG_TH
   const int d = tid < n_seen ? u.drafted[first + tid] : -1;
   const unsigned seen = tid < n_seen ? a.mask[(size_t)row * a.words + (tid >> 5)] >> (tid & 31) & 1 : 0;
   if (rank == 0 && tid == 0) a.status[row] = ok ? VLAC_OK : VLAC_ERR_INVALID_ARG;
-  const bool any = ok && (h2 > h0 || first >= 0 || b1 > b0);                              // is anything said of single tokens (uniform)
+  const bool lists = ok && (h2 > h0 || first >= 0 || b1 > b0);                            // is anything said of single tokens (uniform)
   const unsigned char* allow = u.allow && allow_row >= 0 ? (const unsigned char*)(u.allow + (size_t)allow_row * a.allow_words) : nullptr;
-  const T* in = (const T*)a.in + (size_t)row * a.stride;
-  T* out = a.out ? (T*)a.out + (size_t)row * a.out_stride : nullptr;
+  const T* const row_in = (const T*)a.in + (size_t)row * a.stride;
+  const int off = SHIFTED ? (int)(((uintptr_t)row_in & 15u) / sizeof(T)) : 0, v_end = off + a.vocab;             // places of the row's tokens: off .. v_end
+  const int v_lo = SHIFTED ? (off + N - 1) / N * N : 0, v_hi = SHIFTED ? v_end / N * N : v_end;              // of its whole pieces
+  const T* const in = row_in - off;
+  T* const out = a.out ? (T*)a.out + (size_t)row * a.out_stride - off : nullptr;
+  auto allowed = [&](int place) { return !allow || (allow[(place - off) >> 3] >> ((place - off) & 7) & 1); };
   int best = LG_NONE, best1 = LG_NONE;          // largest key of the unmarked tokens, and of the marked ones
-  unsigned best_at = 0, best_of = 0, best1_at = 0;                      // first token of the batch that has it, and which of the batch count; the token
-  const int end = ok ? (int)min((long long)a.vocab, (long long)(rank + 1) * a.per) : 0;
+  unsigned best_at = 0, best_of = 0, best1_at = 0;                      // first place of the batch that has it, and which of the batch count; the place
+  const int end = ok ? (int)min((long long)v_end, (long long)(rank + 1) * a.per) : 0;
   int most = LG_RUN;
   for (int c0 = rank * a.per, n; c0 < end; c0 += n) {
     n = min(most, end - c0);
     bool direct = n <= LG_TABLE;
     P x[BATCH];                                 // the first logits, asked for before they are needed
 #pragma unroll
-    for (int q = 0; q < BATCH; ++q) { const int at = (q * LG_THREADS + tid) * N; if (at < n) x[q].load(in + c0 + at); }
+    for (int q = 0; q < BATCH; ++q) { const int at = c0 + (q * LG_THREADS + tid) * N; if ((!SHIFTED || at >= v_lo) && at < min(c0 + n, v_hi)) x[q].load(in + at); }
+    // (the runs begin at multiples of 64: the ends' pieces lie in the row's first run and in its last)
+    const bool head = SHIFTED && c0 < v_lo, any = lists || head || (SHIFTED && v_hi < v_end && c0 + n == v_end);
     // ---- what is said of which tokens
-    for (bool again = any; again;) {
+    for (bool again = any; again;) {            // (a cut run keeps `any`: its part without an end marks nothing)
       __syncthreads();                          // (what was there before is read)
       for (int i = tid * 4; i < (n + 31) >> 5; i += LG_THREADS * 4) *reinterpret_cast<uint4*>(s_mark + i) = make_uint4(0, 0, 0, 0);
       for (int i = tid * 4; i < (direct ? n : LG_TABLE); i += LG_THREADS * 4) {
@@ -200,13 +211,13 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, LG_TH
         return -1;
       };
       auto count = [&](int token, bool made) {
-        const unsigned t = (unsigned)token - (unsigned)c0;
-        const int i = token >= 0 && t < (unsigned)n ? place(t) : -1;
+        const unsigned t = (unsigned)token + (unsigned)off - (unsigned)c0;
+        const int i = (unsigned)token < (unsigned)a.vocab && t < (unsigned)n ? place(t) : -1;
         if (i >= 0) { if (made) atomicAdd(&s_made[i], 1u); else atomicOr(&s_made[i], LG_SEEN); }
       };
       auto add = [&](int token, int number) {
-        const unsigned t = (unsigned)token - (unsigned)c0;
-        const int i = token >= 0 && t < (unsigned)n ? place(t) : -1;
+        const unsigned t = (unsigned)token + (unsigned)off - (unsigned)c0;
+        const int i = (unsigned)token < (unsigned)a.vocab && t < (unsigned)n ? place(t) : -1;
         if (i >= 0) atomicMax(&s_bias[i], number);
       };
 #pragma unroll
@@ -222,6 +233,10 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, LG_TH
       for (int j = tid + LG_THREADS; j < n_seen; j += LG_THREADS)
         if (a.mask[(size_t)row * a.words + (j >> 5)] >> (j & 31) & 1) count(u.drafted[first + j], true);
       if (b >= 0) add(b, tid + 1);
+      if (SHIFTED && tid < 2 * N) {                 // the ends
+        const int v = tid < N ? off + tid : max(v_hi, v_lo) + tid - N;
+        if (v < (tid < N ? min(v_lo, v_end) : v_end) && (unsigned)(v - c0) < (unsigned)n) place((unsigned)(v - c0));
+      }
       for (int i = b0 + tid + LG_THREADS; i < b1; i += LG_THREADS) add(u.bias_token[i], i - b0 + 1);
       __syncthreads();
       again = s_full;                           // (never of a direct run)
@@ -229,20 +244,29 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, LG_TH
     }
     // ---- the run: BATCH pieces of a thread at a time, the next ones asked for in front of that.  Of a batch only the largest element is looked at; which
     // of its elements that is, is found out in the end.
-    const unsigned char *may_b = allow ? allow + ((c0 + tid * N) >> 3) : nullptr, *mark_b = reinterpret_cast<const unsigned char*>(s_mark) + (tid * N >> 3);
+    const unsigned char* mark_b = reinterpret_cast<const unsigned char*>(s_mark) + (tid * N >> 3);
     const T* from = in + c0 + tid * N;
     T* to = out ? out + c0 + tid * N : nullptr;
     constexpr int STEP = LG_THREADS * N, ALL_STEP = BATCH * STEP;       // tokens of a piece of every thread, of a batch
-    auto batch = [&](int at0, auto whole) {                             // whole: no thread has a piece behind the end of the run
+    const int n_vec = min(n, v_hi - c0);                                // whole pieces lie in front of this
+    // bits of the mask: a piece's first token lies off behind a multiple of N, its bits in one byte or in two
+    const int b_first = (c0 + tid * N - off) >> 3, b_shift = (c0 + tid * N - off) & 7, b_room = a.allow_words * 4 - 1 - b_first;
+    const unsigned char* may_b = allow ? allow + b_first : nullptr;     // (of whole pieces no byte in front of the mask is read)
+    auto batch = [&](int at0, auto whole) {                             // whole: every thread has BATCH whole pieces
       typename P::Max m = P::none();
       unsigned of = 0;
 #pragma unroll
       for (int q = 0; q < BATCH; ++q) {
-        if (!decltype(whole)::value && at0 + q * STEP + tid * N >= n) continue;
-        unsigned stay = 0xffu;                                          // (c0 is a multiple of 32, a piece's first token one of N)
-        if (may_b) stay = may_b[(at0 + q * STEP) >> 3];
+        const int at = at0 + q * STEP + tid * N;
+        if (!decltype(whole)::value && (at >= n_vec || (SHIFTED && c0 + at < v_lo))) continue;
+        unsigned stay = P::ALL;                                         // (c0 is a multiple of 32, a piece's first place one of N)
+        if (may_b) {
+          stay = may_b[(at0 + q * STEP) >> 3];
+          if (SHIFTED) stay |= (unsigned)may_b[min(((at0 + q * STEP) >> 3) + 1, b_room)] << 8;
+          if (N < 8 || SHIFTED) stay = stay >> b_shift & P::ALL;
+        }
         unsigned mark = any ? mark_b[(at0 + q * STEP) >> 3] : 0;
-        if (N < 8) { stay = stay >> (tid * N & 7) & P::ALL; mark = mark >> (tid * N & 7) & P::ALL; }
+        if (N < 8) mark = mark >> (tid * N & 7) & P::ALL;
         of |= (stay & ~mark) << q * N;
         P y = x[q];
         y.mask_and_max(stay & ~mark, &m);
@@ -252,15 +276,15 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, LG_TH
       const int k = lg_key(P::largest(m));
       if (k > best && of) { best = k; best_at = c0 + at0 + tid * N; best_of = of; }        // (ascending: of equal ones the first stays)
     };
-    for (int at0 = 0; at0 < n; at0 += ALL_STEP) {
+    for (int at0 = 0; at0 < n_vec; at0 += ALL_STEP) {
       P y[BATCH];
-      if (at0 + 2 * ALL_STEP <= n) {
+      if (at0 + 2 * ALL_STEP <= n_vec && (at0 > 0 || !head)) {
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) y[q].load(from + at0 + ALL_STEP + q * STEP);
         batch(at0, std::true_type());
       } else {
 #pragma unroll
-        for (int q = 0; q < BATCH; ++q) if (at0 + ALL_STEP + q * STEP + tid * N < n) y[q].load(from + at0 + ALL_STEP + q * STEP);
+        for (int q = 0; q < BATCH; ++q) if (at0 + ALL_STEP + q * STEP + tid * N < n_vec) y[q].load(from + at0 + ALL_STEP + q * STEP);
         batch(at0, std::false_type());
       }
 #pragma unroll
@@ -289,19 +313,19 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, LG_TH
           at[q] = c0 + (direct ? i : s_token[i] - 1);
           made[q] = s_made[i]; number[q] = s_bias[i];
           v[q] = L::value(in[at[q]]);
-          may[q] = j < used && (!allow || (allow[at[q] >> 3] >> (at[q] & 7) & 1));        // (what is not allowed is written already)
+          may[q] = allowed(at[q]);
           add[q] = number[q] ? u.bias[b0 + number[q] - 1] : 0.f;
         }
 #pragma unroll
         for (int q = 0; q < LG_EACH; ++q) {
-          if (!may[q]) continue;
+          if (j0 + q * 32 >= used || (!SHIFTED && !may[q])) continue;   // (in whole pieces what is not allowed is written already)
           const unsigned c = made[q] & ~LG_SEEN;
           float y = v[q];
           if (made[q]) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
           if (c) { y = __fsub_rn(y, __fmul_rn(freq, (float)c)); y = __fsub_rn(y, pres); }
           if (number[q]) y = __fadd_rn(y, add[q]);
-          if (out) out[at[q]] = L::round(y);
-          const int k = lg_key(y);
+          if (out) out[at[q]] = L::round(may[q] ? y : -INFINITY);
+          const int k = may[q] ? lg_key(y) : LG_NONE;
           if (k > best1 || (k == best1 && (unsigned)at[q] < best1_at)) { best1 = k; best1_at = at[q]; }
         }
       }
@@ -343,30 +367,36 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(LG_THREADS, LG_TH
     const int k = lane < CTAS ? s_best[lane][0] : LG_NONE;
     top = __reduce_max_sync(0xffffffffu, k);
     at = __reduce_min_sync(0xffffffffu, k == top && lane < CTAS ? (unsigned)s_best[lane][1] : 0xffffffffu);
-    if (lane == 0) a.picked[row] = top != LG_NONE ? (int)at : -1;
+    if (lane == 0) a.picked[row] = top != LG_NONE ? (int)at - off : -1;
   }
 }
 
-template <typename T, int CTAS, int THREADS>
-int launch_logits(LogitsArgs a, bool vec, cudaStream_t s) {
-  a.per = (int)(((long long)a.vocab + CTAS * 64 - 1) / (CTAS * 64) * 64);
-  const int rc = vec ? big_smem<logits_kernel<T, true, CTAS, THREADS>>(lg_smem(CTAS)) : big_smem<logits_kernel<T, false, CTAS, THREADS>>(lg_smem(CTAS));
+template <typename T, int MODE, int CTAS, int THREADS>
+int launch_logits(LogitsArgs a, cudaStream_t s) {
+  a.per = (int)(((long long)a.vocab + (MODE == LG_SHIFTED ? 7 : 0) + CTAS * 64 - 1) / (CTAS * 64) * 64);  // (places: up to 7 more than tokens)
+  const int rc = big_smem<logits_kernel<T, MODE, CTAS, THREADS>>(lg_smem(CTAS));
   if (rc != VLAC_OK) return rc;
-  VLAC_CUDA_CHECK(launch_pdl(vec ? logits_kernel<T, true, CTAS, THREADS> : logits_kernel<T, false, CTAS, THREADS>, dim3(CTAS, a.rows), dim3(THREADS), lg_smem(CTAS), s, a));
+  VLAC_CUDA_CHECK(launch_pdl(logits_kernel<T, MODE, CTAS, THREADS>, dim3(CTAS, a.rows), dim3(THREADS), lg_smem(CTAS), s, a));
   return VLAC_OK;
+}
+template <typename T, int CTAS, int THREADS>
+int launch_logits(const LogitsArgs& a, cudaStream_t s) {
+  const long long size = sizeof(T);
+  const bool whole = a.vocab * size % 16 == 0 && a.stride * size % 16 == 0 && !((uintptr_t)a.in & 15u) &&
+                     (!a.out || (a.out_stride * size % 16 == 0 && !((uintptr_t)a.out & 15u)));
+  const bool alike = !a.out || (((uintptr_t)a.in - (uintptr_t)a.out) % 16 == 0 && (a.stride - a.out_stride) * size % 16 == 0);
+  return whole ? launch_logits<T, LG_WHOLE, CTAS, THREADS>(a, s) : alike ? launch_logits<T, LG_SHIFTED, CTAS, THREADS>(a, s) : launch_logits<T, LG_SINGLE, CTAS, THREADS>(a, s);
 }
 template <typename T>
 int launch_logits(const LogitsArgs& a, cudaStream_t s) {
-  const bool vec = a.vocab * (long long)sizeof(T) % 16 == 0 && a.stride * (long long)sizeof(T) % 16 == 0 && !((uintptr_t)a.in & 15u) &&
-                   (!a.out || (a.out_stride * (long long)sizeof(T) % 16 == 0 && !((uintptr_t)a.out & 15u)));
   // The GPU holds 3 CTAs with the large table an SM, 4 of the others.  As few a row as fill three quarters of its places, since each goes through the row's
   // lists: 310 rows of 50,000 with histories of 3000, one / two a row 39 / 29 us; 512 of 128,000 81 / 81 (without lists 51 / 54); 140 of 50,000 in fp32,
   // two / four 31 / 25; 60 of them, eight (a second wave) / four 24 / 19.  Where not every SM has one, CTAs of 512 threads (one row of 260,000 11.6 -> 9.6).
-  if (a.rows >= 3 * LG_SMS) return launch_logits<T, 1, 256>(a, vec, s);
-  if (a.rows >= 3 * LG_SMS / 2) return launch_logits<T, 2, 256>(a, vec, s);
-  if (a.rows > 3 * LG_SMS / 8) return launch_logits<T, 4, 256>(a, vec, s);
-  if (a.rows > LG_SMS / 8) return launch_logits<T, 8, 256>(a, vec, s);
-  return launch_logits<T, 8, 512>(a, vec, s);
+  if (a.rows >= 3 * LG_SMS) return launch_logits<T, 1, 256>(a, s);
+  if (a.rows >= 3 * LG_SMS / 2) return launch_logits<T, 2, 256>(a, s);
+  if (a.rows > 3 * LG_SMS / 8) return launch_logits<T, 4, 256>(a, s);
+  if (a.rows > LG_SMS / 8) return launch_logits<T, 8, 256>(a, s);
+  return launch_logits<T, 8, 512>(a, s);
 }
 
 }  // namespace

@@ -567,6 +567,45 @@ def test_logits_strides_and_alignment(vb):
         assert torch.all(out == 7)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 30, 80, 230, 450])
+def test_logits_rows_at_every_alignment(vb, rows, dtype):
+    """Odd vocabularies (each row begins elsewhere to 16 bytes), results aligned like the logits and otherwise, in place; tiny vocabularies; nothing beside the rows is
+    written."""
+    for vocab in (1, 2, 5, 9, 63, 1003, 4097) + ((70007,) if rows < 50 else ()):
+        c = Logits(vb, rows, vocab, dtype, seed=vocab + rows, tree=[rows] if rows < 100 else [50] * (rows // 50) + ([rows % 50] if rows % 50 else []), hist=30)
+        for shift, width in ((0, vocab), (3, vocab + 4), (1, vocab + 7)):
+            only = range(0, rows, max(1, rows // 9))
+            x = torch.full((rows, width), 3.0, dtype=dtype, device="cuda")
+            x[:, shift:shift + vocab] = c.x
+            for out_shift, out_width in ((shift, width), (shift + 1, width + 1), (shift + 8, width + 8)):
+                out = torch.full((rows + 2, out_width), 7.0, dtype=dtype, device="cuda")
+                cut = out[1:-1, out_shift:out_shift + vocab]
+                _, p, st = c.run(x=x[:, shift:shift + vocab], out=cut)
+                c.check(cut, p, st, only=only)
+                cut.fill_(7.0)
+                assert torch.all(out == 7)
+            here = x[:, shift:shift + vocab]
+            _, p, st = c.run(x=here, out=here)
+            c.check(here, p, st, only=only)
+            here.fill_(3.0)
+            assert torch.all(x == 3)
+
+
+def test_logits_beyond_32_bits(vb):
+    """Element offsets beyond 2^31, results in place."""
+    rows, vocab = 17001, 130001
+    x = torch.zeros((rows, vocab), dtype=torch.bfloat16, device="cuda")
+    assert x.numel() > 2 ** 31
+    x[-1, 129999], x[-2, 0], x[5, 77] = 2.0, 1.0, 3.0
+    pen = torch.full((rows,), 0.5, device="cuda")
+    rules = vb.LogitsRules(rows, vocab, history=dev([129999, 129999, 5]), span=dev([[0, 0, 3]] * rows), frequency=pen)
+    p, st = ints(rows), ints(rows)
+    vb.vlac_logits_adjust(x, rules, x, p, st)
+    assert not torch.any(st) and p[-3:].tolist() == [0, 0, 129999] and p[5].item() == 77
+    assert x[-1, [0, 5, 129998, 129999, 130000]].tolist() == [0.0, -0.5, 0.0, 1.0, 0.0] and x[-2, [0, 5, 129999]].tolist() == [1.0, -0.5, -1.0]
+
+
 def test_logits_special_values(vb):
     """Infinities, NaN, ties, zeros of both signs, rows that the grammar leaves nothing of."""
     c = Logits(vb, 8, 9000, seed=2, tree=(8,), masks=3)
