@@ -453,7 +453,8 @@ typedef struct {
  *   pos    device int32 [rows], the position that row r is rotated to, or NULL: the position it is written to.  An entry with a
  *          position outside [0, n_pos) is refused (INVALID_ARG); without rotation positions are not looked at
  *   q      n_heads heads of head_dim a row (n_heads = 0: none, q and q_out are not looked at); strides and alignment as k_rows.  q_out may be q
- *          itself (same stride); no other row of q_out shares memory with rows of q, k_rows or v_rows (INVALID_ARG), nor with the pool
+ *          itself (same stride); no other row of q_out shares memory with rows of q, k_rows or v_rows, and none with K or V of the pool
+ *          (INVALID_ARG).  q, like k_rows and v_rows, none of the rows of the pool that the call writes
  * A row_ptr that falls refuses all.  Other arguments, codes and refusals as vlac_pages_write; rows of refused entries and rows behind row_ptr[n] stay as they were, in q_out too. */
 int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int* start, const int* row_ptr, int n, int rows, const vlac_rope* rope,
                       const int* pos, int n_heads, const void* q, long long q_stride, void* q_out, long long q_out_stride, const void* k_rows,

@@ -289,6 +289,7 @@ int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int
     if (rows_overlap((uintptr_t)k_rows, 2ull * k_stride, (uintptr_t)q_out, 2ull * q_out_stride, 2ull * w, 2ull * wq, rows) ||
         rows_overlap((uintptr_t)v_rows, 2ull * v_stride, (uintptr_t)q_out, 2ull * q_out_stride, 2ull * w, 2ull * wq, rows))
       return VLAC_ERR_INVALID_ARG;
+    if (rows_in_pool(p, q_out, 2ull * q_out_stride, 2ull * wq, rows)) return VLAC_ERR_INVALID_ARG;
   }
   int n_sm = 0;
   rc = sm_count(&n_sm);

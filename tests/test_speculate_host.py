@@ -124,3 +124,16 @@ def test_host_forms():
     assert np.allclose(s, [[np.sin(3.0), np.sin(0.003 / 4)]])
     y, _ = ref.turned(np.array([[[1.0, 2.0, 3.0, 4.0]]]), None, 0, np.array([[0.0]]), np.array([[1.0]]), False, 0, 0)
     assert y.tolist() == [[[-2.0, 1.0, 3.0, 4.0]]]
+
+
+def test_queries_into_the_pool_are_refused(vb):
+    """Rotated queries written over K or V: any layer, the pool's first and last bytes, rows on both sides of it."""
+    side, far = FAKE + (1 << 32), FAKE + (1 << 33)
+    p = _struct(vb, v=side)
+    layer = 40 * 16 * 4 * 64 * 2
+    for begin in (FAKE, side):
+        for at in (begin, begin + layer, begin + 2 * layer - 16, begin + layer - 512, begin - 3 * 512 - 16, begin - 2048 + 16):
+            assert _append(vb, p, q=far, q_out=at, k=far + (1 << 20), v=far + (1 << 21)) == INVALID, (begin, at)
+        # queries that live there, in place; a row of a wide buffer that lies inside the pool
+        assert _append(vb, p, q=begin, q_out=begin, k=far, v=far) == INVALID
+        assert _append(vb, p, q=far, q_out=begin - (1 << 19), out_stride=1 << 18, k=far + (1 << 24), v=far + (1 << 24)) == INVALID
