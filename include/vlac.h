@@ -387,8 +387,8 @@ int vlac_pages_from_cache(const vlac_pages* p, vlac_cache* cache, int seq, int s
  *            one of them at a time (two captured graphs that may overlap need two)
  *   scale    finite, also times log2(e)
  *   q, out   device, the pool's type, row r at r*q_stride / r*out_stride elements (multiples of 8, at least n_heads*head_dim), 16-byte
- *            aligned;  lse  device fp32 [rows][n_heads] or NULL.  No row of out shares memory with a row of q (INVALID_ARG: queries are
- *            still read while results are written; columns of one buffer are fine), nor with lse or the pool */
+ *            aligned;  lse  device fp32 [rows][n_heads] or NULL.  No row of out shares memory with a row of q (queries are still read while results
+ *            are written; columns of one buffer are fine), nor with lse or K and V of the pool (INVALID_ARG) */
 typedef struct {
   int n, rows, n_heads;
   void* mem;

@@ -4,7 +4,6 @@
 #include "vlac_internal.h"
 #include <limits.h>
 #include <atomic>
-#include <initializer_list>
 
 static inline int pages_shift(int page_size) {
   int s = 0;
@@ -72,15 +71,16 @@ static inline bool rows_overlap(uintptr_t q, unsigned long long qs, uintptr_t ou
 static inline size_t pages_row(const vlac_pages* p) { return (size_t)p->n_kv_heads * p->head_dim; }
 static inline size_t pages_layer(const vlac_pages* p) { return (size_t)p->n_pages * p->page_size * pages_row(p); }
 
-// Whether a row of out (row r: w bytes from out + r * stride on, stride >= w) shares a byte with K or V of the pool, in any layer.
+// Whether a row of out (row r: w bytes from out + r * stride on, stride >= w) shares a byte with [a, a + bytes).
+static inline bool rows_touch(const void* at, unsigned long long bytes, const void* out, unsigned long long stride, unsigned long long w, int rows) {
+  const unsigned long long a = (uintptr_t)at, o = (uintptr_t)out;
+  const unsigned long long r = o + w > a ? 0 : (a - o - w) / stride + 1;                  // the first row that ends behind a
+  return r < (unsigned long long)rows && o + r * stride < a + bytes;
+}
+// The same for K and V of the pool, in any layer.
 static inline bool rows_in_pool(const vlac_pages* p, const void* out, unsigned long long stride, unsigned long long w, int rows) {
   const unsigned long long bytes = 2ull * p->n_layers * pages_layer(p);
-  for (const void* pool : {(const void*)p->k, (const void*)p->v}) {
-    const unsigned long long a = (uintptr_t)pool, o = (uintptr_t)out;
-    const unsigned long long r = o + w > a ? 0 : (a - o - w) / stride + 1;                // the first row that ends behind the pool's begin
-    if (r < (unsigned long long)rows && o + r * stride < a + bytes) return true;
-  }
-  return false;
+  return rows_touch(p->k, bytes, out, stride, w, rows) || rows_touch(p->v, bytes, out, stride, w, rows);
 }
 
 __device__ __forceinline__ void cluster_sync_all() {

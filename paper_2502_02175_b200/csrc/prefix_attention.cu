@@ -1535,6 +1535,8 @@ int attention(const vlac_pages* p, int layer, const vlac_prefix* plan, const vla
   if (!q || !out || q_stride < w || out_stride < w || q_stride % 8 || out_stride % 8 || (((uintptr_t)q | (uintptr_t)out) & 15u) || ((uintptr_t)lse & 3u))
     return VLAC_ERR_INVALID_ARG;
   if (rows_overlap((uintptr_t)q, 2ull * q_stride, (uintptr_t)out, 2ull * out_stride, 2ull * w, 2ull * w, plan->rows)) return VLAC_ERR_INVALID_ARG;
+  if (rows_in_pool(p, out, 2ull * out_stride, 2ull * w, plan->rows)) return VLAC_ERR_INVALID_ARG;
+  if (lse && rows_touch(lse, 4ull * plan->rows * plan->n_heads, out, 2ull * out_stride, 2ull * w, plan->rows)) return VLAC_ERR_INVALID_ARG;
   if (tree && (!tree->mask || (uintptr_t)tree->mask & 3u)) return VLAC_ERR_INVALID_ARG;
   AttnArgs a = {};
   if (tree) { a.mask = tree->mask; a.words = (tree->max_rows + 31) / 32; }

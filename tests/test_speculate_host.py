@@ -137,3 +137,22 @@ def test_queries_into_the_pool_are_refused(vb):
         # queries that live there, in place; a row of a wide buffer that lies inside the pool
         assert _append(vb, p, q=begin, q_out=begin, k=far, v=far) == INVALID
         assert _append(vb, p, q=far, q_out=begin - (1 << 19), out_stride=1 << 18, k=far + (1 << 24), v=far + (1 << 24)) == INVALID
+
+
+def test_attention_results_over_the_pool_or_the_sums_are_refused(vb):
+    """Rows of out share no memory with K, V or lse (plain and with a tree)."""
+    side, far = FAKE + (1 << 32), FAKE + (1 << 33)
+    p, plan, tree = _struct(vb, v=side), vb.vlac_prefix(2, 4, 4, FAKE, 1 << 40), _tree(vb)
+    layer = 40 * 16 * 4 * 64 * 2
+
+    def call(out, stride=256, lse=None):
+        head = C.byref(p), 1, C.byref(plan)
+        return {vb.lib.vlac_prefix_attention(*head, far, 256, 1.0, out, stride, lse, None), vb.lib.vlac_tree_attention(*head, C.byref(tree), far, 256, 1.0, out, stride, lse, None)}
+    for begin in (FAKE, side):
+        for at in (begin, begin + layer, begin + 2 * layer - 16, begin - 3 * 512 - 16):
+            assert call(at) == {INVALID}, (begin, at)
+        assert call(begin - (1 << 19), stride=1 << 18) == {INVALID}
+    out = far + (1 << 20)
+    for lse in (out, out - 60, out + 3 * 512 + 508, out + 512):                  # (4 rows of 4 sums: 64 bytes)
+        assert call(out, lse=lse) == {INVALID}, lse - out
+    assert call(out, stride=1 << 12, lse=out + 3 * (1 << 13) - 4) == {INVALID}
