@@ -279,6 +279,7 @@ int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int
   if ((rope->q_gain || rope->k_gain) && !(rope->eps >= 0.f && isfinite(rope->eps))) return VLAC_ERR_INVALID_ARG;
   if (n == 0) return VLAC_OK;
   if (!seqs || !row_ptr || !status || (rows > 0 && (!k_rows || !v_rows))) return VLAC_ERR_INVALID_ARG;
+  if (((uintptr_t)seqs | (uintptr_t)start | (uintptr_t)row_ptr | (uintptr_t)pos | (uintptr_t)status) & 3u) return VLAC_ERR_INVALID_ARG;
   const long long w = (long long)pages_row(p), wq = (long long)n_heads * p->head_dim;
   if (k_stride < w || v_stride < w || k_stride % 8 || v_stride % 8 || (((uintptr_t)k_rows | (uintptr_t)v_rows) & 15u)) return VLAC_ERR_INVALID_ARG;
   if (n_heads > 0 && rows > 0) {

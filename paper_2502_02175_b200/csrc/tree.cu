@@ -224,7 +224,7 @@ int vlac_tree_plan(const vlac_pages* p, const vlac_tree* tree, const int* seqs, 
   if (tree->rows > 0 && (!tree->mask || !tree->pos || !tree->entry || ((uintptr_t)tree->mask | (uintptr_t)tree->pos | (uintptr_t)tree->entry) & 3u))
     return VLAC_ERR_INVALID_ARG;
   if (tree->n == 0) return VLAC_OK;
-  if (!status) return VLAC_ERR_INVALID_ARG;
+  if (!status || ((uintptr_t)seqs | (uintptr_t)status) & 3u) return VLAC_ERR_INVALID_ARG;
   VLAC_CUDA_CHECK(launch_pdl(tree_plan_kernel, dim3(tree->n + 1), dim3(TP_THREADS), 0, (cudaStream_t)stream, tree_args(p, tree, seqs, status)));
   return VLAC_OK;
 }
@@ -237,6 +237,9 @@ int vlac_tree_accept(const vlac_pages* p, const vlac_tree* tree, const int* seqs
   if (n_keep < 0 || n_keep == INT_MAX) return VLAC_ERR_INVALID_ARG;
   if (tree->n == 0) return VLAC_OK;
   if (!seqs || !count || !keep_ptr || !status || (n_keep > 0 && !keep) || (tree->rows > 0 && (!drafted || !chosen || !path || !tokens))) return VLAC_ERR_INVALID_ARG;
+  if (((uintptr_t)seqs | (uintptr_t)drafted | (uintptr_t)chosen | (uintptr_t)count | (uintptr_t)path | (uintptr_t)tokens | (uintptr_t)keep_ptr | (uintptr_t)keep |
+       (uintptr_t)status) & 3u)
+    return VLAC_ERR_INVALID_ARG;
   AcceptArgs a = {tree_args(p, tree, seqs, status), drafted, chosen, count, path, tokens, keep_ptr, keep, n_keep};
   const int smem = TA_WARPS * tree->max_rows * 4;                       // at most 128 KB
   if (tree->n <= TA_ONE && n_keep <= TA_SHORT) {

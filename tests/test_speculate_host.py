@@ -156,3 +156,15 @@ def test_attention_results_over_the_pool_or_the_sums_are_refused(vb):
     for lse in (out, out - 60, out + 3 * 512 + 508, out + 512):                  # (4 rows of 4 sums: 64 bytes)
         assert call(out, lse=lse) == {INVALID}, lse - out
     assert call(out, stride=1 << 12, lse=out + 3 * (1 << 13) - 4) == {INVALID}
+
+
+def test_lists_off_their_alignment_are_refused(vb):
+    """A list of ints that does not begin at a multiple of 4 bytes would be a misaligned read on the device."""
+    p, t = _struct(vb), _tree(vb)
+    for name in ("seqs", "row_ptr", "status", "start", "pos"):
+        assert _append(vb, **{name: FAKE + 2}) == INVALID, name
+    for seqs, status in ((FAKE + 1, FAKE), (FAKE, FAKE + 2)):
+        assert vb.lib.vlac_tree_plan(C.byref(p), C.byref(t), seqs, status, None) == INVALID
+    for i in range(9):
+        a = [FAKE + 2 if j == i else FAKE for j in range(9)]
+        assert vb.lib.vlac_tree_accept(C.byref(p), C.byref(t), *a[:8], 4, a[8], None) == INVALID, i
