@@ -427,7 +427,8 @@ int vlac_selftest_prefix_wait(const vlac_pages* p, int layer, const vlac_prefix*
  * length that the weights were trained for (the interpolation by parts of the YaRN paper, arXiv 2309.00071, whose attention temperature is the
  * amplitude).
  *   rot_dim  even, 2..256;  theta > 0, factor > 0, original_len >= 0, amplitude finite; turns_low < turns_high where original_len > 0; no frequency
- *            of 65536 turns a position or more (an angle is right to its own size times 2^-63)
+ *            of 65536 turns a position or more (an angle is right to its own size times 2^-59, a g_i between 0 and 1 to
+ *            turns_i / (turns_high - turns_low) times that)
  *   first >= 0, n_pos >= 0, first + n_pos <= 2^31 - 1;  cos, sin  device fp32 [n_pos][rot_dim/2] */
 typedef struct {
   int rot_dim;

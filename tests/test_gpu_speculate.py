@@ -807,3 +807,24 @@ def test_two_captured_steps_at_once(vb):
     torch.cuda.synchronize()
     for _, _, out, x, p, _ in work:
         assert torch.equal(out, base) and torch.equal(x, want[0]) and torch.equal(p, want[1])
+
+
+# ------------------------------------------------------------------------------------------------ bounds and expectations of their own
+@pytest.mark.parametrize("rot,theta", [(256, 3e-6), (250, 2.5e-6), (254, 1e-4), (128, 10000.0), (256, 1e6), (96, 500000.0), (6, 100.0), (34, 0.5)])
+def test_tables_of_far_positions(vb, rot, theta):
+    """Every frequency at the last positions there are, against 60 decimal digits: the angle is right to 2^-59 of its own size (frequencies up to 48,000 turns a position
+    show it: 10^14 turns), 64-bit arithmetic on a reduced angle adds less than 2^-44, the table's own rounding 2^-24."""
+    import decimal
+    D = decimal.Decimal
+    first, n_pos = 2 ** 31 - 20, 19
+    cos, sin = (torch.zeros((n_pos, rot // 2), device="cuda") for _ in range(2))
+    vb.vlac_rope_tables(cos, sin, theta, first=first)
+    with decimal.localcontext() as ctx:
+        ctx.prec = 60
+        two_pi = D("6.28318530717958647692528676655900576839433879875021164194988918461563281257")
+        per = [D(theta) ** (D(-2 * i) / D(rot)) / two_pi for i in range(rot // 2)]
+        turns = [[(first + p) * f for f in per] for p in range(n_pos)]
+        angle = np.array([[float((t - t.to_integral_value()) * two_pi) for t in row] for row in turns])
+        size = np.array([[float(t * two_pi) for t in row] for row in turns])
+    for got, want in ((cos, np.cos(angle)), (sin, np.sin(angle))):
+        assert np.all(np.abs(host(got) - want) <= 2.0 ** -59 * size + 2.0 ** -24 * np.abs(want) + 2.0 ** -44)
