@@ -828,3 +828,41 @@ def test_tables_of_far_positions(vb, rot, theta):
         size = np.array([[float(t * two_pi) for t in row] for row in turns])
     for got, want in ((cos, np.cos(angle)), (sin, np.sin(angle))):
         assert np.all(np.abs(host(got) - want) <= 2.0 ** -59 * size + 2.0 ** -24 * np.abs(want) + 2.0 ** -44)
+
+
+class ParentsCase(TreeCase):
+    """What a row sees comes from the parents alone; `none`: entries that the tree plan refuses, whose rows see only what lies in front of the tree."""
+    none = ()
+
+    def want(self, i, layer=0, q=None):
+        slot, nq = self.seqs[i], self.nq[i]
+        n = int(self.pages.len[slot])
+        t = self.pages.table[slot, :-(-n // self.page)].long()
+        k, v = (host(x[layer, t].reshape(-1, self.kv_heads, self.d)[:n]) for x in (self.pages.k, self.pages.v))
+        r0 = sum(self.nq[:i])
+        seen = ref.seen_by(self.parents[i], n)
+        if i in self.none:
+            seen[:, n - nq:] = False
+        return ref.tree_attention(k, v, host((self.q if q is None else q)[r0:r0 + nq]), n, nq, self.heads // self.kv_heads, self.scale, HALF[self.dtype], seen)
+
+
+@pytest.mark.parametrize("reach", [1, 2, 2000])
+@pytest.mark.parametrize("groups", TREES, ids=str)
+def test_tree_attention_by_parents(vb, groups, reach):
+    for heads, kv_heads, d, dtype, columns in ((4, 1, 128, torch.bfloat16, 0), (2, 2, 64, torch.float16, 30000)):
+        c = ParentsCase(vb, TREES[groups], heads, kv_heads, d, dtype=dtype, seed=reach, columns=columns, reach=reach)
+        c.check(*c.run())
+
+
+def test_tree_attention_of_refused_trees_by_parents(vb):
+    c = ParentsCase(vb, [(48, [(9, 5), (20, 11), (7, 4)]), (0, [(6, 6)])], seed=4)
+    c.tree.parent[6], c.tree.parent[21] = 9, 1                                  # of entry 1, and of entry 3, which sees nothing then
+    c.none = (1, 3)
+    plan, st, st2 = vb.PrefixPlan(c.pages, 4, c.rows, c.heads), ints(4), ints(4)
+    out, lse = torch.full_like(c.q, 5.0), torch.full((c.rows, c.heads), 5.0, device="cuda")
+    vb.vlac_tree_plan(c.pages, c.tree, dev(c.seqs), st2)
+    vb.vlac_prefix_plan(c.pages, plan, dev(c.seqs), c.tree.q_ptr, st)
+    vb.vlac_tree_attention(c.pages, 0, plan, c.tree, c.q, c.scale, out, lse)
+    assert st.tolist() == [0] * 4 and st2.tolist() == [0, -1, 0, -1]
+    c.check(out, lse, only=(0, 1, 2))
+    assert torch.all(out[20:] == 0) and torch.all(torch.isneginf(lse[20:]))
