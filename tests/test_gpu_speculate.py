@@ -866,3 +866,27 @@ def test_tree_attention_of_refused_trees_by_parents(vb):
     assert st.tolist() == [0] * 4 and st2.tolist() == [0, -1, 0, -1]
     c.check(out, lse, only=(0, 1, 2))
     assert torch.all(out[20:] == 0) and torch.all(torch.isneginf(lse[20:]))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 30, 80, 230, 450])
+@pytest.mark.parametrize("lie", ["whole", "shifted", "single"])
+def test_logits_infinities_as_they_are(vb, lie, rows, dtype):
+    """What is not allowed is -infinity itself, not the type's lowest value, and infinities and lowest values among the logits stay what they are."""
+    vocab = 4096 if lie == "whole" else 4099
+    c = Logits(vb, rows, vocab, dtype, seed=rows, tree=[rows] if rows < 100 else [50] * (rows // 50) + ([rows % 50] if rows % 50 else []), masks=3, allow=0.3)
+    low = torch.finfo(dtype).min
+    c.x[:, ::7], c.x[:, 3::11], c.x[:, 5::501], c.x[:, 1234::2000] = low, float("-inf"), -low, float("inf")
+    c.x[rows // 2, 17::600] = float("nan")
+    pad = 1 if lie == "single" else 0
+    out = torch.full((rows, vocab + pad), 7.0, dtype=dtype, device="cuda")
+    _, p, st = c.run(out=out[:, pad:])
+    assert st.tolist() == [0] * rows
+    for r in {*range(0, rows, max(1, rows // 9)), rows // 2}:
+        x, at = c.want(r)
+        got, want = out[r, pad:].cpu(), torch.from_numpy(x).to(dtype)
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got[~got.isnan()], want[~want.isnan()]) and p[r].item() == at
+        assert torch.all(torch.isneginf(got[torch.from_numpy(~c.bits[c.arow[r], :vocab])])) if c.arow[r] >= 0 else True
+    here = c.x.clone()
+    c.run(x=here, out=here)
+    assert torch.equal(here.isnan(), out[:, pad:].isnan()) and torch.equal(here.nan_to_num(7.0, float("inf"), float("-inf")), out[:, pad:].nan_to_num(7.0, float("inf"), float("-inf")))
