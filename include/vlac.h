@@ -425,7 +425,7 @@ int vlac_selftest_prefix_wait(const vlac_pages* p, int layer, const vlac_prefix*
  *     cos[p][i] = amplitude * cos((first + p) * f_i * (g_i + (1 - g_i) / factor)),  sin alike
  * factor stretches the positions (1: none): all frequencies alike with original_len = 0, otherwise only those that turn seldom over the
  * length that the weights were trained for (the interpolation by parts of the YaRN paper, arXiv 2309.00071, whose attention temperature is the
- * amplitude).
+ * amplitude; it blends by turns, and the tables of code that blends linearly over the index i between two dimensions cannot be had from this call).
  *   rot_dim  even, 2..256;  theta > 0, factor > 0, original_len >= 0, amplitude finite; turns_low < turns_high where original_len > 0; no frequency
  *            of 65536 turns a position or more (an angle is right to its own size times 2^-59, a g_i between 0 and 1 to
  *            turns_i / (turns_high - turns_low) times that)
@@ -437,8 +437,8 @@ typedef struct {
 int vlac_rope_tables(const vlac_rope_scaling* r, int first, int n_pos, float* cos, float* sin, void* stream);
 
 /* How vlac_pages_append treats a head's query or key before it is stored, in this order and rounded once at the end:
- *   q_gain, k_gain  device [head_dim] of the pool's type, or NULL: x -> x / sqrt(mean(x^2) + eps) * gain over the head's dimensions (sums in
- *                   fp32: components beyond 10^18 overflow them)
+ *   q_gain, k_gain  device [head_dim] of the pool's type, or NULL: x -> x / sqrt(mean(x^2) + eps) * gain over the head's dimensions (16-byte aligned; sums
+ *                   in fp32: components beyond 10^18 overflow them, and with eps = 0 a head of none beyond 10^-19 is lost in them; eps >= 0)
  *   rot_dim         0 or a multiple of 16 up to head_dim: the first rot_dim dimensions are rotated, pairs (i, i + rot_dim/2), or with
  *                   interleaved = 1 (2i, 2i + 1):  (x, y) -> (x cos - y sin, x sin + y cos)
  *   cos, sin        device fp32 [n_pos][rot_dim/2], 16-byte aligned (not read with rot_dim = 0) */
@@ -464,7 +464,7 @@ int vlac_pages_append(const vlac_pages* p, int layer, const int* seqs, const int
 /* Trees of drafted tokens, one per entry of a list.
  *   q_ptr    device int32 [n + 1]: rows q_ptr[i] .. q_ptr[i+1] (at most max_rows, 1..VLAC_TREE_MAX_ROWS) are the nq_i newest rows of slot seqs[i]
  *   parent   device int32 [rows]: the row's parent within its entry, a row in front of it; -1: none (what it extends is the sequence)
- * and what vlac_tree_plan makes of them (a caller may write mask itself: any bits, of its own rows too):
+ * and what vlac_tree_plan makes of them (a caller may write mask itself: any bits, of its own rows too; vlac_logits_adjust goes by entry then as well):
  *   mask     device uint32 [rows][ceil(max_rows/32)]: bit j = the row sees row j of its entry (its ancestors and itself)
  *   pos      device int32 [rows]: len - nq_i + depth, the position to rotate to;  entry  device int32 [rows]: the row's entry
  * Status as for the paged calls, INVALID_ARG also for a parent out of range and nq_i > len, TOO_LARGE for nq_i > max_rows; rows of refused

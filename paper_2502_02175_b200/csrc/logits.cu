@@ -15,7 +15,12 @@ namespace {
 
 constexpr int LG_RUN = 131072;                  // tokens whose marks a CTA holds at once
 // Tokens whose counts a CTA holds: a run of at most as many by their place in it ("direct"), of a longer one the marked tokens by a hash.  Few rows: more, so
-// that an eighth of 32,000 tokens is direct; many: fewer, so that four CTAs fit an SM.
+// that an eighth of 32,000 tokens is direct; many: fewer, so that four CTAs fit an SM.  A hash table that overflows, from 1000 to 1400 different tokens a CTA on, costs
+// much: the rest of the CTA's share goes in direct runs, and the row's lists are gone through for each.  us, rows of 128,000 in bf16 by different tokens a row:
+//   512 rows, a CTA each       1000 76    1400 248   2000 370   4000 583   8000 967
+//   256 rows, two CTAs each    1000 40    2000 49    4000 287   8000 602
+//   100 rows, four CTAs each   1000 20    2000 24    4000 33    8000 243
+//    25 rows, eight CTAs each  1000 11    2000 12.5  4000 17    8000 25    32000 292
 __host__ __device__ constexpr int lg_table(int ctas) { return ctas == 8 ? 4096 : 2048; }
 constexpr int LG_TRIES = 64;                    // where a token finds no entry in as many tries, the run is cut into direct ones
 constexpr int LG_LOOK = 4;                      // tokens of the history that a thread asks for at once
@@ -123,7 +128,7 @@ template <typename T, bool VEC> struct Piece {
 
 // LG_WHOLE: rows of whole, aligned 16-byte pieces.  LG_SHIFTED: a row may begin and end anywhere, its results like its logits.  Places are counted from the 16-byte boundary in front of the row, so that pieces are
 // whole and aligned; token t has place t + off.  What lies in a piece that the row does not fill (at most 7 tokens at each end) is marked and done with
-// the marked tokens (512 rows of 126,953 in bf16: 82 us, one element at a time 210).  LG_SINGLE: results that lie otherwise than their logits.
+// the marked tokens (512 rows of 126,953 in bf16: 78 us, one element at a time 210).  LG_SINGLE: results that lie otherwise than their logits.
 // CTAS share a row.  Few rows are shared by 8, so that there are enough CTAs; many by fewer, since every one of them goes through the row's lists.
 enum { LG_SINGLE = 0, LG_WHOLE = 1, LG_SHIFTED = 2 };
 template <typename T, int MODE, int CTAS, int LG_THREADS>

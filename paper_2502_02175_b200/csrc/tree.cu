@@ -43,7 +43,9 @@ __device__ __forceinline__ void tree_blank(const TreeArgs& a, int from, int to) 
 }
 
 // A CTA an entry, and one for the rows of none.  A row's ancestors are found by walking up; their indices fall, so that its mask is filled word
-// by word from the last on.  Bound: launch and two dependent reads (about 3 us in a captured step).
+// by word from the last on.  Bound: launch and two dependent reads (trees of tens of rows, about 3 us in a captured step); in large deep trees the walk, a
+// dependent read a step and thread (1024 rows, one tree or 16 of them: all children of the first 21 to 25 us, random parents 31, each behind one of the four rows
+// in front of it 300, a chain 749).
 __global__ void __launch_bounds__(TP_THREADS) tree_plan_kernel(TreeArgs a) {
   __shared__ int s_parent[VLAC_TREE_MAX_ROWS];
   const int tid = threadIdx.x, i = blockIdx.x;
